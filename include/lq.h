@@ -385,6 +385,101 @@ int lq_profile_read(lq_plan* plan, double* total_ms, int64_t* launches);
 const char* lq_error_string(int code);
 const char* lq_last_error(void);
 
+/* ---- Quantised key-value cache ---------------------------------------------------------------------------------
+ * Keys and values of a model's attention layers, kept the way a message keeps a gradient in bucket scope: every
+ * (token, head) row x of head_dim coordinates is a bucket with its own fp32 L^q norm N, its coordinates are rounded to
+ * the level set of their (layer, keys or values), and a coordinate is one symbol, 2 * level index + sign.
+ *   N = fp32(||x||_q), the sum in fp64; u = min(|x| * fp32(1/N), 1); tau = the last level <= u, at most n - 2;
+ *   the upper neighbour is taken if rho * (l_{tau+1} - l_tau) < u - l_tau, all fp32 numbers; the value kept is
+ *   sign * level * N.  rho = 1/2 rounds to the nearest level (the lower one in the middle); with a step, rho is a Philox4x32-10
+ *   uniform on the 2^-23 grid (key = seed, counter = (coordinate / 4, 2 * layer + kind, slot, step), word coordinate % 4,
+ *   where head h's coordinates start at h * padded size) and the rounding is unbiased.
+ *   A row that is all zero, whose norm is below the smallest normal float, or that holds NaN or Inf is kept as zeros with
+ *   norm 0; NaN and Inf set LQ_CACHE_NONFINITE.
+ * Symbols have 4 bits (8 levels, bits = 3) or 8 (128 levels, bits = 7), for keys and values apart.  Levels are numbers of
+ * 11 bits: lq_cache_set_levels rounds to fp16, so that the products on the matrix units round no value of the cache.
+ *
+ * Pages: a page holds page_size tokens (a power of two from 16 to 1024) of ONE layer: lq_cache_page_words() 32-bit words,
+ * for each head its page_size rows of keys, its rows of values, the keys' norms, the values' norms.  A row is `padded`
+ * symbols, little endian, padded = 64, 128 or 256, the least that holds head_dim; the symbols past it are 0.  Pages of a
+ * layer are one array [num_pages][page_words], owned by the caller, 16-byte aligned; slot = page * page_size + token's place.
+ * Concurrency: the calls below keep nothing in the object but the flags, so calls on different streams, and graphs that
+ * replay at the same time, do not disturb one another as long as the caller's own buffers (pages, outputs, workspace) do not.
+ * The calls run on the device on which the cache was made, whichever is current. */
+#define LQ_KEYS    0
+#define LQ_VALUES  1
+#define LQ_F32     0
+#define LQ_F16     1
+#define LQ_BF16    2
+#define LQ_CACHE_NONFINITE     1u  /* a row with NaN or Inf, or whose norm overflows, was kept as zeros */
+#define LQ_CACHE_BAD_SLOT      2u  /* a slot past the last page: skipped by a write, zeros from a read */
+#define LQ_CACHE_BAD_POSITION  4u  /* a position outside the rotary table: token not written; NaN from attention */
+#define LQ_CACHE_BAD_PAGE      8u  /* a page number outside [0, num_pages) inside a sequence: its tokens are left out */
+#define LQ_CACHE_BAD_LENGTH   16u  /* a negative length (taken as 0), or one past its table (taken as the table's tokens) */
+
+typedef struct lq_cache lq_cache;
+
+/* Rows [tokens][heads][head_dim] in device memory; strides in elements; the coordinates of a row side by side. */
+typedef struct {
+    void* data;
+    int64_t token_stride, head_stride;
+    int32_t type;                 /* LQ_F32, LQ_F16 or LQ_BF16 */
+} lq_rows;
+
+/* Rotary positions: the first `dim` coordinates of a row are dim/2 pairs, (i, i + dim/2) or, interleaved, (2i, 2i + 1);
+ * pair (a, b) becomes (a c - b s, b c + a s), each product and the sum rounded to fp32, with c and s from the table's row of
+ * the token's position.  Longer contexts and other bases are a matter of the table. */
+typedef struct {
+    const float* table;           /* [positions][dim]: dim/2 cosines, then dim/2 sines */
+    const int64_t* at;            /* dev [tokens]; lq_cache_attend also takes NULL: every sequence's last position */
+    int64_t positions;
+    int32_t dim;                  /* even, 2..head_dim */
+    int32_t interleaved;
+} lq_rotary;
+
+/* num_layers 1..65536; kv_heads 1..1024; head_dim 1..256; bits 3 or 7; q: 0 (infinity norm), 1 or 2.  Level sets start
+ * uniform.  Allocates its level tables on the current device; may synchronise. */
+int lq_cache_create(lq_cache** out, int32_t num_layers, int32_t kv_heads, int32_t head_dim, int32_t page_size,
+                    int32_t bits_keys, int32_t bits_values, int32_t q, uint64_t seed);
+int lq_cache_destroy(lq_cache* cache);            /* synchronises the device; NULL is accepted */
+int64_t lq_cache_page_words(const lq_cache* cache);
+/* Any of the outputs may be NULL. */
+int lq_cache_info(const lq_cache* cache, int32_t* kv_heads, int32_t* head_dim, int32_t* page_size, int32_t* device);
+
+/* Level set of (layer, kind), kind = LQ_KEYS or LQ_VALUES: n = 2^bits values from 0 to 1, strictly increasing also after
+ * rounding to fp16 (else LQ_EINVAL); a set of lq_fit_levels can be taken as it is where that holds.  Rows written before
+ * a set are read with the new levels.  get returns the rounded set.  Both synchronise the device. */
+int lq_cache_set_levels(lq_cache* cache, int32_t layer, int32_t kind, const float* host_levels, int32_t n);
+int lq_cache_get_levels(const lq_cache* cache, int32_t layer, int32_t kind, float* host_levels, int32_t n);
+
+/* LQ_CACHE_* flags of the calls since the last lq_cache_status, which clears them.  Synchronises the device. */
+int lq_cache_status(lq_cache* cache, uint32_t* flags);
+
+/* Quantises rows of keys and values [tokens][kv_heads][head_dim] into slots [tokens] (dev) of one layer's pages; a negative
+ * slot is skipped (padding of a batch).  rotary: NULL, or the keys are rotated first (rotary->at must then be given).
+ * step: -1 rounds to the nearest level, 0..2^32-1 unbiased.  Slots of a call have to differ: a slot that occurs
+ * twice ends with symbols of either token. */
+int lq_cache_write(lq_cache* cache, int32_t layer, const lq_rows* keys, const lq_rows* values, int64_t tokens,
+                   const int64_t* slots, uint32_t* pages, int64_t num_pages, int64_t step, const lq_rotary* rotary,
+                   void* stream);
+/* The values of slots [tokens] (dev) as rows; zeros for a negative slot.  One fp32 product a value, rounded to the row's type. */
+int lq_cache_read(lq_cache* cache, int32_t layer, const uint32_t* pages, int64_t num_pages, int64_t tokens,
+                  const int64_t* slots, const lq_rows* keys, const lq_rows* values, void* stream);
+
+/* Attention of one new token a sequence: for sequence b and each of its `heads` queries (a multiple of kv_heads; query
+ * heads h * heads/kv_heads and on belong to head h of the cache)
+ *   s_j = scale * q . k_j,  out = sum_j softmax(s)_j v_j,  lse = log sum_j exp(s_j)
+ * over the tokens max(0, length - window) <= j < length (window 0: all).  Token j sits in page table[b][j / page_size] at
+ * place j % page_size.  A sequence with nothing to see gives zeros and lse = -infinity.  Sums and softmax are in fp32.
+ *   queries, out [batch][heads][head_dim] of one type; table dev [batch][table_width]; lengths dev [batch]; lse dev
+ *   [batch][heads] or NULL; rotary: NULL, or the queries are rotated first, without rounding them to their type.
+ *   workspace: dev, 16-byte aligned, of lq_cache_workspace() bytes; its contents need not be kept or cleared. */
+int64_t lq_cache_workspace(const lq_cache* cache);
+int lq_cache_attend(lq_cache* cache, int32_t layer, const lq_rows* queries, int64_t batch, int32_t heads,
+                    const uint32_t* pages, int64_t num_pages, const int32_t* table, int64_t table_width,
+                    const int32_t* lengths, float scale, int64_t window, const lq_rotary* rotary, const lq_rows* out,
+                    float* lse, void* workspace, int64_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -22,6 +22,11 @@ NUM_BINS = 386
 HIST_STRIDE = 512
 STATUS_ZERO_NORM = 1
 STATUS_NONFINITE = 2
+CACHE_NONFINITE = 1             # a row with NaN or Inf was kept as zeros
+CACHE_BAD_SLOT = 2              # a slot past the last page
+CACHE_BAD_POSITION = 4          # a position outside the rotary table
+CACHE_BAD_PAGE = 8              # a page number outside the pages
+CACHE_BAD_LENGTH = 16           # a length below 0 or past its table
 CODE_BROKEN = 1                 # a decode met an invalid stream
 CODE_GAVE_UP = 2                # an encode waited in vain
 STEP_AUTO = 0xFFFFFFFF          # lq_quantize_pack: take the step index from the plan's device-side iteration counter
@@ -33,6 +38,8 @@ EXPORTS = ["lq_plan_create", "lq_plan_destroy", "lq_plan_padded_elems", "lq_plan
            "qoda_get_scalars", "lq_code_build", "lq_code_universal", "lq_code_set", "lq_code_get", "lq_plan_blocks", "lq_entropy_encode",
            "lq_entropy_decode", "lq_entropy_wait", "lq_entropy_status", "lq_level_probabilities", "lq_symbol_counts", "qoda_set_alt_rates", "qoda_set_average", "qoda_get_alt_scalars", "lq_get_statistics", "lq_vector_norm_static", "lq_profile_enable",
            "lq_profile_read",
+           "lq_cache_create", "lq_cache_destroy", "lq_cache_page_words", "lq_cache_info", "lq_cache_set_levels", "lq_cache_get_levels",
+           "lq_cache_status", "lq_cache_write", "lq_cache_read", "lq_cache_workspace", "lq_cache_attend",
            "lq_error_string", "lq_last_error"]
 KERNEL_NAMES = ["norm_partial", "norm_finalize", "quantize_pack", "stat_finalize", "qoda_scalars",
                 "decode", "fit", "alt_finalize", "average", "block_live"]
@@ -40,6 +47,16 @@ KERNEL_NAMES = ["norm_partial", "norm_finalize", "quantize_pack", "stat_finalize
 
 class LqError(RuntimeError):
     pass
+
+
+class Rows(C.Structure):
+    """lq_rows of include/lq.h"""
+    _fields_ = [("data", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64), ("type", C.c_int32)]
+
+
+class Rotary(C.Structure):
+    """lq_rotary of include/lq.h"""
+    _fields_ = [("table", C.c_void_p), ("at", C.c_void_p), ("positions", C.c_int64), ("dim", C.c_int32), ("interleaved", C.c_int32)]
 
 
 _lib = None
@@ -98,6 +115,18 @@ def load_library() -> C.CDLL:
     L.lq_vector_norm_static.argtypes = [vp, i64, i32, vp, vp, vp]
     L.lq_profile_enable.argtypes = [vp, i32]
     L.lq_profile_read.argtypes = [vp, C.POINTER(C.c_double), C.POINTER(i64)]
+    L.lq_cache_create.argtypes = [C.POINTER(vp), i32, i32, i32, i32, i32, i32, i32, u64]
+    L.lq_cache_destroy.argtypes = [vp]
+    L.lq_cache_page_words.argtypes = [vp]; L.lq_cache_page_words.restype = i64
+    L.lq_cache_workspace.argtypes = [vp]; L.lq_cache_workspace.restype = i64
+    L.lq_cache_info.argtypes = [vp, C.POINTER(i32), C.POINTER(i32), C.POINTER(i32), C.POINTER(i32)]
+    L.lq_cache_set_levels.argtypes = [vp, i32, i32, C.POINTER(C.c_float), i32]
+    L.lq_cache_get_levels.argtypes = [vp, i32, i32, C.POINTER(C.c_float), i32]
+    L.lq_cache_status.argtypes = [vp, C.POINTER(u32)]
+    rows, rotary = C.POINTER(Rows), C.POINTER(Rotary)
+    L.lq_cache_write.argtypes = [vp, i32, rows, rows, i64, vp, vp, i64, i64, rotary, vp]
+    L.lq_cache_read.argtypes = [vp, i32, vp, i64, i64, vp, rows, rows, vp]
+    L.lq_cache_attend.argtypes = [vp, i32, rows, i64, i32, vp, i64, vp, i64, vp, C.c_float, i64, rotary, rows, vp, vp, i64, vp]
     L.lq_error_string.argtypes = [C.c_int]; L.lq_error_string.restype = C.c_char_p
     L.lq_last_error.argtypes = []; L.lq_last_error.restype = C.c_char_p
     for name in EXPORTS:
@@ -345,3 +374,79 @@ class Plan:
     def zero_hist(self, device="cuda") -> torch.Tensor:
         return torch.zeros((self.num_workers, max(self.num_layers, 1), HIST_STRIDE), dtype=torch.int32,
                            device=device)
+
+
+class Cache:
+    """Owns one lq_cache: a key-value cache in the framework's quantised form (include/lq.h).  Methods carry the names of the C entry
+    points; tensors have to be on the device that was current when the cache was made, and calls run on its current stream."""
+
+    _KINDS = {"keys": 0, "values": 1}
+    _LAYOUTS = {"half": False, "interleaved": True}
+
+    def __init__(self, num_layers: int, kv_heads: int, head_dim: int, page_size: int = 64, bits=(3, 3), q: int = 0, seed: int = 0):
+        L = load_library()
+        self.bits = (int(bits), int(bits)) if isinstance(bits, int) else (int(bits[0]), int(bits[1]))
+        self.num_layers, self.kv_heads, self.head_dim, self.page_size = int(num_layers), int(kv_heads), int(head_dim), int(page_size)
+        self.q, self.seed = int(q), int(seed)
+        h = C.c_void_p()
+        _check(L.lq_cache_create(C.byref(h), self.num_layers, self.kv_heads, self.head_dim, self.page_size, *self.bits, self.q,
+                                 C.c_uint64(self.seed)))
+        self._h, self._addr = h, h.value
+        self.page_words = int(L.lq_cache_page_words(h))
+        device = C.c_int32()
+        _check(L.lq_cache_info(h, None, None, None, C.byref(device)))
+        self.device = torch.device("cuda", device.value)
+
+    def close(self) -> None:
+        if getattr(self, "_h", None):
+            load_library().lq_cache_destroy(self._h)
+            self._h = self._addr = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def empty_pages(self, num_pages: int) -> torch.Tensor:
+        """[num_pages][page_words] pages of one layer; a slot that was not written yet holds zeros."""
+        return torch.zeros((num_pages, self.page_words), dtype=torch.int32, device=self.device)
+
+    def lq_cache_set_levels(self, layer: int, kind: str, levels) -> None:
+        """Level set of the layer's "keys" or "values", rounded to numbers of 11 bits."""
+        arr = (C.c_float * len(levels))(*[float(x) for x in levels])
+        _check(load_library().lq_cache_set_levels(self._h, layer, self._KINDS[kind], arr, len(levels)))
+
+    def lq_cache_get_levels(self, layer: int, kind: str) -> List[float]:
+        n = 1 << self.bits[self._KINDS[kind]]
+        arr = (C.c_float * n)()
+        _check(load_library().lq_cache_get_levels(self._h, layer, self._KINDS[kind], arr, n))
+        return list(arr)
+
+    def lq_cache_status(self) -> int:
+        """CACHE_* flags of the calls since the last time, added up."""
+        flags = C.c_uint32(0)
+        _check(load_library().lq_cache_status(self._h, C.byref(flags)))
+        return flags.value
+
+    def lq_cache_write(self, layer: int, keys, values, slots, pages, step: Optional[int] = None, rotary=None, positions=None,
+                       layout: str = "half") -> None:
+        """Quantises keys and values [tokens][kv_heads][head_dim] into slots [tokens] (int64, page * page_size + place; negative:
+        skipped).  step: None rounds to the nearest level, a number unbiased.  rotary: a table of lq_rotary_table, by which the
+        keys are turned at positions [tokens] first; layout: pairs as halves of the rotated coordinates, or interleaved."""
+        if step is not None and step < 0:
+            raise LqError(f"step {step} is negative")
+        _native.lq_cache_write(self._addr, layer, keys, values, slots, pages, -1 if step is None else step, rotary, positions,
+                               self._LAYOUTS[layout])
+
+    def lq_cache_read(self, layer: int, pages, slots, keys, values) -> None:
+        """The rows of slots [tokens] into keys and values [tokens][kv_heads][head_dim]; zeros for a negative slot."""
+        _native.lq_cache_read(self._addr, layer, pages, slots, keys, values)
+
+    def lq_cache_attend(self, layer: int, queries, pages, table, lengths, out, lse=None, scale: Optional[float] = None, window: int = 0,
+                        rotary=None, positions=None, layout: str = "half") -> None:
+        """Attention of one new token a sequence: queries and out [batch][heads][head_dim], table [batch][pages of a sequence]
+        and lengths [batch] int32, lse [batch][heads] fp32.  scale: 1 / sqrt(head_dim) unless given; window: how many of the last
+        tokens are seen (0: all); rotary: the queries are turned first, at positions [batch] or each sequence's last one."""
+        _native.lq_cache_attend(self._addr, layer, queries, pages, table, lengths, out, lse,
+                                self.head_dim ** -0.5 if scale is None else scale, window, rotary, positions, self._LAYOUTS[layout])

@@ -1,0 +1,108 @@
+// The quantised key-value cache: what its host side and its kernels share (not part of the public ABI).
+//
+// Layout of a page, in 32-bit words, for each head in turn (RowShape::head_words of them):
+//   page_size rows of keys, page_size rows of values, page_size norms of keys, page_size norms of values (fp32).
+// A row holds `padded` symbols of 4 or 8 bits, little endian, 2 * level index + sign, zeros past head_dim.  padded is 64,
+// 128 or 256, the sizes that the attention kernel is compiled for.  Rows stay in the order of their tokens and coordinates:
+// a warp of the attention kernel reads 16 tokens, and with tokens and coordinates dealt to lanes as below
+// each lane's share of a row is one run of 4 to 16 bytes, so no other arrangement is needed to feed matrix instructions.
+#pragma once
+
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "lq.h"
+
+namespace lq {
+
+constexpr int kCacheLevels = 128;       // most levels of a set (7 bits)
+constexpr int kCachePairs = 256;        // entries of the look-up table by bytes
+
+// Device tables of one (layer, keys or values).
+struct CacheTable {
+    float levels[kCacheLevels];         // numbers of 11 bits (set_levels rounds them)
+    // By byte of a row: 4-bit symbols: the two signed levels as fp16, the first symbol's in the low half;
+    // 8-bit symbols: the signed level as fp16 in both halves.
+    uint32_t pairs[kCachePairs];
+};
+
+struct CacheShape {
+    int32_t heads, dim, padded;
+    int32_t page_shift;                 // log2(tokens of a page)
+    int32_t sym_bits[2];                // 4 or 8: keys, values
+    int32_t row_words[2];
+    int32_t q;                          // norm: 0 infinity, 1, 2
+    int64_t head_words, page_words;
+};
+
+// Rows [tokens][heads][dim] with any strides (in elements) between tokens and heads, coordinates side by side.
+struct CacheRows {
+    void* data;
+    int64_t token_stride, head_stride;
+    int32_t type;                       // LQ_F32, LQ_F16, LQ_BF16
+    int32_t wide;                       // every row starts on a 16-byte boundary
+};
+
+struct CacheRotary {
+    const float* table;                 // [positions][dim]: cosines of dim / 2 angles, then sines; NULL: none
+    const int64_t* at;                  // position of every token; NULL in lq_cache_attend: the last token's
+    int64_t positions;
+    int32_t dim;
+    int32_t interleaved;
+};
+
+struct CacheWriteArgs {
+    CacheShape shape;
+    const CacheTable* tables;           // keys, values
+    CacheRows rows[2];
+    CacheRotary rotary;
+    const int64_t* slots;
+    uint32_t* pages;
+    uint32_t* flags;
+    int64_t tokens, num_slots;
+    uint32_t seed_lo, seed_hi, layer, step;
+    int32_t unbiased;
+};
+
+struct CacheReadArgs {
+    CacheShape shape;
+    const CacheTable* tables;
+    CacheRows rows[2];
+    const int64_t* slots;
+    const uint32_t* pages;
+    uint32_t* flags;
+    int64_t tokens, num_slots;
+};
+
+struct CacheAttendArgs {
+    CacheShape shape;
+    const CacheTable* tables;
+    CacheRows queries, out;
+    CacheRotary rotary;
+    const uint32_t* pages;
+    const int32_t* table;               // [batch][table_width] page numbers
+    const int32_t* lengths;
+    float* lse;                         // [batch][heads * group] or NULL
+    float* partial;                     // workspace, see lq_cache_attend.cuh
+    uint32_t* flags;
+    int64_t num_pages, table_width, window;
+    float scale;                        // of the scores, times log2(e)
+    int32_t batch, group, group_blocks; // queries a head, and their blocks of 8
+    int32_t grid;
+    int32_t split;                      // whether a sequence may be split over CTAs at all
+};
+
+cudaError_t launch_cache_write(const CacheWriteArgs& a, cudaStream_t s);
+cudaError_t launch_cache_read(const CacheReadArgs& a, cudaStream_t s);
+
+// One of each per padded head size (lq_cache_attend_<size>.cu).
+cudaError_t launch_cache_attend_64(const CacheAttendArgs& a, cudaStream_t s);
+cudaError_t launch_cache_attend_128(const CacheAttendArgs& a, cudaStream_t s);
+cudaError_t launch_cache_attend_256(const CacheAttendArgs& a, cudaStream_t s);
+// CTAs of the attention kernel that an SM holds at once, and what each may leave in the workspace: a record, then two partial
+// sums of 8 queries.
+__host__ __device__ constexpr int cache_attend_resident(int padded, int bits_k, int bits_v) { return padded == 256 || bits_k + bits_v > 8 ? 1 : 2; }
+constexpr int kCacheRecordBytes = 16;
+constexpr int cache_partial_floats(int padded) { return 8 * (padded + 4); }
+
+}  // namespace lq
