@@ -14,7 +14,7 @@ using namespace lq;
 
 struct lq_cache {
     CacheShape shape{};
-    int32_t layers = 0, bits[2] = {0, 0}, device = 0, grid = 0;
+    int32_t layers = 0, bits[2] = {0, 0}, device = 0, sms = 0;
     uint64_t seed = 0;
     CacheTable* tables = nullptr;          // dev [layers][2]
     uint32_t* flags = nullptr;             // dev [1]
@@ -131,7 +131,7 @@ int check_slots(const lq_cache* c, int64_t tokens, const int64_t* slots)
 
 int64_t workspace_of(const lq_cache* c)
 {
-    return (int64_t)c->grid * (kCacheRecordBytes + 2 * 4 * cache_partial_floats(c->shape.padded));
+    return (int64_t)c->sms * cache_attend_teams(c->shape.padded) * (kCacheRecordBytes + 2 * 4 * cache_partial_floats(c->shape.padded));
 }
 
 #define LQ_TRY(expr) do { const int c_ = (expr); if (c_ != LQ_OK) return c_; } while (0)
@@ -185,9 +185,8 @@ int lq_cache_create(lq_cache** out, int32_t num_layers, int32_t kv_heads, int32_
             std::memcpy(&c->levels[((size_t)m * 2 + k) * kCacheLevels], t.levels, sizeof t.levels);
         }
     }
-    int sms = 0;
     cudaError_t e = cudaGetDevice(&c->device);
-    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, c->device);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&c->sms, cudaDevAttrMultiProcessorCount, c->device);
     if (e == cudaSuccess) e = cudaMalloc(reinterpret_cast<void**>(&c->tables), host.size() * sizeof(CacheTable));
     if (e == cudaSuccess) e = cudaMemcpy(c->tables, host.data(), host.size() * sizeof(CacheTable), cudaMemcpyHostToDevice);
     if (e == cudaSuccess) e = cudaMalloc(reinterpret_cast<void**>(&c->flags), sizeof(uint32_t));
@@ -198,7 +197,6 @@ int lq_cache_create(lq_cache** out, int32_t num_layers, int32_t kv_heads, int32_
         delete c;
         return lq_set_error(e == cudaErrorMemoryAllocation ? LQ_ENOMEM : LQ_ECUDA, "cache setup: %s", cudaGetErrorString(e));
     }
-    c->grid = sms * cache_attend_resident(s.padded, s.sym_bits[0], s.sym_bits[1]);
     *out = c;
     return LQ_OK;
 }
@@ -333,7 +331,7 @@ int lq_cache_attend(lq_cache* cache, int32_t layer, const lq_rows* queries, int6
     a.group = heads / s.heads; a.group_blocks = (a.group + 7) / 8;
     // the dealing out of work multiplies its units with the grid in 64 bits
     const double tokens = (double)std::min<int64_t>(table_width << s.page_shift, INT32_MAX);
-    if ((tokens / 128 + 1) * (double)batch * s.heads * a.group_blocks * cache->grid > 4e18)
+    if ((tokens / 128 + 1) * (double)batch * s.heads * a.group_blocks * cache->sms * 2 > 4e18)
         return lq_set_error(LQ_EINVAL, "batch, heads and table_width are too large together");
     if (batch == 0) return LQ_OK;
     a.shape = s; a.tables = cache->tables + (size_t)layer * 2;
@@ -341,7 +339,7 @@ int lq_cache_attend(lq_cache* cache, int32_t layer, const lq_rows* queries, int6
     a.num_pages = num_pages; a.table_width = table_width; a.window = window;
     a.scale = scale * 1.44269504088896341f;
     a.batch = (int32_t)batch;
-    a.grid = cache->grid;
+    a.sms = cache->sms;
     // 128 tokens are one unit, which is never split
     int64_t tiles = (table_width << s.page_shift) / 16;
     if (window > 0) tiles = std::min(tiles, window / 16 + 2);

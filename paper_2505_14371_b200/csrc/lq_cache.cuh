@@ -88,7 +88,7 @@ struct CacheAttendArgs {
     int64_t num_pages, table_width, window;
     float scale;                        // of the scores, times log2(e)
     int32_t batch, group, group_blocks; // queries a head, and their blocks of 8
-    int32_t grid;
+    int32_t sms;                        // CTAs
     int32_t split;                      // whether a sequence may be split over CTAs at all
 };
 
@@ -99,9 +99,9 @@ cudaError_t launch_cache_read(const CacheReadArgs& a, cudaStream_t s);
 cudaError_t launch_cache_attend_64(const CacheAttendArgs& a, cudaStream_t s);
 cudaError_t launch_cache_attend_128(const CacheAttendArgs& a, cudaStream_t s);
 cudaError_t launch_cache_attend_256(const CacheAttendArgs& a, cudaStream_t s);
-// CTAs of the attention kernel that an SM holds at once, and what each may leave in the workspace: a record, then two partial
-// sums of 8 queries.
-__host__ __device__ constexpr int cache_attend_resident(int padded, int bits_k, int bits_v) { return padded == 256 || bits_k + bits_v > 8 ? 1 : 2; }
+// Teams of 8 warps that share an SM in the attention kernel (its registers: rows of 256 need twice as many a thread), and what
+// each may leave in the workspace: a record, then two partial sums of 8 queries.
+__host__ __device__ constexpr int cache_attend_teams(int padded) { return padded == 256 ? 1 : 2; }
 constexpr int kCacheRecordBytes = 16;
 constexpr int cache_partial_floats(int padded) { return 8 * (padded + 4); }
 

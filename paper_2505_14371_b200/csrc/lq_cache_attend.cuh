@@ -24,40 +24,76 @@
 // coordinate in a register: with 4 bits two rows' words are merged into bytes of the two tokens (4 instructions for 16
 // coordinates) before the look-up.
 //
-// Split.  Units of 128 tokens (8 warps x 16) of all (sequence, head, 8 queries) in a row are dealt out evenly to a grid that
-// the GPU holds at once; every CTA finds its share from the lengths, on the device.  A CTA that has all of a
-// segment (sequence, head, 8 queries) writes its output; the others leave partial sums in the workspace, at most two a CTA, and the CTA
-// where a segment begins leaves a record of it, from which a second kernel joins them in the order of the CTAs.
+// Feeding.  The codes and norms of a tile are four runs of a page.  A warp copies them by 16-byte cp.async into stages of shared
+// memory of its own, kStages tiles deep, so nothing but a wait for its own copies stands between warps.  In a stage the tokens are four
+// groups of 4 rows with a gap behind each, and the tile's tokens are dealt to the rows of the operands (token_row) such that
+// both the keys' and the values' reads meet every bank once.
+//
+// Split.  Units of 128 tokens (8 warps x 16) of all (sequence, head, 8 queries) in a row are dealt out evenly to teams of 8 warps, as
+// many as the GPU holds at once (two a CTA, which share the look-up table; one for rows of 256); every team finds its
+// share from the lengths, on the device.  A team that has all of a segment (sequence, head, 8 queries) writes its output; the others leave
+// partial sums in the workspace, at most two a team, and the team where a segment begins leaves a record of it, from which a
+// second kernel joins them in the order of the teams.
 #pragma once
 
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
 #include "lq_cache.cuh"
+#include "lq_internal.cuh"
 
 namespace lq {
 namespace attend {
 
-constexpr int kWarps = 8;
-constexpr int kThreads = 32 * kWarps;
+constexpr int kTeamWarps = 8;
+constexpr int kTeam = 32 * kTeamWarps;  // threads
 constexpr int kTile = 16;               // tokens of a warp at a time
 constexpr int kQueries = 8;             // queries a segment
 constexpr int kTableBytes = 256 * 256;  // entry e: 32 copies for the keys, 32 for the values
+constexpr int kStageBytes = 148 << 10;  // for the stages of all warps
 constexpr float kLow = -1e30f;          // a reference before its first score
 constexpr float kSlack = 8.0f;          // how far (log2) a score may pass its reference
 constexpr float kLift = 6.0f;           // weights are 2^kLift at their reference: at most 2^14 as fp16, and exact down to 2^-20
 
-// Workspace: `grid` records of 16 bytes, then 2 * grid partials of kQueries * (padded + 4) floats (sums; reference, reference
-// of the weights, denominator, unused).
+// Workspace: a record for every team, then two partials of kCacheRecordBytes a team (sums; reference, reference of the weights,
+// denominator, unused).
 struct Record { int32_t sequence, head_block, last, pad; };
 static_assert(sizeof(Record) == kCacheRecordBytes && kQueries == 8, "the workspace is sized by lq_cache.cuh");
 template <int P>
 constexpr int64_t kPartial = cache_partial_floats(P);
 
+// A tile of one warp in shared memory: keys, values, 16 norms of keys, 16 of values.
+template <int P, int WK, int WV>
+struct Stage {
+    static constexpr int kRowK = P * WK / 8, kRowV = P * WV / 8;                            // bytes
+    // Gap behind each group of 4 rows.  Values: lane t's rows sit in group t or t ^ 1, and a phase of a read takes 32 bytes
+    // of each of four rows: 32.  Keys: a phase takes 32 or 64 bytes of rows whose groups are neighbours.
+    static constexpr int kGapK = kRowK == 64 ? 0 : 64, kGapV = 32;
+    static constexpr int kGroupK = 4 * kRowK + kGapK, kGroupV = 4 * kRowV + kGapV;
+    static constexpr int kValues = 4 * kGroupK, kNorms = kValues + 4 * kGroupV, kBytes = kNorms + 8 * kTile;
+    static constexpr int kTeams = cache_attend_teams(P), kWarps = kTeams * kTeamWarps;
+    static constexpr int kFit = kStageBytes / (kWarps * kBytes);
+    static constexpr int kStages = kFit > 6 ? 6 : kFit;
+    static constexpr int kWarpBytes = kStages * kBytes;
+    static constexpr int kSumBytes = kQueries * (P + 4) * 4;                                // a warp's sums, in its stages' place
+    static_assert(kStages >= 2 && kWarpBytes >= kSumBytes && kBytes % 16 == 0, "stages");
+};
+
 template <int P>
-__host__ __device__ constexpr int combine_bytes() { return kWarps * 2 * 4 * (P + 4) * 4; }
-template <int P>
-__host__ __device__ constexpr int smem_bytes() { return kTableBytes + combine_bytes<P>() + 2 * kQueries * (P + 8) * 2 + (kQueries + kWarps * kQueries * 3 + kQueries * (kWarps + 4) + 64) * 4; }
+struct TeamShared {
+    int64_t words[18];                  // schedule
+    float factor[kQueries];             // scale * log2(e) / the query's power of two
+    float stats[kTeamWarps][kQueries][3];
+    float share[kQueries][kTeamWarps + 4];      // factor of each warp's sums; then ref, ref_w, total
+    alignas(16) __half q[2][kQueries][P + 8];   // the queries, and what their rounding left
+};
+
+template <int P, int WK, int WV>
+constexpr int smem_bytes()
+{
+    using X = Stage<P, WK, WV>;
+    return kTableBytes + X::kWarps * X::kWarpBytes + X::kTeams * (int)sizeof(TeamShared<P>);
+}
 
 __device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 __device__ __forceinline__ float lg2(float x) { float y; asm("lg2.approx.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
@@ -94,6 +130,17 @@ __device__ __forceinline__ uint32_t look(const char* table, uint32_t w, uint32_t
     return *reinterpret_cast<const uint32_t*>(table + __byte_perm(w, lane_base, 0x5504 | (kByte << 4)));
 }
 
+__device__ __forceinline__ void copy16(uint32_t to, const void* from)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to), "l"(from) : "memory");
+}
+__device__ __forceinline__ void commit_copies() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int kLeft>
+__device__ __forceinline__ void wait_copies() { asm volatile("cp.async.wait_group %0;" :: "n"(kLeft) : "memory"); }
+
+// Barrier of one team.
+__device__ __forceinline__ void team_sync(int team) { asm volatile("bar.sync %0, %1;" :: "r"(team + 1), "n"(kTeam) : "memory"); }
+
 __device__ __forceinline__ float load_any(const CacheRows& r, int64_t at)
 {
     if (r.type == LQ_F32) return static_cast<const float*>(r.data)[at];
@@ -112,7 +159,7 @@ __device__ __forceinline__ void store_any(const CacheRows& r, int64_t at, float 
 struct Extent {
     int64_t first, length;
     int64_t tile0, tile1;
-    __device__ __forceinline__ int64_t units() const { return (tile1 - tile0 + kWarps - 1) / kWarps; }
+    __device__ __forceinline__ int64_t units() const { return (tile1 - tile0 + kTeamWarps - 1) / kTeamWarps; }
 };
 
 __device__ __forceinline__ Extent extent_of(const CacheAttendArgs& a, int sequence)
@@ -128,6 +175,38 @@ __device__ __forceinline__ Extent extent_of(const CacheAttendArgs& a, int sequen
     return e;
 }
 
+// Which token of a tile is row r of the operands (row r + 8: two tokens on): rows 2t and 2t + 1, which lane t holds of the
+// values, are in groups t and t ^ 1.
+__device__ __forceinline__ int token_row(int r)
+{
+    const int t = r >> 1;
+    return (r & 1) ? 4 * (t ^ 1) + 1 : 4 * t;
+}
+
+// Starts the copies of the tile at `row0` of a page into the stage at `to` (shared address).
+template <int P, int WK, int WV>
+__device__ __forceinline__ void copy_tile(uint32_t to, const char* head, int page_shift, int row0, int lane)
+{
+    using X = Stage<P, WK, WV>;
+    auto section = [&](const char* from, uint32_t at, auto row_bytes, auto gap) {
+        constexpr int kRow = decltype(row_bytes)::value, kGap = decltype(gap)::value, kPieces = kRow;      // 16 rows of kRow / 16 pieces
+#pragma unroll
+        for (int i = 0; i < kPieces; i += 32) {
+            // a group of 4 rows is kRow / 4 pieces
+            const int piece = i + lane;
+            copy16(at + piece * 16 + piece / (kRow / 4) * kGap, from + piece * 16);
+        }
+    };
+    const char* keys = head + row0 * X::kRowK;
+    const char* values = head + (X::kRowK << page_shift) + row0 * X::kRowV;
+    section(keys, to, std::integral_constant<int, X::kRowK>(), std::integral_constant<int, X::kGapK>());
+    section(values, to + X::kValues, std::integral_constant<int, X::kRowV>(), std::integral_constant<int, X::kGapV>());
+    if (lane < 8) {
+        const char* norms = head + ((X::kRowK + X::kRowV) << page_shift) + row0 * 4 + ((lane & 4) << page_shift);
+        copy16(to + X::kNorms + lane * 16, norms + (lane & 3) * 16);
+    }
+}
+
 // Codes and norms of one tile, as one warp's lanes hold them.
 template <int P, int WK, int WV>
 struct Tile {
@@ -136,52 +215,39 @@ struct Tile {
     static constexpr int kKeyChunks = kKeyBytes / kKeyChunk, kValueChunks = kValueBytes / kValueChunk;
     uint32_t k[2][kKeyBytes / 4];       // rows lane / 4 and lane / 4 + 8
     uint32_t v[4][kValueBytes / 4];     // rows 2t, 2t+1, 2t+8, 2t+9 with t = lane % 4
-    float nk[2], nv[2];                 // norms of rows lane / 4 and lane / 4 + 8
 };
 
 template <int kBytes>
-__device__ __forceinline__ void load_run(uint32_t* to, const uint32_t* from)
+__device__ __forceinline__ void take_run(uint32_t* to, const char* from)
 {
-    if constexpr (kBytes == 16) *reinterpret_cast<uint4*>(to) = __ldg(reinterpret_cast<const uint4*>(from));
-    else if constexpr (kBytes == 8) *reinterpret_cast<uint2*>(to) = __ldg(reinterpret_cast<const uint2*>(from));
-    else *to = __ldg(from);
+    if constexpr (kBytes == 16) *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(from);
+    else if constexpr (kBytes == 8) *reinterpret_cast<uint2*>(to) = *reinterpret_cast<const uint2*>(from);
+    else *to = *reinterpret_cast<const uint32_t*>(from);
 }
 
+// `keys`: the stage, at this lane's place in the row of token_row(lane / 4).
 template <int P, int WK, int WV>
-__device__ __forceinline__ void load_tile(Tile<P, WK, WV>& t, const CacheAttendArgs& a, int page, int row0, int head, int lane)
+__device__ __forceinline__ void take_keys(Tile<P, WK, WV>& t, const char* keys)
 {
     using X = Tile<P, WK, WV>;
-    constexpr int kRowK = P * WK / 32, kRowV = P * WV / 32;
-    if (page < 0) {                     // not there: the tile's tokens are masked; its codes have to be something
-#pragma unroll
-        for (int r = 0; r < 2; ++r)
-#pragma unroll
-            for (int i = 0; i < X::kKeyBytes / 4; ++i) t.k[r][i] = 0;
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-#pragma unroll
-            for (int i = 0; i < X::kValueBytes / 4; ++i) t.v[r][i] = 0;
-        t.nk[0] = t.nk[1] = t.nv[0] = t.nv[1] = 0.0f;
-        return;
-    }
-    const int page_size = 1 << a.shape.page_shift, g = lane >> 2, q = lane & 3;
-    const uint32_t* base = a.pages + page * a.shape.page_words + head * a.shape.head_words;
-    const uint32_t* keys = base + (row0 + g) * kRowK;
 #pragma unroll
     for (int r = 0; r < 2; ++r)
 #pragma unroll
         for (int c = 0; c < X::kKeyChunks; ++c)
-            load_run<X::kKeyChunk>(&t.k[r][c * X::kKeyChunk / 4], keys + 8 * r * kRowK + (4 * c + q) * (X::kKeyChunk / 4));
-    const uint32_t* values = base + page_size * kRowK + (row0 + 2 * q) * kRowV;
+            take_run<X::kKeyChunk>(&t.k[r][c * X::kKeyChunk / 4], keys + 2 * r * Stage<P, WK, WV>::kRowK + 4 * c * X::kKeyChunk);
+}
+
+// `even`, `odd`: likewise in the rows of token_row(2t) and token_row(2t + 1).
+template <int P, int WK, int WV>
+__device__ __forceinline__ void take_values(Tile<P, WK, WV>& t, const char* even, const char* odd)
+{
+    using X = Tile<P, WK, WV>;
 #pragma unroll
     for (int r = 0; r < 4; ++r)
 #pragma unroll
         for (int c = 0; c < X::kValueChunks; ++c)
-            load_run<X::kValueChunk>(&t.v[r][c * X::kValueChunk / 4],
-                                     values + ((r & 1) + 8 * (r >> 1)) * kRowV + (8 * c + g) * (X::kValueChunk / 4));
-    const float* norms = reinterpret_cast<const float*>(base + page_size * (kRowK + kRowV)) + row0 + g;
-    t.nk[0] = __ldg(norms); t.nk[1] = __ldg(norms + 8);
-    t.nv[0] = __ldg(norms + page_size); t.nv[1] = __ldg(norms + page_size + 8);
+            take_run<X::kValueChunk>(&t.v[r][c * X::kValueChunk / 4],
+                                     (r & 1 ? odd : even) + (r >> 1) * 2 * Stage<P, WK, WV>::kRowV + 8 * c * X::kValueChunk);
 }
 
 // kExact 0: q is one fp16 number; 1: a sum of two; 2: q and the weights are.
@@ -275,31 +341,9 @@ __device__ __forceinline__ int key_coordinate(int s, int t)
     return (4 * c + t) * kEach + 4 * s % kEach;
 }
 
-// Where the shared memory's parts are.
-template <int P>
-struct Shared {
-    char* table;
-    float* combine;                     // [warp][query % 2][query / 2][P + 4]
-    __half* q;                          // [2][kQueries][P + 8]: q, and what its rounding left
-    float* factor;                      // [kQueries]: scale * log2(e) / the query's power of two
-    float* stats;                       // [warp][kQueries][3]
-    float* share;                       // [kQueries][kWarps + 4]: factor of each warp's sums; then ref, ref_w, total
-    int64_t* words;                     // [32] for the schedule
-    __device__ explicit Shared(char* s)
-    {
-        table = s;
-        combine = reinterpret_cast<float*>(s + kTableBytes);
-        words = reinterpret_cast<int64_t*>(s + kTableBytes + combine_bytes<P>());
-        q = reinterpret_cast<__half*>(words + 32);
-        factor = reinterpret_cast<float*>(q + 2 * kQueries * (P + 8));
-        stats = factor + kQueries;
-        share = stats + kWarps * kQueries * 3;
-    }
-};
-
 // Warp `w` brings query w of the block into shared memory: rotated, times its power of two, as fp16 and the rest.
 template <int P>
-__device__ __forceinline__ void stage_query(const Shared<P>& sh, const CacheAttendArgs& a, int sequence, int head, int block, int w, int lane, int64_t length)
+__device__ __forceinline__ void stage_query(TeamShared<P>& sh, const CacheAttendArgs& a, int sequence, int head, int block, int w, int lane, int64_t length)
 {
     const int query = block * kQueries + w;
     float x[P / 32];
@@ -343,57 +387,63 @@ __device__ __forceinline__ void stage_query(const Shared<P>& sh, const CacheAtte
     for (int i = 0; i < P / 32; ++i) {
         const float y = x[i] * up;
         const __half h = __float2half_rn(y);
-        sh.q[w * (P + 8) + lane + 32 * i] = h;
-        sh.q[(kQueries + w) * (P + 8) + lane + 32 * i] = __float2half_rn(y - __half2float(h));
+        sh.q[0][w][lane + 32 * i] = h;
+        sh.q[1][w][lane + 32 * i] = __float2half_rn(y - __half2float(h));
     }
     if (lane == 0) sh.factor[w] = a.scale * down;
 }
 
 template <int P, int WK, int WV, int kExact>
-__global__ void __launch_bounds__(kThreads, cache_attend_resident(P, WK, WV)) attend_kernel(const __grid_constant__ CacheAttendArgs a)
+__global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_kernel(const __grid_constant__ CacheAttendArgs a)
 {
+    using X = Stage<P, WK, WV>;
+    using T = Tile<P, WK, WV>;
     extern __shared__ __align__(128) char smem[];
-    const Shared<P> sh(smem);
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
+    char* const table = smem;
+    const int team = threadIdx.x / kTeam, tid = threadIdx.x % kTeam, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
+    char* const stages = smem + kTableBytes + (team * kTeamWarps + warp) * X::kWarpBytes;
+    TeamShared<P>& sh = reinterpret_cast<TeamShared<P>*>(smem + kTableBytes + X::kWarps * X::kWarpBytes)[team];
 
-    {   // the look-up table: thread e writes the copies of entry e, a warp's lanes at different banks
-        const uint32_t k = __ldg(a.tables[LQ_KEYS].pairs + tid), v = __ldg(a.tables[LQ_VALUES].pairs + tid);
-        uint4* row = reinterpret_cast<uint4*>(sh.table + tid * 256);
+    {   // the look-up table: a thread writes copies of one entry, a warp's lanes at different banks
+        const bool mine = X::kTeams == 1 || team == 0, other = X::kTeams == 1 || team == 1;
+        const uint32_t k = mine ? __ldg(a.tables[LQ_KEYS].pairs + tid) : 0, v = other ? __ldg(a.tables[LQ_VALUES].pairs + tid) : 0;
+        uint4* row = reinterpret_cast<uint4*>(table + tid * 256);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            row[(j + lane) & 7] = make_uint4(k, k, k, k);
-            row[8 + ((j + lane) & 7)] = make_uint4(v, v, v, v);
+            if (mine) row[(j + lane) & 7] = make_uint4(k, k, k, k);
+            if (other) row[8 + ((j + lane) & 7)] = make_uint4(v, v, v, v);
         }
     }
+    pdl_wait();
+    pdl_launch_next();
 
-    // ---- this CTA's share of all units
-    const int head_blocks = a.shape.heads * a.group_blocks;
+    // ---- this team's share of all units
+    const int head_blocks = a.shape.heads * a.group_blocks, me = blockIdx.x * X::kTeams + team, teams = gridDim.x * X::kTeams;
     int64_t sum = 0;
-    for (int b = tid; b < a.batch; b += kThreads) {
+    for (int b = tid; b < a.batch; b += kTeam) {
         sum += extent_of(a, b).units();
         const int n = __ldg(a.lengths + b);
-        if (blockIdx.x == 0 && (n < 0 || n > a.table_width << a.shape.page_shift)) atomicOr(a.flags, LQ_CACHE_BAD_LENGTH);
+        if (me == 0 && (n < 0 || n > a.table_width << a.shape.page_shift)) atomicOr(a.flags, LQ_CACHE_BAD_LENGTH);
     }
 #pragma unroll
     for (int o = 16; o > 0; o /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     if (lane == 0) sh.words[warp] = sum;
-    if (tid == 0) sh.words[16] = -1;
-    __syncthreads();
+    __syncthreads();                    // (the table is there too)
     int64_t all = 0;
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) all += sh.words[w];
+    for (int w = 0; w < kTeamWarps; ++w) all += sh.words[w];
     all *= head_blocks;
-    // no more CTAs than units take part, so that none between two that share a segment is without a unit
-    const int64_t grid = min(all, (int64_t)gridDim.x);
-    const int64_t begin = blockIdx.x < grid ? all * blockIdx.x / grid : 0, end = blockIdx.x < grid ? all * (blockIdx.x + 1) / grid : 0;
+    // no more teams than units take part, so that none between two that share a segment is without a unit
+    const int64_t parts = min(all, (int64_t)teams);
+    const int64_t begin = me < parts ? all * me / parts : 0, end = me < parts ? all * (me + 1) / parts : 0;
     Record* records = reinterpret_cast<Record*>(a.partial);
-    float* partials = a.partial + (int64_t)gridDim.x * (sizeof(Record) / 4);
-    if (tid == 0) records[blockIdx.x].sequence = -1;
+    float* partials = a.partial + (int64_t)teams * (sizeof(Record) / 4);
+    if (tid == 0) records[me].sequence = -1;
 
     if (begin < end) {
         // the sequence that unit `begin` belongs to, and the units before it
         int64_t before = 0;
-        for (int base = 0; base < a.batch; base += kThreads) {
+        for (int base = 0; base < a.batch; base += kTeam) {
             const int b = base + tid;
             const int64_t mine = b < a.batch ? extent_of(a, b).units() * head_blocks : 0;
             int64_t scan = mine;
@@ -402,12 +452,12 @@ __global__ void __launch_bounds__(kThreads, cache_attend_resident(P, WK, WV)) at
                 const int64_t up = __shfl_up_sync(0xffffffffu, scan, o);
                 if (lane >= o) scan += up;
             }
-            __syncthreads();
+            team_sync(team);
             if (lane == 31) sh.words[warp] = scan;
-            __syncthreads();
+            team_sync(team);
             int64_t whole = 0;
 #pragma unroll
-            for (int w = 0; w < kWarps; ++w) {
+            for (int w = 0; w < kTeamWarps; ++w) {
                 if (w == warp) scan += before + whole;
                 whole += sh.words[w];
             }
@@ -415,29 +465,61 @@ __global__ void __launch_bounds__(kThreads, cache_attend_resident(P, WK, WV)) at
             before += whole;
             if (before > begin) break;
         }
-        __syncthreads();
+        team_sync(team);
         int sequence = (int)sh.words[16];
         Extent x = extent_of(a, sequence);
         int64_t units = x.units();
         const int64_t offset = begin - sh.words[17];
         int hb = (int)(offset / units);
         int64_t chunk = offset - hb * units, at = begin;
-        const uint32_t base_k = 4 * lane, base_v = 128 + 4 * lane;
-        const int tile_shift = a.shape.page_shift - 4;
+
+        const uint32_t base_k = 4 * lane, base_v = 128 + 4 * lane, stage0 = (uint32_t)__cvta_generic_to_shared(stages);
+        const int tile_shift = a.shape.page_shift - 4, tile_mask = (1 << tile_shift) - 1;
+        // this lane's places in a stage
+        const int row = token_row(g), row_even = token_row(2 * t), row_odd = token_row(2 * t + 1);
+        const char* const keys = stages + (row >> 2) * X::kGroupK + (row & 3) * X::kRowK + t * T::kKeyChunk;
+        const char* const even = stages + X::kValues + (row_even >> 2) * X::kGroupV + (row_even & 3) * X::kRowV + g * T::kValueChunk;
+        const char* const odd = stages + X::kValues + (row_odd >> 2) * X::kGroupV + (row_odd & 3) * X::kRowV + g * T::kValueChunk;
+        const char* const norms = stages + X::kNorms + row * 4;
 
         while (at < end) {
-            const int64_t count = min(units - chunk, end - at);        // units of this segment that are ours
+            const int count = (int)min(units - chunk, end - at);       // units of this segment that are ours
             const int head = hb / a.group_blocks, block = hb - head * a.group_blocks;
-            __syncthreads();                                            // the last segment's shared memory has been read
+            // ---- the first copies: tile j of this warp is tile0 + 8 j of the sequence
+            const int32_t* pages = a.table + (int64_t)sequence * a.table_width;
+            const int tile0 = (int)(x.tile0 + chunk * kTeamWarps) + warp, stop = (int)min(x.tile1, x.tile0 + (chunk + count) * kTeamWarps);
+            const int tiles = stop > tile0 ? (stop - tile0 + kTeamWarps - 1) / kTeamWarps : 0;
+            const char* const bytes = reinterpret_cast<const char*>(a.pages) + head * a.shape.head_words * 4;
+            uint32_t missing = 0;                                       // bit s: the tile in stage s is on a page that is not there
+            int page = -1;                                              // lane l: of tile (32 i + l), i as far as copies are
+            auto start = [&](int j, int stage) {
+                if (j < tiles) {
+                    if (j % 32 == 0) {
+                        page = -1;
+                        if (j + lane < tiles) {
+                            page = __ldg(pages + ((tile0 + (j + lane) * kTeamWarps) >> tile_shift));
+                            if (page < 0 || page >= a.num_pages) { page = -1; atomicOr(a.flags, LQ_CACHE_BAD_PAGE); }
+                        }
+                    }
+                    const int p = __shfl_sync(0xffffffffu, page, j % 32);
+                    missing = p < 0 ? missing | 1u << stage : missing & ~(1u << stage);
+                    if (p >= 0)
+                        copy_tile<P, WK, WV>(stage0 + stage * X::kBytes, bytes + p * a.shape.page_words * 4, a.shape.page_shift,
+                                             ((tile0 + j * kTeamWarps) & tile_mask) * kTile, lane);
+                }
+                commit_copies();
+            };
+            for (int j = 0; j < X::kStages - 1; ++j) start(j, j);
+
             stage_query<P>(sh, a, sequence, head, block, warp, lane, x.length);
-            __syncthreads();
+            team_sync(team);
             uint32_t q[P / 16][2], q2[kExact ? P / 16 : 1][2];
 #pragma unroll
             for (int s = 0; s < P / 16; ++s) {
-                const uint2 w = *reinterpret_cast<const uint2*>(sh.q + g * (P + 8) + key_coordinate<P, WK>(s, t));
+                const uint2 w = *reinterpret_cast<const uint2*>(&sh.q[0][g][key_coordinate<P, WK>(s, t)]);
                 q[s][0] = w.x; q[s][1] = w.y;
                 if constexpr (kExact > 0) {
-                    const uint2 w2 = *reinterpret_cast<const uint2*>(sh.q + (kQueries + g) * (P + 8) + key_coordinate<P, WK>(s, t));
+                    const uint2 w2 = *reinterpret_cast<const uint2*>(&sh.q[1][g][key_coordinate<P, WK>(s, t)]);
                     q2[s][0] = w2.x; q2[s][1] = w2.y;
                 }
             }
@@ -445,33 +527,33 @@ __global__ void __launch_bounds__(kThreads, cache_attend_resident(P, WK, WV)) at
 
             Sums<P, WK, WV, kExact> S;
             S.clear();
-            const int32_t* row = a.table + (int64_t)sequence * a.table_width;
-            auto page_of = [&](int64_t tile) {
-                const int p = __ldg(row + (tile >> tile_shift));
-                if (p >= 0 && p < a.num_pages) return p;
-                if (lane == 0) atomicOr(a.flags, LQ_CACHE_BAD_PAGE);
-                return -1;
-            };
-            int64_t tile = x.tile0 + chunk * kWarps + warp;
-            const int64_t stop = min(x.tile1, x.tile0 + (chunk + count) * kWarps);
-            Tile<P, WK, WV> cur, next;
-            int page = -1, page_next = -1, page_after = -1;
-            if (tile < stop) { page = page_of(tile); }
-            if (tile + kWarps < stop) page_next = page_of(tile + kWarps);
-            if (tile < stop) load_tile<P, WK, WV>(cur, a, page, (int)(tile & ((1 << tile_shift) - 1)) * kTile, head, lane);
-            for (; tile < stop; tile += kWarps) {
-                const bool more = tile + kWarps < stop;
-                if (tile + 2 * kWarps < stop) page_after = page_of(tile + 2 * kWarps);
-                if (more) load_tile<P, WK, WV>(next, a, page_next, (int)((tile + kWarps) & ((1 << tile_shift) - 1)) * kTile, head, lane);
+            int stage = 0, ahead = X::kStages - 1;
+            for (int j = 0; j < tiles; ++j) {
+                __syncwarp();                                           // every lane has read the stage that is filled next
+                start(j + X::kStages - 1, ahead);
+                wait_copies<X::kStages - 1>();
+                __syncwarp();
+                const int place = stage * X::kBytes;
+                const bool there = !(missing >> stage & 1);
+                if (++stage == X::kStages) stage = 0;
+                if (++ahead == X::kStages) ahead = 0;
+                if (!there) continue;
 
+                T cur;
                 float c[4];
-                scores<P, WK, WV, (kExact > 0)>(c, cur, q, q2, sh.table, base_k);
-                const int64_t token = tile * kTile + g;
-                const bool in0 = page >= 0 && token >= x.first && token < x.length;
-                const bool in1 = page >= 0 && token + 8 >= x.first && token + 8 < x.length;
-                const float s0 = in0 ? c[0] * (f0 * cur.nk[0]) : -INFINITY, s1 = in0 ? c[1] * (f1 * cur.nk[0]) : -INFINITY;
-                const float s2 = in1 ? c[2] * (f0 * cur.nk[1]) : -INFINITY, s3 = in1 ? c[3] * (f1 * cur.nk[1]) : -INFINITY;
-                const float lv0 = in0 ? lg2(cur.nv[0]) : -INFINITY, lv1 = in1 ? lg2(cur.nv[1]) : -INFINITY;
+                take_keys(cur, keys + place);
+                scores<P, WK, WV, (kExact > 0)>(c, cur, q, q2, table, base_k);
+                const float nk0 = *reinterpret_cast<const float*>(norms + place), nk1 = *reinterpret_cast<const float*>(norms + place + 8);
+                const float nv0 = *reinterpret_cast<const float*>(norms + place + 64), nv1 = *reinterpret_cast<const float*>(norms + place + 72);
+                take_values(cur, even + place, odd + place);
+                float s0 = c[0] * (f0 * nk0), s1 = c[1] * (f1 * nk0), s2 = c[2] * (f0 * nk1), s3 = c[3] * (f1 * nk1);
+                float lv0 = lg2(nv0), lv1 = lg2(nv1);
+                const int64_t first = (int64_t)(tile0 + j * kTeamWarps) * kTile;
+                if (first < x.first || first + kTile > x.length) {      // the ends of what is seen
+                    const int64_t token = first + row;
+                    if (token < x.first || token >= x.length) s0 = s1 = lv0 = -INFINITY;
+                    if (token + 2 < x.first || token + 2 >= x.length) s2 = s3 = lv1 = -INFINITY;
+                }
                 const float w0 = s0 + lv0, w1 = s1 + lv0, w2 = s2 + lv1, w3 = s3 + lv1;
                 const float top0 = fmaxf(s0, s2), top1 = fmaxf(s1, s3), topw0 = fmaxf(w0, w2), topw1 = fmaxf(w1, w3);
                 const bool passed = top0 > S.ref[0] + kSlack || top1 > S.ref[1] + kSlack || topw0 > S.ref_w[0] + kSlack || topw1 > S.ref_w[1] + kSlack;
@@ -503,12 +585,10 @@ __global__ void __launch_bounds__(kThreads, cache_attend_resident(P, WK, WV)) at
                     b2[0] = transposed(halves(r0.x, r0.y));
                     b2[1] = transposed(halves(r1.x, r1.y));
                 }
-                weigh<P, WK, WV, (kExact == 2)>(S.acc, cur, b, b2, sh.table, base_v);
-                if (more) cur = next;
-                page = page_next; page_next = page_after;
+                weigh<P, WK, WV, (kExact == 2)>(S.acc, cur, b, b2, table, base_v);
             }
 
-            // ---- the warps' sums added up
+            // ---- the warps' sums added up, through the stages
 #pragma unroll
             for (int o = 4; o < 32; o *= 2) {
                 S.total[0] += __shfl_xor_sync(0xffffffffu, S.total[0], o);
@@ -517,47 +597,46 @@ __global__ void __launch_bounds__(kThreads, cache_attend_resident(P, WK, WV)) at
             if (g == 0) {
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    float* st = sh.stats + (warp * kQueries + 2 * t + i) * 3;
+                    float* st = sh.stats[warp][2 * t + i];
                     st[0] = S.ref[i]; st[1] = S.ref_w[i]; st[2] = S.total[i];
                 }
             }
+            wait_copies<0>();
+            __syncwarp();
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                float* to = sh.combine + ((warp * 2 + i) * 4 + t) * (P + 4);
+                float* to = reinterpret_cast<float*>(stages) + (i * 4 + t) * (P + 4);
 #pragma unroll
                 for (int m = 0; m < P / 16; m += 2)
                     *reinterpret_cast<float4*>(to + value_coordinate<P, WV>(m, g)) =
                         make_float4(S.acc[m][i], S.acc[m][2 + i], S.acc[m + 1][i], S.acc[m + 1][2 + i]);
             }
-            __syncthreads();
+            team_sync(team);
             if (tid < kQueries) {
                 float r = kLow, rw = kLow, total = 0.0f;
-                for (int w = 0; w < kWarps; ++w) {
-                    const float* st = sh.stats + (w * kQueries + tid) * 3;
-                    r = fmaxf(r, st[0]); rw = fmaxf(rw, st[1]);
+                for (int w = 0; w < kTeamWarps; ++w) { r = fmaxf(r, sh.stats[w][tid][0]); rw = fmaxf(rw, sh.stats[w][tid][1]); }
+                for (int w = 0; w < kTeamWarps; ++w) {
+                    total += sh.stats[w][tid][2] * ex2(sh.stats[w][tid][0] - r);
+                    sh.share[tid][w] = ex2(sh.stats[w][tid][1] - rw);
                 }
-                for (int w = 0; w < kWarps; ++w) {
-                    const float* st = sh.stats + (w * kQueries + tid) * 3;
-                    total += st[2] * ex2(st[0] - r);
-                    sh.share[tid * (kWarps + 4) + w] = ex2(st[1] - rw);
-                }
-                float* o = sh.share + tid * (kWarps + 4) + kWarps;
-                o[0] = r; o[1] = rw; o[2] = total;
+                sh.share[tid][kTeamWarps] = r; sh.share[tid][kTeamWarps + 1] = rw; sh.share[tid][kTeamWarps + 2] = total;
             }
-            __syncthreads();
-            const bool starts = chunk == 0, whole = starts && chunk + count == units;
-            const int slot = 2 * blockIdx.x + starts;
-            for (int i = tid; i < kQueries * P / 4; i += kThreads) {
+            team_sync(team);
+            const bool starts = chunk == 0, whole = starts && count == units;
+            const int slot = 2 * me + starts;
+            const char* const team_stages = smem + kTableBytes + team * kTeamWarps * X::kWarpBytes;
+            for (int i = tid; i < kQueries * P / 4; i += kTeam) {
                 const int query = i / (P / 4), d = (i % (P / 4)) * 4;
-                const float* share = sh.share + query * (kWarps + 4);
+                const float* share = sh.share[query];
                 float4 sum4 = make_float4(0, 0, 0, 0);
 #pragma unroll
-                for (int w = 0; w < kWarps; ++w) {
-                    const float4 v = *reinterpret_cast<const float4*>(sh.combine + ((w * 2 + (query & 1)) * 4 + (query >> 1)) * (P + 4) + d);
+                for (int w = 0; w < kTeamWarps; ++w) {
+                    const float4 v = *reinterpret_cast<const float4*>(
+                        reinterpret_cast<const float*>(team_stages + w * X::kWarpBytes) + ((query & 1) * 4 + (query >> 1)) * (P + 4) + d);
                     const float f = share[w];
                     sum4.x += v.x * f; sum4.y += v.y * f; sum4.z += v.z * f; sum4.w += v.w * f;
                 }
-                const float r = share[kWarps], rw = share[kWarps + 1], total = share[kWarps + 2];
+                const float r = share[kTeamWarps], rw = share[kTeamWarps + 1], total = share[kTeamWarps + 2];
                 if (whole) {
                     if (block * kQueries + query < a.group) {
                         const float f = total != 0.0f ? ex2(rw - r - kLift) / total : 0.0f;
@@ -576,12 +655,11 @@ __global__ void __launch_bounds__(kThreads, cache_attend_resident(P, WK, WV)) at
                 }
             }
             if (starts && !whole && tid == 0) {
-                // the CTA that has the segment's last unit: the largest c whose share begins at or before it
+                // the team that has the segment's last unit: the largest one whose share begins at or before it
                 const int64_t unit = at + units - 1;
-                const int64_t c = ((unit + 1) * grid - 1) / all;
                 Record rec;
-                rec.sequence = sequence; rec.head_block = hb; rec.last = (int32_t)c; rec.pad = 0;
-                records[blockIdx.x] = rec;
+                rec.sequence = sequence; rec.head_block = hb; rec.last = (int32_t)(((unit + 1) * parts - 1) / all); rec.pad = 0;
+                records[me] = rec;
             }
             at += count;
             chunk = 0;
@@ -589,23 +667,26 @@ __global__ void __launch_bounds__(kThreads, cache_attend_resident(P, WK, WV)) at
                 hb = 0;
                 do { x = extent_of(a, ++sequence); units = x.units(); } while (units == 0);
             }
+            team_sync(team);                                            // the sums have been read
         }
     }
 
     // sequences without a token to see
-    for (int b = blockIdx.x; b < a.batch; b += gridDim.x) {
+    for (int b = me; b < a.batch; b += teams) {
         if (extent_of(a, b).units() > 0) continue;
         const int queries = a.shape.heads * a.group;
-        for (int64_t i = tid; i < (int64_t)queries * a.shape.dim; i += kThreads)
+        for (int64_t i = tid; i < (int64_t)queries * a.shape.dim; i += kTeam)
             store_any(a.out, b * a.out.token_stride + (i / a.shape.dim) * a.out.head_stride + i % a.shape.dim, 0.0f);
-        if (a.lse) for (int i = tid; i < queries; i += kThreads) a.lse[(int64_t)b * queries + i] = -INFINITY;
+        if (a.lse) for (int i = tid; i < queries; i += kTeam) a.lse[(int64_t)b * queries + i] = -INFINITY;
     }
 }
 
-// Joins the partial sums of a segment that began in CTA `blockIdx.x` and went on in others; a warp a query.
+// Joins the partial sums of a segment that began in team `blockIdx.x` and went on in others; a warp a query.
 template <int P>
-__global__ void __launch_bounds__(kThreads) attend_join_kernel(const __grid_constant__ CacheAttendArgs a)
+__global__ void __launch_bounds__(kTeam) attend_join_kernel(const __grid_constant__ CacheAttendArgs a)
 {
+    pdl_wait();
+    pdl_launch_next();
     const Record rec = reinterpret_cast<const Record*>(a.partial)[blockIdx.x];
     if (rec.sequence < 0) return;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -645,11 +726,14 @@ __global__ void __launch_bounds__(kThreads) attend_join_kernel(const __grid_cons
 template <int P, int WK, int WV, int kExact>
 cudaError_t launch_as(const CacheAttendArgs& a, cudaStream_t s)
 {
-    const cudaError_t e = cudaFuncSetAttribute(attend_kernel<P, WK, WV, kExact>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_bytes<P>());
-    if (e != cudaSuccess) return e;
-    attend_kernel<P, WK, WV, kExact><<<a.grid, kThreads, smem_bytes<P>(), s>>>(a);
-    if (a.split) attend_join_kernel<P><<<a.grid, kThreads, 0, s>>>(a);
-    return cudaGetLastError();
+    using X = Stage<P, WK, WV>;
+    constexpr int kBytes = smem_bytes<P, WK, WV>();
+    static_assert(kBytes <= 227 << 10, "shared memory of an SM");
+    static std::atomic<uint64_t> configured{0};
+    cudaError_t e = opt_in_shared_memory(configured, kBytes, attend_kernel<P, WK, WV, kExact>);
+    if (e == cudaSuccess) e = lq::launch(attend_kernel<P, WK, WV, kExact>, a.sms, X::kTeams * kTeam, kBytes, s, a);
+    if (e == cudaSuccess && a.split) e = lq::launch(attend_join_kernel<P>, a.sms * X::kTeams, kTeam, 0, s, a);
+    return e;
 }
 
 template <int P, int WK, int WV>
