@@ -50,7 +50,10 @@ constexpr int kTeam = 32 * kTeamWarps;  // threads
 constexpr int kTile = 16;               // tokens of a warp at a time
 constexpr int kQueries = 8;             // queries a segment
 constexpr int kTableBytes = 256 * 256;  // entry e: 32 copies for the keys, 32 for the values
-constexpr int kStageBytes = 148 << 10;  // for the stages of all warps
+// Shared memory, by address: 64 KB below the table hold stages of some warps, the table starts at 64 KB, so that a byte of a row
+// is the second byte of its entry's address, behind it come the other warps' stages.  (The first KB of a CTA's shared memory is the
+// system's; the last one that a CTA can have is left free, so that the places below hold wherever in the first the kernel's own begins.)
+constexpr int kTableAt = 1 << 16, kSystemBytes = 1 << 10, kEnd = (227 << 10);
 constexpr float kLow = -1e30f;          // a reference before its first score
 constexpr float kSlack = 8.0f;          // how far (log2) a score may pass its reference
 constexpr float kLift = 6.0f;           // weights are 2^kLift at their reference: at most 2^14 as fp16, and exact down to 2^-20
@@ -62,6 +65,17 @@ static_assert(sizeof(Record) == kCacheRecordBytes && kQueries == 8, "the workspa
 template <int P>
 constexpr int64_t kPartial = cache_partial_floats(P);
 
+template <int P>
+struct TeamShared {
+    int64_t words[18];                  // schedule
+    float factor[kQueries];             // scale * log2(e) / the query's power of two
+    float stats[kTeamWarps][kQueries][3];
+    float share[kQueries][kTeamWarps + 4];      // factor of each warp's sums; then ref, ref_w, total
+    alignas(16) __half q[2][kQueries][P + 8];   // the queries, and what their rounding left
+};
+template <int P>
+constexpr int kTeamSharedBytes = (int)sizeof(TeamShared<P>);
+
 // A tile of one warp in shared memory: keys, values, 16 norms of keys, 16 of values.
 template <int P, int WK, int WV>
 struct Stage {
@@ -72,28 +86,24 @@ struct Stage {
     static constexpr int kGroupK = 4 * kRowK + kGapK, kGroupV = 4 * kRowV + kGapV;
     static constexpr int kValues = 4 * kGroupK, kNorms = kValues + 4 * kGroupV, kBytes = kNorms + 8 * kTile;
     static constexpr int kTeams = cache_attend_teams(P), kWarps = kTeams * kTeamWarps;
-    static constexpr int kFit = kStageBytes / (kWarps * kBytes);
-    static constexpr int kStages = kFit > 6 ? 6 : kFit;
-    static constexpr int kWarpBytes = kStages * kBytes;
+    // as many stages as fit for all warps, on both sides of the table; behind them a KB for what a team shares
+    static constexpr int low(int stages) { return (kTableAt - kSystemBytes) / (stages * kBytes); }
+    static constexpr int high(int stages) { return (kEnd - kTableAt - kTableBytes - kTeams * kTeamSharedBytes<P>) / (stages * kBytes); }
+    static constexpr int fit() { int n = 6; while (low(n) + high(n) < kWarps) --n; return n; }
+    static constexpr int kStages = fit();
+    static constexpr int kWarpBytes = kStages * kBytes, kLow = low(kStages) < kWarps ? low(kStages) : kWarps;
+    static constexpr int kTeamsAt = kTableAt + kTableBytes + (kWarps - kLow) * kWarpBytes;
+    // Shared address of a warp's stages.
+    static __device__ __forceinline__ int stages_at(int warp)
+    {
+        return warp < kLow ? kSystemBytes + warp * kWarpBytes : kTableAt + kTableBytes + (warp - kLow) * kWarpBytes;
+    }
     static constexpr int kSumBytes = kQueries * (P + 4) * 4;                                // a warp's sums, in its stages' place
     static_assert(kStages >= 2 && kWarpBytes >= kSumBytes && kBytes % 16 == 0, "stages");
 };
 
-template <int P>
-struct TeamShared {
-    int64_t words[18];                  // schedule
-    float factor[kQueries];             // scale * log2(e) / the query's power of two
-    float stats[kTeamWarps][kQueries][3];
-    float share[kQueries][kTeamWarps + 4];      // factor of each warp's sums; then ref, ref_w, total
-    alignas(16) __half q[2][kQueries][P + 8];   // the queries, and what their rounding left
-};
-
 template <int P, int WK, int WV>
-constexpr int smem_bytes()
-{
-    using X = Stage<P, WK, WV>;
-    return kTableBytes + X::kWarps * X::kWarpBytes + X::kTeams * (int)sizeof(TeamShared<P>);
-}
+constexpr int smem_bytes() { return Stage<P, WK, WV>::kTeamsAt + Stage<P, WK, WV>::kTeams * kTeamSharedBytes<P>; }
 
 __device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 __device__ __forceinline__ float lg2(float x) { float y; asm("lg2.approx.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
@@ -123,11 +133,13 @@ __device__ __forceinline__ float2 rest_of(uint32_t rounded, float lo, float hi)
     return make_float2(lo - r.x, hi - r.y);
 }
 
-// The table's word for byte kByte of `w`; lane_base: 4 * lane (+ 128 for the values).
+// The table's word for byte kByte of `w`; lane_base: kTableAt + 4 * lane (+ 128 for the values).
 template <int kByte>
-__device__ __forceinline__ uint32_t look(const char* table, uint32_t w, uint32_t lane_base)
+__device__ __forceinline__ uint32_t look(uint32_t w, uint32_t lane_base)
 {
-    return *reinterpret_cast<const uint32_t*>(table + __byte_perm(w, lane_base, 0x5504 | (kByte << 4)));
+    uint32_t v;                         // (the table does not change once it is there: no need to keep the order of these loads)
+    asm("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(__byte_perm(w, lane_base, 0x7604 | (kByte << 4))));
+    return v;
 }
 
 __device__ __forceinline__ void copy16(uint32_t to, const void* from)
@@ -267,7 +279,7 @@ struct Sums {
 // First product: the 16 x 8 scores of a tile before their factors.
 template <int P, int WK, int WV, bool kTwo>
 __device__ __forceinline__ void scores(float (&c)[4], const Tile<P, WK, WV>& t, const uint32_t (&q)[P / 16][2],
-                                       const uint32_t (&q2)[kTwo ? P / 16 : 1][2], const char* table, uint32_t lane_base)
+                                       const uint32_t (&q2)[kTwo ? P / 16 : 1][2], uint32_t lane_base)
 {
     c[0] = c[1] = c[2] = c[3] = 0.0f;
 #pragma unroll
@@ -276,18 +288,18 @@ __device__ __forceinline__ void scores(float (&c)[4], const Tile<P, WK, WV>& t, 
         if constexpr (WK == 4) {
             const uint32_t w0 = t.k[0][s / 2], w1 = t.k[1][s / 2];
             if (s % 2 == 0) {
-                a0 = look<0>(table, w0, lane_base); a2 = look<1>(table, w0, lane_base);
-                a1 = look<0>(table, w1, lane_base); a3 = look<1>(table, w1, lane_base);
+                a0 = look<0>(w0, lane_base); a2 = look<1>(w0, lane_base);
+                a1 = look<0>(w1, lane_base); a3 = look<1>(w1, lane_base);
             } else {
-                a0 = look<2>(table, w0, lane_base); a2 = look<3>(table, w0, lane_base);
-                a1 = look<2>(table, w1, lane_base); a3 = look<3>(table, w1, lane_base);
+                a0 = look<2>(w0, lane_base); a2 = look<3>(w0, lane_base);
+                a1 = look<2>(w1, lane_base); a3 = look<3>(w1, lane_base);
             }
         } else {
             const uint32_t w0 = t.k[0][s], w1 = t.k[1][s];
-            a0 = __byte_perm(look<0>(table, w0, lane_base), look<1>(table, w0, lane_base), 0x5410);
-            a2 = __byte_perm(look<2>(table, w0, lane_base), look<3>(table, w0, lane_base), 0x5410);
-            a1 = __byte_perm(look<0>(table, w1, lane_base), look<1>(table, w1, lane_base), 0x5410);
-            a3 = __byte_perm(look<2>(table, w1, lane_base), look<3>(table, w1, lane_base), 0x5410);
+            a0 = __byte_perm(look<0>(w0, lane_base), look<1>(w0, lane_base), 0x5410);
+            a2 = __byte_perm(look<2>(w0, lane_base), look<3>(w0, lane_base), 0x5410);
+            a1 = __byte_perm(look<0>(w1, lane_base), look<1>(w1, lane_base), 0x5410);
+            a3 = __byte_perm(look<2>(w1, lane_base), look<3>(w1, lane_base), 0x5410);
         }
         mma(c, a0, a1, a2, a3, q[s][0], q[s][1]);
         if constexpr (kTwo) mma(c, a0, a1, a2, a3, q2[s][0], q2[s][1]);
@@ -297,7 +309,7 @@ __device__ __forceinline__ void scores(float (&c)[4], const Tile<P, WK, WV>& t, 
 // Second product: acc[m] += values^T x weights.  Lane (g, t) has coordinates of row g of A: even ones, of row g + 8: odd ones.
 template <int P, int WK, int WV, bool kTwo>
 __device__ __forceinline__ void weigh(float (&acc)[P / 16][4], const Tile<P, WK, WV>& t, const uint32_t (&b)[2],
-                                      const uint32_t (&b2)[2], const char* table, uint32_t lane_base)
+                                      const uint32_t (&b2)[2], uint32_t lane_base)
 {
     auto step = [&](int m, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3) {
         mma(acc[m], a0, a1, a2, a3, b[0], b[1]);
@@ -309,16 +321,16 @@ __device__ __forceinline__ void weigh(float (&acc)[P / 16][4], const Tile<P, WK,
         if constexpr (WV == 4) {
             const uint32_t e = (w0 & 0x0f0f0f0fu) | ((w1 << 4) & 0xf0f0f0f0u), o = ((w0 >> 4) & 0x0f0f0f0fu) | (w1 & 0xf0f0f0f0u);
             const uint32_t e2 = (w2 & 0x0f0f0f0fu) | ((w3 << 4) & 0xf0f0f0f0u), o2 = ((w2 >> 4) & 0x0f0f0f0fu) | (w3 & 0xf0f0f0f0u);
-            step(4 * i, look<0>(table, e, lane_base), look<0>(table, o, lane_base), look<0>(table, e2, lane_base), look<0>(table, o2, lane_base));
-            step(4 * i + 1, look<1>(table, e, lane_base), look<1>(table, o, lane_base), look<1>(table, e2, lane_base), look<1>(table, o2, lane_base));
-            step(4 * i + 2, look<2>(table, e, lane_base), look<2>(table, o, lane_base), look<2>(table, e2, lane_base), look<2>(table, o2, lane_base));
-            step(4 * i + 3, look<3>(table, e, lane_base), look<3>(table, o, lane_base), look<3>(table, e2, lane_base), look<3>(table, o2, lane_base));
+            step(4 * i, look<0>(e, lane_base), look<0>(o, lane_base), look<0>(e2, lane_base), look<0>(o2, lane_base));
+            step(4 * i + 1, look<1>(e, lane_base), look<1>(o, lane_base), look<1>(e2, lane_base), look<1>(o2, lane_base));
+            step(4 * i + 2, look<2>(e, lane_base), look<2>(o, lane_base), look<2>(e2, lane_base), look<2>(o2, lane_base));
+            step(4 * i + 3, look<3>(e, lane_base), look<3>(o, lane_base), look<3>(e2, lane_base), look<3>(o2, lane_base));
         } else {
             auto two = [&](uint32_t x, uint32_t y) { return __byte_perm(x, y, 0x5410); };
-            step(2 * i, two(look<0>(table, w0, lane_base), look<0>(table, w1, lane_base)), two(look<1>(table, w0, lane_base), look<1>(table, w1, lane_base)),
-                 two(look<0>(table, w2, lane_base), look<0>(table, w3, lane_base)), two(look<1>(table, w2, lane_base), look<1>(table, w3, lane_base)));
-            step(2 * i + 1, two(look<2>(table, w0, lane_base), look<2>(table, w1, lane_base)), two(look<3>(table, w0, lane_base), look<3>(table, w1, lane_base)),
-                 two(look<2>(table, w2, lane_base), look<2>(table, w3, lane_base)), two(look<3>(table, w2, lane_base), look<3>(table, w3, lane_base)));
+            step(2 * i, two(look<0>(w0, lane_base), look<0>(w1, lane_base)), two(look<1>(w0, lane_base), look<1>(w1, lane_base)),
+                 two(look<0>(w2, lane_base), look<0>(w3, lane_base)), two(look<1>(w2, lane_base), look<1>(w3, lane_base)));
+            step(2 * i + 1, two(look<2>(w0, lane_base), look<2>(w1, lane_base)), two(look<3>(w0, lane_base), look<3>(w1, lane_base)),
+                 two(look<2>(w2, lane_base), look<2>(w3, lane_base)), two(look<3>(w2, lane_base), look<3>(w3, lane_base)));
         }
     }
 }
@@ -399,10 +411,11 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
     using X = Stage<P, WK, WV>;
     using T = Tile<P, WK, WV>;
     extern __shared__ __align__(128) char smem[];
-    char* const table = smem;
+    char* const shared = smem - __cvta_generic_to_shared(smem);         // shared address 0
+    char* const table = shared + kTableAt;
     const int team = threadIdx.x / kTeam, tid = threadIdx.x % kTeam, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
-    char* const stages = smem + kTableBytes + (team * kTeamWarps + warp) * X::kWarpBytes;
-    TeamShared<P>& sh = reinterpret_cast<TeamShared<P>*>(smem + kTableBytes + X::kWarps * X::kWarpBytes)[team];
+    char* const stages = shared + X::stages_at(team * kTeamWarps + warp);
+    TeamShared<P>& sh = reinterpret_cast<TeamShared<P>*>(shared + X::kTeamsAt)[team];
 
     {   // the look-up table: a thread writes copies of one entry, a warp's lanes at different banks
         const bool mine = X::kTeams == 1 || team == 0, other = X::kTeams == 1 || team == 1;
@@ -473,7 +486,7 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
         int hb = (int)(offset / units);
         int64_t chunk = offset - hb * units, at = begin;
 
-        const uint32_t base_k = 4 * lane, base_v = 128 + 4 * lane, stage0 = (uint32_t)__cvta_generic_to_shared(stages);
+        const uint32_t base_k = kTableAt + 4 * lane, base_v = base_k + 128, stage0 = (uint32_t)X::stages_at(team * kTeamWarps + warp);
         const int tile_shift = a.shape.page_shift - 4, tile_mask = (1 << tile_shift) - 1;
         // this lane's places in a stage
         const int row = token_row(g), row_even = token_row(2 * t), row_odd = token_row(2 * t + 1);
@@ -542,7 +555,7 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
                 T cur;
                 float c[4];
                 take_keys(cur, keys + place);
-                scores<P, WK, WV, (kExact > 0)>(c, cur, q, q2, table, base_k);
+                scores<P, WK, WV, (kExact > 0)>(c, cur, q, q2, base_k);
                 const float nk0 = *reinterpret_cast<const float*>(norms + place), nk1 = *reinterpret_cast<const float*>(norms + place + 8);
                 const float nv0 = *reinterpret_cast<const float*>(norms + place + 64), nv1 = *reinterpret_cast<const float*>(norms + place + 72);
                 take_values(cur, even + place, odd + place);
@@ -585,7 +598,7 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
                     b2[0] = transposed(halves(r0.x, r0.y));
                     b2[1] = transposed(halves(r1.x, r1.y));
                 }
-                weigh<P, WK, WV, (kExact == 2)>(S.acc, cur, b, b2, table, base_v);
+                weigh<P, WK, WV, (kExact == 2)>(S.acc, cur, b, b2, base_v);
             }
 
             // ---- the warps' sums added up, through the stages
@@ -624,7 +637,6 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
             team_sync(team);
             const bool starts = chunk == 0, whole = starts && count == units;
             const int slot = 2 * me + starts;
-            const char* const team_stages = smem + kTableBytes + team * kTeamWarps * X::kWarpBytes;
             for (int i = tid; i < kQueries * P / 4; i += kTeam) {
                 const int query = i / (P / 4), d = (i % (P / 4)) * 4;
                 const float* share = sh.share[query];
@@ -632,7 +644,7 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
 #pragma unroll
                 for (int w = 0; w < kTeamWarps; ++w) {
                     const float4 v = *reinterpret_cast<const float4*>(
-                        reinterpret_cast<const float*>(team_stages + w * X::kWarpBytes) + ((query & 1) * 4 + (query >> 1)) * (P + 4) + d);
+                        reinterpret_cast<const float*>(shared + X::stages_at(team * kTeamWarps + w)) + ((query & 1) * 4 + (query >> 1)) * (P + 4) + d);
                     const float f = share[w];
                     sum4.x += v.x * f; sum4.y += v.y * f; sum4.z += v.z * f; sum4.w += v.w * f;
                 }
