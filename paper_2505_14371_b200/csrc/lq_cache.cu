@@ -340,10 +340,10 @@ int lq_cache_attend(lq_cache* cache, int32_t layer, const lq_rows* queries, int6
     a.scale = scale * 1.44269504088896341f;
     a.batch = (int32_t)batch;
     a.sms = cache->sms;
-    // 128 tokens are one unit, which is never split
+    // a unit is never split
     int64_t tiles = (table_width << s.page_shift) / 16;
     if (window > 0) tiles = std::min(tiles, window / 16 + 2);
-    a.split = tiles > 8;
+    a.split = tiles > cache_attend_unit(s.padded, s.sym_bits[0], s.sym_bits[1]);
     LQ_ON_DEVICE(cache);
     LQ_CUDA(s.padded == 64 ? launch_cache_attend_64(a, (cudaStream_t)stream)
             : s.padded == 128 ? launch_cache_attend_128(a, (cudaStream_t)stream) : launch_cache_attend_256(a, (cudaStream_t)stream));

@@ -102,6 +102,9 @@ cudaError_t launch_cache_attend_256(const CacheAttendArgs& a, cudaStream_t s);
 // Teams of 8 warps that share an SM in the attention kernel (its registers: rows of 256 need twice as many a thread), and what
 // each may leave in the workspace: a record, then two partial sums of 8 queries.
 __host__ __device__ constexpr int cache_attend_teams(int padded) { return padded == 256 ? 1 : 2; }
+// Tiles of 16 tokens that a warp takes at a time (two where two stages of two fit for every warp), and those of a unit of work.
+__host__ __device__ constexpr int cache_attend_pair(int padded, int bits_k, int bits_v) { return padded * (bits_k + bits_v) <= 1024 ? 2 : 1; }
+__host__ __device__ constexpr int cache_attend_unit(int padded, int bits_k, int bits_v) { return 8 * cache_attend_pair(padded, bits_k, bits_v); }
 constexpr int kCacheRecordBytes = 16;
 constexpr int cache_partial_floats(int padded) { return 8 * (padded + 4); }
 

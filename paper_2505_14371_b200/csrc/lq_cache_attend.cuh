@@ -29,7 +29,7 @@
 // groups of 4 rows with a gap behind each, and the tile's tokens are dealt to the rows of the operands (token_row) such that
 // both the keys' and the values' reads meet every bank once.
 //
-// Split.  Units of 128 tokens (8 warps x 16) of all (sequence, head, 8 queries) in a row are dealt out evenly to teams of 8 warps, as
+// Split.  Units of 128 tokens (8 warps x 16; 256 where a warp takes two tiles at a time) of all (sequence, head, 8 queries) in a row are dealt out evenly to teams of 8 warps, as
 // many as the GPU holds at once (two a CTA, which share the look-up table; one for rows of 256); every team finds its
 // share from the lengths, on the device.  A team that has all of a segment (sequence, head, 8 queries) writes its output; the others leave
 // partial sums in the workspace, at most two a team, and the team where a segment begins leaves a record of it, from which a
@@ -86,10 +86,11 @@ struct Stage {
     static constexpr int kGroupK = 4 * kRowK + kGapK, kGroupV = 4 * kRowV + kGapV;
     static constexpr int kValues = 4 * kGroupK, kNorms = kValues + 4 * kGroupV, kBytes = kNorms + 8 * kTile;
     static constexpr int kTeams = cache_attend_teams(P), kWarps = kTeams * kTeamWarps;
+    static constexpr int kPair = cache_attend_pair(P, WK, WV), kUnit = cache_attend_unit(P, WK, WV);
     // as many stages as fit for all warps, on both sides of the table; behind them a KB for what a team shares
     static constexpr int low(int stages) { return (kTableAt - kSystemBytes) / (stages * kBytes); }
     static constexpr int high(int stages) { return (kEnd - kTableAt - kTableBytes - kTeams * kTeamSharedBytes<P>) / (stages * kBytes); }
-    static constexpr int fit() { int n = 6; while (low(n) + high(n) < kWarps) --n; return n; }
+    static constexpr int fit() { int n = 6; while (low(n) + high(n) < kWarps) n -= kPair; return n; }
     static constexpr int kStages = fit();
     static constexpr int kWarpBytes = kStages * kBytes, kLow = low(kStages) < kWarps ? low(kStages) : kWarps;
     static constexpr int kTeamsAt = kTableAt + kTableBytes + (kWarps - kLow) * kWarpBytes;
@@ -99,14 +100,14 @@ struct Stage {
         return warp < kLow ? kSystemBytes + warp * kWarpBytes : kTableAt + kTableBytes + (warp - kLow) * kWarpBytes;
     }
     static constexpr int kSumBytes = kQueries * (P + 4) * 4;                                // a warp's sums, in its stages' place
-    static_assert(kStages >= 2 && kWarpBytes >= kSumBytes && kBytes % 16 == 0, "stages");
+    static_assert(kStages >= 2 * kPair && kStages % kPair == 0 && kWarpBytes >= kSumBytes && kBytes % 16 == 0, "stages");
 };
 
 template <int P, int WK, int WV>
 constexpr int smem_bytes() { return Stage<P, WK, WV>::kTeamsAt + Stage<P, WK, WV>::kTeams * kTeamSharedBytes<P>; }
 
 __device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
-__device__ __forceinline__ float lg2(float x) { float y; asm("lg2.approx.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+__device__ __forceinline__ float lg2(float x) { float y; asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 
 __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
@@ -167,23 +168,23 @@ __device__ __forceinline__ void store_any(const CacheRows& r, int64_t at, float 
     else static_cast<__nv_bfloat16*>(r.data)[at] = __float2bfloat16_rn(v);
 }
 
-// What a sequence has to be read of: tokens [first, length), as tiles [tile0, tile1), and units of them.
+// What a sequence has to be read of: tokens [first, length), as tiles [tile0, tile1).
 struct Extent {
-    int64_t first, length;
-    int64_t tile0, tile1;
-    __device__ __forceinline__ int64_t units() const { return (tile1 - tile0 + kTeamWarps - 1) / kTeamWarps; }
+    uint32_t first, length;             // (a tile's last token may be just past 2^31)
+    int32_t tile0, tile1;
+    template <int kUnit>
+    __device__ __forceinline__ int64_t units() const { return (tile1 - tile0 + kUnit - 1) / kUnit; }
 };
 
 __device__ __forceinline__ Extent extent_of(const CacheAttendArgs& a, int sequence)
 {
     Extent e;
-    e.length = __ldg(a.lengths + sequence);
     const int64_t most = a.table_width << a.shape.page_shift;
-    if (e.length < 0) e.length = 0;
-    if (e.length > most) e.length = most;
-    e.first = a.window > 0 && e.length > a.window ? e.length - a.window : 0;
-    e.tile0 = e.first / kTile;
-    e.tile1 = (e.length + kTile - 1) / kTile;
+    const int n = __ldg(a.lengths + sequence);
+    e.length = n < 0 ? 0 : n > most ? (uint32_t)most : (uint32_t)n;
+    e.first = a.window > 0 && e.length > a.window ? e.length - (uint32_t)a.window : 0;
+    e.tile0 = (int32_t)(e.first / kTile);
+    e.tile1 = (int32_t)((e.length + kTile - 1) / kTile);
     return e;
 }
 
@@ -281,6 +282,7 @@ template <int P, int WK, int WV, bool kTwo>
 __device__ __forceinline__ void scores(float (&c)[4], const Tile<P, WK, WV>& t, const uint32_t (&q)[P / 16][2],
                                        const uint32_t (&q2)[kTwo ? P / 16 : 1][2], uint32_t lane_base)
 {
+    float c2[4] = {};
     c[0] = c[1] = c[2] = c[3] = 0.0f;
 #pragma unroll
     for (int s = 0; s < P / 16; ++s) {
@@ -302,8 +304,9 @@ __device__ __forceinline__ void scores(float (&c)[4], const Tile<P, WK, WV>& t, 
             a3 = __byte_perm(look<2>(w1, lane_base), look<3>(w1, lane_base), 0x5410);
         }
         mma(c, a0, a1, a2, a3, q[s][0], q[s][1]);
-        if constexpr (kTwo) mma(c, a0, a1, a2, a3, q2[s][0], q2[s][1]);
+        if constexpr (kTwo) mma(c2, a0, a1, a2, a3, q2[s][0], q2[s][1]);
     }
+    if constexpr (kTwo) { c[0] += c2[0]; c[1] += c2[1]; c[2] += c2[2]; c[3] += c2[3]; }
 }
 
 // Second product: acc[m] += values^T x weights.  Lane (g, t) has coordinates of row g of A: even ones, of row g + 8: odd ones.
@@ -434,7 +437,7 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
     const int head_blocks = a.shape.heads * a.group_blocks, me = blockIdx.x * X::kTeams + team, teams = gridDim.x * X::kTeams;
     int64_t sum = 0;
     for (int b = tid; b < a.batch; b += kTeam) {
-        sum += extent_of(a, b).units();
+        sum += extent_of(a, b).template units<X::kUnit>();
         const int n = __ldg(a.lengths + b);
         if (me == 0 && (n < 0 || n > a.table_width << a.shape.page_shift)) atomicOr(a.flags, LQ_CACHE_BAD_LENGTH);
     }
@@ -458,7 +461,7 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
         int64_t before = 0;
         for (int base = 0; base < a.batch; base += kTeam) {
             const int b = base + tid;
-            const int64_t mine = b < a.batch ? extent_of(a, b).units() * head_blocks : 0;
+            const int64_t mine = b < a.batch ? extent_of(a, b).template units<X::kUnit>() * head_blocks : 0;
             int64_t scan = mine;
 #pragma unroll
             for (int o = 1; o < 32; o *= 2) {
@@ -481,12 +484,13 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
         team_sync(team);
         int sequence = (int)sh.words[16];
         Extent x = extent_of(a, sequence);
-        int64_t units = x.units();
+        int64_t units = x.template units<X::kUnit>();
         const int64_t offset = begin - sh.words[17];
         int hb = (int)(offset / units);
         int64_t chunk = offset - hb * units, at = begin;
 
         const uint32_t base_k = kTableAt + 4 * lane, base_v = base_k + 128, stage0 = (uint32_t)X::stages_at(team * kTeamWarps + warp);
+        const int64_t page_bytes = a.shape.page_words * 4;
         const int tile_shift = a.shape.page_shift - 4, tile_mask = (1 << tile_shift) - 1;
         // this lane's places in a stage
         const int row = token_row(g), row_even = token_row(2 * t), row_odd = token_row(2 * t + 1);
@@ -498,31 +502,35 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
         while (at < end) {
             const int count = (int)min(units - chunk, end - at);       // units of this segment that are ours
             const int head = hb / a.group_blocks, block = hb - head * a.group_blocks;
-            // ---- the first copies: tile j of this warp is tile0 + 8 j of the sequence
+            // ---- the first copies: this warp's tiles are kPair of every unit
             const int32_t* pages = a.table + (int64_t)sequence * a.table_width;
-            const int tile0 = (int)(x.tile0 + chunk * kTeamWarps) + warp, stop = (int)min(x.tile1, x.tile0 + (chunk + count) * kTeamWarps);
-            const int tiles = stop > tile0 ? (stop - tile0 + kTeamWarps - 1) / kTeamWarps : 0;
+            const int tile0 = x.tile0 + (int)chunk * X::kUnit + warp * X::kPair, stop = min(x.tile1, x.tile0 + ((int)chunk + count) * X::kUnit);
+            const int rounds = stop > tile0 ? (stop - tile0 + X::kUnit - 1) / X::kUnit : 0;
             const char* const bytes = reinterpret_cast<const char*>(a.pages) + head * a.shape.head_words * 4;
-            uint32_t missing = 0;                                       // bit s: the tile in stage s is on a page that is not there
-            int page = -1;                                              // lane l: of tile (32 i + l), i as far as copies are
-            auto start = [&](int j, int stage) {
-                if (j < tiles) {
-                    if (j % 32 == 0) {
+            auto tile_of = [&](int n) { return tile0 + n / X::kPair * X::kUnit + n % X::kPair; };      // of the warp's n-th tile
+            uint32_t missing = 0;                                       // bit s: stage s holds no tile: past the end, or on a page that is not there
+            int page = -1;                                              // lane l: of the warp's tile 32 i + l, i as far as copies are
+            auto start = [&](int round, int stage) {
+                if (round < rounds) {
+                    if (round * X::kPair % 32 == 0) {
+                        const int tile = tile_of(round * X::kPair + lane);
                         page = -1;
-                        if (j + lane < tiles) {
-                            page = __ldg(pages + ((tile0 + (j + lane) * kTeamWarps) >> tile_shift));
+                        if (tile < stop) {
+                            page = __ldg(pages + (tile >> tile_shift));
                             if (page < 0 || page >= a.num_pages) { page = -1; atomicOr(a.flags, LQ_CACHE_BAD_PAGE); }
                         }
                     }
-                    const int p = __shfl_sync(0xffffffffu, page, j % 32);
-                    missing = p < 0 ? missing | 1u << stage : missing & ~(1u << stage);
-                    if (p >= 0)
-                        copy_tile<P, WK, WV>(stage0 + stage * X::kBytes, bytes + p * a.shape.page_words * 4, a.shape.page_shift,
-                                             ((tile0 + j * kTeamWarps) & tile_mask) * kTile, lane);
+#pragma unroll
+                    for (int h = 0; h < X::kPair; ++h) {
+                        const int n = round * X::kPair + h, p = __shfl_sync(0xffffffffu, page, n % 32);
+                        missing = p < 0 ? missing | 1u << (stage + h) : missing & ~(1u << (stage + h));
+                        if (p >= 0)
+                            copy_tile<P, WK, WV>(stage0 + (stage + h) * X::kBytes, bytes + p * page_bytes, a.shape.page_shift, (tile_of(n) & tile_mask) * kTile, lane);
+                    }
                 }
                 commit_copies();
             };
-            for (int j = 0; j < X::kStages - 1; ++j) start(j, j);
+            for (int j = 0; j < X::kStages / X::kPair - 1; ++j) start(j, j * X::kPair);
 
             stage_query<P>(sh, a, sequence, head, block, warp, lane, x.length);
             team_sync(team);
@@ -540,45 +548,59 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
 
             Sums<P, WK, WV, kExact> S;
             S.clear();
-            int stage = 0, ahead = X::kStages - 1;
-            for (int j = 0; j < tiles; ++j) {
-                __syncwarp();                                           // every lane has read the stage that is filled next
-                start(j + X::kStages - 1, ahead);
-                wait_copies<X::kStages - 1>();
+            int stage = 0, ahead = X::kStages - X::kPair;
+            for (int j = 0; j < rounds; ++j) {
+                __syncwarp();                                           // every lane has read the stages that are filled next
+                start(j + X::kStages / X::kPair - 1, ahead);
+                wait_copies<X::kStages / X::kPair - 1>();
                 __syncwarp();
                 const int place = stage * X::kBytes;
-                const bool there = !(missing >> stage & 1);
-                if (++stage == X::kStages) stage = 0;
-                if (++ahead == X::kStages) ahead = 0;
-                if (!there) continue;
+                const uint32_t gone = missing >> stage & ((1u << X::kPair) - 1);
+                if ((stage += X::kPair) == X::kStages) stage = 0;
+                if ((ahead += X::kPair) == X::kStages) ahead = 0;
+                if (gone == (1u << X::kPair) - 1) continue;
 
-                T cur;
-                float c[4];
-                take_keys(cur, keys + place);
-                scores<P, WK, WV, (kExact > 0)>(c, cur, q, q2, base_k);
-                const float nk0 = *reinterpret_cast<const float*>(norms + place), nk1 = *reinterpret_cast<const float*>(norms + place + 8);
-                const float nv0 = *reinterpret_cast<const float*>(norms + place + 64), nv1 = *reinterpret_cast<const float*>(norms + place + 72);
-                take_values(cur, even + place, odd + place);
-                float s0 = c[0] * (f0 * nk0), s1 = c[1] * (f1 * nk0), s2 = c[2] * (f0 * nk1), s3 = c[3] * (f1 * nk1);
-                float lv0 = lg2(nv0), lv1 = lg2(nv1);
-                const int64_t first = (int64_t)(tile0 + j * kTeamWarps) * kTile;
-                if (first < x.first || first + kTile > x.length) {      // the ends of what is seen
-                    const int64_t token = first + row;
-                    if (token < x.first || token >= x.length) s0 = s1 = lv0 = -INFINITY;
-                    if (token + 2 < x.first || token + 2 >= x.length) s2 = s3 = lv1 = -INFINITY;
+                float s[X::kPair][4], w[X::kPair][4];
+#pragma unroll
+                for (int h = 0; h < X::kPair; ++h) {
+                    T cur;
+                    float c[4];
+                    take_keys(cur, keys + place + h * X::kBytes);
+                    scores<P, WK, WV, (kExact > 0)>(c, cur, q, q2, base_k);
+                    const char* n = norms + place + h * X::kBytes;
+                    const float nk0 = *reinterpret_cast<const float*>(n), nk1 = *reinterpret_cast<const float*>(n + 8);
+                    s[h][0] = c[0] * (f0 * nk0); s[h][1] = c[1] * (f1 * nk0); s[h][2] = c[2] * (f0 * nk1); s[h][3] = c[3] * (f1 * nk1);
+                    w[h][0] = w[h][1] = lg2(*reinterpret_cast<const float*>(n + 64));
+                    w[h][2] = w[h][3] = lg2(*reinterpret_cast<const float*>(n + 72));
                 }
-                const float w0 = s0 + lv0, w1 = s1 + lv0, w2 = s2 + lv1, w3 = s3 + lv1;
-                const float top0 = fmaxf(s0, s2), top1 = fmaxf(s1, s3), topw0 = fmaxf(w0, w2), topw1 = fmaxf(w1, w3);
-                const bool passed = top0 > S.ref[0] + kSlack || top1 > S.ref[1] + kSlack || topw0 > S.ref_w[0] + kSlack || topw1 > S.ref_w[1] + kSlack;
+                const uint32_t first = (uint32_t)(tile0 + j * X::kUnit) * kTile;
+                if (gone || first < x.first || first + X::kPair * kTile > x.length) {       // the ends of what is seen
+#pragma unroll
+                    for (int h = 0; h < X::kPair; ++h)
+#pragma unroll
+                        for (int i = 0; i < 4; i += 2) {
+                            const uint32_t token = first + h * kTile + row + i;
+                            if ((gone >> h & 1) || token < x.first || token >= x.length) s[h][i] = s[h][i + 1] = w[h][i] = w[h][i + 1] = -INFINITY;
+                        }
+                }
+                float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};        // of s, of w
+#pragma unroll
+                for (int h = 0; h < X::kPair; ++h)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        w[h][i] += s[h][i];
+                        top[i & 1] = fmaxf(top[i & 1], s[h][i]);
+                        top[2 + (i & 1)] = fmaxf(top[2 + (i & 1)], w[h][i]);
+                    }
+                const bool passed = top[0] > S.ref[0] + kSlack || top[1] > S.ref[1] + kSlack || top[2] > S.ref_w[0] + kSlack || top[3] > S.ref_w[1] + kSlack;
                 if (__any_sync(0xffffffffu, passed)) {
-                    float m[4] = {top0, top1, topw0, topw1};
 #pragma unroll
                     for (int o = 4; o < 32; o *= 2)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) m[i] = fmaxf(m[i], __shfl_xor_sync(0xffffffffu, m[i], o));
+                        for (int i = 0; i < 4; ++i) top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], o));
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
-                        const float r = fmaxf(S.ref[i], m[i]), rw = fmaxf(S.ref_w[i], m[2 + i]);
+                        const float r = fmaxf(S.ref[i], top[i]), rw = fmaxf(S.ref_w[i], top[2 + i]);
                         S.total[i] *= ex2(S.ref[i] - r);
                         const float f = ex2(S.ref_w[i] - rw);
                         S.ref[i] = r; S.ref_w[i] = rw;
@@ -586,19 +608,25 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
                         for (int k = 0; k < P / 16; ++k) { S.acc[k][i] *= f; S.acc[k][2 + i] *= f; }
                     }
                 }
-                S.total[0] += ex2(s0 - S.ref[0]) + ex2(s2 - S.ref[0]);
-                S.total[1] += ex2(s1 - S.ref[1]) + ex2(s3 - S.ref[1]);
-                const float e0 = ex2(w0 - S.ref_w[0] + kLift), e1 = ex2(w1 - S.ref_w[1] + kLift);
-                const float e2 = ex2(w2 - S.ref_w[0] + kLift), e3 = ex2(w3 - S.ref_w[1] + kLift);
-                const uint32_t h0 = halves(e0, e1), h1 = halves(e2, e3);
-                const uint32_t b[2] = {transposed(h0), transposed(h1)};
-                uint32_t b2[2] = {0, 0};
-                if constexpr (kExact == 2) {
-                    const float2 r0 = rest_of(h0, e0, e1), r1 = rest_of(h1, e2, e3);
-                    b2[0] = transposed(halves(r0.x, r0.y));
-                    b2[1] = transposed(halves(r1.x, r1.y));
+#pragma unroll
+                for (int h = 0; h < X::kPair; ++h) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        S.total[i & 1] += ex2(s[h][i] - S.ref[i & 1]);
+                        w[h][i] = ex2(w[h][i] - (S.ref_w[i & 1] - kLift));
+                    }
+                    const uint32_t h0 = halves(w[h][0], w[h][1]), h1 = halves(w[h][2], w[h][3]);
+                    const uint32_t b[2] = {transposed(h0), transposed(h1)};
+                    uint32_t b2[2] = {0, 0};
+                    if constexpr (kExact == 2) {
+                        const float2 r0 = rest_of(h0, w[h][0], w[h][1]), r1 = rest_of(h1, w[h][2], w[h][3]);
+                        b2[0] = transposed(halves(r0.x, r0.y));
+                        b2[1] = transposed(halves(r1.x, r1.y));
+                    }
+                    T cur;
+                    take_values(cur, even + place + h * X::kBytes, odd + place + h * X::kBytes);
+                    weigh<P, WK, WV, (kExact == 2)>(S.acc, cur, b, b2, base_v);
                 }
-                weigh<P, WK, WV, (kExact == 2)>(S.acc, cur, b, b2, base_v);
             }
 
             // ---- the warps' sums added up, through the stages
@@ -677,7 +705,7 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
             chunk = 0;
             if (at < end && ++hb == head_blocks) {
                 hb = 0;
-                do { x = extent_of(a, ++sequence); units = x.units(); } while (units == 0);
+                do { x = extent_of(a, ++sequence); units = x.template units<X::kUnit>(); } while (units == 0);
             }
             team_sync(team);                                            // the sums have been read
         }
@@ -685,7 +713,7 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
 
     // sequences without a token to see
     for (int b = me; b < a.batch; b += teams) {
-        if (extent_of(a, b).units() > 0) continue;
+        if (extent_of(a, b).template units<X::kUnit>() > 0) continue;
         const int queries = a.shape.heads * a.group;
         for (int64_t i = tid; i < (int64_t)queries * a.shape.dim; i += kTeam)
             store_any(a.out, b * a.out.token_stride + (i / a.shape.dim) * a.out.head_stride + i % a.shape.dim, 0.0f);
