@@ -62,10 +62,36 @@ bool rounded_levels(const float* levels, int n, float* out)
     return true;
 }
 
+void fill_search(CacheSearch& s, const float* levels, int n, bool nearest)
+{
+    const int edges = nearest ? n - 1 : n - 2;
+    for (float& e : s.edge) e = INFINITY;
+    for (int j = 1; j <= edges; ++j) {
+        if (nearest) {
+            const double middle = ((double)levels[j - 1] + (double)levels[j]) / 2;      // exact: multiples of 2^-25 up to 1
+            float e = (float)middle;
+            if (!((double)e > middle)) e = std::nextafterf(e, 2.0f);
+            s.edge[j] = e;
+        } else {
+            s.edge[j] = levels[j];
+        }
+    }
+    s.steps = 0;
+    int at = 0, to = 0;                 // edges at or below the two ends of a bin (either end's number may be in it)
+    for (int b = 0; b <= kCacheBins; ++b) {
+        while (at < edges && (double)s.edge[at + 1] <= (b - 0.5) / kCacheBins) ++at;
+        while (to < edges && (double)s.edge[to + 1] <= (b + 0.5) / kCacheBins) ++to;
+        s.start[b] = (uint8_t)at;
+        s.steps = std::max(s.steps, to - at);
+    }
+}
+
 void fill_table(CacheTable& t, const float* levels, int bits)
 {
     std::memset(&t, 0, sizeof t);
     for (int j = 0; j < 1 << bits; ++j) t.levels[j] = levels[j];
+    fill_search(t.nearest, levels, 1 << bits, true);
+    fill_search(t.floor, levels, 1 << bits, false);
     auto half_of = [&](uint32_t sym) {
         const __half_raw h = __float2half_rn(levels[sym >> 1]);
         return (uint32_t)h.x | ((sym & 1) << 15);
@@ -121,12 +147,20 @@ int check_pages(const lq_cache* c, int32_t layer, const void* pages, int64_t num
 
 int check_slots(const lq_cache* c, int64_t tokens, const int64_t* slots)
 {
-    // 256 threads a block, padded / 8 threads a row, 2 * heads rows a token
-    const int64_t most = (int64_t)INT32_MAX * 256 / (2 * c->shape.heads * (c->shape.padded / 8));
+    const int64_t most = INT32_MAX / c->shape.heads;        // (token, head) pairs are counted in 31 bits
     if (tokens < 0 || tokens > most) return lq_set_error(LQ_EINVAL, "tokens = %lld out of [0, %lld]", (long long)tokens, (long long)most);
     if (tokens > 0 && !slots) return lq_set_error(LQ_EINVAL, "slots is NULL");
     if (!aligned(slots, 8)) return lq_set_error(LQ_EINVAL, "slots must be 8-byte aligned");
     return LQ_OK;
+}
+
+// r / heads = floor(r * ceil(2^(31 + s) / heads) / 2^(31 + s)) for r < 2^31 with 2^s >= heads.
+CacheRowsOf rows_of(int heads)
+{
+    CacheRowsOf d{};
+    while ((1 << d.shift) < heads) ++d.shift;
+    d.factor = (uint32_t)((((uint64_t)1 << (31 + d.shift)) + heads - 1) / heads);
+    return d;
 }
 
 int64_t workspace_of(const lq_cache* c)
@@ -281,6 +315,7 @@ int lq_cache_write(lq_cache* cache, int32_t layer, const lq_rows* keys, const lq
     if (tokens == 0) return LQ_OK;
     a.shape = cache->shape; a.tables = cache->tables + (size_t)layer * 2;
     a.slots = slots; a.pages = pages; a.flags = cache->flags; a.tokens = tokens; a.num_slots = num_pages << cache->shape.page_shift;
+    a.by_head = rows_of(cache->shape.heads);
     a.seed_lo = (uint32_t)cache->seed; a.seed_hi = (uint32_t)(cache->seed >> 32);
     a.layer = (uint32_t)layer; a.unbiased = step >= 0; a.step = step >= 0 ? (uint32_t)step : 0;
     LQ_ON_DEVICE(cache);
@@ -301,6 +336,7 @@ int lq_cache_read(lq_cache* cache, int32_t layer, const uint32_t* pages, int64_t
     if (tokens == 0) return LQ_OK;
     a.shape = cache->shape; a.tables = cache->tables + (size_t)layer * 2;
     a.slots = slots; a.pages = pages; a.flags = cache->flags; a.tokens = tokens; a.num_slots = num_pages << cache->shape.page_shift;
+    a.by_head = rows_of(cache->shape.heads);
     LQ_ON_DEVICE(cache);
     LQ_CUDA(launch_cache_read(a, (cudaStream_t)stream));
     return LQ_OK;

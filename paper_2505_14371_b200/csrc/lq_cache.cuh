@@ -18,9 +18,21 @@ namespace lq {
 constexpr int kCacheLevels = 128;       // most levels of a set (7 bits)
 constexpr int kCachePairs = 256;        // entries of the look-up table by bytes
 
+constexpr int kCacheBins = 2048;        // of the search: round(2048 u)
+
+// Where u falls: index = how many of edge[1..] are <= u.  For rounding to the nearest level edge[j] is the least fp32 number above
+// the middle of levels j - 1 and j; for unbiased rounding it is level j, up to the last but one.  Entries behind are +infinity.
+struct alignas(16) CacheSearch {
+    float edge[kCacheLevels + 4];
+    uint8_t start[kCacheBins + 16];     // by bin: edges at or below all of its numbers
+    int32_t steps;                      // most edges inside a bin
+    int32_t pad[3];
+};
+
 // Device tables of one (layer, keys or values).
-struct CacheTable {
+struct alignas(16) CacheTable {
     float levels[kCacheLevels];         // numbers of 11 bits (set_levels rounds them)
+    CacheSearch nearest, floor;
     // By byte of a row: 4-bit symbols: the two signed levels as fp16, the first symbol's in the low half;
     // 8-bit symbols: the signed level as fp16 in both halves.
     uint32_t pairs[kCachePairs];
@@ -51,6 +63,9 @@ struct CacheRotary {
     int32_t interleaved;
 };
 
+// r / heads for 0 <= r < 2^31 as a product: umulhi(2 r, factor) >> shift.
+struct CacheRowsOf { uint32_t factor, shift; };
+
 struct CacheWriteArgs {
     CacheShape shape;
     const CacheTable* tables;           // keys, values
@@ -60,6 +75,7 @@ struct CacheWriteArgs {
     uint32_t* pages;
     uint32_t* flags;
     int64_t tokens, num_slots;
+    CacheRowsOf by_head;
     uint32_t seed_lo, seed_hi, layer, step;
     int32_t unbiased;
 };
@@ -72,6 +88,7 @@ struct CacheReadArgs {
     const uint32_t* pages;
     uint32_t* flags;
     int64_t tokens, num_slots;
+    CacheRowsOf by_head;
 };
 
 struct CacheAttendArgs {

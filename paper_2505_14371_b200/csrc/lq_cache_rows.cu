@@ -7,6 +7,8 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <type_traits>
+
 #include "lq_cache.cuh"
 #include "lq_internal.cuh"
 
@@ -118,172 +120,237 @@ __device__ __forceinline__ float row_norm(const float (&x)[kEach], int q, bool& 
     return bad || n < 1.17549435e-38f ? 0.0f : n;
 }
 
-template <typename T, int kLanes>
-__global__ void __launch_bounds__(kRowThreads) cache_write_kernel(const __grid_constant__ CacheWriteArgs a)
+// The (token, head) pair of this group of lanes and where its slot is.
+struct Place {
+    int64_t token, slot;
+    int head;
+};
+
+__device__ __forceinline__ Place place_of(uint32_t r, int heads, const CacheRowsOf& by, const int64_t* slots)
 {
-    const int64_t thread = (int64_t)blockIdx.x * kRowThreads + threadIdx.x;
-    const int64_t rows = a.tokens * 2 * a.shape.heads;
-    const int64_t r = thread / kLanes;
-    const int lane = (int)(thread % kLanes), d = lane * kEach;
-    // every lane of a warp takes part in the reductions, those past the last row with zeros
-    const int64_t token = r < rows ? r / (2 * a.shape.heads) : 0;
-    const int within = r < rows ? (int)(r - token * 2 * a.shape.heads) : 0;
-    const int kind = within >= a.shape.heads, head = within - kind * a.shape.heads;
-    int64_t slot = -1, position = 0;
-    if (r < rows) {
-        slot = __ldg(a.slots + token);
-        if (a.rotary.table) position = __ldg(a.rotary.at + token);
-        if (slot >= a.num_slots) { slot = -1; if (lane == 0) atomicOr(a.flags, LQ_CACHE_BAD_SLOT); }
-        if (slot >= 0 && a.rotary.table && (position < 0 || position >= a.rotary.positions)) {
-            slot = -1;
-            if (lane == 0) atomicOr(a.flags, LQ_CACHE_BAD_POSITION);
-        }
-    }
-    const bool live = slot >= 0;
+    Place p;
+    const uint32_t token = __umulhi(2 * r, by.factor) >> by.shift;
+    p.token = token;
+    p.head = (int)(r - token * heads);
+    p.slot = __ldg(slots + token);
+    return p;
+}
 
-    float x[kEach] = {};
-    if (live) {
-        const CacheRows& in = a.rows[kind];
-        const T* row = static_cast<const T*>(in.data) + token * in.token_stride + head * in.head_stride;
-        load8(x, row, d, a.shape.dim, in.wide);
-        if (kind == LQ_KEYS && a.rotary.table) rotate8(x, row, d, a.rotary, position);
-    }
-    bool bad;
-    const float norm = row_norm<kLanes>(x, a.shape.q, bad);
-    if (!live) return;
-    if (bad && lane == 0) atomicOr(a.flags, LQ_CACHE_NONFINITE);
+// What a kernel of rows keeps of the level tables.
+struct SharedSearch {
+    CacheSearch search;
+    float2 low_gap[kCacheLevels];       // a level and the gap above it
+};
 
+// Symbols 2 * index + sign of 8 coordinates, packed as the row has them (hi: the upper four of 8 bits).
+template <bool kUnbiased>
+__device__ __forceinline__ void symbols8(const float (&x)[kEach], float norm, int bits, const SharedSearch& t, const uint32_t (&rnd)[kEach],
+                                         uint32_t& lo, uint32_t& hi)
+{
     const float inv = norm > 0.0f ? __fdiv_rn(1.0f, norm) : 0.0f;
-    const int bits = a.shape.sym_bits[kind], last = (1 << (bits - 1)) - 2;      // index of the last interval
-    const float* levels = a.tables[kind].levels;
-    uint32_t rnd[kEach];
-    if (a.unbiased) {
-        const uint32_t c0 = (uint32_t)(head * a.shape.padded + d) / 4;
-        uint32_t w[4];
+    auto above = [&](int at, int i, float u) {          // unbiased: whether the upper neighbour is taken
+        const float2 lg = t.low_gap[at];
+        return __fmul_rn(__fmul_rn((float)(rnd[i] >> 9), 1.1920928955078125e-7f), lg.y) < __fsub_rn(u, lg.x);
+    };
+    lo = hi = 0;
+    if (bits == 4) {                    // 7 edges, from registers
+        const float4 e0 = *reinterpret_cast<const float4*>(t.search.edge), e1 = *reinterpret_cast<const float4*>(t.search.edge + 4);
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            philox4x32_10(c0 + j, 2 * a.layer + kind, (uint32_t)slot, a.step, a.seed_lo, a.seed_hi, w);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) rnd[4 * j + i] = w[i];
+        for (int i = 0; i < kEach; ++i) {
+            const float u = fminf(__fmul_rn(fabsf(x[i]), inv), 1.0f);
+            const bool p4 = u >= e1.x;
+            const bool p2 = u >= (p4 ? e1.z : e0.z);
+            const float a = p4 ? e1.y : e0.y, b = p4 ? e1.w : e0.w;
+            const bool p1 = u >= (p2 ? b : a);
+            uint32_t at = (p4 ? 8u : 0u) + (p2 ? 4u : 0u) + (p1 ? 2u : 0u);
+            if (kUnbiased) at += above(at / 2, i, u) ? 2 : 0;
+            lo |= (at + (x[i] < 0.0f ? 1u : 0u)) << (4 * i);
         }
-    }
-    uint32_t sym[kEach];
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-        const float u = norm > 0.0f ? fminf(__fmul_rn(fabsf(x[i]), inv), 1.0f) : 0.0f;
-        int at = 0;
-        for (int step = (last + 2) / 2; step > 0; step /= 2) {
-            const int t = at + step;
-            if (t <= last && __ldg(levels + t) <= u) at = t;
-        }
-        const float low = __ldg(levels + at), gap = __fsub_rn(__ldg(levels + at + 1), low);
-        const float rho = a.unbiased ? __fmul_rn((float)(rnd[i] >> 9), 1.1920928955078125e-7f) : 0.5f;
-        at += __fmul_rn(rho, gap) < __fsub_rn(u, low);
-        sym[i] = norm > 0.0f ? 2 * at + (x[i] < 0.0f) : 0;
-    }
-
-    const int64_t page = slot >> a.shape.page_shift, place = slot & ((1 << a.shape.page_shift) - 1);
-    const int64_t page_size = (int64_t)1 << a.shape.page_shift;
-    uint32_t* base = a.pages + page * a.shape.page_words + head * a.shape.head_words;
-    uint32_t* codes = base + (kind ? page_size * a.shape.row_words[0] : 0) + place * a.shape.row_words[kind];
-    if (bits == 4) {
-        uint32_t w = 0;
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) w |= sym[i] << (4 * i);
-        codes[lane] = w;
     } else {
-        uint2 w = make_uint2(0, 0);
+        const int steps = t.search.steps;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) { w.x |= sym[i] << (8 * i); w.y |= sym[4 + i] << (8 * i); }
-        reinterpret_cast<uint2*>(codes)[lane] = w;
+        for (int i = 0; i < kEach; ++i) {
+            const float u = fminf(__fmul_rn(fabsf(x[i]), inv), 1.0f);
+            // 4096 + u has round(2048 u) in its last bits
+            uint32_t at = t.search.start[__float_as_uint(__fadd_rn(u, 4096.0f)) - 0x45800000u];
+            for (int s = 0; s < steps; ++s) at += u >= t.search.edge[at + 1] ? 1 : 0;
+            if (kUnbiased) at += above(at, i, u) ? 1 : 0;
+            const uint32_t sym = 2 * at + (x[i] < 0.0f ? 1u : 0u);
+            if (i < 4) lo |= sym << (8 * i); else hi |= sym << (8 * (i - 4));
+        }
     }
-    if (lane == 0) {
-        float* norms = reinterpret_cast<float*>(base + page_size * (a.shape.row_words[0] + a.shape.row_words[1]));
-        norms[kind * page_size + place] = norm;
+    if (!(norm > 0.0f)) lo = hi = 0;
+}
+
+template <typename T, int kLanes, bool kUnbiased>
+__global__ void __launch_bounds__(kRowThreads, kUnbiased ? 3 : 4) cache_write_kernel(const __grid_constant__ CacheWriteArgs a)
+{
+    __shared__ SharedSearch tables[2];
+#pragma unroll
+    for (int kind = 0; kind < 2; ++kind) {
+        const CacheTable& t = a.tables[kind];
+        const CacheSearch& s = kUnbiased ? t.floor : t.nearest;
+        // rows of 4-bit symbols need the edges only
+        const int words = a.shape.sym_bits[kind] == 4 ? 2 : (int)sizeof(CacheSearch) / 16;
+        for (int i = threadIdx.x; i < words; i += kRowThreads)
+            reinterpret_cast<uint4*>(&tables[kind].search)[i] = __ldg(reinterpret_cast<const uint4*>(&s) + i);
+        if (kUnbiased)
+            for (int i = threadIdx.x; i < kCacheLevels - 1; i += kRowThreads) {
+                const float l = __ldg(t.levels + i);
+                tables[kind].low_gap[i] = make_float2(l, __fsub_rn(__ldg(t.levels + i + 1), l));
+            }
+    }
+    __syncthreads();
+    pdl_wait();
+    pdl_launch_next();
+
+    constexpr int kRows = kRowThreads / kLanes;
+    const uint32_t rows = (uint32_t)(a.tokens * a.shape.heads);
+    const int lane = threadIdx.x % kLanes, d = lane * kEach;
+    const int64_t page_size = (int64_t)1 << a.shape.page_shift;
+    for (uint32_t first = blockIdx.x * kRows; first < rows; first += gridDim.x * kRows) {
+        // every lane of a warp takes part in the reductions, those past the last row with zeros
+        const uint32_t r = first + threadIdx.x / kLanes;
+        Place p{};
+        int64_t position = 0;
+        p.slot = -1;
+        if (r < rows) {
+            p = place_of(r, a.shape.heads, a.by_head, a.slots);
+            if (a.rotary.table) position = __ldg(a.rotary.at + p.token);
+            if (p.slot >= a.num_slots) { p.slot = -1; if (lane == 0) atomicOr(a.flags, LQ_CACHE_BAD_SLOT); }
+            if (p.slot >= 0 && a.rotary.table && (position < 0 || position >= a.rotary.positions)) {
+                p.slot = -1;
+                if (lane == 0) atomicOr(a.flags, LQ_CACHE_BAD_POSITION);
+            }
+        }
+        const bool live = p.slot >= 0;
+        const int64_t page = p.slot >> a.shape.page_shift, place = p.slot & (page_size - 1);
+        uint32_t* base = a.pages + page * a.shape.page_words + p.head * a.shape.head_words;
+#pragma unroll 1
+        for (int kind = 0; kind < 2; ++kind) {
+            float x[kEach] = {};
+            if (live) {
+                const CacheRows& in = a.rows[kind];
+                const T* row = static_cast<const T*>(in.data) + p.token * in.token_stride + p.head * in.head_stride;
+                load8(x, row, d, a.shape.dim, in.wide);
+                if (kind == LQ_KEYS && a.rotary.table) rotate8(x, row, d, a.rotary, position);
+            }
+            bool bad;
+            const float norm = row_norm<kLanes>(x, a.shape.q, bad);
+            if (!live) continue;
+            uint32_t rnd[kEach];
+            if (kUnbiased) {
+                const uint32_t c0 = (uint32_t)(p.head * a.shape.padded + d) / 4;
+                uint32_t w[4];
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    philox4x32_10(c0 + j, 2 * a.layer + kind, (uint32_t)p.slot, a.step, a.seed_lo, a.seed_hi, w);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) rnd[4 * j + i] = w[i];
+                }
+            }
+            uint32_t lo, hi;
+            symbols8<kUnbiased>(x, norm, a.shape.sym_bits[kind], tables[kind], rnd, lo, hi);
+            uint32_t* codes = base + (kind ? page_size * a.shape.row_words[0] : 0) + place * a.shape.row_words[kind];
+            if (a.shape.sym_bits[kind] == 4) codes[lane] = lo;
+            else reinterpret_cast<uint2*>(codes)[lane] = make_uint2(lo, hi);
+            if (lane == 0) {
+                reinterpret_cast<float*>(base + page_size * (a.shape.row_words[0] + a.shape.row_words[1]))[kind * page_size + place] = norm;
+                if (bad) atomicOr(a.flags, LQ_CACHE_NONFINITE);
+            }
+        }
     }
 }
 
 template <typename T, int kLanes>
 __global__ void __launch_bounds__(kRowThreads) cache_read_kernel(const __grid_constant__ CacheReadArgs a)
 {
-    const int64_t thread = (int64_t)blockIdx.x * kRowThreads + threadIdx.x;
-    const int64_t r = thread / kLanes;
-    if (r >= a.tokens * 2 * a.shape.heads) return;
-    const int lane = (int)(thread % kLanes), d = lane * kEach;
-    const int64_t token = r / (2 * a.shape.heads);
-    const int within = (int)(r - token * 2 * a.shape.heads);
-    const int kind = within >= a.shape.heads, head = within - kind * a.shape.heads;
-    int64_t slot = __ldg(a.slots + token);
-    if (slot >= a.num_slots) { slot = -1; if (lane == 0) atomicOr(a.flags, LQ_CACHE_BAD_SLOT); }
+    // signed levels by symbol: 16 of them lie in 16 banks, so that no look-up of 4-bit symbols has a conflict
+    __shared__ float values[2][kCachePairs];
+#pragma unroll
+    for (int kind = 0; kind < 2; ++kind)
+        if (threadIdx.x < 1u << a.shape.sym_bits[kind]) {
+            const float l = __ldg(a.tables[kind].levels + threadIdx.x / 2);
+            values[kind][threadIdx.x] = threadIdx.x % 2 ? -l : l;
+        }
+    __syncthreads();
+    pdl_wait();
+    pdl_launch_next();
 
-    float x[kEach] = {};
-    if (slot >= 0) {
-        const int64_t page = slot >> a.shape.page_shift, place = slot & ((1 << a.shape.page_shift) - 1);
-        const int64_t page_size = (int64_t)1 << a.shape.page_shift;
-        const uint32_t* base = a.pages + page * a.shape.page_words + head * a.shape.head_words;
-        const uint32_t* codes = base + (kind ? page_size * a.shape.row_words[0] : 0) + place * a.shape.row_words[kind];
-        const float norm = __ldg(reinterpret_cast<const float*>(base + page_size * (a.shape.row_words[0] + a.shape.row_words[1])) +
-                                 kind * page_size + place);
-        const uint32_t* pairs = a.tables[kind].pairs;
-        if (a.shape.sym_bits[kind] == 4) {
-            const uint32_t w = __ldg(codes + lane);
+    constexpr int kRows = kRowThreads / kLanes;
+    const uint32_t rows = (uint32_t)(a.tokens * a.shape.heads);
+    const int lane = threadIdx.x % kLanes, d = lane * kEach;
+    const int64_t page_size = (int64_t)1 << a.shape.page_shift;
+    for (uint32_t r = blockIdx.x * kRows + threadIdx.x / kLanes; r < rows; r += gridDim.x * kRows) {
+        Place p = place_of(r, a.shape.heads, a.by_head, a.slots);
+        if (p.slot >= a.num_slots) { p.slot = -1; if (lane == 0) atomicOr(a.flags, LQ_CACHE_BAD_SLOT); }
+        const int64_t page = p.slot >> a.shape.page_shift, place = p.slot & (page_size - 1);
+        const uint32_t* base = a.pages + page * a.shape.page_words + p.head * a.shape.head_words;
+        uint2 w[2] = {};
+        float norm[2] = {0.0f, 0.0f};
+        if (p.slot >= 0) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t p = __ldg(pairs + (w >> (8 * i) & 255));
-                const float2 v = __half22float2(reinterpret_cast<const __half2&>(p));
-                x[2 * i] = __fmul_rn(v.x, norm);
-                x[2 * i + 1] = __fmul_rn(v.y, norm);
-            }
-        } else {
-            const uint2 w = __ldg(reinterpret_cast<const uint2*>(codes) + lane);
-#pragma unroll
-            for (int i = 0; i < kEach; ++i) {
-                const uint32_t p = __ldg(pairs + ((i < 4 ? w.x : w.y) >> (8 * (i & 3)) & 255));
-                x[i] = __fmul_rn(__low2float(reinterpret_cast<const __half2&>(p)), norm);
+            for (int kind = 0; kind < 2; ++kind) {
+                const uint32_t* codes = base + (kind ? page_size * a.shape.row_words[0] : 0) + place * a.shape.row_words[kind];
+                norm[kind] = __ldg(reinterpret_cast<const float*>(base + page_size * (a.shape.row_words[0] + a.shape.row_words[1])) +
+                                   kind * page_size + place);
+                if (a.shape.sym_bits[kind] == 4) w[kind].x = __ldg(codes + lane);
+                else w[kind] = __ldg(reinterpret_cast<const uint2*>(codes) + lane);
             }
         }
+#pragma unroll
+        for (int kind = 0; kind < 2; ++kind) {
+            float x[kEach];
+            if (p.slot < 0) {
+#pragma unroll
+                for (int i = 0; i < kEach; ++i) x[i] = 0.0f;
+            } else if (a.shape.sym_bits[kind] == 4) {
+#pragma unroll
+                for (int i = 0; i < kEach; ++i) x[i] = __fmul_rn(values[kind][w[kind].x >> (4 * i) & 15], norm[kind]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < kEach; ++i) x[i] = __fmul_rn(values[kind][(i < 4 ? w[kind].x : w[kind].y) >> (8 * (i & 3)) & 255], norm[kind]);
+            }
+            const CacheRows& out = a.rows[kind];
+            store8(x, static_cast<T*>(out.data) + p.token * out.token_stride + p.head * out.head_stride, d, a.shape.dim, out.wide);
+        }
     }
-    const CacheRows& out = a.rows[kind];
-    store8(x, static_cast<T*>(out.data) + token * out.token_stride + head * out.head_stride, d, a.shape.dim, out.wide);
 }
 
-template <template <typename, int> class K, typename Args>
-cudaError_t by_type_and_size(const Args& a, int type, cudaStream_t s)
+// CTAs: as many as the rows need, at most what an SM holds at once of them.
+constexpr int kRowCtas = 8 * kSms;
+
+template <typename Args, typename Go>
+cudaError_t by_type_and_size(const Args& a, Go go)
 {
-    const int lanes = a.shape.padded / kEach;
-    const int64_t threads = a.tokens * 2 * a.shape.heads * lanes;
-    const int64_t blocks = (threads + kRowThreads - 1) / kRowThreads;
-    if (blocks == 0) return cudaSuccess;
-    auto go = [&](auto t) {
-        using T = decltype(t);
-        if (lanes == 8) return K<T, 8>::launch(a, (unsigned)blocks, s);
-        if (lanes == 16) return K<T, 16>::launch(a, (unsigned)blocks, s);
-        return K<T, 32>::launch(a, (unsigned)blocks, s);
+    const int lanes = a.shape.padded / kEach, type = a.rows[0].type;
+    const int64_t blocks = (a.tokens * a.shape.heads * lanes + kRowThreads - 1) / kRowThreads;
+    const unsigned grid = (unsigned)(blocks < kRowCtas ? blocks : kRowCtas);
+    auto sized = [&](auto t) {
+        if (lanes == 8) return go(t, std::integral_constant<int, 8>(), grid);
+        if (lanes == 16) return go(t, std::integral_constant<int, 16>(), grid);
+        return go(t, std::integral_constant<int, 32>(), grid);
     };
-    return type == LQ_F32 ? go(float()) : type == LQ_F16 ? go(__half()) : go(__nv_bfloat16());
+    return type == LQ_F32 ? sized(float()) : type == LQ_F16 ? sized(__half()) : sized(__nv_bfloat16());
 }
-
-template <typename T, int kLanes>
-struct Write {
-    static cudaError_t launch(const CacheWriteArgs& a, unsigned blocks, cudaStream_t s)
-    {
-        cache_write_kernel<T, kLanes><<<blocks, kRowThreads, 0, s>>>(a);
-        return cudaGetLastError();
-    }
-};
-
-template <typename T, int kLanes>
-struct Read {
-    static cudaError_t launch(const CacheReadArgs& a, unsigned blocks, cudaStream_t s)
-    {
-        cache_read_kernel<T, kLanes><<<blocks, kRowThreads, 0, s>>>(a);
-        return cudaGetLastError();
-    }
-};
 
 }  // namespace
 
-cudaError_t launch_cache_write(const CacheWriteArgs& a, cudaStream_t s) { return by_type_and_size<Write>(a, a.rows[0].type, s); }
-cudaError_t launch_cache_read(const CacheReadArgs& a, cudaStream_t s) { return by_type_and_size<Read>(a, a.rows[0].type, s); }
+cudaError_t launch_cache_write(const CacheWriteArgs& a, cudaStream_t s)
+{
+    return by_type_and_size(a, [&](auto t, auto lanes, unsigned grid) {
+        using T = decltype(t);
+        constexpr int kLanes = decltype(lanes)::value;
+        return a.unbiased ? launch(cache_write_kernel<T, kLanes, true>, grid, kRowThreads, 0, s, a)
+                          : launch(cache_write_kernel<T, kLanes, false>, grid, kRowThreads, 0, s, a);
+    });
+}
+
+cudaError_t launch_cache_read(const CacheReadArgs& a, cudaStream_t s)
+{
+    return by_type_and_size(a, [&](auto t, auto lanes, unsigned grid) {
+        return launch(cache_read_kernel<decltype(t), decltype(lanes)::value>, grid, kRowThreads, 0, s, a);
+    });
+}
 
 }  // namespace lq
