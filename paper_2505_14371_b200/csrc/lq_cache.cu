@@ -84,6 +84,28 @@ void fill_search(CacheSearch& s, const float* levels, int n, bool nearest)
         s.start[b] = (uint8_t)at;
         s.steps = std::max(s.steps, to - at);
     }
+    // the coarsest bins of the pattern that part all edges; the first one has to start below the first edge
+    auto bits = [](float v) { uint32_t b; std::memcpy(&b, &v, sizeof b); return b; };
+    s.entries = 0;
+    for (int shift = 19; shift >= 15 && !s.entries; --shift) {
+        const uint32_t first = (bits(s.edge[1]) - 1) >> shift, last = bits(1.0f) >> shift;
+        if (last - first >= (uint32_t)kCacheBins) break;
+        bool parted = true;
+        for (int j = 2; j <= edges; ++j) parted = parted && bits(s.edge[j]) >> shift != bits(s.edge[j - 1]) >> shift;
+        if (!parted) continue;
+        int j = 0;                      // edges in the bins before
+        for (uint32_t b = first; b <= last; ++b) {
+            uint32_t e = ((uint32_t)j << shift) - (b << shift);
+            if (j < edges && bits(s.edge[j + 1]) >> shift == b) {
+                e += (1u << shift) - (bits(s.edge[j + 1]) & ((1u << shift) - 1));       // a number at or past the edge carries
+                ++j;
+            }
+            s.entry[b - first] = e;
+        }
+        const uint32_t low = first << shift;
+        std::memcpy(&s.lowest, &low, sizeof low);
+        s.shift = shift; s.first = (int32_t)first; s.entries = (int32_t)(last - first + 1);
+    }
 }
 
 void fill_table(CacheTable& t, const float* levels, int bits)
@@ -132,6 +154,7 @@ int take_rotary(const lq_rotary* r, const CacheShape& shape, bool need_at, Cache
     if (need_at && !r->at) return lq_set_error(LQ_EINVAL, "rotary positions (at) are NULL");
     if (!aligned(r->at, 8)) return lq_set_error(LQ_EINVAL, "rotary positions (at) must be 8-byte aligned");
     out->table = r->table; out->at = r->at; out->positions = r->positions; out->dim = r->dim; out->interleaved = r->interleaved != 0;
+    out->wide = r->dim % 16 == 0 && aligned(r->table, 16);
     return LQ_OK;
 }
 

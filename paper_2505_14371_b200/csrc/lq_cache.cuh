@@ -18,15 +18,22 @@ namespace lq {
 constexpr int kCacheLevels = 128;       // most levels of a set (7 bits)
 constexpr int kCachePairs = 256;        // entries of the look-up table by bytes
 
-constexpr int kCacheBins = 2048;        // of the search: round(2048 u)
+constexpr int kCacheBins = 2048;
 
 // Where u falls: index = how many of edge[1..] are <= u.  For rounding to the nearest level edge[j] is the least fp32 number above
 // the middle of levels j - 1 and j; for unbiased rounding it is level j, up to the last but one.  Entries behind are +infinity.
+// Two searches: by one look-up where no bin of u's pattern (16 to 256 bins an octave, from the first edge's to 1) holds two edges, else by linear
+// bins and steps.
 struct alignas(16) CacheSearch {
+    // 1: u's pattern is cut off `shift` bits; entry[bin - first] + pattern has the index above bit `shift`.  Numbers below `lowest`, the
+    // first bin's start, are taken as it.  entries 0: no such table.
+    int32_t shift, first, entries;
+    float lowest;
+    // 2: by round(2048 u): edges at or below all of the bin's numbers, and the most that are inside one
+    int32_t steps, pad[3];
     float edge[kCacheLevels + 4];
-    uint8_t start[kCacheBins + 16];     // by bin: edges at or below all of its numbers
-    int32_t steps;                      // most edges inside a bin
-    int32_t pad[3];
+    uint8_t start[kCacheBins + 16];
+    uint32_t entry[kCacheBins];
 };
 
 // Device tables of one (layer, keys or values).
@@ -61,6 +68,7 @@ struct CacheRotary {
     int64_t positions;
     int32_t dim;
     int32_t interleaved;
+    int32_t wide;                       // 8 coordinates of a lane are turned alike, and their angles read 16 bytes at a time
 };
 
 // r / heads for 0 <= r < 2^31 as a product: umulhi(2 r, factor) >> shift.

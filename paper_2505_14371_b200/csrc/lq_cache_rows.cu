@@ -7,6 +7,7 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <cstddef>
 #include <type_traits>
 
 #include "lq_cache.cuh"
@@ -61,13 +62,44 @@ __device__ __forceinline__ void store8(const float (&x)[kEach], T* row, int d, i
     }
 }
 
+__device__ __forceinline__ void load_angles(float* to, const float* from, int n)
+{
+    for (int i = 0; i < n; i += 4) *reinterpret_cast<float4*>(to + i) = __ldg(reinterpret_cast<const float4*>(from + i));
+}
+
 // The pairs of the first `dim` coordinates turned by the angles of `position`.  x holds coordinates d .. d+7 of `row`; the
 // partners that this lane does not hold come from the row again (the first level cache has it).
 template <typename T>
-__device__ __forceinline__ void rotate8(float (&x)[kEach], const T* row, int d, const CacheRotary& r, int64_t position)
+__device__ __forceinline__ void rotate8(float (&x)[kEach], const T* row, int d, const CacheRotary& r, int64_t position, bool wide)
 {
     const float* c = r.table + position * r.dim;
     const float* s = c + r.dim / 2;
+    if (r.wide && wide) {
+        if (d >= r.dim) return;
+        alignas(16) float cc[kEach], ss[kEach];
+        if (r.interleaved) {
+            load_angles(cc, c + d / 2, kEach / 2);
+            load_angles(ss, s + d / 2, kEach / 2);
+#pragma unroll
+            for (int i = 0; i < kEach; i += 2) {
+                const float a = x[i], b = x[i + 1];
+                x[i] = __fsub_rn(__fmul_rn(a, cc[i / 2]), __fmul_rn(b, ss[i / 2]));
+                x[i + 1] = __fadd_rn(__fmul_rn(b, cc[i / 2]), __fmul_rn(a, ss[i / 2]));
+            }
+            return;
+        }
+        const int half = r.dim / 2;
+        const bool first = d < half;
+        const int p = first ? d : d - half;
+        float y[kEach];
+        load8(y, row, first ? d + half : p, r.dim, true);
+        load_angles(cc, c + p, kEach);
+        load_angles(ss, s + p, kEach);
+        const float sign = first ? -1.0f : 1.0f;                        // (a product's sign is exact)
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) x[i] = __fadd_rn(__fmul_rn(x[i], cc[i]), sign * __fmul_rn(y[i], ss[i]));
+        return;
+    }
     if (r.interleaved) {
 #pragma unroll
         for (int i = 0; i < kEach; i += 2) {
@@ -148,23 +180,16 @@ __device__ __forceinline__ void symbols8(const float (&x)[kEach], float norm, in
                                          uint32_t& lo, uint32_t& hi)
 {
     const float inv = norm > 0.0f ? __fdiv_rn(1.0f, norm) : 0.0f;
-    auto above = [&](int at, int i, float u) {          // unbiased: whether the upper neighbour is taken
-        const float2 lg = t.low_gap[at];
-        return __fmul_rn(__fmul_rn((float)(rnd[i] >> 9), 1.1920928955078125e-7f), lg.y) < __fsub_rn(u, lg.x);
-    };
-    lo = hi = 0;
-    if (bits == 4) {                    // 7 edges, from registers
-        const float4 e0 = *reinterpret_cast<const float4*>(t.search.edge), e1 = *reinterpret_cast<const float4*>(t.search.edge + 4);
+    uint32_t at[kEach];
+    if (t.search.entries) {
+        // (a number just above 1 is in the bin of 1; NaN, in a row that is kept as zeros, becomes `lowest`)
+        const uint32_t* entry = t.search.entry - t.search.first;
+        const int shift = t.search.shift;
+        const float lowest = t.search.lowest;
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
-            const float u = fminf(__fmul_rn(fabsf(x[i]), inv), 1.0f);
-            const bool p4 = u >= e1.x;
-            const bool p2 = u >= (p4 ? e1.z : e0.z);
-            const float a = p4 ? e1.y : e0.y, b = p4 ? e1.w : e0.w;
-            const bool p1 = u >= (p2 ? b : a);
-            uint32_t at = (p4 ? 8u : 0u) + (p2 ? 4u : 0u) + (p1 ? 2u : 0u);
-            if (kUnbiased) at += above(at / 2, i, u) ? 2 : 0;
-            lo |= (at + (x[i] < 0.0f ? 1u : 0u)) << (4 * i);
+            const uint32_t pattern = __float_as_uint(fmaxf(__fmul_rn(fabsf(x[i]), inv), lowest));
+            at[i] = (entry[pattern >> shift] + pattern) >> shift;
         }
     } else {
         const int steps = t.search.steps;
@@ -172,12 +197,22 @@ __device__ __forceinline__ void symbols8(const float (&x)[kEach], float norm, in
         for (int i = 0; i < kEach; ++i) {
             const float u = fminf(__fmul_rn(fabsf(x[i]), inv), 1.0f);
             // 4096 + u has round(2048 u) in its last bits
-            uint32_t at = t.search.start[__float_as_uint(__fadd_rn(u, 4096.0f)) - 0x45800000u];
-            for (int s = 0; s < steps; ++s) at += u >= t.search.edge[at + 1] ? 1 : 0;
-            if (kUnbiased) at += above(at, i, u) ? 1 : 0;
-            const uint32_t sym = 2 * at + (x[i] < 0.0f ? 1u : 0u);
-            if (i < 4) lo |= sym << (8 * i); else hi |= sym << (8 * (i - 4));
+            at[i] = t.search.start[__float_as_uint(__fadd_rn(u, 4096.0f)) - 0x45800000u];
+            for (int s = 0; s < steps; ++s) at[i] += u >= t.search.edge[at[i] + 1] ? 1 : 0;
         }
+    }
+    lo = hi = 0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        if (kUnbiased) {                // whether the upper neighbour is taken
+            const float u = fminf(__fmul_rn(fabsf(x[i]), inv), 1.0f);
+            const float2 lg = t.low_gap[at[i]];
+            at[i] += __fmul_rn(__fmul_rn((float)(rnd[i] >> 9), 1.1920928955078125e-7f), lg.y) < __fsub_rn(u, lg.x) ? 1 : 0;
+        }
+        const uint32_t sign = x[i] < 0.0f ? 1u : 0u;
+        if (bits == 4) lo += (2 * at[i] + sign) << (4 * i);
+        else if (i < 4) lo += (2 * at[i] + sign) << (8 * i);
+        else hi += (2 * at[i] + sign) << (8 * (i - 4));
     }
     if (!(norm > 0.0f)) lo = hi = 0;
 }
@@ -190,10 +225,14 @@ __global__ void __launch_bounds__(kRowThreads, kUnbiased ? 3 : 4) cache_write_ke
     for (int kind = 0; kind < 2; ++kind) {
         const CacheTable& t = a.tables[kind];
         const CacheSearch& s = kUnbiased ? t.floor : t.nearest;
-        // rows of 4-bit symbols need the edges only
-        const int words = a.shape.sym_bits[kind] == 4 ? 2 : (int)sizeof(CacheSearch) / 16;
-        for (int i = threadIdx.x; i < words; i += kRowThreads)
-            reinterpret_cast<uint4*>(&tables[kind].search)[i] = __ldg(reinterpret_cast<const uint4*>(&s) + i);
+        // the head, and the table of one of the two searches
+        uint4* to = reinterpret_cast<uint4*>(&tables[kind].search);
+        const uint4* from = reinterpret_cast<const uint4*>(&s);
+        constexpr int kHead = (int)offsetof(CacheSearch, edge) / 16, kEntry = (int)offsetof(CacheSearch, entry) / 16;
+        static_assert(offsetof(CacheSearch, edge) % 16 == 0 && offsetof(CacheSearch, entry) % 16 == 0, "parts are copied by 16 bytes");
+        const int entries = __ldg(&s.entries), begin = entries ? kEntry : kHead, end = entries ? kEntry + (entries + 3) / 4 : kEntry;
+        if (threadIdx.x < kHead) to[threadIdx.x] = __ldg(from + threadIdx.x);
+        for (int i = begin + threadIdx.x; i < end; i += kRowThreads) to[i] = __ldg(from + i);
         if (kUnbiased)
             for (int i = threadIdx.x; i < kCacheLevels - 1; i += kRowThreads) {
                 const float l = __ldg(t.levels + i);
@@ -233,7 +272,7 @@ __global__ void __launch_bounds__(kRowThreads, kUnbiased ? 3 : 4) cache_write_ke
                 const CacheRows& in = a.rows[kind];
                 const T* row = static_cast<const T*>(in.data) + p.token * in.token_stride + p.head * in.head_stride;
                 load8(x, row, d, a.shape.dim, in.wide);
-                if (kind == LQ_KEYS && a.rotary.table) rotate8(x, row, d, a.rotary, position);
+                if (kind == LQ_KEYS && a.rotary.table) rotate8(x, row, d, a.rotary, position, in.wide);
             }
             bool bad;
             const float norm = row_norm<kLanes>(x, a.shape.q, bad);
