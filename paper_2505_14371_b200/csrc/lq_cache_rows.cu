@@ -131,12 +131,14 @@ __device__ __forceinline__ float row_norm(const float (&x)[kEach], int q, bool& 
 {
     float n;
     if (q == 0) {
-        uint32_t m = 0;                 // magnitudes order as their bit patterns; Inf and NaN come last
+        // the maximum drops NaN: a sum of x * 0 keeps it, and Inf
+        float m = 0.0f, z = 0.0f;
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) m = max(m, __float_as_uint(x[i]) & 0x7fffffffu);
+        for (int i = 0; i < kEach; ++i) { m = fmaxf(m, fabsf(x[i])); z = fmaf(x[i], 0.0f, z); }
+        if (z != 0.0f) m = INFINITY;
 #pragma unroll
-        for (int o = 1; o < kLanes; o *= 2) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
-        n = __uint_as_float(m);
+        for (int o = 1; o < kLanes; o *= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+        n = m;
     } else {
         double sum = 0.0;
 #pragma unroll
@@ -179,7 +181,7 @@ template <bool kUnbiased>
 __device__ __forceinline__ void symbols8(const float (&x)[kEach], float norm, int bits, const SharedSearch& t, const uint32_t (&rnd)[kEach],
                                          uint32_t& lo, uint32_t& hi)
 {
-    const float inv = norm > 0.0f ? __fdiv_rn(1.0f, norm) : 0.0f;
+    const float inv = norm > 0.0f ? __frcp_rn(norm) : 0.0f;
     uint32_t at[kEach];
     if (t.search.entries) {
         // (a number just above 1 is in the bin of 1; NaN, in a row that is kept as zeros, becomes `lowest`)
@@ -201,18 +203,26 @@ __device__ __forceinline__ void symbols8(const float (&x)[kEach], float norm, in
             for (int s = 0; s < steps; ++s) at[i] += u >= t.search.edge[at[i] + 1] ? 1 : 0;
         }
     }
-    lo = hi = 0;
+    if (kUnbiased) {                    // whether the upper neighbour is taken
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-        if (kUnbiased) {                // whether the upper neighbour is taken
+        for (int i = 0; i < kEach; ++i) {
             const float u = fminf(__fmul_rn(fabsf(x[i]), inv), 1.0f);
             const float2 lg = t.low_gap[at[i]];
             at[i] += __fmul_rn(__fmul_rn((float)(rnd[i] >> 9), 1.1920928955078125e-7f), lg.y) < __fsub_rn(u, lg.x) ? 1 : 0;
         }
-        const uint32_t sign = x[i] < 0.0f ? 1u : 0u;
-        if (bits == 4) lo += (2 * at[i] + sign) << (4 * i);
-        else if (i < 4) lo += (2 * at[i] + sign) << (8 * i);
-        else hi += (2 * at[i] + sign) << (8 * (i - 4));
+    }
+    // (x + 0 has no sign where x is -0)
+    lo = hi = 0;
+    if (bits == 4) {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i)
+            lo += at[i] * (2u << (4 * i)) + (__float_as_uint(__fadd_rn(x[i], 0.0f)) >> 31) * (1u << (4 * i));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            lo += at[i] * (2u << (8 * i)) + (__float_as_uint(__fadd_rn(x[i], 0.0f)) >> 31) * (1u << (8 * i));
+            hi += at[4 + i] * (2u << (8 * i)) + (__float_as_uint(__fadd_rn(x[4 + i], 0.0f)) >> 31) * (1u << (8 * i));
+        }
     }
     if (!(norm > 0.0f)) lo = hi = 0;
 }
@@ -244,38 +254,49 @@ __global__ void __launch_bounds__(kRowThreads, kUnbiased ? 3 : 4) cache_write_ke
     pdl_launch_next();
 
     constexpr int kRows = kRowThreads / kLanes;
-    const uint32_t rows = (uint32_t)(a.tokens * a.shape.heads);
-    const int lane = threadIdx.x % kLanes, d = lane * kEach;
-    const int64_t page_size = (int64_t)1 << a.shape.page_shift;
-    for (uint32_t first = blockIdx.x * kRows; first < rows; first += gridDim.x * kRows) {
-        // every lane of a warp takes part in the reductions, those past the last row with zeros
-        const uint32_t r = first + threadIdx.x / kLanes;
-        Place p{};
-        int64_t position = 0;
+    const uint32_t rows = (uint32_t)(a.tokens * a.shape.heads), stride = gridDim.x * kRows;
+    const int lane = threadIdx.x % kLanes, d = lane * kEach, page_size = 1 << a.shape.page_shift;
+    const int norms_at = page_size * (a.shape.row_words[0] + a.shape.row_words[1]);
+    const bool turned = a.rotary.table != nullptr;
+    // slot and position are fetched a round ahead
+    auto fetch = [&](uint32_t r, Place& p, int64_t& position) {
         p.slot = -1;
         if (r < rows) {
             p = place_of(r, a.shape.heads, a.by_head, a.slots);
-            if (a.rotary.table) position = __ldg(a.rotary.at + p.token);
-            if (p.slot >= a.num_slots) { p.slot = -1; if (lane == 0) atomicOr(a.flags, LQ_CACHE_BAD_SLOT); }
-            if (p.slot >= 0 && a.rotary.table && (position < 0 || position >= a.rotary.positions)) {
-                p.slot = -1;
-                if (lane == 0) atomicOr(a.flags, LQ_CACHE_BAD_POSITION);
-            }
+            if (turned) position = __ldg(a.rotary.at + p.token);
         }
+    };
+    Place next;
+    int64_t next_position = 0;
+    fetch(blockIdx.x * kRows + threadIdx.x / kLanes, next, next_position);
+    for (uint32_t first = blockIdx.x * kRows; first < rows; first += stride) {
+        Place p = next;
+        const int64_t position = next_position;
+        fetch(first + stride + threadIdx.x / kLanes, next, next_position);
+        if (p.slot >= a.num_slots) { p.slot = -1; if (lane == 0) atomicOr(a.flags, LQ_CACHE_BAD_SLOT); }
+        if (turned && p.slot >= 0 && (position < 0 || position >= a.rotary.positions)) {
+            p.slot = -1;
+            if (lane == 0) atomicOr(a.flags, LQ_CACHE_BAD_POSITION);
+        }
+        // every lane of a warp takes part in the reductions, those without a row with zeros
         const bool live = p.slot >= 0;
-        const int64_t page = p.slot >> a.shape.page_shift, place = p.slot & (page_size - 1);
-        uint32_t* base = a.pages + page * a.shape.page_words + p.head * a.shape.head_words;
-#pragma unroll 1
-        for (int kind = 0; kind < 2; ++kind) {
-            float x[kEach] = {};
-            if (live) {
+        float x[2][kEach] = {};
+        if (live) {
+            const T* row[2];
+#pragma unroll
+            for (int kind = 0; kind < 2; ++kind) {
                 const CacheRows& in = a.rows[kind];
-                const T* row = static_cast<const T*>(in.data) + p.token * in.token_stride + p.head * in.head_stride;
-                load8(x, row, d, a.shape.dim, in.wide);
-                if (kind == LQ_KEYS && a.rotary.table) rotate8(x, row, d, a.rotary, position, in.wide);
+                row[kind] = static_cast<const T*>(in.data) + p.token * in.token_stride + p.head * in.head_stride;
+                load8(x[kind], row[kind], d, a.shape.dim, in.wide);
             }
+            if (turned) rotate8(x[LQ_KEYS], row[LQ_KEYS], d, a.rotary, position, a.rows[LQ_KEYS].wide);
+        }
+        const int place = (int)p.slot & (page_size - 1);
+        uint32_t* base = a.pages + (p.slot >> a.shape.page_shift) * a.shape.page_words + p.head * a.shape.head_words;
+#pragma unroll
+        for (int kind = 0; kind < 2; ++kind) {
             bool bad;
-            const float norm = row_norm<kLanes>(x, a.shape.q, bad);
+            const float norm = row_norm<kLanes>(x[kind], a.shape.q, bad);
             if (!live) continue;
             uint32_t rnd[kEach];
             if (kUnbiased) {
@@ -289,12 +310,12 @@ __global__ void __launch_bounds__(kRowThreads, kUnbiased ? 3 : 4) cache_write_ke
                 }
             }
             uint32_t lo, hi;
-            symbols8<kUnbiased>(x, norm, a.shape.sym_bits[kind], tables[kind], rnd, lo, hi);
+            symbols8<kUnbiased>(x[kind], norm, a.shape.sym_bits[kind], tables[kind], rnd, lo, hi);
             uint32_t* codes = base + (kind ? page_size * a.shape.row_words[0] : 0) + place * a.shape.row_words[kind];
             if (a.shape.sym_bits[kind] == 4) codes[lane] = lo;
             else reinterpret_cast<uint2*>(codes)[lane] = make_uint2(lo, hi);
             if (lane == 0) {
-                reinterpret_cast<float*>(base + page_size * (a.shape.row_words[0] + a.shape.row_words[1]))[kind * page_size + place] = norm;
+                reinterpret_cast<float*>(base)[norms_at + kind * page_size + place] = norm;
                 if (bad) atomicOr(a.flags, LQ_CACHE_NONFINITE);
             }
         }
