@@ -136,10 +136,12 @@ int take_rows(const char* name, const lq_rows* r, int64_t n, int heads, bool out
     if (output && ((n > 1 && r->token_stride == 0) || (heads > 1 && r->head_stride == 0)))
         return lq_set_error(LQ_EINVAL, "%s: rows of an output share memory (a stride is 0)", name);
     out->data = r->data;
-    out->token_stride = n > 1 ? r->token_stride : 0;
-    out->head_stride = heads > 1 ? r->head_stride : 0;
+    for (const int64_t s : {r->token_stride, r->head_stride})
+        if (s > INT64_MAX / 4 || s < INT64_MIN / 4) return lq_set_error(LQ_EINVAL, "%s: a stride is out of range", name);
+    out->token_bytes = n > 1 ? r->token_stride * size : 0;
+    out->head_bytes = heads > 1 ? r->head_stride * size : 0;
     out->type = r->type;
-    out->wide = aligned(r->data, 16) && out->token_stride * size % 16 == 0 && out->head_stride * size % 16 == 0;
+    out->wide = aligned(r->data, 16) && out->token_bytes % 16 == 0 && out->head_bytes % 16 == 0;
     return LQ_OK;
 }
 
@@ -219,7 +221,7 @@ int lq_cache_create(lq_cache** out, int32_t num_layers, int32_t kv_heads, int32_
     c->layers = num_layers; c->seed = seed;
     c->bits[0] = bits_keys; c->bits[1] = bits_values;
     for (int k = 0; k < 2; ++k) { s.sym_bits[k] = c->bits[k] + 1; s.row_words[k] = s.padded * s.sym_bits[k] / 32; }
-    s.head_words = (int64_t)page_size * (s.row_words[0] + s.row_words[1] + 2);
+    s.head_words = page_size * (s.row_words[0] + s.row_words[1] + 2);
     s.page_words = s.head_words * kv_heads;
 
     std::vector<CacheTable> host;
@@ -270,7 +272,7 @@ int lq_cache_destroy(lq_cache* cache)
     return LQ_OK;
 }
 
-int64_t lq_cache_page_words(const lq_cache* cache) { return cache ? cache->shape.page_words : (int64_t)lq_set_error(LQ_EINVAL, "cache is NULL"); }
+int64_t lq_cache_page_words(const lq_cache* cache) { return cache ? (int64_t)cache->shape.page_words : (int64_t)lq_set_error(LQ_EINVAL, "cache is NULL"); }
 int64_t lq_cache_workspace(const lq_cache* cache) { return cache ? workspace_of(cache) : (int64_t)lq_set_error(LQ_EINVAL, "cache is NULL"); }
 
 int lq_cache_info(const lq_cache* cache, int32_t* kv_heads, int32_t* head_dim, int32_t* page_size, int32_t* device)

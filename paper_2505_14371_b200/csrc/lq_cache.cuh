@@ -51,13 +51,13 @@ struct CacheShape {
     int32_t sym_bits[2];                // 4 or 8: keys, values
     int32_t row_words[2];
     int32_t q;                          // norm: 0 infinity, 1, 2
-    int64_t head_words, page_words;
+    int32_t head_words, page_words;     // (at most 2^28)
 };
 
-// Rows [tokens][heads][dim] with any strides (in elements) between tokens and heads, coordinates side by side.
+// Rows [tokens][heads][dim] with any strides between tokens and heads, coordinates side by side.
 struct CacheRows {
     void* data;
-    int64_t token_stride, head_stride;
+    int64_t token_bytes, head_bytes;    // strides
     int32_t type;                       // LQ_F32, LQ_F16, LQ_BF16
     int32_t wide;                       // every row starts on a 16-byte boundary
 };

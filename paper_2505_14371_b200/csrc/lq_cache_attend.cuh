@@ -154,18 +154,23 @@ __device__ __forceinline__ void wait_copies() { asm volatile("cp.async.wait_grou
 // Barrier of one team.
 __device__ __forceinline__ void team_sync(int team) { asm volatile("bar.sync %0, %1;" :: "r"(team + 1), "n"(kTeam) : "memory"); }
 
-__device__ __forceinline__ float load_any(const CacheRows& r, int64_t at)
+__device__ __forceinline__ char* row_of(const CacheRows& r, int token, int head)
 {
-    if (r.type == LQ_F32) return static_cast<const float*>(r.data)[at];
-    if (r.type == LQ_F16) return __half2float(static_cast<const __half*>(r.data)[at]);
-    return __bfloat162float(static_cast<const __nv_bfloat16*>(r.data)[at]);
+    return static_cast<char*>(r.data) + token * r.token_bytes + head * r.head_bytes;
 }
 
-__device__ __forceinline__ void store_any(const CacheRows& r, int64_t at, float v)
+__device__ __forceinline__ float load_any(int type, const char* row, int d)
 {
-    if (r.type == LQ_F32) static_cast<float*>(r.data)[at] = v;
-    else if (r.type == LQ_F16) static_cast<__half*>(r.data)[at] = __float2half_rn(v);
-    else static_cast<__nv_bfloat16*>(r.data)[at] = __float2bfloat16_rn(v);
+    if (type == LQ_F32) return reinterpret_cast<const float*>(row)[d];
+    if (type == LQ_F16) return __half2float(reinterpret_cast<const __half*>(row)[d]);
+    return __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(row)[d]);
+}
+
+__device__ __forceinline__ void store_any(int type, char* row, int d, float v)
+{
+    if (type == LQ_F32) reinterpret_cast<float*>(row)[d] = v;
+    else if (type == LQ_F16) reinterpret_cast<__half*>(row)[d] = __float2half_rn(v);
+    else reinterpret_cast<__nv_bfloat16*>(row)[d] = __float2bfloat16_rn(v);
 }
 
 // What a sequence has to be read of: tokens [first, length), as tiles [tile0, tile1).
@@ -365,7 +370,8 @@ __device__ __forceinline__ void stage_query(TeamShared<P>& sh, const CacheAttend
     uint32_t top = 0;
     bool lost = false;
     if (query < a.group) {
-        const int64_t row = sequence * a.queries.token_stride + (int64_t)(head * a.group + query) * a.queries.head_stride;
+        const char* const row = row_of(a.queries, sequence, head * a.group + query);
+        const int type = a.queries.type;
         const CacheRotary& r = a.rotary;
         const int half = r.dim / 2;
         const float* cs = r.table;
@@ -377,12 +383,12 @@ __device__ __forceinline__ void stage_query(TeamShared<P>& sh, const CacheAttend
 #pragma unroll
         for (int i = 0; i < P / 32; ++i) {
             const int d = lane + 32 * i;
-            x[i] = d < a.shape.dim ? load_any(a.queries, row + d) : 0.0f;
+            x[i] = d < a.shape.dim ? load_any(type, row, d) : 0.0f;
             if (r.table && d < r.dim && !lost) {
                 const bool first = r.interleaved ? d % 2 == 0 : d < half;
                 const int other = r.interleaved ? d ^ 1 : first ? d + half : d - half;
                 const int p = r.interleaved ? d / 2 : first ? d : d - half;
-                const float c = __ldg(cs + p), s = __ldg(cs + half + p), y = load_any(a.queries, row + other);
+                const float c = __ldg(cs + p), s = __ldg(cs + half + p), y = load_any(type, row, other);
                 x[i] = first ? __fsub_rn(__fmul_rn(x[i], c), __fmul_rn(y, s)) : __fadd_rn(__fmul_rn(x[i], c), __fmul_rn(y, s));
             }
             if (lost) x[i] = __uint_as_float(0x7fffffffu);
@@ -490,7 +496,7 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
         int64_t chunk = offset - hb * units, at = begin;
 
         const uint32_t base_k = kTableAt + 4 * lane, base_v = base_k + 128, stage0 = (uint32_t)X::stages_at(team * kTeamWarps + warp);
-        const int64_t page_bytes = a.shape.page_words * 4;
+        const int64_t page_bytes = (int64_t)a.shape.page_words * 4;
         const int tile_shift = a.shape.page_shift - 4, tile_mask = (1 << tile_shift) - 1;
         // this lane's places in a stage
         const int row = token_row(g), row_even = token_row(2 * t), row_odd = token_row(2 * t + 1);
@@ -506,7 +512,7 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
             const int32_t* pages = a.table + (int64_t)sequence * a.table_width;
             const int tile0 = x.tile0 + (int)chunk * X::kUnit + warp * X::kPair, stop = min(x.tile1, x.tile0 + ((int)chunk + count) * X::kUnit);
             const int rounds = stop > tile0 ? (stop - tile0 + X::kUnit - 1) / X::kUnit : 0;
-            const char* const bytes = reinterpret_cast<const char*>(a.pages) + head * a.shape.head_words * 4;
+            const char* const bytes = reinterpret_cast<const char*>(a.pages + head * a.shape.head_words);
             auto tile_of = [&](int n) { return tile0 + n / X::kPair * X::kUnit + n % X::kPair; };      // of the warp's n-th tile
             uint32_t missing = 0;                                       // bit s: stage s holds no tile: past the end, or on a page that is not there
             int page = -1;                                              // lane l: of the warp's tile 32 i + l, i as far as copies are
@@ -680,10 +686,10 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
                 if (whole) {
                     if (block * kQueries + query < a.group) {
                         const float f = total != 0.0f ? ex2(rw - r - kLift) / total : 0.0f;
-                        const int64_t to = sequence * a.out.token_stride + (int64_t)(head * a.group + block * kQueries + query) * a.out.head_stride;
+                        char* const to = row_of(a.out, sequence, head * a.group + block * kQueries + query);
                         const float o[4] = {sum4.x * f, sum4.y * f, sum4.z * f, sum4.w * f};
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) if (d + k < a.shape.dim) store_any(a.out, to + d + k, o[k]);
+                        for (int k = 0; k < 4; ++k) if (d + k < a.shape.dim) store_any(a.out.type, to, d + k, o[k]);
                         if (d == 0 && a.lse)
                             a.lse[(int64_t)sequence * a.shape.heads * a.group + head * a.group + block * kQueries + query] =
                                 total != 0.0f ? (r + log2f(total)) * 0.693147180559945309f : -INFINITY;
@@ -716,7 +722,7 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
         if (extent_of(a, b).template units<X::kUnit>() > 0) continue;
         const int queries = a.shape.heads * a.group;
         for (int64_t i = tid; i < (int64_t)queries * a.shape.dim; i += kTeam)
-            store_any(a.out, b * a.out.token_stride + (i / a.shape.dim) * a.out.head_stride + i % a.shape.dim, 0.0f);
+            store_any(a.out.type, row_of(a.out, b, (int)(i / a.shape.dim)), (int)(i % a.shape.dim), 0.0f);
         if (a.lse) for (int i = tid; i < queries; i += kTeam) a.lse[(int64_t)b * queries + i] = -INFINITY;
     }
 }
@@ -755,9 +761,9 @@ __global__ void __launch_bounds__(kTeam) attend_join_kernel(const __grid_constan
         for (int i = 0; i < P / 32; ++i) acc[i] += p[lane + 32 * i] * f;
     }
     const float f = total != 0.0f ? ex2(rw - r - kLift) / total : 0.0f;
-    const int64_t to = rec.sequence * a.out.token_stride + (int64_t)(head * a.group + query) * a.out.head_stride;
+    char* const to = row_of(a.out, rec.sequence, head * a.group + query);
 #pragma unroll
-    for (int i = 0; i < P / 32; ++i) if (lane + 32 * i < a.shape.dim) store_any(a.out, to + lane + 32 * i, acc[i] * f);
+    for (int i = 0; i < P / 32; ++i) if (lane + 32 * i < a.shape.dim) store_any(a.out.type, to, lane + 32 * i, acc[i] * f);
     if (lane == 0 && a.lse)
         a.lse[(int64_t)rec.sequence * a.shape.heads * a.group + head * a.group + query] =
             total != 0.0f ? (r + log2f(total)) * 0.693147180559945309f : -INFINITY;

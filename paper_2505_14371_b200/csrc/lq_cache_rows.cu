@@ -31,19 +31,27 @@ template <> __device__ __forceinline__ __nv_bfloat16 of_f32<__nv_bfloat16>(float
 
 // Coordinates d .. d+7 of a row, zeros past its end.  `wide`: the row starts on a 16-byte boundary.
 template <typename T>
-__device__ __forceinline__ void load8(float (&x)[kEach], const T* row, int d, int dim, bool wide)
+struct alignas(16) Eight { T v[kEach]; };
+
+template <typename T>
+__device__ __forceinline__ Eight<T> load8(const T* row, int d, int dim, bool wide)
 {
+    Eight<T> e;
     if (wide && d + kEach <= dim) {
-        constexpr int kWords = kEach * sizeof(T) / 16;
-        alignas(16) T t[kEach];
 #pragma unroll
-        for (int i = 0; i < kWords; ++i) reinterpret_cast<uint4*>(t)[i] = __ldg(reinterpret_cast<const uint4*>(row + d) + i);
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) x[i] = to_f32(t[i]);
+        for (int i = 0; i < (int)(kEach * sizeof(T) / 16); ++i) reinterpret_cast<uint4*>(&e)[i] = __ldg(reinterpret_cast<const uint4*>(row + d) + i);
     } else {
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) x[i] = d + i < dim ? to_f32(row[d + i]) : 0.0f;
+        for (int i = 0; i < kEach; ++i) e.v[i] = d + i < dim ? row[d + i] : of_f32<T>(0.0f);
     }
+    return e;
+}
+
+template <typename T>
+__device__ __forceinline__ void floats(float (&x)[kEach], const Eight<T>& e)
+{
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) x[i] = to_f32(e.v[i]);
 }
 
 template <typename T>
@@ -72,7 +80,7 @@ __device__ __forceinline__ void load_angles(float* to, const float* from, int n)
 template <typename T>
 __device__ __forceinline__ void rotate8(float (&x)[kEach], const T* row, int d, const CacheRotary& r, int64_t position, bool wide)
 {
-    const float* c = r.table + position * r.dim;
+    const float* c = r.table + position * (int64_t)r.dim;
     const float* s = c + r.dim / 2;
     if (r.wide && wide) {
         if (d >= r.dim) return;
@@ -92,7 +100,7 @@ __device__ __forceinline__ void rotate8(float (&x)[kEach], const T* row, int d, 
         const bool first = d < half;
         const int p = first ? d : d - half;
         float y[kEach];
-        load8(y, row, first ? d + half : p, r.dim, true);
+        floats(y, load8(row, first ? d + half : p, r.dim, true));
         load_angles(cc, c + p, kEach);
         load_angles(ss, s + p, kEach);
         const float sign = first ? -1.0f : 1.0f;                        // (a product's sign is exact)
@@ -156,15 +164,15 @@ __device__ __forceinline__ float row_norm(const float (&x)[kEach], int q, bool& 
 
 // The (token, head) pair of this group of lanes and where its slot is.
 struct Place {
-    int64_t token, slot;
-    int head;
+    int64_t slot;
+    int token, head;
 };
 
 __device__ __forceinline__ Place place_of(uint32_t r, int heads, const CacheRowsOf& by, const int64_t* slots)
 {
     Place p;
     const uint32_t token = __umulhi(2 * r, by.factor) >> by.shift;
-    p.token = token;
+    p.token = (int)token;
     p.head = (int)(r - token * heads);
     p.slot = __ldg(slots + token);
     return p;
@@ -228,7 +236,7 @@ __device__ __forceinline__ void symbols8(const float (&x)[kEach], float norm, in
 }
 
 template <typename T, int kLanes, bool kUnbiased>
-__global__ void __launch_bounds__(kRowThreads, kUnbiased ? 3 : 4) cache_write_kernel(const __grid_constant__ CacheWriteArgs a)
+__global__ void __launch_bounds__(kRowThreads, 4) cache_write_kernel(const __grid_constant__ CacheWriteArgs a)
 {
     __shared__ SharedSearch tables[2];
 #pragma unroll
@@ -258,41 +266,44 @@ __global__ void __launch_bounds__(kRowThreads, kUnbiased ? 3 : 4) cache_write_ke
     const int lane = threadIdx.x % kLanes, d = lane * kEach, page_size = 1 << a.shape.page_shift;
     const int norms_at = page_size * (a.shape.row_words[0] + a.shape.row_words[1]);
     const bool turned = a.rotary.table != nullptr;
-    // slot and position are fetched a round ahead
-    auto fetch = [&](uint32_t r, Place& p, int64_t& position) {
-        p.slot = -1;
+    // slot, position and the rows themselves are fetched a round ahead
+    struct Round {
+        Place p;
+        int64_t position;
+        Eight<T> row[2];
+    };
+    auto row_of = [&](int kind, const Place& p) {
+        const CacheRows& in = a.rows[kind];
+        return reinterpret_cast<const T*>(static_cast<const char*>(in.data) + p.token * in.token_bytes + p.head * in.head_bytes);
+    };
+    auto fetch = [&](Round& n, uint32_t r) {
+        n.p.slot = -1;
         if (r < rows) {
-            p = place_of(r, a.shape.heads, a.by_head, a.slots);
-            if (turned) position = __ldg(a.rotary.at + p.token);
+            n.p = place_of(r, a.shape.heads, a.by_head, a.slots);
+            if (turned) n.position = __ldg(a.rotary.at + n.p.token);
+#pragma unroll
+            for (int kind = 0; kind < 2; ++kind) n.row[kind] = load8(row_of(kind, n.p), d, a.shape.dim, a.rows[kind].wide);
         }
     };
-    Place next;
-    int64_t next_position = 0;
-    fetch(blockIdx.x * kRows + threadIdx.x / kLanes, next, next_position);
+    Round next{};
+    fetch(next, blockIdx.x * kRows + threadIdx.x / kLanes);
     for (uint32_t first = blockIdx.x * kRows; first < rows; first += stride) {
-        Place p = next;
-        const int64_t position = next_position;
-        fetch(first + stride + threadIdx.x / kLanes, next, next_position);
+        Place p = next.p;
+        const int64_t position = next.position;
+        // every lane of a warp takes part in the reductions, those without a row with whatever they hold
+        float x[2][kEach];
+        floats(x[0], next.row[0]);
+        floats(x[1], next.row[1]);
+        fetch(next, first + stride + threadIdx.x / kLanes);
         if (p.slot >= a.num_slots) { p.slot = -1; if (lane == 0) atomicOr(a.flags, LQ_CACHE_BAD_SLOT); }
         if (turned && p.slot >= 0 && (position < 0 || position >= a.rotary.positions)) {
             p.slot = -1;
             if (lane == 0) atomicOr(a.flags, LQ_CACHE_BAD_POSITION);
         }
-        // every lane of a warp takes part in the reductions, those without a row with zeros
         const bool live = p.slot >= 0;
-        float x[2][kEach] = {};
-        if (live) {
-            const T* row[2];
-#pragma unroll
-            for (int kind = 0; kind < 2; ++kind) {
-                const CacheRows& in = a.rows[kind];
-                row[kind] = static_cast<const T*>(in.data) + p.token * in.token_stride + p.head * in.head_stride;
-                load8(x[kind], row[kind], d, a.shape.dim, in.wide);
-            }
-            if (turned) rotate8(x[LQ_KEYS], row[LQ_KEYS], d, a.rotary, position, a.rows[LQ_KEYS].wide);
-        }
+        if (turned && live) rotate8(x[LQ_KEYS], row_of(LQ_KEYS, p), d, a.rotary, position, a.rows[LQ_KEYS].wide);
         const int place = (int)p.slot & (page_size - 1);
-        uint32_t* base = a.pages + (p.slot >> a.shape.page_shift) * a.shape.page_words + p.head * a.shape.head_words;
+        uint32_t* base = a.pages + (int64_t)(int)(p.slot >> a.shape.page_shift) * a.shape.page_words + p.head * a.shape.head_words;
 #pragma unroll
         for (int kind = 0; kind < 2; ++kind) {
             bool bad;
@@ -339,13 +350,12 @@ __global__ void __launch_bounds__(kRowThreads) cache_read_kernel(const __grid_co
 
     constexpr int kRows = kRowThreads / kLanes;
     const uint32_t rows = (uint32_t)(a.tokens * a.shape.heads);
-    const int lane = threadIdx.x % kLanes, d = lane * kEach;
-    const int64_t page_size = (int64_t)1 << a.shape.page_shift;
+    const int lane = threadIdx.x % kLanes, d = lane * kEach, page_size = 1 << a.shape.page_shift;
     for (uint32_t r = blockIdx.x * kRows + threadIdx.x / kLanes; r < rows; r += gridDim.x * kRows) {
         Place p = place_of(r, a.shape.heads, a.by_head, a.slots);
         if (p.slot >= a.num_slots) { p.slot = -1; if (lane == 0) atomicOr(a.flags, LQ_CACHE_BAD_SLOT); }
-        const int64_t page = p.slot >> a.shape.page_shift, place = p.slot & (page_size - 1);
-        const uint32_t* base = a.pages + page * a.shape.page_words + p.head * a.shape.head_words;
+        const int place = (int)p.slot & (page_size - 1);
+        const uint32_t* base = a.pages + (int64_t)(int)(p.slot >> a.shape.page_shift) * a.shape.page_words + p.head * a.shape.head_words;
         uint2 w[2] = {};
         float norm[2] = {0.0f, 0.0f};
         if (p.slot >= 0) {
@@ -372,20 +382,18 @@ __global__ void __launch_bounds__(kRowThreads) cache_read_kernel(const __grid_co
                 for (int i = 0; i < kEach; ++i) x[i] = __fmul_rn(values[kind][(i < 4 ? w[kind].x : w[kind].y) >> (8 * (i & 3)) & 255], norm[kind]);
             }
             const CacheRows& out = a.rows[kind];
-            store8(x, static_cast<T*>(out.data) + p.token * out.token_stride + p.head * out.head_stride, d, a.shape.dim, out.wide);
+            store8(x, reinterpret_cast<T*>(static_cast<char*>(out.data) + p.token * out.token_bytes + p.head * out.head_bytes), d, a.shape.dim, out.wide);
         }
     }
 }
 
-// CTAs: as many as the rows need, at most what an SM holds at once of them.
-constexpr int kRowCtas = 8 * kSms;
-
+// CTAs: as many as the rows need, at most as the GPU holds at once (`resident` an SM).
 template <typename Args, typename Go>
-cudaError_t by_type_and_size(const Args& a, Go go)
+cudaError_t by_type_and_size(const Args& a, int resident, Go go)
 {
     const int lanes = a.shape.padded / kEach, type = a.rows[0].type;
     const int64_t blocks = (a.tokens * a.shape.heads * lanes + kRowThreads - 1) / kRowThreads;
-    const unsigned grid = (unsigned)(blocks < kRowCtas ? blocks : kRowCtas);
+    const unsigned grid = (unsigned)(blocks < resident * kSms ? blocks : resident * kSms);
     auto sized = [&](auto t) {
         if (lanes == 8) return go(t, std::integral_constant<int, 8>(), grid);
         if (lanes == 16) return go(t, std::integral_constant<int, 16>(), grid);
@@ -398,7 +406,7 @@ cudaError_t by_type_and_size(const Args& a, Go go)
 
 cudaError_t launch_cache_write(const CacheWriteArgs& a, cudaStream_t s)
 {
-    return by_type_and_size(a, [&](auto t, auto lanes, unsigned grid) {
+    return by_type_and_size(a, 4, [&](auto t, auto lanes, unsigned grid) {
         using T = decltype(t);
         constexpr int kLanes = decltype(lanes)::value;
         return a.unbiased ? launch(cache_write_kernel<T, kLanes, true>, grid, kRowThreads, 0, s, a)
@@ -408,7 +416,7 @@ cudaError_t launch_cache_write(const CacheWriteArgs& a, cudaStream_t s)
 
 cudaError_t launch_cache_read(const CacheReadArgs& a, cudaStream_t s)
 {
-    return by_type_and_size(a, [&](auto t, auto lanes, unsigned grid) {
+    return by_type_and_size(a, 8, [&](auto t, auto lanes, unsigned grid) {
         return launch(cache_read_kernel<decltype(t), decltype(lanes)::value>, grid, kRowThreads, 0, s, a);
     });
 }
