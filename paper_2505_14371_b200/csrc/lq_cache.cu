@@ -136,10 +136,11 @@ int take_rows(const char* name, const lq_rows* r, int64_t n, int heads, bool out
     if (output && ((n > 1 && r->token_stride == 0) || (heads > 1 && r->head_stride == 0)))
         return lq_set_error(LQ_EINVAL, "%s: rows of an output share memory (a stride is 0)", name);
     out->data = r->data;
-    for (const int64_t s : {r->token_stride, r->head_stride})
-        if (s > INT64_MAX / 4 || s < INT64_MIN / 4) return lq_set_error(LQ_EINVAL, "%s: a stride is out of range", name);
-    out->token_bytes = n > 1 ? r->token_stride * size : 0;
-    out->head_bytes = heads > 1 ? r->head_stride * size : 0;
+    const int64_t token = n > 1 ? r->token_stride : 0, head = heads > 1 ? r->head_stride : 0;
+    for (const int64_t s : {token, head})
+        if (s > INT32_MAX / size || s < -(INT32_MAX / size)) return lq_set_error(LQ_EINVAL, "%s: a stride is 2^31 bytes or more", name);
+    out->token_bytes = (int32_t)token * size;
+    out->head_bytes = (int32_t)head * size;
     out->type = r->type;
     out->wide = aligned(r->data, 16) && out->token_bytes % 16 == 0 && out->head_bytes % 16 == 0;
     return LQ_OK;
@@ -152,7 +153,7 @@ int take_rotary(const lq_rotary* r, const CacheShape& shape, bool need_at, Cache
     if (!r->table || !aligned(r->table, 4)) return lq_set_error(LQ_EINVAL, "rotary table is NULL or not 4-byte aligned");
     if (r->dim < 2 || r->dim % 2 || r->dim > shape.dim)
         return lq_set_error(LQ_EINVAL, "rotary dim %d is not an even number from 2 to head_dim = %d", r->dim, shape.dim);
-    if (r->positions < 1) return lq_set_error(LQ_EINVAL, "rotary table has %lld positions", (long long)r->positions);
+    if (r->positions < 1 || r->positions > INT32_MAX) return lq_set_error(LQ_EINVAL, "rotary table has %lld positions: 1 to 2^31 - 1 are wanted", (long long)r->positions);
     if (need_at && !r->at) return lq_set_error(LQ_EINVAL, "rotary positions (at) are NULL");
     if (!aligned(r->at, 8)) return lq_set_error(LQ_EINVAL, "rotary positions (at) must be 8-byte aligned");
     out->table = r->table; out->at = r->at; out->positions = r->positions; out->dim = r->dim; out->interleaved = r->interleaved != 0;

@@ -57,7 +57,7 @@ struct CacheShape {
 // Rows [tokens][heads][dim] with any strides between tokens and heads, coordinates side by side.
 struct CacheRows {
     void* data;
-    int64_t token_bytes, head_bytes;    // strides
+    int32_t token_bytes, head_bytes;    // strides
     int32_t type;                       // LQ_F32, LQ_F16, LQ_BF16
     int32_t wide;                       // every row starts on a 16-byte boundary
 };

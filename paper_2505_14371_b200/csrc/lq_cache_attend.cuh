@@ -156,7 +156,7 @@ __device__ __forceinline__ void team_sync(int team) { asm volatile("bar.sync %0,
 
 __device__ __forceinline__ char* row_of(const CacheRows& r, int token, int head)
 {
-    return static_cast<char*>(r.data) + token * r.token_bytes + head * r.head_bytes;
+    return static_cast<char*>(r.data) + (int64_t)token * r.token_bytes + (int64_t)head * r.head_bytes;
 }
 
 __device__ __forceinline__ float load_any(int type, const char* row, int d)

@@ -18,6 +18,7 @@ namespace {
 
 constexpr int kRowThreads = 256;
 constexpr int kEach = 8;                // coordinates a lane
+constexpr int kWriteCtas = 4;           // CTAs of the writing kernel that an SM holds at once, by its registers
 
 template <typename T> __device__ __forceinline__ float to_f32(T v);
 template <> __device__ __forceinline__ float to_f32<float>(float v) { return v; }
@@ -50,8 +51,17 @@ __device__ __forceinline__ Eight<T> load8(const T* row, int d, int dim, bool wid
 template <typename T>
 __device__ __forceinline__ void floats(float (&x)[kEach], const Eight<T>& e)
 {
+    if constexpr (std::is_same_v<T, __nv_bfloat16>) {   // the upper half of a float: one instruction each
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) x[i] = to_f32(e.v[i]);
+        for (int i = 0; i < kEach; i += 2) {
+            const uint32_t w = reinterpret_cast<const uint32_t*>(&e)[i / 2];
+            x[i] = __uint_as_float(w << 16);
+            x[i + 1] = __uint_as_float(w & 0xffff0000u);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) x[i] = to_f32(e.v[i]);
+    }
 }
 
 template <typename T>
@@ -80,7 +90,7 @@ __device__ __forceinline__ void load_angles(float* to, const float* from, int n)
 template <typename T>
 __device__ __forceinline__ void rotate8(float (&x)[kEach], const T* row, int d, const CacheRotary& r, int64_t position, bool wide)
 {
-    const float* c = r.table + position * (int64_t)r.dim;
+    const float* c = r.table + (int64_t)(uint32_t)position * r.dim;
     const float* s = c + r.dim / 2;
     if (r.wide && wide) {
         if (d >= r.dim) return;
@@ -103,9 +113,9 @@ __device__ __forceinline__ void rotate8(float (&x)[kEach], const T* row, int d, 
         floats(y, load8(row, first ? d + half : p, r.dim, true));
         load_angles(cc, c + p, kEach);
         load_angles(ss, s + p, kEach);
-        const float sign = first ? -1.0f : 1.0f;                        // (a product's sign is exact)
+        const uint32_t flip = first ? 0x80000000u : 0u;                 // (a product's sign is exact)
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) x[i] = __fadd_rn(__fmul_rn(x[i], cc[i]), sign * __fmul_rn(y[i], ss[i]));
+        for (int i = 0; i < kEach; ++i) x[i] = __fadd_rn(__fmul_rn(x[i], cc[i]), __fmul_rn(__uint_as_float(__float_as_uint(y[i]) ^ flip), ss[i]));
         return;
     }
     if (r.interleaved) {
@@ -219,32 +229,36 @@ __device__ __forceinline__ void symbols8(const float (&x)[kEach], float norm, in
             at[i] += __fmul_rn(__fmul_rn((float)(rnd[i] >> 9), 1.1920928955078125e-7f), lg.y) < __fsub_rn(u, lg.x) ? 1 : 0;
         }
     }
-    // (x + 0 has no sign where x is -0)
     lo = hi = 0;
     if (bits == 4) {
 #pragma unroll
-        for (int i = 0; i < kEach; ++i)
-            lo += at[i] * (2u << (4 * i)) + (__float_as_uint(__fadd_rn(x[i], 0.0f)) >> 31) * (1u << (4 * i));
+        for (int i = 0; i < kEach; ++i) {
+            lo += at[i] << (4 * i + 1);
+            if (x[i] < 0.0f) lo += 1u << (4 * i);
+        }
     } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            lo += at[i] * (2u << (8 * i)) + (__float_as_uint(__fadd_rn(x[i], 0.0f)) >> 31) * (1u << (8 * i));
-            hi += at[4 + i] * (2u << (8 * i)) + (__float_as_uint(__fadd_rn(x[4 + i], 0.0f)) >> 31) * (1u << (8 * i));
+            lo += at[i] << (8 * i + 1);
+            hi += at[4 + i] << (8 * i + 1);
+            if (x[i] < 0.0f) lo += 1u << (8 * i);
+            if (x[4 + i] < 0.0f) hi += 1u << (8 * i);
         }
     }
     if (!(norm > 0.0f)) lo = hi = 0;
 }
 
+// blockIdx.y: keys or values.  Rows are fetched a round ahead.
 template <typename T, int kLanes, bool kUnbiased>
-__global__ void __launch_bounds__(kRowThreads, 4) cache_write_kernel(const __grid_constant__ CacheWriteArgs a)
+__global__ void __launch_bounds__(kRowThreads, kWriteCtas) cache_write_kernel(const __grid_constant__ CacheWriteArgs a)
 {
-    __shared__ SharedSearch tables[2];
-#pragma unroll
-    for (int kind = 0; kind < 2; ++kind) {
+    __shared__ SharedSearch table;
+    const int kind = blockIdx.y, bits = a.shape.sym_bits[kind];
+    {
         const CacheTable& t = a.tables[kind];
         const CacheSearch& s = kUnbiased ? t.floor : t.nearest;
         // the head, and the table of one of the two searches
-        uint4* to = reinterpret_cast<uint4*>(&tables[kind].search);
+        uint4* to = reinterpret_cast<uint4*>(&table.search);
         const uint4* from = reinterpret_cast<const uint4*>(&s);
         constexpr int kHead = (int)offsetof(CacheSearch, edge) / 16, kEntry = (int)offsetof(CacheSearch, entry) / 16;
         static_assert(offsetof(CacheSearch, edge) % 16 == 0 && offsetof(CacheSearch, entry) % 16 == 0, "parts are copied by 16 bytes");
@@ -254,7 +268,7 @@ __global__ void __launch_bounds__(kRowThreads, 4) cache_write_kernel(const __gri
         if (kUnbiased)
             for (int i = threadIdx.x; i < kCacheLevels - 1; i += kRowThreads) {
                 const float l = __ldg(t.levels + i);
-                tables[kind].low_gap[i] = make_float2(l, __fsub_rn(__ldg(t.levels + i + 1), l));
+                table.low_gap[i] = make_float2(l, __fsub_rn(__ldg(t.levels + i + 1), l));
             }
     }
     __syncthreads();
@@ -262,73 +276,70 @@ __global__ void __launch_bounds__(kRowThreads, 4) cache_write_kernel(const __gri
     pdl_launch_next();
 
     constexpr int kRows = kRowThreads / kLanes;
-    const uint32_t rows = (uint32_t)(a.tokens * a.shape.heads), stride = gridDim.x * kRows;
+    const uint32_t rows = (uint32_t)(a.tokens * a.shape.heads), stride = gridDim.x * kRows, group = threadIdx.x / kLanes;
     const int lane = threadIdx.x % kLanes, d = lane * kEach, page_size = 1 << a.shape.page_shift;
-    const int norms_at = page_size * (a.shape.row_words[0] + a.shape.row_words[1]);
-    const bool turned = a.rotary.table != nullptr;
-    // slot, position and the rows themselves are fetched a round ahead
-    struct Round {
-        Place p;
-        int64_t position;
-        Eight<T> row[2];
+    const int codes_at = kind ? page_size * a.shape.row_words[0] : 0, row_words = a.shape.row_words[kind];
+    const int norms_at = page_size * (a.shape.row_words[0] + a.shape.row_words[1] + kind);
+    const char* const data = static_cast<const char*>(a.rows[kind].data);
+    const int token_bytes = a.rows[kind].token_bytes, head_bytes = a.rows[kind].head_bytes;
+    const bool wide = a.rows[kind].wide, turned = a.rotary.table != nullptr;
+
+    int64_t next_slot = -1, next_position = 0;
+    int next_head = 0;
+    const T* next_row = nullptr;
+    Eight<T> next = {};
+    auto fetch = [&](uint32_t r) {
+        next_slot = -1;
+        if (r >= rows) return;
+        const Place p = place_of(r, a.shape.heads, a.by_head, a.slots);
+        next_slot = p.slot; next_head = p.head;
+        next_row = reinterpret_cast<const T*>(data + (int64_t)p.token * token_bytes + (int64_t)p.head * head_bytes);
+        next = load8(next_row, d, a.shape.dim, wide);
+        if (turned) next_position = __ldg(a.rotary.at + p.token);
     };
-    auto row_of = [&](int kind, const Place& p) {
-        const CacheRows& in = a.rows[kind];
-        return reinterpret_cast<const T*>(static_cast<const char*>(in.data) + p.token * in.token_bytes + p.head * in.head_bytes);
-    };
-    auto fetch = [&](Round& n, uint32_t r) {
-        n.p.slot = -1;
-        if (r < rows) {
-            n.p = place_of(r, a.shape.heads, a.by_head, a.slots);
-            if (turned) n.position = __ldg(a.rotary.at + n.p.token);
-#pragma unroll
-            for (int kind = 0; kind < 2; ++kind) n.row[kind] = load8(row_of(kind, n.p), d, a.shape.dim, a.rows[kind].wide);
-        }
-    };
-    Round next{};
-    fetch(next, blockIdx.x * kRows + threadIdx.x / kLanes);
+    fetch(blockIdx.x * kRows + group);
     for (uint32_t first = blockIdx.x * kRows; first < rows; first += stride) {
-        Place p = next.p;
-        const int64_t position = next.position;
         // every lane of a warp takes part in the reductions, those without a row with whatever they hold
-        float x[2][kEach];
-        floats(x[0], next.row[0]);
-        floats(x[1], next.row[1]);
-        fetch(next, first + stride + threadIdx.x / kLanes);
-        if (p.slot >= a.num_slots) { p.slot = -1; if (lane == 0) atomicOr(a.flags, LQ_CACHE_BAD_SLOT); }
-        if (turned && p.slot >= 0 && (position < 0 || position >= a.rotary.positions)) {
-            p.slot = -1;
-            if (lane == 0) atomicOr(a.flags, LQ_CACHE_BAD_POSITION);
+        int64_t slot = next_slot;
+        const int64_t position = next_position;
+        const int head = next_head;
+        const T* const row = next_row;
+        float x[kEach];
+        floats(x, next);
+        fetch(first + stride + group);
+        if (slot >= a.num_slots) { slot = -1; if (lane == 0) atomicOr(a.flags, LQ_CACHE_BAD_SLOT); }
+        if (turned && slot >= 0) {
+            if ((uint64_t)position >= (uint64_t)a.rotary.positions) {
+                slot = -1;
+                if (lane == 0) atomicOr(a.flags, LQ_CACHE_BAD_POSITION);
+            } else if (kind == LQ_KEYS) {
+                rotate8(x, row, d, a.rotary, position, wide);
+            }
         }
-        const bool live = p.slot >= 0;
-        if (turned && live) rotate8(x[LQ_KEYS], row_of(LQ_KEYS, p), d, a.rotary, position, a.rows[LQ_KEYS].wide);
-        const int place = (int)p.slot & (page_size - 1);
-        uint32_t* base = a.pages + (int64_t)(int)(p.slot >> a.shape.page_shift) * a.shape.page_words + p.head * a.shape.head_words;
+        bool bad;
+        const float norm = row_norm<kLanes>(x, a.shape.q, bad);
+        if (slot < 0) continue;
+        const int place = (int)slot & (page_size - 1);
+        uint32_t* base = a.pages + (int64_t)((uint32_t)slot >> a.shape.page_shift) * a.shape.page_words + head * a.shape.head_words;
+        uint32_t rnd[kEach];
+        if (kUnbiased) {
+            const uint32_t c0 = (uint32_t)(head * a.shape.padded + d) / 4;
+            uint32_t w[4];
 #pragma unroll
-        for (int kind = 0; kind < 2; ++kind) {
-            bool bad;
-            const float norm = row_norm<kLanes>(x[kind], a.shape.q, bad);
-            if (!live) continue;
-            uint32_t rnd[kEach];
-            if (kUnbiased) {
-                const uint32_t c0 = (uint32_t)(p.head * a.shape.padded + d) / 4;
-                uint32_t w[4];
+            for (int j = 0; j < 2; ++j) {
+                philox4x32_10(c0 + j, 2 * a.layer + kind, (uint32_t)slot, a.step, a.seed_lo, a.seed_hi, w);
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    philox4x32_10(c0 + j, 2 * a.layer + kind, (uint32_t)p.slot, a.step, a.seed_lo, a.seed_hi, w);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) rnd[4 * j + i] = w[i];
-                }
+                for (int i = 0; i < 4; ++i) rnd[4 * j + i] = w[i];
             }
-            uint32_t lo, hi;
-            symbols8<kUnbiased>(x[kind], norm, a.shape.sym_bits[kind], tables[kind], rnd, lo, hi);
-            uint32_t* codes = base + (kind ? page_size * a.shape.row_words[0] : 0) + place * a.shape.row_words[kind];
-            if (a.shape.sym_bits[kind] == 4) codes[lane] = lo;
-            else reinterpret_cast<uint2*>(codes)[lane] = make_uint2(lo, hi);
-            if (lane == 0) {
-                reinterpret_cast<float*>(base)[norms_at + kind * page_size + place] = norm;
-                if (bad) atomicOr(a.flags, LQ_CACHE_NONFINITE);
-            }
+        }
+        uint32_t lo, hi;
+        symbols8<kUnbiased>(x, norm, bits, table, rnd, lo, hi);
+        uint32_t* codes = base + codes_at + place * row_words;
+        if (bits == 4) codes[lane] = lo;
+        else reinterpret_cast<uint2*>(codes)[lane] = make_uint2(lo, hi);
+        if (lane == 0) {
+            reinterpret_cast<float*>(base)[norms_at + place] = norm;
+            if (bad) atomicOr(a.flags, LQ_CACHE_NONFINITE);
         }
     }
 }
@@ -355,7 +366,7 @@ __global__ void __launch_bounds__(kRowThreads) cache_read_kernel(const __grid_co
         Place p = place_of(r, a.shape.heads, a.by_head, a.slots);
         if (p.slot >= a.num_slots) { p.slot = -1; if (lane == 0) atomicOr(a.flags, LQ_CACHE_BAD_SLOT); }
         const int place = (int)p.slot & (page_size - 1);
-        const uint32_t* base = a.pages + (int64_t)(int)(p.slot >> a.shape.page_shift) * a.shape.page_words + p.head * a.shape.head_words;
+        const uint32_t* base = a.pages + (int64_t)((uint32_t)p.slot >> a.shape.page_shift) * a.shape.page_words + p.head * a.shape.head_words;
         uint2 w[2] = {};
         float norm[2] = {0.0f, 0.0f};
         if (p.slot >= 0) {
@@ -382,7 +393,7 @@ __global__ void __launch_bounds__(kRowThreads) cache_read_kernel(const __grid_co
                 for (int i = 0; i < kEach; ++i) x[i] = __fmul_rn(values[kind][(i < 4 ? w[kind].x : w[kind].y) >> (8 * (i & 3)) & 255], norm[kind]);
             }
             const CacheRows& out = a.rows[kind];
-            store8(x, reinterpret_cast<T*>(static_cast<char*>(out.data) + p.token * out.token_bytes + p.head * out.head_bytes), d, a.shape.dim, out.wide);
+            store8(x, reinterpret_cast<T*>(static_cast<char*>(out.data) + (int64_t)p.token * out.token_bytes + (int64_t)p.head * out.head_bytes), d, a.shape.dim, out.wide);
         }
     }
 }
@@ -406,11 +417,11 @@ cudaError_t by_type_and_size(const Args& a, int resident, Go go)
 
 cudaError_t launch_cache_write(const CacheWriteArgs& a, cudaStream_t s)
 {
-    return by_type_and_size(a, 4, [&](auto t, auto lanes, unsigned grid) {
+    return by_type_and_size(a, kWriteCtas / 2, [&](auto t, auto lanes, unsigned grid) {
         using T = decltype(t);
         constexpr int kLanes = decltype(lanes)::value;
-        return a.unbiased ? launch(cache_write_kernel<T, kLanes, true>, grid, kRowThreads, 0, s, a)
-                          : launch(cache_write_kernel<T, kLanes, false>, grid, kRowThreads, 0, s, a);
+        return a.unbiased ? launch(cache_write_kernel<T, kLanes, true>, dim3(grid, 2), kRowThreads, 0, s, a)
+                          : launch(cache_write_kernel<T, kLanes, false>, dim3(grid, 2), kRowThreads, 0, s, a);
     });
 }
 
