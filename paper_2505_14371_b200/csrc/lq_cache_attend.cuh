@@ -361,13 +361,11 @@ __device__ __forceinline__ int key_coordinate(int s, int t)
     return (4 * c + t) * kEach + 4 * s % kEach;
 }
 
-// Warp `w` brings query w of the block into shared memory: rotated, times its power of two, as fp16 and the rest.
+// Query w of the block by warp w, rotated.
 template <int P>
-__device__ __forceinline__ void stage_query(TeamShared<P>& sh, const CacheAttendArgs& a, int sequence, int head, int block, int w, int lane, int64_t length)
+__device__ __forceinline__ void load_query(float (&x)[P / 32], const CacheAttendArgs& a, int sequence, int head, int block, int w, int lane, int64_t length)
 {
     const int query = block * kQueries + w;
-    float x[P / 32];
-    uint32_t top = 0;
     bool lost = false;
     if (query < a.group) {
         const char* const row = row_of(a.queries, sequence, head * a.group + query);
@@ -392,13 +390,21 @@ __device__ __forceinline__ void stage_query(TeamShared<P>& sh, const CacheAttend
                 x[i] = first ? __fsub_rn(__fmul_rn(x[i], c), __fmul_rn(y, s)) : __fadd_rn(__fmul_rn(x[i], c), __fmul_rn(y, s));
             }
             if (lost) x[i] = __uint_as_float(0x7fffffffu);
-            top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
         }
         if (lost && lane == 0) atomicOr(a.flags, LQ_CACHE_BAD_POSITION);
     } else {
 #pragma unroll
         for (int i = 0; i < P / 32; ++i) x[i] = 0.0f;
     }
+}
+
+// ... and brought into shared memory: times its power of two, as fp16 and the rest.
+template <int P>
+__device__ __forceinline__ void stage_query(TeamShared<P>& sh, const float (&x)[P / 32], float scale, int w, int lane)
+{
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < P / 32; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
     top = __reduce_max_sync(0xffffffffu, top);
     // 2^e brings the largest coordinate to [2^14, 2^15); Inf and NaN stay what they are
     int e = top >= 0x7f800000u || top == 0 ? 0 : 141 - (int)(top >> 23);
@@ -411,7 +417,7 @@ __device__ __forceinline__ void stage_query(TeamShared<P>& sh, const CacheAttend
         sh.q[0][w][lane + 32 * i] = h;
         sh.q[1][w][lane + 32 * i] = __float2half_rn(y - __half2float(h));
     }
-    if (lane == 0) sh.factor[w] = a.scale * down;
+    if (lane == 0) sh.factor[w] = scale * down;
 }
 
 template <int P, int WK, int WV, int kExact>
@@ -441,20 +447,36 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
 
     // ---- this team's share of all units
     const int head_blocks = a.shape.heads * a.group_blocks, me = blockIdx.x * X::kTeams + team, teams = gridDim.x * X::kTeams;
-    int64_t sum = 0;
-    for (int b = tid; b < a.batch; b += kTeam) {
-        sum += extent_of(a, b).template units<X::kUnit>();
-        const int n = __ldg(a.lengths + b);
-        if (me == 0 && (n < 0 || n > a.table_width << a.shape.page_shift)) atomicOr(a.flags, LQ_CACHE_BAD_LENGTH);
-    }
+    // units of sequence `b`, summed up to it within the team's threads: the last warp-wide step of a scan
+    auto units_of = [&](int b) { return b < a.batch ? extent_of(a, b).template units<X::kUnit>() * head_blocks : 0; };
+    auto warp_scan = [&](int64_t v) {
 #pragma unroll
-    for (int o = 16; o > 0; o /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    if (lane == 0) sh.words[warp] = sum;
+        for (int o = 1; o < 32; o *= 2) {
+            const int64_t up = __shfl_up_sync(0xffffffffu, v, o);
+            if (lane >= o) v += up;
+        }
+        return v;
+    };
+    // the first kTeam sequences, which are all of most batches, are scanned once; the rest only counted here
+    const int64_t mine0 = units_of(tid);
+    int64_t scan0 = warp_scan(mine0), rest = 0;
+    for (int b = tid + kTeam; b < a.batch; b += kTeam) rest += units_of(b);
+    if (a.batch > kTeam) rest = warp_scan(rest);
+    if (lane == 31) { sh.words[warp] = scan0; sh.words[kTeamWarps + warp] = rest; }
+    if (me == 0)
+        for (int b = tid; b < a.batch; b += kTeam) {
+            const int n = __ldg(a.lengths + b);
+            if (n < 0 || n > a.table_width << a.shape.page_shift) atomicOr(a.flags, LQ_CACHE_BAD_LENGTH);
+        }
     __syncthreads();                    // (the table is there too)
-    int64_t all = 0;
+    int64_t all = 0, before = 0;        // units of all sequences, and of the first kTeam
 #pragma unroll
-    for (int w = 0; w < kTeamWarps; ++w) all += sh.words[w];
-    all *= head_blocks;
+    for (int w = 0; w < kTeamWarps; ++w) {
+        if (w == warp) scan0 += before;
+        before += sh.words[w];
+        all += sh.words[kTeamWarps + w];
+    }
+    all += before;
     // no more teams than units take part, so that none between two that share a segment is without a unit
     const int64_t parts = min(all, (int64_t)teams);
     const int64_t begin = me < parts ? all * me / parts : 0, end = me < parts ? all * (me + 1) / parts : 0;
@@ -464,28 +486,22 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
 
     if (begin < end) {
         // the sequence that unit `begin` belongs to, and the units before it
-        int64_t before = 0;
-        for (int base = 0; base < a.batch; base += kTeam) {
-            const int b = base + tid;
-            const int64_t mine = b < a.batch ? extent_of(a, b).template units<X::kUnit>() * head_blocks : 0;
-            int64_t scan = mine;
-#pragma unroll
-            for (int o = 1; o < 32; o *= 2) {
-                const int64_t up = __shfl_up_sync(0xffffffffu, scan, o);
-                if (lane >= o) scan += up;
-            }
+        auto found = [&](int b, int64_t mine, int64_t scan) {
+            if (begin >= scan - mine && begin < scan) { sh.words[16] = b; sh.words[17] = scan - mine; }
+        };
+        found(tid, mine0, scan0);
+        for (int base = kTeam; before <= begin; base += kTeam) {
+            const int64_t mine = units_of(base + tid);
+            int64_t scan = warp_scan(mine);
             team_sync(team);
             if (lane == 31) sh.words[warp] = scan;
             team_sync(team);
-            int64_t whole = 0;
 #pragma unroll
             for (int w = 0; w < kTeamWarps; ++w) {
-                if (w == warp) scan += before + whole;
-                whole += sh.words[w];
+                if (w == warp) scan += before;
+                before += sh.words[w];
             }
-            if (begin >= scan - mine && begin < scan) { sh.words[16] = b; sh.words[17] = scan - mine; }
-            before += whole;
-            if (before > begin) break;
+            found(base + tid, mine, scan);
         }
         team_sync(team);
         int sequence = (int)sh.words[16];
@@ -536,9 +552,10 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
                 }
                 commit_copies();
             };
+            float mine[P / 32];
+            load_query<P>(mine, a, sequence, head, block, warp, lane, x.length);
             for (int j = 0; j < X::kStages / X::kPair - 1; ++j) start(j, j * X::kPair);
-
-            stage_query<P>(sh, a, sequence, head, block, warp, lane, x.length);
+            stage_query<P>(sh, mine, a.scale, warp, lane);
             team_sync(team);
             uint32_t q[P / 16][2], q2[kExact ? P / 16 : 1][2];
 #pragma unroll
@@ -727,22 +744,25 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
     }
 }
 
-// Joins the partial sums of a segment that began in team `blockIdx.x` and went on in others; a warp a query.
+// Joins the partial sums of a segment that began in team `blockIdx.x` and went on in others: kJoinWarps warps a query, each
+// with a share of the teams, so that what has to be read is under way at once (one warp a query took 8 us for 37 teams).
+constexpr int kJoinWarps = 4;
 template <int P>
-__global__ void __launch_bounds__(kTeam) attend_join_kernel(const __grid_constant__ CacheAttendArgs a)
+__global__ void __launch_bounds__(32 * kQueries* kJoinWarps) attend_join_kernel(const __grid_constant__ CacheAttendArgs a)
 {
+    constexpr int kVectors = P / 128 > 0 ? P / 128 : 1;                 // of 4 coordinates a lane
+    __shared__ float4 sums[kJoinWarps][kQueries][kVectors][32];
+    __shared__ float totals[kJoinWarps][kQueries];
     pdl_wait();
     pdl_launch_next();
     const Record rec = reinterpret_cast<const Record*>(a.partial)[blockIdx.x];
     if (rec.sequence < 0) return;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int head = rec.head_block / a.group_blocks, query = (rec.head_block - head * a.group_blocks) * kQueries + warp;
-    if (query >= a.group) return;
-    const float* partials = a.partial + (int64_t)gridDim.x * (sizeof(Record) / 4) + warp * (P + 4);
-    auto part = [&](int c) { return partials + (2 * (int64_t)c + (c == (int)blockIdx.x)) * kPartial<P>; };
+    const int lane = threadIdx.x & 31, q = (threadIdx.x >> 5) % kQueries, share = (threadIdx.x >> 5) / kQueries, begin = blockIdx.x;
+    const float* partials = a.partial + (int64_t)gridDim.x * (sizeof(Record) / 4) + q * (P + 4);
+    auto part = [&](int c) { return partials + (2 * (int64_t)c + (c == begin)) * kPartial<P>; };
     float r = kLow, rw = kLow;
-    for (int c = blockIdx.x + lane; c <= rec.last; c += 32) {
-        const float4 st = *reinterpret_cast<const float4*>(part(c) + P);
+    for (int c = begin + lane; c <= rec.last; c += 32) {
+        const float2 st = *reinterpret_cast<const float2*>(part(c) + P);
         r = fmaxf(r, st.x); rw = fmaxf(rw, st.y);
     }
 #pragma unroll
@@ -750,20 +770,42 @@ __global__ void __launch_bounds__(kTeam) attend_join_kernel(const __grid_constan
         r = fmaxf(r, __shfl_xor_sync(0xffffffffu, r, o));
         rw = fmaxf(rw, __shfl_xor_sync(0xffffffffu, rw, o));
     }
-    float total = 0.0f, acc[P / 32] = {};
+    float total = 0.0f;
+    float4 acc[kVectors] = {};
 #pragma unroll 4
-    for (int c = blockIdx.x; c <= rec.last; ++c) {
+    for (int c = begin + share; c <= rec.last; c += kJoinWarps) {
         const float* p = part(c);
         const float4 st = *reinterpret_cast<const float4*>(p + P);
         total += st.z * ex2(st.x - r);
         const float f = ex2(st.y - rw);
 #pragma unroll
-        for (int i = 0; i < P / 32; ++i) acc[i] += p[lane + 32 * i] * f;
+        for (int i = 0; i < kVectors; ++i) {
+            if (P >= 128 || lane < P / 4) {
+                const float4 v = *reinterpret_cast<const float4*>(p + 4 * (lane + 32 * i));
+                acc[i].x += v.x * f; acc[i].y += v.y * f; acc[i].z += v.z * f; acc[i].w += v.w * f;
+            }
+        }
     }
+#pragma unroll
+    for (int i = 0; i < kVectors; ++i) sums[share][q][i][lane] = acc[i];
+    if (lane == 0) totals[share][q] = total;
+    __syncthreads();
+    const int head = rec.head_block / a.group_blocks, query = (rec.head_block - head * a.group_blocks) * kQueries + q;
+    if (share > 0 || query >= a.group) return;
+    for (int s = 1; s < kJoinWarps; ++s) total += totals[s][q];
     const float f = total != 0.0f ? ex2(rw - r - kLift) / total : 0.0f;
     char* const to = row_of(a.out, rec.sequence, head * a.group + query);
 #pragma unroll
-    for (int i = 0; i < P / 32; ++i) if (lane + 32 * i < a.shape.dim) store_any(a.out.type, to, lane + 32 * i, acc[i] * f);
+    for (int i = 0; i < kVectors; ++i) {
+        for (int s = 1; s < kJoinWarps; ++s) {
+            const float4 v = sums[s][q][i][lane];
+            acc[i].x += v.x; acc[i].y += v.y; acc[i].z += v.z; acc[i].w += v.w;
+        }
+        const int d = 4 * (lane + 32 * i);
+        const float o[4] = {acc[i].x * f, acc[i].y * f, acc[i].z * f, acc[i].w * f};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) if (d + k < a.shape.dim) store_any(a.out.type, to, d + k, o[k]);
+    }
     if (lane == 0 && a.lse)
         a.lse[(int64_t)rec.sequence * a.shape.heads * a.group + head * a.group + query] =
             total != 0.0f ? (r + log2f(total)) * 0.693147180559945309f : -INFINITY;
@@ -778,7 +820,7 @@ cudaError_t launch_as(const CacheAttendArgs& a, cudaStream_t s)
     static std::atomic<uint64_t> configured{0};
     cudaError_t e = opt_in_shared_memory(configured, kBytes, attend_kernel<P, WK, WV, kExact>);
     if (e == cudaSuccess) e = lq::launch(attend_kernel<P, WK, WV, kExact>, a.sms, X::kTeams * kTeam, kBytes, s, a);
-    if (e == cudaSuccess && a.split) e = lq::launch(attend_join_kernel<P>, a.sms * X::kTeams, kTeam, 0, s, a);
+    if (e == cudaSuccess && a.split) e = lq::launch(attend_join_kernel<P>, a.sms * X::kTeams, 32 * kQueries * kJoinWarps, 0, s, a);
     return e;
 }
 
