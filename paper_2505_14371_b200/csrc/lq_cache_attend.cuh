@@ -54,6 +54,7 @@ constexpr int kTableBytes = 256 * 256;  // entry e: 32 copies for the keys, 32 f
 // is the second byte of its entry's address, behind it come the other warps' stages.  (The first KB of a CTA's shared memory is the
 // system's; the last one that a CTA can have is left free, so that the places below hold wherever in the first the kernel's own begins.)
 constexpr int kTableAt = 1 << 16, kSystemBytes = 1 << 10, kEnd = (227 << 10);
+constexpr int kStart = 2;               // what a segment costs beside its units, in units
 constexpr float kLow = -1e30f;          // a reference before its first score
 constexpr float kSlack = 8.0f;          // how far (log2) a score may pass its reference
 constexpr float kLift = 6.0f;           // weights are 2^kLift at their reference: at most 2^14 as fp16, and exact down to 2^-20
@@ -447,8 +448,11 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
 
     // ---- this team's share of all units
     const int head_blocks = a.shape.heads * a.group_blocks, me = blockIdx.x * X::kTeams + team, teams = gridDim.x * X::kTeams;
-    // units of sequence `b`, summed up to it within the team's threads: the last warp-wide step of a scan
-    auto units_of = [&](int b) { return b < a.batch ? extent_of(a, b).template units<X::kUnit>() * head_blocks : 0; };
+    // what the segments of sequence `b` cost: units, and kStart for each segment that has any
+    auto units_of = [&](int b) -> int64_t {
+        const int64_t u = b < a.batch ? extent_of(a, b).template units<X::kUnit>() : 0;
+        return u ? (u + kStart) * head_blocks : 0;
+    };
     auto warp_scan = [&](int64_t v) {
 #pragma unroll
         for (int o = 1; o < 32; o *= 2) {
@@ -508,8 +512,8 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
         Extent x = extent_of(a, sequence);
         int64_t units = x.template units<X::kUnit>();
         const int64_t offset = begin - sh.words[17];
-        int hb = (int)(offset / units);
-        int64_t chunk = offset - hb * units, at = begin;
+        int hb = (int)(offset / (units + kStart));
+        int64_t chunk = offset - hb * (units + kStart) - kStart, at = begin;      // below 0: what comes before the segment's first unit
 
         const uint32_t base_k = kTableAt + 4 * lane, base_v = base_k + 128, stage0 = (uint32_t)X::stages_at(team * kTeamWarps + warp);
         const int64_t page_bytes = (int64_t)a.shape.page_words * 4;
@@ -522,7 +526,10 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
         const char* const norms = stages + X::kNorms + row * 4;
 
         while (at < end) {
-            const int count = (int)min(units - chunk, end - at);       // units of this segment that are ours
+            const int64_t ours = min(units - chunk, end - at);
+            const int count = (int)(ours + min(chunk, (int64_t)0));     // units of this segment that are ours
+            if (count <= 0) break;                                      // (the end of our share)
+            if (chunk < 0) chunk = 0;
             const int head = hb / a.group_blocks, block = hb - head * a.group_blocks;
             // ---- the first copies: this warp's tiles are kPair of every unit
             const int32_t* pages = a.table + (int64_t)sequence * a.table_width;
@@ -719,13 +726,13 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
             }
             if (starts && !whole && tid == 0) {
                 // the team that has the segment's last unit: the largest one whose share begins at or before it
-                const int64_t unit = at + units - 1;
+                const int64_t unit = at + ours - count + units - 1;
                 Record rec;
                 rec.sequence = sequence; rec.head_block = hb; rec.last = (int32_t)(((unit + 1) * parts - 1) / all); rec.pad = 0;
                 records[me] = rec;
             }
-            at += count;
-            chunk = 0;
+            at += ours;
+            chunk = -kStart;
             if (at < end && ++hb == head_blocks) {
                 hb = 0;
                 do { x = extent_of(a, ++sequence); units = x.template units<X::kUnit>(); } while (units == 0);
