@@ -202,29 +202,41 @@ __device__ __forceinline__ int token_row(int r)
     return (r & 1) ? 4 * (t ^ 1) + 1 : 4 * t;
 }
 
-// Starts the copies of the tile at `row0` of a page into the stage at `to` (shared address).
+// Copies of tiles into stages.  A lane's pieces of 16 bytes lie at the same places of every tile, so that per tile there is
+// little to work out: a tile's keys and values are one run each, and lane i takes the pieces i, i + 32, ...
 template <int P, int WK, int WV>
-__device__ __forceinline__ void copy_tile(uint32_t to, const char* head, int page_shift, int row0, int lane)
-{
+struct Copier {
     using X = Stage<P, WK, WV>;
-    auto section = [&](const char* from, uint32_t at, auto row_bytes, auto gap) {
-        constexpr int kRow = decltype(row_bytes)::value, kGap = decltype(gap)::value, kPieces = kRow;      // 16 rows of kRow / 16 pieces
-#pragma unroll
-        for (int i = 0; i < kPieces; i += 32) {
-            // a group of 4 rows is kRow / 4 pieces
-            const int piece = i + lane;
-            copy16(at + piece * 16 + piece / (kRow / 4) * kGap, from + piece * 16);
-        }
-    };
-    const char* keys = head + row0 * X::kRowK;
-    const char* values = head + (X::kRowK << page_shift) + row0 * X::kRowV;
-    section(keys, to, std::integral_constant<int, X::kRowK>(), std::integral_constant<int, X::kGapK>());
-    section(values, to + X::kValues, std::integral_constant<int, X::kRowV>(), std::integral_constant<int, X::kGapV>());
-    if (lane < 8) {
-        const char* norms = head + ((X::kRowK + X::kRowV) << page_shift) + row0 * 4 + ((lane & 4) << page_shift);
-        copy16(to + X::kNorms + lane * 16, norms + (lane & 3) * 16);
+    const char* codes;                  // the layer's pages, at this lane's first piece
+    const char* norms;                  // ... at its piece of the norms (lanes 0 to 3: of the keys', 4 to 7: of the values')
+    uint32_t page_bytes, values_at;
+    uint32_t to, to_norms;              // shared addresses
+    __device__ __forceinline__ Copier(const CacheAttendArgs& a, uint32_t stage0, int lane)
+    {
+        const char* pages = reinterpret_cast<const char*>(a.pages);
+        codes = pages + lane * 16;
+        norms = pages + ((X::kRowK + X::kRowV) << a.shape.page_shift) + ((lane & 4) << a.shape.page_shift) + (lane & 3) * 16;
+        page_bytes = (uint32_t)a.shape.page_words * 4;
+        values_at = X::kRowK << a.shape.page_shift;
+        to = stage0;
+        to_norms = stage0 + X::kNorms + lane * 16;
     }
-}
+    // `head_at`: bytes of a page before the head's part; `lane` as at the start
+    __device__ __forceinline__ void tile(int stage, uint32_t page, uint32_t head_at, uint32_t row0, int lane) const
+    {
+        const int at = stage * X::kBytes;
+        const uint64_t from = (uint64_t)page * page_bytes + head_at;
+        const char* keys = codes + from + row0 * X::kRowK;
+        const char* values = codes + from + values_at + row0 * X::kRowV;
+#pragma unroll
+        for (int i = 0; i < X::kRowK; i += 32)      // (16 rows are kRow pieces; a group of 4 rows is kRow / 4 of them)
+            copy16(to + at + (i + lane) * 16 + (i + lane) / (X::kRowK / 4) * X::kGapK, keys + i * 16);
+#pragma unroll
+        for (int i = 0; i < X::kRowV; i += 32)
+            copy16(to + at + X::kValues + (i + lane) * 16 + (i + lane) / (X::kRowV / 4) * X::kGapV, values + i * 16);
+        if (lane < 8) copy16(to_norms + at, norms + from + row0 * 4);
+    }
+};
 
 // Codes and norms of one tile, as one warp's lanes hold them.
 template <int P, int WK, int WV>
@@ -269,8 +281,13 @@ __device__ __forceinline__ void take_values(Tile<P, WK, WV>& t, const char* even
                                      (r & 1 ? odd : even) + (r >> 1) * 2 * Stage<P, WK, WV>::kRowV + 8 * c * X::kValueChunk);
 }
 
-// kExact 0: q is one fp16 number; 1: a sum of two; 2: q and the weights are.
-template <int P, int WK, int WV, int kExact>
+// How queries and weights are rounded to fp16.  kPlain: a query is one number (exactly, for fp16 and bf16 that are not rotated);
+// kTwo: a sum of two, with a second product for the rest; kTwoBoth: and the weights are.  With up to 4 queries a head the rests
+// take columns 4 to 7 of the same product (kBeside: of queries, kBesideBoth: of queries and weights), which costs neither
+// registers nor products: 32 sequences of 8192 tokens, rows of 128, rotated bf16 queries 92 -> 82 us, fp32 100 -> 82.
+constexpr int kPlain = 0, kTwo = 1, kTwoBoth = 2, kBeside = 3, kBesideBoth = 4;
+
+template <int P>
 struct Sums {
     float acc[P / 16][4];
     float ref[2], ref_w[2], total[2];   // of queries 2t and 2t + 1
@@ -399,8 +416,8 @@ __device__ __forceinline__ void load_query(float (&x)[P / 32], const CacheAttend
     }
 }
 
-// ... and brought into shared memory: times its power of two, as fp16 and the rest.
-template <int P>
+// ... and brought into shared memory: times its power of two, as fp16 and the rest; kRests: warps 4 to 7 bring the rests of queries 0 to 3.
+template <int P, bool kRests>
 __device__ __forceinline__ void stage_query(TeamShared<P>& sh, const float (&x)[P / 32], float scale, int w, int lane)
 {
     uint32_t top = 0;
@@ -414,18 +431,19 @@ __device__ __forceinline__ void stage_query(TeamShared<P>& sh, const float (&x)[
 #pragma unroll
     for (int i = 0; i < P / 32; ++i) {
         const float y = x[i] * up;
-        const __half h = __float2half_rn(y);
-        sh.q[0][w][lane + 32 * i] = h;
-        sh.q[1][w][lane + 32 * i] = __float2half_rn(y - __half2float(h));
+        const __half h = __float2half_rn(y), rest = __float2half_rn(y - __half2float(h));
+        sh.q[0][w][lane + 32 * i] = kRests && w >= 4 ? rest : h;
+        sh.q[1][w][lane + 32 * i] = rest;
     }
     if (lane == 0) sh.factor[w] = scale * down;
 }
 
-template <int P, int WK, int WV, int kExact>
+template <int P, int WK, int WV, int kMode>
 __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_kernel(const __grid_constant__ CacheAttendArgs a)
 {
     using X = Stage<P, WK, WV>;
     using T = Tile<P, WK, WV>;
+    constexpr bool kSecond = kMode == kTwo || kMode == kTwoBoth, kRests = kMode == kBeside || kMode == kBesideBoth;
     extern __shared__ __align__(128) char smem[];
     char* const shared = smem - __cvta_generic_to_shared(smem);         // shared address 0
     char* const table = shared + kTableAt;
@@ -516,7 +534,7 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
         int64_t chunk = offset - hb * (units + kStart) - kStart, at = begin;      // below 0: what comes before the segment's first unit
 
         const uint32_t base_k = kTableAt + 4 * lane, base_v = base_k + 128, stage0 = (uint32_t)X::stages_at(team * kTeamWarps + warp);
-        const int64_t page_bytes = (int64_t)a.shape.page_words * 4;
+        const Copier<P, WK, WV> copier(a, stage0, lane);
         const int tile_shift = a.shape.page_shift - 4, tile_mask = (1 << tile_shift) - 1;
         // this lane's places in a stage
         const int row = token_row(g), row_even = token_row(2 * t), row_odd = token_row(2 * t + 1);
@@ -535,7 +553,7 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
             const int32_t* pages = a.table + (int64_t)sequence * a.table_width;
             const int tile0 = x.tile0 + (int)chunk * X::kUnit + warp * X::kPair, stop = min(x.tile1, x.tile0 + ((int)chunk + count) * X::kUnit);
             const int rounds = stop > tile0 ? (stop - tile0 + X::kUnit - 1) / X::kUnit : 0;
-            const char* const bytes = reinterpret_cast<const char*>(a.pages + head * a.shape.head_words);
+            const uint32_t head_at = (uint32_t)(head * a.shape.head_words) * 4;
             auto tile_of = [&](int n) { return tile0 + n / X::kPair * X::kUnit + n % X::kPair; };      // of the warp's n-th tile
             uint32_t missing = 0;                                       // bit s: stage s holds no tile: past the end, or on a page that is not there
             int page = -1;                                              // lane l: of the warp's tile 32 i + l, i as far as copies are
@@ -553,30 +571,29 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
                     for (int h = 0; h < X::kPair; ++h) {
                         const int n = round * X::kPair + h, p = __shfl_sync(0xffffffffu, page, n % 32);
                         missing = p < 0 ? missing | 1u << (stage + h) : missing & ~(1u << (stage + h));
-                        if (p >= 0)
-                            copy_tile<P, WK, WV>(stage0 + (stage + h) * X::kBytes, bytes + p * page_bytes, a.shape.page_shift, (tile_of(n) & tile_mask) * kTile, lane);
+                        if (p >= 0) copier.tile(stage + h, (uint32_t)p, head_at, (uint32_t)(tile_of(n) & tile_mask) * kTile, lane);
                     }
                 }
                 commit_copies();
             };
             float mine[P / 32];
-            load_query<P>(mine, a, sequence, head, block, warp, lane, x.length);
+            load_query<P>(mine, a, sequence, head, block, kRests ? warp % 4 : warp, lane, x.length);
             for (int j = 0; j < X::kStages / X::kPair - 1; ++j) start(j, j * X::kPair);
-            stage_query<P>(sh, mine, a.scale, warp, lane);
+            stage_query<P, kRests>(sh, mine, a.scale, warp, lane);
             team_sync(team);
-            uint32_t q[P / 16][2], q2[kExact ? P / 16 : 1][2];
+            uint32_t q[P / 16][2], q2[kSecond ? P / 16 : 1][2];
 #pragma unroll
             for (int s = 0; s < P / 16; ++s) {
                 const uint2 w = *reinterpret_cast<const uint2*>(&sh.q[0][g][key_coordinate<P, WK>(s, t)]);
                 q[s][0] = w.x; q[s][1] = w.y;
-                if constexpr (kExact > 0) {
+                if constexpr (kSecond) {
                     const uint2 w2 = *reinterpret_cast<const uint2*>(&sh.q[1][g][key_coordinate<P, WK>(s, t)]);
                     q2[s][0] = w2.x; q2[s][1] = w2.y;
                 }
             }
             const float f0 = sh.factor[2 * t], f1 = sh.factor[2 * t + 1];
 
-            Sums<P, WK, WV, kExact> S;
+            Sums<P> S;
             S.clear();
             int stage = 0, ahead = X::kStages - X::kPair;
             for (int j = 0; j < rounds; ++j) {
@@ -596,7 +613,10 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
                     T cur;
                     float c[4];
                     take_keys(cur, keys + place + h * X::kBytes);
-                    scores<P, WK, WV, (kExact > 0)>(c, cur, q, q2, base_k);
+                    scores<P, WK, WV, kSecond>(c, cur, q, q2, base_k);
+                    if constexpr (kRests)               // columns 4 to 7 are the rests of columns 0 to 3
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) c[i] += __shfl_xor_sync(0xffffffffu, c[i], 2);
                     const char* n = norms + place + h * X::kBytes;
                     const float nk0 = *reinterpret_cast<const float*>(n), nk1 = *reinterpret_cast<const float*>(n + 8);
                     s[h][0] = c[0] * (f0 * nk0); s[h][1] = c[1] * (f1 * nk0); s[h][2] = c[2] * (f0 * nk1); s[h][3] = c[3] * (f1 * nk1);
@@ -645,17 +665,21 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
                         S.total[i & 1] += ex2(s[h][i] - S.ref[i & 1]);
                         w[h][i] = ex2(w[h][i] - (S.ref_w[i & 1] - kLift));
                     }
-                    const uint32_t h0 = halves(w[h][0], w[h][1]), h1 = halves(w[h][2], w[h][3]);
+                    uint32_t h0 = halves(w[h][0], w[h][1]), h1 = halves(w[h][2], w[h][3]);
+                    if constexpr (kMode == kBesideBoth) {
+                        const float2 r0 = rest_of(h0, w[h][0], w[h][1]), r1 = rest_of(h1, w[h][2], w[h][3]);
+                        if (t >= 2) { h0 = halves(r0.x, r0.y); h1 = halves(r1.x, r1.y); }
+                    }
                     const uint32_t b[2] = {transposed(h0), transposed(h1)};
                     uint32_t b2[2] = {0, 0};
-                    if constexpr (kExact == 2) {
+                    if constexpr (kMode == kTwoBoth) {
                         const float2 r0 = rest_of(h0, w[h][0], w[h][1]), r1 = rest_of(h1, w[h][2], w[h][3]);
                         b2[0] = transposed(halves(r0.x, r0.y));
                         b2[1] = transposed(halves(r1.x, r1.y));
                     }
                     T cur;
                     take_values(cur, even + place + h * X::kBytes, odd + place + h * X::kBytes);
-                    weigh<P, WK, WV, (kExact == 2)>(S.acc, cur, b, b2, base_v);
+                    weigh<P, WK, WV, (kMode == kTwoBoth)>(S.acc, cur, b, b2, base_v);
                 }
             }
 
@@ -695,15 +719,20 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
             team_sync(team);
             const bool starts = chunk == 0, whole = starts && count == units;
             const int slot = 2 * me + starts;
-            for (int i = tid; i < kQueries * P / 4; i += kTeam) {
+            for (int i = tid; i < (kRests ? 4 : kQueries) * P / 4; i += kTeam) {
                 const int query = i / (P / 4), d = (i % (P / 4)) * 4;
                 const float* share = sh.share[query];
                 float4 sum4 = make_float4(0, 0, 0, 0);
 #pragma unroll
                 for (int w = 0; w < kTeamWarps; ++w) {
-                    const float4 v = *reinterpret_cast<const float4*>(
+                    float4 v = *reinterpret_cast<const float4*>(
                         reinterpret_cast<const float*>(shared + X::stages_at(team * kTeamWarps + w)) + ((query & 1) * 4 + (query >> 1)) * (P + 4) + d);
                     const float f = share[w];
+                    if constexpr (kMode == kBesideBoth) {               // what the weights' rounding left, of query + 4
+                        const float4 u = *reinterpret_cast<const float4*>(
+                            reinterpret_cast<const float*>(shared + X::stages_at(team * kTeamWarps + w)) + ((query & 1) * 4 + (query >> 1) + 2) * (P + 4) + d);
+                        v.x += u.x; v.y += u.y; v.z += u.z; v.w += u.w;
+                    }
                     sum4.x += v.x * f; sum4.y += v.y * f; sum4.z += v.z * f; sum4.w += v.w * f;
                 }
                 const float r = share[kTeamWarps], rw = share[kTeamWarps + 1], total = share[kTeamWarps + 2];
@@ -818,31 +847,33 @@ __global__ void __launch_bounds__(32 * kQueries* kJoinWarps) attend_join_kernel(
             total != 0.0f ? (r + log2f(total)) * 0.693147180559945309f : -INFINITY;
 }
 
-template <int P, int WK, int WV, int kExact>
+template <int P, int WK, int WV, int kMode>
 cudaError_t launch_as(const CacheAttendArgs& a, cudaStream_t s)
 {
     using X = Stage<P, WK, WV>;
     constexpr int kBytes = smem_bytes<P, WK, WV>();
     static_assert(kBytes <= 227 << 10, "shared memory of an SM");
     static std::atomic<uint64_t> configured{0};
-    cudaError_t e = opt_in_shared_memory(configured, kBytes, attend_kernel<P, WK, WV, kExact>);
-    if (e == cudaSuccess) e = lq::launch(attend_kernel<P, WK, WV, kExact>, a.sms, X::kTeams * kTeam, kBytes, s, a);
+    cudaError_t e = opt_in_shared_memory(configured, kBytes, attend_kernel<P, WK, WV, kMode>);
+    if (e == cudaSuccess) e = lq::launch(attend_kernel<P, WK, WV, kMode>, a.sms, X::kTeams * kTeam, kBytes, s, a);
     if (e == cudaSuccess && a.split) e = lq::launch(attend_join_kernel<P>, a.sms * X::kTeams, 32 * kQueries * kJoinWarps, 0, s, a);
     return e;
 }
 
 template <int P, int WK, int WV>
-cudaError_t launch_exact(const CacheAttendArgs& a, cudaStream_t s)
+cudaError_t launch_mode(const CacheAttendArgs& a, cudaStream_t s)
 {
-    if (a.queries.type == LQ_F32) return launch_as<P, WK, WV, 2>(a, s);
-    return a.rotary.table ? launch_as<P, WK, WV, 1>(a, s) : launch_as<P, WK, WV, 0>(a, s);
+    const bool beside = a.group <= 4;
+    if (a.queries.type == LQ_F32) return beside ? launch_as<P, WK, WV, kBesideBoth>(a, s) : launch_as<P, WK, WV, kTwoBoth>(a, s);
+    if (a.rotary.table) return beside ? launch_as<P, WK, WV, kBeside>(a, s) : launch_as<P, WK, WV, kTwo>(a, s);
+    return launch_as<P, WK, WV, kPlain>(a, s);
 }
 
 template <int P>
 cudaError_t launch(const CacheAttendArgs& a, cudaStream_t s)
 {
-    if (a.shape.sym_bits[0] == 4) return a.shape.sym_bits[1] == 4 ? launch_exact<P, 4, 4>(a, s) : launch_exact<P, 4, 8>(a, s);
-    return a.shape.sym_bits[1] == 4 ? launch_exact<P, 8, 4>(a, s) : launch_exact<P, 8, 8>(a, s);
+    if (a.shape.sym_bits[0] == 4) return a.shape.sym_bits[1] == 4 ? launch_mode<P, 4, 4>(a, s) : launch_mode<P, 4, 8>(a, s);
+    return a.shape.sym_bits[1] == 4 ? launch_mode<P, 8, 4>(a, s) : launch_mode<P, 8, 8>(a, s);
 }
 
 }  // namespace attend
