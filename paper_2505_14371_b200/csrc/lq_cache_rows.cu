@@ -1,7 +1,8 @@
 // Rows of the key-value cache: quantised as they are written, and read back.
 //
-// A row (token, head, keys or values) of `padded` coordinates is taken by padded / 8 lanes, 8 coordinates each: 16 bytes of
-// fp16 or bf16 input in one load, one 32-bit word of 4-bit symbols (or two of 8-bit ones) in one store, two Philox blocks.
+// A lane takes 8 coordinates of a row (token, head, keys or values) at a time: 16 bytes of fp16 or bf16 in one load or store, one
+// 32-bit word of 4-bit symbols (or two of 8-bit ones), two Philox blocks.  The writing kernel gives a lane two such parts (lane i those
+// from 8 i and from padded / 2 + 8 i): with one, what a row costs besides its coordinates was a third of the instructions.
 // Its norm is an all-reduce over those lanes.  Bound: the bytes of the rows on one side and of the page on the other; for
 // few tokens the latency of slot -> row -> norm -> store.
 #include <cuda_bf16.h>
@@ -17,8 +18,9 @@ namespace lq {
 namespace {
 
 constexpr int kRowThreads = 256;
-constexpr int kEach = 8;                // coordinates a lane
-constexpr int kWriteCtas = 4;           // CTAs of the writing kernel that an SM holds at once, by its registers
+constexpr int kEach = 8;                // coordinates at a time
+constexpr int kParts = 2;               // ... of a lane of the writing kernel
+constexpr int kWriteCtas = 3;           // CTAs of the writing kernel that an SM holds at once, by its registers
 
 template <typename T> __device__ __forceinline__ float to_f32(T v);
 template <> __device__ __forceinline__ float to_f32<float>(float v) { return v; }
@@ -145,14 +147,16 @@ __device__ __forceinline__ void rotate8(float (&x)[kEach], const T* row, int d, 
 
 // N as the cache keeps it (0: the row is kept as zeros); bad: NaN, Inf or a norm that overflows.  Same value in all lanes.
 template <int kLanes>
-__device__ __forceinline__ float row_norm(const float (&x)[kEach], int q, bool& bad)
+__device__ __forceinline__ float row_norm(const float (&x)[kParts][kEach], int q, bool& bad)
 {
     float n;
     if (q == 0) {
         // the maximum drops NaN: a sum of x * 0 keeps it, and Inf
         float m = 0.0f, z = 0.0f;
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) { m = fmaxf(m, fabsf(x[i])); z = fmaf(x[i], 0.0f, z); }
+        for (int c = 0; c < kParts; ++c)
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) { m = fmaxf(m, fabsf(x[c][i])); z = fmaf(x[c][i], 0.0f, z); }
         if (z != 0.0f) m = INFINITY;
 #pragma unroll
         for (int o = 1; o < kLanes; o *= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
@@ -160,10 +164,12 @@ __device__ __forceinline__ float row_norm(const float (&x)[kEach], int q, bool& 
     } else {
         double sum = 0.0;
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            const double a = fabs((double)x[i]);
-            sum = q == 1 ? sum + a : fma(a, a, sum);
-        }
+        for (int c = 0; c < kParts; ++c)
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+                const double a = fabs((double)x[c][i]);
+                sum = q == 1 ? sum + a : fma(a, a, sum);
+            }
 #pragma unroll
         for (int o = 1; o < kLanes; o *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, o);
         n = (float)(q == 1 ? sum : sqrt(sum));
@@ -196,10 +202,9 @@ struct SharedSearch {
 
 // Symbols 2 * index + sign of 8 coordinates, packed as the row has them (hi: the upper four of 8 bits).
 template <bool kUnbiased>
-__device__ __forceinline__ void symbols8(const float (&x)[kEach], float norm, int bits, const SharedSearch& t, const uint32_t (&rnd)[kEach],
+__device__ __forceinline__ void symbols8(const float (&x)[kEach], float norm, float inv, int bits, const SharedSearch& t, const uint32_t (&rnd)[kEach],
                                          uint32_t& lo, uint32_t& hi)
 {
-    const float inv = norm > 0.0f ? __frcp_rn(norm) : 0.0f;
     uint32_t at[kEach];
     if (t.search.entries) {
         // (a number just above 1 is in the bin of 1; NaN, in a row that is kept as zeros, becomes `lowest`)
@@ -248,17 +253,17 @@ __device__ __forceinline__ void symbols8(const float (&x)[kEach], float norm, in
     if (!(norm > 0.0f)) lo = hi = 0;
 }
 
-// blockIdx.y: keys or values.  Rows are fetched a round ahead.
+// Every CTA has its share of the keys, which are rotated, and then of the values.  Rows are fetched a round ahead.
 template <typename T, int kLanes, bool kUnbiased>
 __global__ void __launch_bounds__(kRowThreads, kWriteCtas) cache_write_kernel(const __grid_constant__ CacheWriteArgs a)
 {
-    __shared__ SharedSearch table;
-    const int kind = blockIdx.y, bits = a.shape.sym_bits[kind];
-    {
+    __shared__ SharedSearch tables[2];
+#pragma unroll 1
+    for (int kind = 0; kind < 2; ++kind) {
         const CacheTable& t = a.tables[kind];
         const CacheSearch& s = kUnbiased ? t.floor : t.nearest;
         // the head, and the table of one of the two searches
-        uint4* to = reinterpret_cast<uint4*>(&table.search);
+        uint4* to = reinterpret_cast<uint4*>(&tables[kind].search);
         const uint4* from = reinterpret_cast<const uint4*>(&s);
         constexpr int kHead = (int)offsetof(CacheSearch, edge) / 16, kEntry = (int)offsetof(CacheSearch, entry) / 16;
         static_assert(offsetof(CacheSearch, edge) % 16 == 0 && offsetof(CacheSearch, entry) % 16 == 0, "parts are copied by 16 bytes");
@@ -268,7 +273,7 @@ __global__ void __launch_bounds__(kRowThreads, kWriteCtas) cache_write_kernel(co
         if (kUnbiased)
             for (int i = threadIdx.x; i < kCacheLevels - 1; i += kRowThreads) {
                 const float l = __ldg(t.levels + i);
-                table.low_gap[i] = make_float2(l, __fsub_rn(__ldg(t.levels + i + 1), l));
+                tables[kind].low_gap[i] = make_float2(l, __fsub_rn(__ldg(t.levels + i + 1), l));
             }
     }
     __syncthreads();
@@ -277,69 +282,86 @@ __global__ void __launch_bounds__(kRowThreads, kWriteCtas) cache_write_kernel(co
 
     constexpr int kRows = kRowThreads / kLanes;
     const uint32_t rows = (uint32_t)(a.tokens * a.shape.heads), stride = gridDim.x * kRows, group = threadIdx.x / kLanes;
-    const int lane = threadIdx.x % kLanes, d = lane * kEach, page_size = 1 << a.shape.page_shift;
-    const int codes_at = kind ? page_size * a.shape.row_words[0] : 0, row_words = a.shape.row_words[kind];
-    const int norms_at = page_size * (a.shape.row_words[0] + a.shape.row_words[1] + kind);
-    const char* const data = static_cast<const char*>(a.rows[kind].data);
-    const int token_bytes = a.rows[kind].token_bytes, head_bytes = a.rows[kind].head_bytes;
-    const bool wide = a.rows[kind].wide, turned = a.rotary.table != nullptr;
+    const int lane = threadIdx.x % kLanes, page_size = 1 << a.shape.page_shift;
+    auto from = [&](int part) { return (part * kLanes + lane) * kEach; };        // first coordinate of a part
+    const bool turned = a.rotary.table != nullptr;
+#pragma unroll 1
+    for (int kind = 0; kind < 2; ++kind) {
+        const SharedSearch& table = tables[kind];
+        const int bits = a.shape.sym_bits[kind];
+        const int codes_at = kind ? page_size * a.shape.row_words[0] : 0, row_words = a.shape.row_words[kind];
+        const int norms_at = page_size * (a.shape.row_words[0] + a.shape.row_words[1] + kind);
+        const char* const data = static_cast<const char*>(a.rows[kind].data);
+        const int token_bytes = a.rows[kind].token_bytes, head_bytes = a.rows[kind].head_bytes;
+        const bool wide = a.rows[kind].wide;
 
-    int64_t next_slot = -1, next_position = 0;
-    int next_head = 0;
-    const T* next_row = nullptr;
-    Eight<T> next = {};
-    auto fetch = [&](uint32_t r) {
-        next_slot = -1;
-        if (r >= rows) return;
-        const Place p = place_of(r, a.shape.heads, a.by_head, a.slots);
-        next_slot = p.slot; next_head = p.head;
-        next_row = reinterpret_cast<const T*>(data + (int64_t)p.token * token_bytes + (int64_t)p.head * head_bytes);
-        next = load8(next_row, d, a.shape.dim, wide);
-        if (turned) next_position = __ldg(a.rotary.at + p.token);
-    };
-    fetch(blockIdx.x * kRows + group);
-    for (uint32_t first = blockIdx.x * kRows; first < rows; first += stride) {
-        // every lane of a warp takes part in the reductions, those without a row with whatever they hold
-        int64_t slot = next_slot;
-        const int64_t position = next_position;
-        const int head = next_head;
-        const T* const row = next_row;
-        float x[kEach];
-        floats(x, next);
-        fetch(first + stride + group);
-        if (slot >= a.num_slots) { slot = -1; if (lane == 0) atomicOr(a.flags, LQ_CACHE_BAD_SLOT); }
-        if (turned && slot >= 0) {
-            if ((uint64_t)position >= (uint64_t)a.rotary.positions) {
-                slot = -1;
-                if (lane == 0) atomicOr(a.flags, LQ_CACHE_BAD_POSITION);
-            } else if (kind == LQ_KEYS) {
-                rotate8(x, row, d, a.rotary, position, wide);
-            }
-        }
-        bool bad;
-        const float norm = row_norm<kLanes>(x, a.shape.q, bad);
-        if (slot < 0) continue;
-        const int place = (int)slot & (page_size - 1);
-        uint32_t* base = a.pages + (int64_t)((uint32_t)slot >> a.shape.page_shift) * a.shape.page_words + head * a.shape.head_words;
-        uint32_t rnd[kEach];
-        if (kUnbiased) {
-            const uint32_t c0 = (uint32_t)(head * a.shape.padded + d) / 4;
-            uint32_t w[4];
+        int64_t next_slot = -1, next_position = 0;
+        int next_head = 0;
+        const T* next_row = nullptr;
+        Eight<T> next[kParts] = {};
+        auto fetch = [&](uint32_t r) {
+            next_slot = -1;
+            if (r >= rows) return;
+            const Place p = place_of(r, a.shape.heads, a.by_head, a.slots);
+            next_slot = p.slot; next_head = p.head;
+            next_row = reinterpret_cast<const T*>(data + (int64_t)p.token * token_bytes + (int64_t)p.head * head_bytes);
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                philox4x32_10(c0 + j, 2 * a.layer + kind, (uint32_t)slot, a.step, a.seed_lo, a.seed_hi, w);
+            for (int c = 0; c < kParts; ++c) next[c] = load8(next_row, from(c), a.shape.dim, wide);
+            if (turned) next_position = __ldg(a.rotary.at + p.token);
+        };
+        fetch(blockIdx.x * kRows + group);
+        for (uint32_t first = blockIdx.x * kRows; first < rows; first += stride) {
+            // every lane of a warp takes part in the reductions, those without a row with whatever they hold
+            int64_t slot = next_slot;
+            const int64_t position = next_position;
+            const int head = next_head;
+            const T* const row = next_row;
+            float x[kParts][kEach];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) rnd[4 * j + i] = w[i];
+            for (int c = 0; c < kParts; ++c) floats(x[c], next[c]);
+            fetch(first + stride + group);
+            if (slot >= a.num_slots) { slot = -1; if (lane == 0) atomicOr(a.flags, LQ_CACHE_BAD_SLOT); }
+            if (turned && slot >= 0) {
+                if ((uint64_t)position >= (uint64_t)a.rotary.positions) {
+                    slot = -1;
+                    if (lane == 0) atomicOr(a.flags, LQ_CACHE_BAD_POSITION);
+                } else if (kind == LQ_KEYS) {
+#pragma unroll
+                    for (int c = 0; c < kParts; ++c) {
+                        rotate8(x[c], row, from(c), a.rotary, position, wide);
+                        asm volatile("" ::: "memory");                  // (the angles of one part at a time: registers)
+                    }
+                }
             }
-        }
-        uint32_t lo, hi;
-        symbols8<kUnbiased>(x, norm, bits, table, rnd, lo, hi);
-        uint32_t* codes = base + codes_at + place * row_words;
-        if (bits == 4) codes[lane] = lo;
-        else reinterpret_cast<uint2*>(codes)[lane] = make_uint2(lo, hi);
-        if (lane == 0) {
-            reinterpret_cast<float*>(base)[norms_at + place] = norm;
-            if (bad) atomicOr(a.flags, LQ_CACHE_NONFINITE);
+            bool bad;
+            const float norm = row_norm<kLanes>(x, a.shape.q, bad);
+            if (slot < 0) continue;
+            const float inv = norm > 0.0f ? __frcp_rn(norm) : 0.0f;
+            const int place = (int)slot & (page_size - 1);
+            uint32_t* base = a.pages + (int64_t)((uint32_t)slot >> a.shape.page_shift) * a.shape.page_words + head * a.shape.head_words;
+            uint32_t* codes = base + codes_at + place * row_words;
+#pragma unroll
+            for (int c = 0; c < kParts; ++c) {
+                uint32_t rnd[kEach];
+                if (kUnbiased) {
+                    const uint32_t c0 = (uint32_t)(head * a.shape.padded + from(c)) / 4;
+                    uint32_t w[4];
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        philox4x32_10(c0 + j, 2 * a.layer + kind, (uint32_t)slot, a.step, a.seed_lo, a.seed_hi, w);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) rnd[4 * j + i] = w[i];
+                    }
+                }
+                uint32_t lo, hi;
+                symbols8<kUnbiased>(x[c], norm, inv, bits, table, rnd, lo, hi);
+                if (bits == 4) codes[c * kLanes + lane] = lo;
+                else reinterpret_cast<uint2*>(codes)[c * kLanes + lane] = make_uint2(lo, hi);
+            }
+            if (lane == 0) {
+                reinterpret_cast<float*>(base)[norms_at + place] = norm;
+                if (bad) atomicOr(a.flags, LQ_CACHE_NONFINITE);
+            }
         }
     }
 }
@@ -398,17 +420,17 @@ __global__ void __launch_bounds__(kRowThreads) cache_read_kernel(const __grid_co
     }
 }
 
-// CTAs: as many as the rows need, at most as the GPU holds at once (`resident` an SM).
+// CTAs: as many as the rows need with `each` coordinates a lane, at most as the GPU holds at once (`resident` an SM).
 template <typename Args, typename Go>
-cudaError_t by_type_and_size(const Args& a, int resident, Go go)
+cudaError_t by_type_and_size(const Args& a, int each, int resident, Go go)
 {
-    const int lanes = a.shape.padded / kEach, type = a.rows[0].type;
+    const int lanes = a.shape.padded / each, type = a.rows[0].type;
     const int64_t blocks = (a.tokens * a.shape.heads * lanes + kRowThreads - 1) / kRowThreads;
     const unsigned grid = (unsigned)(blocks < resident * kSms ? blocks : resident * kSms);
     auto sized = [&](auto t) {
-        if (lanes == 8) return go(t, std::integral_constant<int, 8>(), grid);
-        if (lanes == 16) return go(t, std::integral_constant<int, 16>(), grid);
-        return go(t, std::integral_constant<int, 32>(), grid);
+        if (a.shape.padded == 64) return go(t, std::integral_constant<int, 64>(), grid);
+        if (a.shape.padded == 128) return go(t, std::integral_constant<int, 128>(), grid);
+        return go(t, std::integral_constant<int, 256>(), grid);
     };
     return type == LQ_F32 ? sized(float()) : type == LQ_F16 ? sized(__half()) : sized(__nv_bfloat16());
 }
@@ -417,18 +439,18 @@ cudaError_t by_type_and_size(const Args& a, int resident, Go go)
 
 cudaError_t launch_cache_write(const CacheWriteArgs& a, cudaStream_t s)
 {
-    return by_type_and_size(a, kWriteCtas / 2, [&](auto t, auto lanes, unsigned grid) {
+    return by_type_and_size(a, kEach * kParts, kWriteCtas, [&](auto t, auto padded, unsigned grid) {
         using T = decltype(t);
-        constexpr int kLanes = decltype(lanes)::value;
-        return a.unbiased ? launch(cache_write_kernel<T, kLanes, true>, dim3(grid, 2), kRowThreads, 0, s, a)
-                          : launch(cache_write_kernel<T, kLanes, false>, dim3(grid, 2), kRowThreads, 0, s, a);
+        constexpr int kLanes = decltype(padded)::value / (kEach * kParts);
+        return a.unbiased ? launch(cache_write_kernel<T, kLanes, true>, grid, kRowThreads, 0, s, a)
+                          : launch(cache_write_kernel<T, kLanes, false>, grid, kRowThreads, 0, s, a);
     });
 }
 
 cudaError_t launch_cache_read(const CacheReadArgs& a, cudaStream_t s)
 {
-    return by_type_and_size(a, 8, [&](auto t, auto lanes, unsigned grid) {
-        return launch(cache_read_kernel<decltype(t), decltype(lanes)::value>, grid, kRowThreads, 0, s, a);
+    return by_type_and_size(a, kEach, 8, [&](auto t, auto padded, unsigned grid) {
+        return launch(cache_read_kernel<decltype(t), decltype(padded)::value / kEach>, grid, kRowThreads, 0, s, a);
     });
 }
 
