@@ -160,18 +160,35 @@ __device__ __forceinline__ char* row_of(const CacheRows& r, int token, int head)
     return static_cast<char*>(r.data) + (int64_t)token * r.token_bytes + (int64_t)head * r.head_bytes;
 }
 
-__device__ __forceinline__ float load_any(int type, const char* row, int d)
-{
-    if (type == LQ_F32) return reinterpret_cast<const float*>(row)[d];
-    if (type == LQ_F16) return __half2float(reinterpret_cast<const __half*>(row)[d]);
-    return __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(row)[d]);
-}
-
 __device__ __forceinline__ void store_any(int type, char* row, int d, float v)
 {
     if (type == LQ_F32) reinterpret_cast<float*>(row)[d] = v;
     else if (type == LQ_F16) reinterpret_cast<__half*>(row)[d] = __float2half_rn(v);
     else reinterpret_cast<__nv_bfloat16*>(row)[d] = __float2bfloat16_rn(v);
+}
+
+// Coordinates d .. d+3 of an output row.
+template <bool kFloat>
+__device__ __forceinline__ void store_four(const CacheRows& r, char* row, int d, int dim, float4 v)
+{
+    if (r.wide && d + 4 <= dim) {
+        if constexpr (kFloat) {
+            *reinterpret_cast<float4*>(row + 4 * d) = v;
+        } else {
+            uint2 w;
+            if (r.type == LQ_BF16) {
+                const __nv_bfloat162 a = __floats2bfloat162_rn(v.x, v.y), b = __floats2bfloat162_rn(v.z, v.w);
+                w = make_uint2(reinterpret_cast<const uint32_t&>(a), reinterpret_cast<const uint32_t&>(b));
+            } else {
+                w = make_uint2(halves(v.x, v.y), halves(v.z, v.w));
+            }
+            *reinterpret_cast<uint2*>(row + 2 * d) = w;
+        }
+        return;
+    }
+    const float o[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) if (d + k < dim) store_any(r.type, row, d + k, o[k]);
 }
 
 // What a sequence has to be read of: tokens [first, length), as tiles [tile0, tile1).
@@ -379,42 +396,65 @@ __device__ __forceinline__ int key_coordinate(int s, int t)
     return (4 * c + t) * kEach + 4 * s % kEach;
 }
 
-// Query w of the block by warp w, rotated.
-template <int P>
-__device__ __forceinline__ void load_query(float (&x)[P / 32], const CacheAttendArgs& a, int sequence, int head, int block, int w, int lane, int64_t length)
-{
-    const int query = block * kQueries + w;
-    bool lost = false;
-    if (query < a.group) {
-        const char* const row = row_of(a.queries, sequence, head * a.group + query);
-        const int type = a.queries.type;
+// Query w of the block by warp w, in two steps: what has to be fetched is asked for, without a look at it, before the segment's first
+// copies, and made into numbers and rotated behind them (in one step the copies came 2000 cycles later).
+template <int P, bool kFloat>
+struct Query {
+    uint32_t x[P / 32], y[P / 32];      // coordinates lane, lane + 32, ... as they are stored, and the partners of rotated ones
+    float c[P / 32], s[P / 32];
+    bool lost = false;                  // the position is not in the table
+
+    static __device__ __forceinline__ uint32_t raw(const char* row, int d)
+    {
+        if constexpr (kFloat) return __ldg(reinterpret_cast<const uint32_t*>(row) + d);
+        else return __ldg(reinterpret_cast<const unsigned short*>(row) + d);
+    }
+    static __device__ __forceinline__ float number(uint32_t v, int type)
+    {
+        if constexpr (kFloat) return __uint_as_float(v);
+        else return type == LQ_BF16 ? __uint_as_float(v << 16) : __half2float(__ushort_as_half((unsigned short)v));
+    }
+    __device__ __forceinline__ void fetch(const CacheAttendArgs& a, int sequence, int head, int query, int lane, uint32_t length)
+    {
         const CacheRotary& r = a.rotary;
+        const bool live = query < a.group;
+        const char* const row = row_of(a.queries, sequence, head * a.group + query);
+        const float* angles = r.table;
         const int half = r.dim / 2;
-        const float* cs = r.table;
-        if (r.table) {
-            const int64_t at = r.at ? __ldg(r.at + sequence) : (length > 0 ? length - 1 : 0);
+        if (r.table && live) {
+            const int64_t at = r.at ? __ldg(r.at + sequence) : (length > 0 ? (int64_t)length - 1 : 0);
             lost = at < 0 || at >= r.positions;
-            if (!lost) cs += at * r.dim;
+            if (lost) { if (lane == 0) atomicOr(a.flags, LQ_CACHE_BAD_POSITION); }
+            else angles += at * r.dim;
         }
 #pragma unroll
         for (int i = 0; i < P / 32; ++i) {
             const int d = lane + 32 * i;
-            x[i] = d < a.shape.dim ? load_any(type, row, d) : 0.0f;
-            if (r.table && d < r.dim && !lost) {
-                const bool first = r.interleaved ? d % 2 == 0 : d < half;
-                const int other = r.interleaved ? d ^ 1 : first ? d + half : d - half;
-                const int p = r.interleaved ? d / 2 : first ? d : d - half;
-                const float c = __ldg(cs + p), s = __ldg(cs + half + p), y = load_any(type, row, other);
-                x[i] = first ? __fsub_rn(__fmul_rn(x[i], c), __fmul_rn(y, s)) : __fadd_rn(__fmul_rn(x[i], c), __fmul_rn(y, s));
+            x[i] = live && d < a.shape.dim ? raw(row, d) : 0;
+            if (r.table && live && !lost && d < r.dim) {
+                const int p = r.interleaved ? d / 2 : d < half ? d : d - half;
+                c[i] = __ldg(angles + p); s[i] = __ldg(angles + half + p);
+                y[i] = raw(row, r.interleaved ? d ^ 1 : d < half ? d + half : d - half);
             }
-            if (lost) x[i] = __uint_as_float(0x7fffffffu);
         }
-        if (lost && lane == 0) atomicOr(a.flags, LQ_CACHE_BAD_POSITION);
-    } else {
-#pragma unroll
-        for (int i = 0; i < P / 32; ++i) x[i] = 0.0f;
     }
-}
+    __device__ __forceinline__ void finish(float (&out)[P / 32], const CacheAttendArgs& a, int lane) const
+    {
+        const CacheRotary& r = a.rotary;
+#pragma unroll
+        for (int i = 0; i < P / 32; ++i) {
+            const int d = lane + 32 * i;
+            const float v = number(x[i], a.queries.type);
+            out[i] = v;
+            if (r.table && d < r.dim) {
+                const float u = number(y[i], a.queries.type);
+                out[i] = (r.interleaved ? d % 2 == 0 : d < r.dim / 2) ? __fsub_rn(__fmul_rn(v, c[i]), __fmul_rn(u, s[i]))
+                                                                     : __fadd_rn(__fmul_rn(v, c[i]), __fmul_rn(u, s[i]));
+            }
+            if (lost) out[i] = __uint_as_float(0x7fffffffu);
+        }
+    }
+};
 
 // ... and brought into shared memory: times its power of two, as fp16 and the rest; kRests: warps 4 to 7 bring the rests of queries 0 to 3.
 template <int P, bool kRests>
@@ -444,6 +484,7 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
     using X = Stage<P, WK, WV>;
     using T = Tile<P, WK, WV>;
     constexpr bool kSecond = kMode == kTwo || kMode == kTwoBoth, kRests = kMode == kBeside || kMode == kBesideBoth;
+    constexpr bool kFloat = kMode == kTwoBoth || kMode == kBesideBoth;
     extern __shared__ __align__(128) char smem[];
     char* const shared = smem - __cvta_generic_to_shared(smem);         // shared address 0
     char* const table = shared + kTableAt;
@@ -501,7 +542,10 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
     all += before;
     // no more teams than units take part, so that none between two that share a segment is without a unit
     const int64_t parts = min(all, (int64_t)teams);
-    const int64_t begin = me < parts ? all * me / parts : 0, end = me < parts ? all * (me + 1) / parts : 0;
+    auto share_of = [&](int i) -> int64_t {     // (a division of 64 bits takes some 200 cycles)
+        return all < 1 << 20 ? (int64_t)((uint32_t)all * (uint32_t)i / (uint32_t)parts) : all * i / parts;
+    };
+    const int64_t begin = me < parts ? share_of(me) : 0, end = me < parts ? share_of(me + 1) : 0;
     Record* records = reinterpret_cast<Record*>(a.partial);
     float* partials = a.partial + (int64_t)teams * (sizeof(Record) / 4);
     if (tid == 0) records[me].sequence = -1;
@@ -530,7 +574,7 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
         Extent x = extent_of(a, sequence);
         int64_t units = x.template units<X::kUnit>();
         const int64_t offset = begin - sh.words[17];
-        int hb = (int)(offset / (units + kStart));
+        int hb = offset < 1 << 30 ? (int)((uint32_t)offset / (uint32_t)(units + kStart)) : (int)(offset / (units + kStart));
         int64_t chunk = offset - hb * (units + kStart) - kStart, at = begin;      // below 0: what comes before the segment's first unit
 
         const uint32_t base_k = kTableAt + 4 * lane, base_v = base_k + 128, stage0 = (uint32_t)X::stages_at(team * kTeamWarps + warp);
@@ -557,14 +601,17 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
             auto tile_of = [&](int n) { return tile0 + n / X::kPair * X::kUnit + n % X::kPair; };      // of the warp's n-th tile
             uint32_t missing = 0;                                       // bit s: stage s holds no tile: past the end, or on a page that is not there
             int page = -1;                                              // lane l: of the warp's tile 32 i + l, i as far as copies are
+            auto page_of = [&](int n) { const int tile = tile_of(n); return tile < stop ? __ldg(pages + (tile >> tile_shift)) : -1; };
+            const int first_pages = page_of(lane);
+            Query<P, kFloat> query_raw;
+            query_raw.fetch(a, sequence, head, block * kQueries + (kRests ? warp % 4 : warp), lane, x.length);
             auto start = [&](int round, int stage) {
                 if (round < rounds) {
                     if (round * X::kPair % 32 == 0) {
-                        const int tile = tile_of(round * X::kPair + lane);
-                        page = -1;
-                        if (tile < stop) {
-                            page = __ldg(pages + (tile >> tile_shift));
-                            if (page < 0 || page >= a.num_pages) { page = -1; atomicOr(a.flags, LQ_CACHE_BAD_PAGE); }
+                        page = round == 0 ? first_pages : page_of(round * X::kPair + lane);
+                        if (page < 0 || page >= a.num_pages) {
+                            if (tile_of(round * X::kPair + lane) < stop) atomicOr(a.flags, LQ_CACHE_BAD_PAGE);
+                            page = -1;
                         }
                     }
 #pragma unroll
@@ -576,9 +623,9 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
                 }
                 commit_copies();
             };
-            float mine[P / 32];
-            load_query<P>(mine, a, sequence, head, block, kRests ? warp % 4 : warp, lane, x.length);
             for (int j = 0; j < X::kStages / X::kPair - 1; ++j) start(j, j * X::kPair);
+            float mine[P / 32];
+            query_raw.finish(mine, a, lane);
             stage_query<P, kRests>(sh, mine, a.scale, warp, lane);
             team_sync(team);
             uint32_t q[P / 16][2], q2[kSecond ? P / 16 : 1][2];
@@ -707,6 +754,8 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
                         make_float4(S.acc[m][i], S.acc[m][2 + i], S.acc[m + 1][i], S.acc[m + 1][2 + i]);
             }
             team_sync(team);
+            const bool starts = chunk == 0, whole = starts && count == units;
+            const int slot = 2 * me + starts;
             if (tid < kQueries) {
                 float r = kLow, rw = kLow, total = 0.0f;
                 for (int w = 0; w < kTeamWarps; ++w) { r = fmaxf(r, sh.stats[w][tid][0]); rw = fmaxf(rw, sh.stats[w][tid][1]); }
@@ -714,11 +763,16 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
                     total += sh.stats[w][tid][2] * ex2(sh.stats[w][tid][0] - r);
                     sh.share[tid][w] = ex2(sh.stats[w][tid][1] - rw);
                 }
-                sh.share[tid][kTeamWarps] = r; sh.share[tid][kTeamWarps + 1] = rw; sh.share[tid][kTeamWarps + 2] = total;
+                if (whole) {                    // the segment's own: what is left to multiply by, and the logarithm
+                    sh.share[tid][kTeamWarps] = total != 0.0f ? ex2(rw - r - kLift) / total : 0.0f;
+                    if (a.lse && block * kQueries + tid < a.group)
+                        a.lse[(int64_t)sequence * a.shape.heads * a.group + head * a.group + block * kQueries + tid] =
+                            total != 0.0f ? (r + log2f(total)) * 0.693147180559945309f : -INFINITY;
+                } else {
+                    *reinterpret_cast<float4*>(partials + slot * kPartial<P> + tid * (P + 4) + P) = make_float4(r, rw, total, 0.0f);
+                }
             }
             team_sync(team);
-            const bool starts = chunk == 0, whole = starts && count == units;
-            const int slot = 2 * me + starts;
             for (int i = tid; i < (kRests ? 4 : kQueries) * P / 4; i += kTeam) {
                 const int query = i / (P / 4), d = (i % (P / 4)) * 4;
                 const float* share = sh.share[query];
@@ -735,22 +789,14 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
                     }
                     sum4.x += v.x * f; sum4.y += v.y * f; sum4.z += v.z * f; sum4.w += v.w * f;
                 }
-                const float r = share[kTeamWarps], rw = share[kTeamWarps + 1], total = share[kTeamWarps + 2];
                 if (whole) {
                     if (block * kQueries + query < a.group) {
-                        const float f = total != 0.0f ? ex2(rw - r - kLift) / total : 0.0f;
-                        char* const to = row_of(a.out, sequence, head * a.group + block * kQueries + query);
-                        const float o[4] = {sum4.x * f, sum4.y * f, sum4.z * f, sum4.w * f};
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) if (d + k < a.shape.dim) store_any(a.out.type, to, d + k, o[k]);
-                        if (d == 0 && a.lse)
-                            a.lse[(int64_t)sequence * a.shape.heads * a.group + head * a.group + block * kQueries + query] =
-                                total != 0.0f ? (r + log2f(total)) * 0.693147180559945309f : -INFINITY;
+                        const float f = share[kTeamWarps];
+                        store_four<kFloat>(a.out, row_of(a.out, sequence, head * a.group + block * kQueries + query), d, a.shape.dim,
+                                           make_float4(sum4.x * f, sum4.y * f, sum4.z * f, sum4.w * f));
                     }
                 } else {
-                    float* to = partials + slot * kPartial<P> + query * (P + 4);
-                    *reinterpret_cast<float4*>(to + d) = sum4;
-                    if (d == 0) *reinterpret_cast<float4*>(to + P) = make_float4(r, rw, total, 0.0f);
+                    *reinterpret_cast<float4*>(partials + slot * kPartial<P> + query * (P + 4) + d) = sum4;
                 }
             }
             if (starts && !whole && tid == 0) {
