@@ -473,8 +473,9 @@ int lq_cache_read(lq_cache* cache, int32_t layer, const uint32_t* pages, int64_t
  * place j % page_size.  A sequence with nothing to see gives zeros and lse = -infinity.  Sums and softmax are in fp32.
  *   queries, out [batch][heads][head_dim] of one type; table dev [batch][table_width]; lengths dev [batch]; lse dev
  *   [batch][heads] or NULL; rotary: NULL, or the queries are rotated first, without rounding them to their type.
- *   workspace: dev, 16-byte aligned, of lq_cache_workspace() bytes; its contents need not be kept or cleared. */
-int64_t lq_cache_workspace(const lq_cache* cache);
+ *   workspace: dev, 16-byte aligned, of the bytes that lq_cache_workspace() says for this table_width and window (0: NULL will do);
+ *   its contents need not be kept or cleared. */
+int64_t lq_cache_workspace(const lq_cache* cache, int64_t table_width, int64_t window);
 int lq_cache_attend(lq_cache* cache, int32_t layer, const lq_rows* queries, int64_t batch, int32_t heads,
                     const uint32_t* pages, int64_t num_pages, const int32_t* table, int64_t table_width,
                     const int32_t* lengths, float scale, int64_t window, const lq_rotary* rotary, const lq_rows* out,

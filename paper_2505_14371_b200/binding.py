@@ -118,7 +118,7 @@ def load_library() -> C.CDLL:
     L.lq_cache_create.argtypes = [C.POINTER(vp), i32, i32, i32, i32, i32, i32, i32, u64]
     L.lq_cache_destroy.argtypes = [vp]
     L.lq_cache_page_words.argtypes = [vp]; L.lq_cache_page_words.restype = i64
-    L.lq_cache_workspace.argtypes = [vp]; L.lq_cache_workspace.restype = i64
+    L.lq_cache_workspace.argtypes = [vp, i64, i64]; L.lq_cache_workspace.restype = i64
     L.lq_cache_info.argtypes = [vp, C.POINTER(i32), C.POINTER(i32), C.POINTER(i32), C.POINTER(i32)]
     L.lq_cache_set_levels.argtypes = [vp, i32, i32, C.POINTER(C.c_float), i32]
     L.lq_cache_get_levels.argtypes = [vp, i32, i32, C.POINTER(C.c_float), i32]

@@ -189,9 +189,19 @@ CacheRowsOf rows_of(int heads)
     return d;
 }
 
-int64_t workspace_of(const lq_cache* c)
+// Most tiles of 16 tokens that a sequence has to be read of.
+int64_t tiles_of(const lq_cache* c, int64_t table_width, int64_t window)
 {
-    return (int64_t)c->sms * cache_attend_teams(c->shape.padded) * (kCacheRecordBytes + 2 * 4 * cache_partial_floats(c->shape.padded));
+    const int64_t all = (table_width << c->shape.page_shift) / 16;
+    return window > 0 ? std::min<int64_t>(all, window / 16 + 2) : all;
+}
+
+// None where no sequence can be split: a unit never is.
+int64_t workspace_of(const lq_cache* c, int64_t table_width, int64_t window)
+{
+    const CacheShape& s = c->shape;
+    if (tiles_of(c, table_width, window) <= cache_attend_unit(s.padded, s.sym_bits[0], s.sym_bits[1])) return 0;
+    return (int64_t)c->sms * cache_attend_teams(s.padded) * (kCacheRecordBytes + 2 * 4 * cache_partial_floats(s.padded));
 }
 
 #define LQ_TRY(expr) do { const int c_ = (expr); if (c_ != LQ_OK) return c_; } while (0)
@@ -274,7 +284,13 @@ int lq_cache_destroy(lq_cache* cache)
 }
 
 int64_t lq_cache_page_words(const lq_cache* cache) { return cache ? (int64_t)cache->shape.page_words : (int64_t)lq_set_error(LQ_EINVAL, "cache is NULL"); }
-int64_t lq_cache_workspace(const lq_cache* cache) { return cache ? workspace_of(cache) : (int64_t)lq_set_error(LQ_EINVAL, "cache is NULL"); }
+
+int64_t lq_cache_workspace(const lq_cache* cache, int64_t table_width, int64_t window)
+{
+    if (!cache) return lq_set_error(LQ_EINVAL, "cache is NULL");
+    if (table_width < 0 || table_width > INT32_MAX || window < 0) return lq_set_error(LQ_EINVAL, "table_width or window out of range");
+    return workspace_of(cache, table_width, window);
+}
 
 int lq_cache_info(const lq_cache* cache, int32_t* kv_heads, int32_t* head_dim, int32_t* page_size, int32_t* device)
 {
@@ -388,8 +404,9 @@ int lq_cache_attend(lq_cache* cache, int32_t layer, const lq_rows* queries, int6
     if (!std::isfinite(scale)) return lq_set_error(LQ_EINVAL, "scale is not a finite number");
     if (window < 0) return lq_set_error(LQ_EINVAL, "window = %lld is negative", (long long)window);
     LQ_TRY(take_rotary(rotary, s, false, &a.rotary));
-    if (!workspace || !aligned(workspace, 16) || workspace_bytes < workspace_of(cache))
-        return lq_set_error(LQ_EINVAL, "workspace has to be 16-byte aligned and of %lld bytes or more", (long long)workspace_of(cache));
+    const int64_t needed = workspace_of(cache, table_width, window);
+    if (needed > 0 && (!workspace || !aligned(workspace, 16) || workspace_bytes < needed))
+        return lq_set_error(LQ_EINVAL, "workspace has to be 16-byte aligned and of %lld bytes or more", (long long)needed);
     a.group = heads / s.heads; a.group_blocks = (a.group + 7) / 8;
     // the dealing out of work multiplies its units with the grid in 64 bits
     const double tokens = (double)std::min<int64_t>(table_width << s.page_shift, INT32_MAX);
@@ -397,15 +414,11 @@ int lq_cache_attend(lq_cache* cache, int32_t layer, const lq_rows* queries, int6
         return lq_set_error(LQ_EINVAL, "batch, heads and table_width are too large together");
     if (batch == 0) return LQ_OK;
     a.shape = s; a.tables = cache->tables + (size_t)layer * 2;
-    a.pages = pages; a.table = table; a.lengths = lengths; a.lse = lse; a.partial = static_cast<float*>(workspace); a.flags = cache->flags;
+    a.pages = pages; a.table = table; a.lengths = lengths; a.lse = lse; a.partial = needed > 0 ? static_cast<float*>(workspace) : nullptr; a.flags = cache->flags;
     a.num_pages = num_pages; a.table_width = table_width; a.window = window;
     a.scale = scale * 1.44269504088896341f;
     a.batch = (int32_t)batch;
     a.sms = cache->sms;
-    // a unit is never split
-    int64_t tiles = (table_width << s.page_shift) / 16;
-    if (window > 0) tiles = std::min(tiles, window / 16 + 2);
-    a.split = tiles > cache_attend_unit(s.padded, s.sym_bits[0], s.sym_bits[1]);
     LQ_ON_DEVICE(cache);
     LQ_CUDA(s.padded == 64 ? launch_cache_attend_64(a, (cudaStream_t)stream)
             : s.padded == 128 ? launch_cache_attend_128(a, (cudaStream_t)stream) : launch_cache_attend_256(a, (cudaStream_t)stream));

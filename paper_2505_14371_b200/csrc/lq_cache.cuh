@@ -108,13 +108,12 @@ struct CacheAttendArgs {
     const int32_t* table;               // [batch][table_width] page numbers
     const int32_t* lengths;
     float* lse;                         // [batch][heads * group] or NULL
-    float* partial;                     // workspace, see lq_cache_attend.cuh
+    float* partial;                     // workspace, see lq_cache_attend.cuh; NULL: no sequence can be split
     uint32_t* flags;
     int64_t num_pages, table_width, window;
     float scale;                        // of the scores, times log2(e)
     int32_t batch, group, group_blocks; // queries a head, and their blocks of 8
     int32_t sms;                        // CTAs
-    int32_t split;                      // whether a sequence may be split over CTAs at all
 };
 
 cudaError_t launch_cache_write(const CacheWriteArgs& a, cudaStream_t s);

@@ -548,7 +548,7 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
     const int64_t begin = me < parts ? share_of(me) : 0, end = me < parts ? share_of(me + 1) : 0;
     Record* records = reinterpret_cast<Record*>(a.partial);
     float* partials = a.partial + (int64_t)teams * (sizeof(Record) / 4);
-    if (tid == 0) records[me].sequence = -1;
+    if (tid == 0 && a.partial) records[me].sequence = -1;
 
     if (begin < end) {
         // the sequence that unit `begin` belongs to, and the units before it
@@ -902,7 +902,7 @@ cudaError_t launch_as(const CacheAttendArgs& a, cudaStream_t s)
     static std::atomic<uint64_t> configured{0};
     cudaError_t e = opt_in_shared_memory(configured, kBytes, attend_kernel<P, WK, WV, kMode>);
     if (e == cudaSuccess) e = lq::launch(attend_kernel<P, WK, WV, kMode>, a.sms, X::kTeams * kTeam, kBytes, s, a);
-    if (e == cudaSuccess && a.split) e = lq::launch(attend_join_kernel<P>, a.sms * X::kTeams, 32 * kQueries * kJoinWarps, 0, s, a);
+    if (e == cudaSuccess && a.partial) e = lq::launch(attend_join_kernel<P>, a.sms * X::kTeams, 32 * kQueries * kJoinWarps, 0, s, a);
     return e;
 }
 

@@ -321,11 +321,11 @@ PyObject* cache_attend(PyObject*, PyObject* const* a, Py_ssize_t n)
     const int64_t window = PyErr_Occurred() ? 0 : PyLong_AsLongLong(a[9]);
     if (PyErr_Occurred() || !rotary_of(a[10], a[11], a[12], c, batch, &r, &turned)) return nullptr;
     // from torch's allocator, on the stream that the call runs on: a workspace of its own for every call, also in a graph
-    const int64_t bytes = lq_cache_workspace(c.cache);
-    const at::Tensor space = at::empty({bytes}, l->options().dtype(at::kByte));
+    const int64_t bytes = lq_cache_workspace(c.cache, t->size(1), window < 0 ? 0 : window);
+    const at::Tensor space = bytes > 0 ? at::empty({bytes}, l->options().dtype(at::kByte)) : at::Tensor();
     return call_on(c, [&](void* s) {
         return lq_cache_attend(c.cache, layer, &q, batch, static_cast<int32_t>(heads), p, pages, table, t->size(1), lengths, static_cast<float>(scale),
-                               window, turned ? &r : nullptr, &o, lse, space.data_ptr(), bytes, s);
+                               window, turned ? &r : nullptr, &o, lse, bytes > 0 ? space.data_ptr() : nullptr, bytes, s);
     });
 }
 

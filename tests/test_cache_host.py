@@ -26,7 +26,7 @@ def test_shapes_that_are_refused(lib, args, word):
 
 def test_calls_without_a_cache(lib):
     assert lib.lq_cache_destroy(None) == 0
-    assert lib.lq_cache_page_words(None) == -1 and lib.lq_cache_workspace(None) == -1
+    assert lib.lq_cache_page_words(None) == -1 and lib.lq_cache_workspace(None, 1, 0) == -1
     assert lib.lq_cache_status(None, C.byref(C.c_uint32())) == -1
     assert lib.lq_cache_write(None, 0, None, None, 0, None, None, 0, -1, None, None) == -1
     assert lib.lq_cache_read(None, 0, None, 0, 0, None, None, None, None) == -1

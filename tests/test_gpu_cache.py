@@ -547,8 +547,16 @@ def test_calls_that_are_refused():
     r = rows_t(q.data_ptr(), 256, 64, 0)
     o = rows_t(out.data_ptr(), 256, 64, 0)
     space = torch.empty(64, dtype=torch.uint8, device="cuda")
-    rc = lib.lq_cache_attend(c._h, 0, r, 2, 4, pages.data_ptr(), 4, table.data_ptr(), 2, n.data_ptr(), 1.0, 0, None, o, None, space.data_ptr(), 64, None)
-    assert rc == -1 and b"workspace" in lib.lq_last_error()
+    wide = torch.zeros((2, 100), dtype=torch.int32, device="cuda")
+    for window in (0, 1500):
+        assert lib.lq_cache_workspace(c._h, 100, window) > 64
+        rc = lib.lq_cache_attend(c._h, 0, r, 2, 4, pages.data_ptr(), 4, wide.data_ptr(), 100, n.data_ptr(), 1.0, window, None, o, None, space.data_ptr(), 64, None)
+        assert rc == -1 and b"workspace" in lib.lq_last_error()
+    # sequences that cannot be split need none
+    assert lib.lq_cache_workspace(c._h, 2, 0) == 0 and lib.lq_cache_workspace(c._h, 100, 60) == 0
+    assert lib.lq_cache_attend(c._h, 0, r, 2, 4, pages.data_ptr(), 4, table.data_ptr(), 2, n.data_ptr(), 1.0, 0, None, o, None, None, 0, None) == 0
+    assert lib.lq_cache_workspace(c._h, -1, 0) == -1 and lib.lq_cache_workspace(c._h, 1, -1) == -1
+    torch.cuda.synchronize()
     c.close()
     for call in (lambda: write(0, k, k, slots, pages), lambda: attend(0, q, pages, table, n, out), lambda: c.lq_cache_status()):
         with pytest.raises(lq.LqError):
