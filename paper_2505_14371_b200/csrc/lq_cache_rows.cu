@@ -1,8 +1,9 @@
 // Rows of the key-value cache: quantised as they are written, and read back.
 //
 // A lane takes 8 coordinates of a row (token, head, keys or values) at a time: 16 bytes of fp16 or bf16 in one load or store, one
-// 32-bit word of 4-bit symbols (or two of 8-bit ones), two Philox blocks.  The writing kernel gives a lane two such parts (lane i those
-// from 8 i and from padded / 2 + 8 i): with one, what a row costs besides its coordinates was a third of the instructions.
+// 32-bit word of 4-bit symbols (or two of 8-bit ones), two Philox blocks.  The writing kernel gives a lane two such parts of rows of 128
+// and 256 (lane i those from 8 i and from padded / 2 + 8 i): with one, what a row costs besides its coordinates was a third of the
+// instructions (16384 tokens of 8 heads of 128 54 us, 44 with two); rows of 64 have one (9600 tokens of 10 heads of 41, unbiased: 36 us, 39 with two).
 // Its norm is an all-reduce over those lanes.  Bound: the bytes of the rows on one side and of the page on the other; for
 // few tokens the latency of slot -> row -> norm -> store.
 #include <cuda_bf16.h>
@@ -19,7 +20,8 @@ namespace {
 
 constexpr int kRowThreads = 256;
 constexpr int kEach = 8;                // coordinates at a time
-constexpr int kParts = 2;               // ... of a lane of the writing kernel
+template <int P>
+constexpr int kPartsOf = P >= 128 ? 2 : 1;      // ... of a lane of the writing kernel
 constexpr int kWriteCtas = 3;           // CTAs of the writing kernel that an SM holds at once, by its registers
 
 template <typename T> __device__ __forceinline__ float to_f32(T v);
@@ -146,7 +148,7 @@ __device__ __forceinline__ void rotate8(float (&x)[kEach], const T* row, int d, 
 }
 
 // N as the cache keeps it (0: the row is kept as zeros); bad: NaN, Inf or a norm that overflows.  Same value in all lanes.
-template <int kLanes>
+template <int kLanes, int kParts>
 __device__ __forceinline__ float row_norm(const float (&x)[kParts][kEach], int q, bool& bad)
 {
     float n;
@@ -254,9 +256,10 @@ __device__ __forceinline__ void symbols8(const float (&x)[kEach], float norm, fl
 }
 
 // Every CTA has its share of the keys, which are rotated, and then of the values.  Rows are fetched a round ahead.
-template <typename T, int kLanes, bool kUnbiased>
+template <typename T, int P, bool kUnbiased>
 __global__ void __launch_bounds__(kRowThreads, kWriteCtas) cache_write_kernel(const __grid_constant__ CacheWriteArgs a)
 {
+    constexpr int kParts = kPartsOf<P>, kLanes = P / (kEach * kParts);
     __shared__ SharedSearch tables[2];
 #pragma unroll 1
     for (int kind = 0; kind < 2; ++kind) {
@@ -334,7 +337,7 @@ __global__ void __launch_bounds__(kRowThreads, kWriteCtas) cache_write_kernel(co
                 }
             }
             bool bad;
-            const float norm = row_norm<kLanes>(x, a.shape.q, bad);
+            const float norm = row_norm<kLanes, kParts>(x, a.shape.q, bad);
             if (slot < 0) continue;
             const float inv = norm > 0.0f ? __frcp_rn(norm) : 0.0f;
             const int place = (int)slot & (page_size - 1);
@@ -439,11 +442,11 @@ cudaError_t by_type_and_size(const Args& a, int each, int resident, Go go)
 
 cudaError_t launch_cache_write(const CacheWriteArgs& a, cudaStream_t s)
 {
-    return by_type_and_size(a, kEach * kParts, kWriteCtas, [&](auto t, auto padded, unsigned grid) {
+    return by_type_and_size(a, a.shape.padded >= 128 ? kEach * kPartsOf<128> : kEach * kPartsOf<64>, kWriteCtas, [&](auto t, auto padded, unsigned grid) {
         using T = decltype(t);
-        constexpr int kLanes = decltype(padded)::value / (kEach * kParts);
-        return a.unbiased ? launch(cache_write_kernel<T, kLanes, true>, grid, kRowThreads, 0, s, a)
-                          : launch(cache_write_kernel<T, kLanes, false>, grid, kRowThreads, 0, s, a);
+        constexpr int P = decltype(padded)::value;
+        return a.unbiased ? launch(cache_write_kernel<T, P, true>, grid, kRowThreads, 0, s, a)
+                          : launch(cache_write_kernel<T, P, false>, grid, kRowThreads, 0, s, a);
     });
 }
 
