@@ -257,6 +257,13 @@ int lq_cache_create(lq_cache** out, int32_t num_layers, int32_t kv_heads, int32_
     }
     cudaError_t e = cudaGetDevice(&c->device);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&c->sms, cudaDevAttrMultiProcessorCount, c->device);
+    // the attention kernel places its shared memory by address (lq_cache_attend.cuh)
+    int reserved = 0;
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&reserved, cudaDevAttrReservedSharedMemoryPerBlock, c->device);
+    if (e == cudaSuccess && reserved > 1024) {
+        delete c;
+        return lq_set_error(LQ_ECUDA, "cache setup: %d bytes of shared memory are the system's, 1024 at most are expected", reserved);
+    }
     if (e == cudaSuccess) e = cudaMalloc(reinterpret_cast<void**>(&c->tables), host.size() * sizeof(CacheTable));
     if (e == cudaSuccess) e = cudaMemcpy(c->tables, host.data(), host.size() * sizeof(CacheTable), cudaMemcpyHostToDevice);
     if (e == cudaSuccess) e = cudaMalloc(reinterpret_cast<void**>(&c->flags), sizeof(uint32_t));

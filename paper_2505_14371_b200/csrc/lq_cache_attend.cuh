@@ -29,11 +29,17 @@
 // groups of 4 rows with a gap behind each, and the tile's tokens are dealt to the rows of the operands (token_row) such that
 // both the keys' and the values' reads meet every bank once.
 //
-// Split.  Units of 128 tokens (8 warps x 16; 256 where a warp takes two tiles at a time) of all (sequence, head, 8 queries) in a row are dealt out evenly to teams of 8 warps, as
-// many as the GPU holds at once (two a CTA, which share the look-up table; one for rows of 256); every team finds its
-// share from the lengths, on the device.  A team that has all of a segment (sequence, head, 8 queries) writes its output; the others leave
-// partial sums in the workspace, at most two a team, and the team where a segment begins leaves a record of it, from which a
-// second kernel joins them in the order of the teams.
+// Split.  Units of 128 tokens (8 warps x 16; 256 where a warp takes two tiles at a time) of all (sequence, head, 8 queries) in a
+// row are dealt out evenly to teams of 8 warps, as many as the GPU holds at once (two a CTA, which share the look-up table;
+// one for rows of 256); every team finds its share from the lengths, on the device.  The start of a segment (sequence, head,
+// 8 queries) counts as two units more: 64 sequences of 250 to 16384 tokens 140 -> 102 us.  A team that has all of a segment writes its
+// output; the others leave partial sums in the workspace, at most two a team, and the team where a segment begins leaves a
+// record of it, from which a second kernel joins them in the order of the teams, so that the same call gives the same bits.
+//
+// What bounds it: the instructions that load from shared memory (98 a tile of 16 tokens and 128 coordinates at one a cycle and SM,
+// where DRAM would need 93 cycles), of which 60 % of the cycles are used, as the 16 warps of an SM wait for one another's
+// results; 32 sequences of 8192 tokens, 8 heads of 128 in 4 bits: 80 us, where the copy bandwidth would take 43.6.  Short
+// sequences: a segment's chain of page, copy, products, sum and output, some 4 us.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -680,6 +686,8 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
                             if ((gone >> h & 1) || token < x.first || token >= x.length) s[h][i] = s[h][i + 1] = w[h][i] = w[h][i + 1] = -INFINITY;
                         }
                 }
+                T values;                       // the first tile's before what the scores go through (1 to 2 % where there are two)
+                take_values(values, even + place, odd + place);
                 float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};        // of s, of w
 #pragma unroll
                 for (int h = 0; h < X::kPair; ++h)
@@ -724,9 +732,8 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
                         b2[0] = transposed(halves(r0.x, r0.y));
                         b2[1] = transposed(halves(r1.x, r1.y));
                     }
-                    T cur;
-                    take_values(cur, even + place + h * X::kBytes, odd + place + h * X::kBytes);
-                    weigh<P, WK, WV, (kMode == kTwoBoth)>(S.acc, cur, b, b2, base_v);
+                    if (h > 0) take_values(values, even + place + h * X::kBytes, odd + place + h * X::kBytes);
+                    weigh<P, WK, WV, (kMode == kTwoBoth)>(S.acc, values, b, b2, base_v);
                 }
             }
 

@@ -90,29 +90,41 @@ def test_rows_are_written_bit_for_bit(tokens, heads, dim, page, bits, q, kind, p
         assert np.array_equal(keep(gn).view(np.uint32), keep(was[2 + i]).view(np.uint32))
 
 
-def test_values_on_and_beside_every_border():
+def crowded(n):
+    """Levels of which most are neighbours among the numbers of 11 bits, just above 1/2 and just above 2^-14."""
+    near = [0.5 + j * 2.0 ** -11 for j in range(n // 2)] + [2.0 ** -14 + j * 2.0 ** -24 for j in range(n - 2 - n // 2)]
+    return [0.0] + sorted(near) + [1.0]
+
+
+@pytest.mark.parametrize("bits,levels", [(3, None), (7, None), (3, crowded(8)), (7, crowded(128)), (7, [j / 127 for j in range(128)]),
+                                         (3, [0, 2.0 ** -24, 2.0 ** -23, 2.0 ** -20, 2.0 ** -16, 2.0 ** -8, 0.25, 1])])
+@pytest.mark.parametrize("step", [None, 3])
+def test_values_on_and_beside_every_border(bits, levels, step):
     """Rows of one large value (the norm is 1) and values at levels, at the middles between them, and one step off either."""
-    for bits in (3, 7):
-        c = make(1, 256, 16, (bits, bits), 0)
-        lv = np.array(c.lq_cache_get_levels(0, "keys"), np.float32)
-        pts = np.concatenate([lv, (lv[1:] + lv[:-1]) / 2]).astype(np.float32)
-        pts = np.concatenate([pts, np.nextafter(pts, np.float32(0)), np.nextafter(pts, np.float32(2)), -pts, [np.float32(1e-42), 0, -0.0]])
-        pts = pts[np.abs(pts) <= 1]
-        per = 255
-        count = -(-len(pts) // per)
-        x = np.zeros((count, 1, 256), np.float32)
-        x[:, 0, 0] = 1
-        for i in range(count):
-            part = pts[i * per: (i + 1) * per]
-            x[i, 0, 1: 1 + len(part)] = part
-        k = torch.from_numpy(x).cuda()
-        pages = c.empty_pages(-(-count // 16))
-        c.lq_cache_write(0, k, k, torch.arange(count, device="cuda"), pages)
-        got = sections(c, pages)
-        for kind, name in ((0, "keys"), (1, "values")):
-            sym, norm = R.quantise(x, c.lq_cache_get_levels(0, name), 0, np.float32(0.5))
-            g = np.moveaxis(got[kind], 2, 1).reshape(-1, 1, 256)[:count]
-            assert np.array_equal(g, sym)
+    c = make(1, 256, 16, (bits, bits), 0)
+    if levels:
+        for kind in ("keys", "values"):
+            c.lq_cache_set_levels(0, kind, levels)
+    lv = np.array(c.lq_cache_get_levels(0, "keys"), np.float32)
+    pts = np.concatenate([lv, (lv[1:] + lv[:-1]) / 2]).astype(np.float32)
+    pts = np.concatenate([pts, np.nextafter(pts, np.float32(0)), np.nextafter(pts, np.float32(2)), -pts, [np.float32(1e-42), 0, -0.0]])
+    pts = pts[np.abs(pts) <= 1]
+    per = 255
+    count = -(-len(pts) // per)
+    x = np.zeros((count, 1, 256), np.float32)
+    x[:, 0, 0] = 1
+    for i in range(count):
+        part = pts[i * per: (i + 1) * per]
+        x[i, 0, 1: 1 + len(part)] = part
+    k = torch.from_numpy(x).cuda()
+    pages = c.empty_pages(-(-count // 16))
+    c.lq_cache_write(0, k, k, torch.arange(count, device="cuda"), pages, step=step)
+    got = sections(c, pages)
+    for kind, name in ((0, "keys"), (1, "values")):
+        rho = np.float32(0.5) if step is None else R.uniforms(SEED, 0, kind, np.arange(count), 1, 256, step)
+        sym, norm = R.quantise(x, c.lq_cache_get_levels(0, name), 0, rho)
+        g = np.moveaxis(got[kind], 2, 1).reshape(-1, 1, 256)[:count]
+        assert np.array_equal(g, sym)
 
 
 def test_rows_that_cannot_be_kept():
