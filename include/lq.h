@@ -458,7 +458,7 @@ int lq_cache_status(lq_cache* cache, uint32_t* flags);
 /* Quantises rows of keys and values [tokens][kv_heads][head_dim] into slots [tokens] (dev) of one layer's pages; a negative
  * slot is skipped (padding of a batch).  rotary: NULL, or the keys are rotated first (rotary->at must then be given).
  * step: -1 rounds to the nearest level, 0..2^32-1 unbiased.  Slots of a call have to differ: a slot that occurs
- * twice ends with symbols of either token. */
+ * twice ends with symbols and norms of both tokens, in any mixture. */
 int lq_cache_write(lq_cache* cache, int32_t layer, const lq_rows* keys, const lq_rows* values, int64_t tokens,
                    const int64_t* slots, uint32_t* pages, int64_t num_pages, int64_t step, const lq_rotary* rotary,
                    void* stream);
