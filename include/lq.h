@@ -437,7 +437,7 @@ typedef struct {
     int32_t interleaved;
 } lq_rotary;
 
-/* num_layers 1..65536; kv_heads 1..1024; head_dim 1..256; bits 3 or 7; q: 0 (infinity norm), 1 or 2.  Level sets start
+/* num_layers 1..4096; kv_heads 1..1024; head_dim 1..256; bits 3 or 7; q: 0 (infinity norm), 1 or 2.  Level sets start
  * uniform.  Allocates its level tables on the current device; may synchronise. */
 int lq_cache_create(lq_cache** out, int32_t num_layers, int32_t kv_heads, int32_t head_dim, int32_t page_size,
                     int32_t bits_keys, int32_t bits_values, int32_t q, uint64_t seed);
@@ -448,7 +448,7 @@ int lq_cache_info(const lq_cache* cache, int32_t* kv_heads, int32_t* head_dim, i
 
 /* Level set of (layer, kind), kind = LQ_KEYS or LQ_VALUES: n = 2^bits values from 0 to 1, strictly increasing also after
  * rounding to fp16 (else LQ_EINVAL); a set of lq_fit_levels can be taken as it is where that holds.  Rows written before
- * a set are read with the new levels.  get returns the rounded set.  Both synchronise the device. */
+ * a set are read with the new levels.  set synchronises the device; get returns the rounded set. */
 int lq_cache_set_levels(lq_cache* cache, int32_t layer, int32_t kind, const float* host_levels, int32_t n);
 int lq_cache_get_levels(const lq_cache* cache, int32_t layer, int32_t kind, float* host_levels, int32_t n);
 

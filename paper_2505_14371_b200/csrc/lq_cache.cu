@@ -215,7 +215,7 @@ int lq_cache_create(lq_cache** out, int32_t num_layers, int32_t kv_heads, int32_
 {
     if (!out) return lq_set_error(LQ_EINVAL, "out is NULL");
     *out = nullptr;
-    if (num_layers < 1 || num_layers > 65536) return lq_set_error(LQ_EINVAL, "num_layers must be in [1, 65536], got %d", num_layers);
+    if (num_layers < 1 || num_layers > 4096) return lq_set_error(LQ_EINVAL, "num_layers must be in [1, 4096], got %d", num_layers);
     if (kv_heads < 1 || kv_heads > 1024) return lq_set_error(LQ_EINVAL, "kv_heads must be in [1, 1024], got %d", kv_heads);
     if (head_dim < 1 || head_dim > 256) return lq_set_error(LQ_EINVAL, "head_dim must be in [1, 256], got %d", head_dim);
     if (page_size < 16 || page_size > 1024 || (page_size & (page_size - 1)))

@@ -15,7 +15,7 @@ def lib():
     return lq.load_library()
 
 
-@pytest.mark.parametrize("args,word", [((0, 1, 64, 16, 3, 3, 0), b"num_layers"), ((1, 0, 64, 16, 3, 3, 0), b"kv_heads"), ((1, 1, 0, 16, 3, 3, 0), b"head_dim"),
+@pytest.mark.parametrize("args,word", [((0, 1, 64, 16, 3, 3, 0), b"num_layers"), ((4097, 1, 64, 16, 3, 3, 0), b"num_layers"), ((1, 0, 64, 16, 3, 3, 0), b"kv_heads"), ((1, 1, 0, 16, 3, 3, 0), b"head_dim"),
                                        ((1, 1, 257, 16, 3, 3, 0), b"head_dim"), ((1, 1, 64, 8, 3, 3, 0), b"page_size"), ((1, 1, 64, 48, 3, 3, 0), b"page_size"),
                                        ((1, 1, 64, 2048, 3, 3, 0), b"page_size"), ((1, 1, 64, 16, 4, 3, 0), b"bits"), ((1, 1, 64, 16, 3, 8, 0), b"bits"),
                                        ((1, 1, 64, 16, 3, 3, 3), b"q must"), ((1, 1, 64, 16, 3, 3, -1), b"q must")])
