@@ -841,7 +841,7 @@ __global__ void __launch_bounds__(32 * kQueries* kJoinWarps) attend_join_kernel(
 {
     constexpr int kVectors = P / 128 > 0 ? P / 128 : 1;                 // of 4 coordinates a lane
     __shared__ float4 sums[kJoinWarps][kQueries][kVectors][32];
-    __shared__ float totals[kJoinWarps][kQueries];
+    __shared__ float4 stats[kJoinWarps][kQueries];      // reference, reference of the weights, denominator
     pdl_wait();
     pdl_launch_next();
     const Record rec = reinterpret_cast<const Record*>(a.partial)[blockIdx.x];
@@ -849,49 +849,51 @@ __global__ void __launch_bounds__(32 * kQueries* kJoinWarps) attend_join_kernel(
     const int lane = threadIdx.x & 31, q = (threadIdx.x >> 5) % kQueries, share = (threadIdx.x >> 5) / kQueries, begin = blockIdx.x;
     const float* partials = a.partial + (int64_t)gridDim.x * (sizeof(Record) / 4) + q * (P + 4);
     auto part = [&](int c) { return partials + (2 * (int64_t)c + (c == begin)) * kPartial<P>; };
-    float r = kLow, rw = kLow;
-    for (int c = begin + lane; c <= rec.last; c += 32) {
-        const float2 st = *reinterpret_cast<const float2*>(part(c) + P);
-        r = fmaxf(r, st.x); rw = fmaxf(rw, st.y);
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o /= 2) {
-        r = fmaxf(r, __shfl_xor_sync(0xffffffffu, r, o));
-        rw = fmaxf(rw, __shfl_xor_sync(0xffffffffu, rw, o));
-    }
-    float total = 0.0f;
+    // the references move as the teams come, so that nothing is read twice or waited for
+    float r = kLow, rw = kLow, total = 0.0f;
     float4 acc[kVectors] = {};
-#pragma unroll 4
+#pragma unroll (P == 256 ? 4 : 8)
     for (int c = begin + share; c <= rec.last; c += kJoinWarps) {
         const float* p = part(c);
-        const float4 st = *reinterpret_cast<const float4*>(p + P);
-        total += st.z * ex2(st.x - r);
-        const float f = ex2(st.y - rw);
+        const float4 st = __ldcg(reinterpret_cast<const float4*>(p + P));
+        const float r1 = fmaxf(r, st.x), rw1 = fmaxf(rw, st.y), old = ex2(rw - rw1), f = ex2(st.y - rw1);
+        total = total * ex2(r - r1) + st.z * ex2(st.x - r1);
+        r = r1; rw = rw1;
 #pragma unroll
         for (int i = 0; i < kVectors; ++i) {
             if (P >= 128 || lane < P / 4) {
-                const float4 v = *reinterpret_cast<const float4*>(p + 4 * (lane + 32 * i));
-                acc[i].x += v.x * f; acc[i].y += v.y * f; acc[i].z += v.z * f; acc[i].w += v.w * f;
+                const float4 v = __ldcg(reinterpret_cast<const float4*>(p + 4 * (lane + 32 * i)));
+                acc[i].x = acc[i].x * old + v.x * f; acc[i].y = acc[i].y * old + v.y * f;
+                acc[i].z = acc[i].z * old + v.z * f; acc[i].w = acc[i].w * old + v.w * f;
             }
         }
     }
 #pragma unroll
     for (int i = 0; i < kVectors; ++i) sums[share][q][i][lane] = acc[i];
-    if (lane == 0) totals[share][q] = total;
+    if (lane == 0) stats[share][q] = make_float4(r, rw, total, 0.0f);
     __syncthreads();
     const int head = rec.head_block / a.group_blocks, query = (rec.head_block - head * a.group_blocks) * kQueries + q;
     if (share > 0 || query >= a.group) return;
-    for (int s = 1; s < kJoinWarps; ++s) total += totals[s][q];
-    const float f = total != 0.0f ? ex2(rw - r - kLift) / total : 0.0f;
+    for (int s = 1; s < kJoinWarps; ++s) { r = fmaxf(r, stats[s][q].x); rw = fmaxf(rw, stats[s][q].y); }
+    float f[kJoinWarps];
+    total = 0.0f;
+#pragma unroll
+    for (int s = 0; s < kJoinWarps; ++s) {
+        total += stats[s][q].z * ex2(stats[s][q].x - r);
+        f[s] = ex2(stats[s][q].y - rw);
+    }
+    const float out = total != 0.0f ? ex2(rw - r - kLift) / total : 0.0f;
     char* const to = row_of(a.out, rec.sequence, head * a.group + query);
 #pragma unroll
     for (int i = 0; i < kVectors; ++i) {
-        for (int s = 1; s < kJoinWarps; ++s) {
-            const float4 v = sums[s][q][i][lane];
-            acc[i].x += v.x; acc[i].y += v.y; acc[i].z += v.z; acc[i].w += v.w;
+        float4 v = make_float4(0, 0, 0, 0);
+#pragma unroll
+        for (int s = 0; s < kJoinWarps; ++s) {
+            const float4 u = sums[s][q][i][lane];
+            v.x += u.x * f[s]; v.y += u.y * f[s]; v.z += u.z * f[s]; v.w += u.w * f[s];
         }
+        const float o[4] = {v.x * out, v.y * out, v.z * out, v.w * out};
         const int d = 4 * (lane + 32 * i);
-        const float o[4] = {acc[i].x * f, acc[i].y * f, acc[i].z * f, acc[i].w * f};
 #pragma unroll
         for (int k = 0; k < 4; ++k) if (d + k < a.shape.dim) store_any(a.out.type, to, d + k, o[k]);
     }
