@@ -8,8 +8,8 @@
 // kSlack, which the threads of a warp vote on, and sums are rescaled then.  Scores, p, w and all sums are fp32.  Roundings to
 // fewer bits: q as fp16 after a power of two per query (exact for fp16 and bf16 queries; rotated and fp32 ones are taken as
 // a sum of two fp16 numbers, 22 bits), and w as fp16, 11 bits, for the second product (with fp32 outputs as a sum of two as
-// well): the rounding of a weight is at most an eighth of the output's own for bf16 and equal to it for fp16, and independent
-// from token to token.
+// well, and with fp16 ones of up to 4 queries a head): the rounding of a weight is at most an eighth of the output's own for
+// bf16 and equal to it for fp16, and independent from token to token.
 //
 // Work.  A warp takes 16 tokens of one head at a time: the keys are the A operand (16 tokens x 16 coordinates) of
 // mma.m16n8k16, 8 queries the B operand; the scores' fragment, transposed by two movmatrix, is the B operand of the second
@@ -308,7 +308,8 @@ __device__ __forceinline__ void take_values(Tile<P, WK, WV>& t, const char* even
 // kTwo: a sum of two, with a second product for the rest; kTwoBoth: and the weights are.  With up to 4 queries a head the rests
 // take columns 4 to 7 of the same product (kBeside: of queries, kBesideBoth: of queries and weights), which costs neither
 // registers nor products: 32 sequences of 8192 tokens, rows of 128, rotated bf16 queries 92 -> 82 us, fp32 100 -> 82.
-constexpr int kPlain = 0, kTwo = 1, kTwoBoth = 2, kBeside = 3, kBesideBoth = 4;
+// fp16 outputs take that for their weights too (kBesideHalf: kBesideBoth for rows of 16 bits).
+constexpr int kPlain = 0, kTwo = 1, kTwoBoth = 2, kBeside = 3, kBesideBoth = 4, kBesideHalf = 5;
 
 template <int P>
 struct Sums {
@@ -489,7 +490,8 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
 {
     using X = Stage<P, WK, WV>;
     using T = Tile<P, WK, WV>;
-    constexpr bool kSecond = kMode == kTwo || kMode == kTwoBoth, kRests = kMode == kBeside || kMode == kBesideBoth;
+    constexpr bool kSecond = kMode == kTwo || kMode == kTwoBoth, kRestsBoth = kMode == kBesideBoth || kMode == kBesideHalf;
+    constexpr bool kRests = kMode == kBeside || kRestsBoth;
     constexpr bool kFloat = kMode == kTwoBoth || kMode == kBesideBoth;
     extern __shared__ __align__(128) char smem[];
     char* const shared = smem - __cvta_generic_to_shared(smem);         // shared address 0
@@ -721,7 +723,7 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
                         w[h][i] = ex2(w[h][i] - (S.ref_w[i & 1] - kLift));
                     }
                     uint32_t h0 = halves(w[h][0], w[h][1]), h1 = halves(w[h][2], w[h][3]);
-                    if constexpr (kMode == kBesideBoth) {
+                    if constexpr (kRestsBoth) {
                         const float2 r0 = rest_of(h0, w[h][0], w[h][1]), r1 = rest_of(h1, w[h][2], w[h][3]);
                         if (t >= 2) { h0 = halves(r0.x, r0.y); h1 = halves(r1.x, r1.y); }
                     }
@@ -789,7 +791,7 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
                     float4 v = *reinterpret_cast<const float4*>(
                         reinterpret_cast<const float*>(shared + X::stages_at(team * kTeamWarps + w)) + ((query & 1) * 4 + (query >> 1)) * (P + 4) + d);
                     const float f = share[w];
-                    if constexpr (kMode == kBesideBoth) {               // what the weights' rounding left, of query + 4
+                    if constexpr (kRestsBoth) {               // what the weights' rounding left, of query + 4
                         const float4 u = *reinterpret_cast<const float4*>(
                             reinterpret_cast<const float*>(shared + X::stages_at(team * kTeamWarps + w)) + ((query & 1) * 4 + (query >> 1) + 2) * (P + 4) + d);
                         v.x += u.x; v.y += u.y; v.z += u.z; v.w += u.w;
@@ -920,6 +922,7 @@ cudaError_t launch_mode(const CacheAttendArgs& a, cudaStream_t s)
 {
     const bool beside = a.group <= 4;
     if (a.queries.type == LQ_F32) return beside ? launch_as<P, WK, WV, kBesideBoth>(a, s) : launch_as<P, WK, WV, kTwoBoth>(a, s);
+    if (beside && a.queries.type == LQ_F16) return launch_as<P, WK, WV, kBesideHalf>(a, s);
     if (a.rotary.table) return beside ? launch_as<P, WK, WV, kBeside>(a, s) : launch_as<P, WK, WV, kTwo>(a, s);
     return launch_as<P, WK, WV, kPlain>(a, s);
 }
