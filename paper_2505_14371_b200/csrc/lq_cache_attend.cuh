@@ -36,6 +36,9 @@
 // output; the others leave partial sums in the workspace, at most two a team, and the team where a segment begins leaves a
 // record of it, from which a second kernel joins them in the order of the teams, so that the same call gives the same bits.
 //
+// Loads.  Both kernels start beside their predecessor, which may be what writes the lengths, pages, queries or partial sums: what is
+// read behind pdl_wait is read by ordinary loads, by cp.async, or by intrinsics on a pointer from fresh().
+//
 // What bounds it: the instructions that load from shared memory (98 a tile of 16 tokens and 128 coordinates at one a cycle and SM,
 // where DRAM would need 93 cycles), of which 60 % of the cycles are used, as the 16 warps of an SM wait for one another's
 // results; 32 sequences of 8192 tokens, 8 heads of 128 in 4 bits: 80 us, where the copy bandwidth would take 43.6.  Short
@@ -209,7 +212,7 @@ __device__ __forceinline__ Extent extent_of(const CacheAttendArgs& a, int sequen
 {
     Extent e;
     const int64_t most = a.table_width << a.shape.page_shift;
-    const int n = __ldg(a.lengths + sequence);
+    const int n = a.lengths[sequence];
     e.length = n < 0 ? 0 : n > most ? (uint32_t)most : (uint32_t)n;
     e.first = a.window > 0 && e.length > a.window ? e.length - (uint32_t)a.window : 0;
     e.tile0 = (int32_t)(e.first / kTile);
@@ -413,8 +416,8 @@ struct Query {
 
     static __device__ __forceinline__ uint32_t raw(const char* row, int d)
     {
-        if constexpr (kFloat) return __ldg(reinterpret_cast<const uint32_t*>(row) + d);
-        else return __ldg(reinterpret_cast<const unsigned short*>(row) + d);
+        if constexpr (kFloat) return reinterpret_cast<const uint32_t*>(row)[d];
+        else return reinterpret_cast<const unsigned short*>(row)[d];
     }
     static __device__ __forceinline__ float number(uint32_t v, int type)
     {
@@ -429,7 +432,7 @@ struct Query {
         const float* angles = r.table;
         const int half = r.dim / 2;
         if (r.table && live) {
-            const int64_t at = r.at ? __ldg(r.at + sequence) : (length > 0 ? (int64_t)length - 1 : 0);
+            const int64_t at = r.at ? r.at[sequence] : (length > 0 ? (int64_t)length - 1 : 0);
             lost = at < 0 || at >= r.positions;
             if (lost) { if (lane == 0) atomicOr(a.flags, LQ_CACHE_BAD_POSITION); }
             else angles += at * r.dim;
@@ -440,7 +443,7 @@ struct Query {
             x[i] = live && d < a.shape.dim ? raw(row, d) : 0;
             if (r.table && live && !lost && d < r.dim) {
                 const int p = r.interleaved ? d / 2 : d < half ? d : d - half;
-                c[i] = __ldg(angles + p); s[i] = __ldg(angles + half + p);
+                c[i] = angles[p]; s[i] = angles[half + p];
                 y[i] = raw(row, r.interleaved ? d ^ 1 : d < half ? d + half : d - half);
             }
         }
@@ -502,7 +505,7 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
 
     {   // the look-up table: a thread writes copies of one entry, a warp's lanes at different banks
         const bool mine = X::kTeams == 1 || team == 0, other = X::kTeams == 1 || team == 1;
-        const uint32_t k = mine ? __ldg(a.tables[LQ_KEYS].pairs + tid) : 0, v = other ? __ldg(a.tables[LQ_VALUES].pairs + tid) : 0;
+        const uint32_t k = mine ? a.tables[LQ_KEYS].pairs[tid] : 0, v = other ? a.tables[LQ_VALUES].pairs[tid] : 0;
         uint4* row = reinterpret_cast<uint4*>(table + tid * 256);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -536,7 +539,7 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
     if (lane == 31) { sh.words[warp] = scan0; sh.words[kTeamWarps + warp] = rest; }
     if (me == 0)
         for (int b = tid; b < a.batch; b += kTeam) {
-            const int n = __ldg(a.lengths + b);
+            const int n = a.lengths[b];
             if (n < 0 || n > a.table_width << a.shape.page_shift) atomicOr(a.flags, LQ_CACHE_BAD_LENGTH);
         }
     __syncthreads();                    // (the table is there too)
@@ -609,7 +612,7 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
             auto tile_of = [&](int n) { return tile0 + n / X::kPair * X::kUnit + n % X::kPair; };      // of the warp's n-th tile
             uint32_t missing = 0;                                       // bit s: stage s holds no tile: past the end, or on a page that is not there
             int page = -1;                                              // lane l: of the warp's tile 32 i + l, i as far as copies are
-            auto page_of = [&](int n) { const int tile = tile_of(n); return tile < stop ? __ldg(pages + (tile >> tile_shift)) : -1; };
+            auto page_of = [&](int n) { const int tile = tile_of(n); return tile < stop ? pages[tile >> tile_shift] : -1; };
             const int first_pages = page_of(lane);
             Query<P, kFloat> query_raw;
             query_raw.fetch(a, sequence, head, block * kQueries + (kRests ? warp % 4 : warp), lane, x.length);
@@ -846,10 +849,11 @@ __global__ void __launch_bounds__(32 * kQueries* kJoinWarps) attend_join_kernel(
     __shared__ float4 stats[kJoinWarps][kQueries];      // reference, reference of the weights, denominator
     pdl_wait();
     pdl_launch_next();
-    const Record rec = reinterpret_cast<const Record*>(a.partial)[blockIdx.x];
+    const float* const workspace = fresh(a.partial);
+    const Record rec = reinterpret_cast<const Record*>(workspace)[blockIdx.x];
     if (rec.sequence < 0) return;
     const int lane = threadIdx.x & 31, q = (threadIdx.x >> 5) % kQueries, share = (threadIdx.x >> 5) / kQueries, begin = blockIdx.x;
-    const float* partials = a.partial + (int64_t)gridDim.x * (sizeof(Record) / 4) + q * (P + 4);
+    const float* partials = workspace + (int64_t)gridDim.x * (sizeof(Record) / 4) + q * (P + 4);
     auto part = [&](int c) { return partials + (2 * (int64_t)c + (c == begin)) * kPartial<P>; };
     // the references move as the teams come, so that nothing is read twice or waited for
     float r = kLow, rw = kLow, total = 0.0f;

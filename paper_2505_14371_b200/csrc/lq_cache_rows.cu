@@ -9,6 +9,9 @@
 // What bounds them.  Writing: instructions, some 33 a coordinate (rotation 15 of a key's, look-up and packing 14, norm 4), at 70 %
 // of the issue slots; 76 MB read and 9 MB written in 44 us.  Reading: its writes, 3.7 TB/s beside 1 TB/s of reads (100 003 tokens in
 // 112 us; a plain fill writes 3.9 TB/s).  Few tokens: latency of slot -> row -> norm -> store, and the host.
+//
+// Both kernels start beside their predecessor, which may be what writes their slots, rows, positions or pages (a row is read back right
+// after it was written): all that is read behind pdl_wait is read by ordinary loads, never through the read-only path.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -47,7 +50,7 @@ __device__ __forceinline__ Eight<T> load8(const T* row, int d, int dim, bool wid
     Eight<T> e;
     if (wide && d + kEach <= dim) {
 #pragma unroll
-        for (int i = 0; i < (int)(kEach * sizeof(T) / 16); ++i) reinterpret_cast<uint4*>(&e)[i] = __ldg(reinterpret_cast<const uint4*>(row + d) + i);
+        for (int i = 0; i < (int)(kEach * sizeof(T) / 16); ++i) reinterpret_cast<uint4*>(&e)[i] = __ldca(reinterpret_cast<const uint4*>(row + d) + i);
     } else {
 #pragma unroll
         for (int i = 0; i < kEach; ++i) e.v[i] = d + i < dim ? row[d + i] : of_f32<T>(0.0f);
@@ -89,15 +92,15 @@ __device__ __forceinline__ void store8(const float (&x)[kEach], T* row, int d, i
 
 __device__ __forceinline__ void load_angles(float* to, const float* from, int n)
 {
-    for (int i = 0; i < n; i += 4) *reinterpret_cast<float4*>(to + i) = __ldg(reinterpret_cast<const float4*>(from + i));
+    for (int i = 0; i < n; i += 4) *reinterpret_cast<float4*>(to + i) = __ldca(reinterpret_cast<const float4*>(from + i));
 }
 
 // The pairs of the first `dim` coordinates turned by the angles of `position`.  x holds coordinates d .. d+7 of `row`; the
 // partners that this lane does not hold come from the row again (the first level cache has it).
 template <typename T>
-__device__ __forceinline__ void rotate8(float (&x)[kEach], const T* row, int d, const CacheRotary& r, int64_t position, bool wide)
+__device__ __forceinline__ void rotate8(float (&x)[kEach], const T* row, int d, const CacheRotary& r, const float* angles, int64_t position, bool wide)
 {
-    const float* c = r.table + (int64_t)(uint32_t)position * r.dim;
+    const float* c = angles + (int64_t)(uint32_t)position * r.dim;
     const float* s = c + r.dim / 2;
     if (r.wide && wide) {
         if (d >= r.dim) return;
@@ -129,7 +132,7 @@ __device__ __forceinline__ void rotate8(float (&x)[kEach], const T* row, int d, 
 #pragma unroll
         for (int i = 0; i < kEach; i += 2) {
             if (d + i < r.dim) {
-                const float cc = __ldg(c + (d + i) / 2), ss = __ldg(s + (d + i) / 2), a = x[i], b = x[i + 1];
+                const float cc = __ldca(c + (d + i) / 2), ss = __ldca(s + (d + i) / 2), a = x[i], b = x[i + 1];
                 x[i] = __fsub_rn(__fmul_rn(a, cc), __fmul_rn(b, ss));
                 x[i + 1] = __fadd_rn(__fmul_rn(b, cc), __fmul_rn(a, ss));
             }
@@ -142,7 +145,7 @@ __device__ __forceinline__ void rotate8(float (&x)[kEach], const T* row, int d, 
             if (e < r.dim) {
                 const bool first = e < half;
                 const int p = first ? e : e - half;
-                const float cc = __ldg(c + p), ss = __ldg(s + p), other = to_f32(row[first ? e + half : p]);
+                const float cc = __ldca(c + p), ss = __ldca(s + p), other = to_f32(row[first ? e + half : p]);
                 x[i] = first ? __fsub_rn(__fmul_rn(x[i], cc), __fmul_rn(other, ss))
                              : __fadd_rn(__fmul_rn(x[i], cc), __fmul_rn(other, ss));
             }
@@ -195,7 +198,7 @@ __device__ __forceinline__ Place place_of(uint32_t r, int heads, const CacheRows
     const uint32_t token = __umulhi(2 * r, by.factor) >> by.shift;
     p.token = (int)token;
     p.head = (int)(r - token * heads);
-    p.slot = __ldg(slots + token);
+    p.slot = __ldca(slots + token);
     return p;
 }
 
@@ -273,13 +276,13 @@ __global__ void __launch_bounds__(kRowThreads, kWriteCtas) cache_write_kernel(co
         const uint4* from = reinterpret_cast<const uint4*>(&s);
         constexpr int kHead = (int)offsetof(CacheSearch, edge) / 16, kEntry = (int)offsetof(CacheSearch, entry) / 16;
         static_assert(offsetof(CacheSearch, edge) % 16 == 0 && offsetof(CacheSearch, entry) % 16 == 0, "parts are copied by 16 bytes");
-        const int entries = __ldg(&s.entries), begin = entries ? kEntry : kHead, end = entries ? kEntry + (entries + 3) / 4 : kEntry;
-        if (threadIdx.x < kHead) to[threadIdx.x] = __ldg(from + threadIdx.x);
-        for (int i = begin + threadIdx.x; i < end; i += kRowThreads) to[i] = __ldg(from + i);
+        const int entries = s.entries, begin = entries ? kEntry : kHead, end = entries ? kEntry + (entries + 3) / 4 : kEntry;
+        if (threadIdx.x < kHead) to[threadIdx.x] = from[threadIdx.x];
+        for (int i = begin + threadIdx.x; i < end; i += kRowThreads) to[i] = from[i];
         if (kUnbiased)
             for (int i = threadIdx.x; i < kCacheLevels - 1; i += kRowThreads) {
-                const float l = __ldg(t.levels + i);
-                tables[kind].low_gap[i] = make_float2(l, __fsub_rn(__ldg(t.levels + i + 1), l));
+                const float l = t.levels[i];
+                tables[kind].low_gap[i] = make_float2(l, __fsub_rn(t.levels[i + 1], l));
             }
     }
     __syncthreads();
@@ -291,13 +294,16 @@ __global__ void __launch_bounds__(kRowThreads, kWriteCtas) cache_write_kernel(co
     const int lane = threadIdx.x % kLanes, page_size = 1 << a.shape.page_shift;
     auto from = [&](int part) { return (part * kLanes + lane) * kEach; };        // first coordinate of a part
     const bool turned = a.rotary.table != nullptr;
+    const int64_t* const slots = fresh(a.slots);
+    const int64_t* const positions = fresh(a.rotary.at);
+    const float* const angles = fresh(a.rotary.table);
 #pragma unroll 1
     for (int kind = 0; kind < 2; ++kind) {
         const SharedSearch& table = tables[kind];
         const int bits = a.shape.sym_bits[kind];
         const int codes_at = kind ? page_size * a.shape.row_words[0] : 0, row_words = a.shape.row_words[kind];
         const int norms_at = page_size * (a.shape.row_words[0] + a.shape.row_words[1] + kind);
-        const char* const data = static_cast<const char*>(a.rows[kind].data);
+        const char* const data = fresh(static_cast<const char*>(a.rows[kind].data));
         const int token_bytes = a.rows[kind].token_bytes, head_bytes = a.rows[kind].head_bytes;
         const bool wide = a.rows[kind].wide;
 
@@ -308,12 +314,12 @@ __global__ void __launch_bounds__(kRowThreads, kWriteCtas) cache_write_kernel(co
         auto fetch = [&](uint32_t r) {
             next_slot = -1;
             if (r >= rows) return;
-            const Place p = place_of(r, a.shape.heads, a.by_head, a.slots);
+            const Place p = place_of(r, a.shape.heads, a.by_head, slots);
             next_slot = p.slot; next_head = p.head;
             next_row = reinterpret_cast<const T*>(data + (int64_t)p.token * token_bytes + (int64_t)p.head * head_bytes);
 #pragma unroll
             for (int c = 0; c < kParts; ++c) next[c] = load8(next_row, from(c), a.shape.dim, wide);
-            if (turned) next_position = __ldg(a.rotary.at + p.token);
+            if (turned) next_position = __ldca(positions + p.token);
         };
         fetch(blockIdx.x * kRows + group);
         for (uint32_t first = blockIdx.x * kRows; first < rows; first += stride) {
@@ -334,7 +340,7 @@ __global__ void __launch_bounds__(kRowThreads, kWriteCtas) cache_write_kernel(co
                 } else if (kind == LQ_KEYS) {
 #pragma unroll
                     for (int c = 0; c < kParts; ++c) {
-                        rotate8(x[c], row, from(c), a.rotary, position, wide);
+                        rotate8(x[c], row, from(c), a.rotary, angles, position, wide);
                         asm volatile("" ::: "memory");                  // (the angles of one part at a time: registers)
                     }
                 }
@@ -380,7 +386,7 @@ __global__ void __launch_bounds__(kRowThreads) cache_read_kernel(const __grid_co
 #pragma unroll
     for (int kind = 0; kind < 2; ++kind)
         if (threadIdx.x < 1u << a.shape.sym_bits[kind]) {
-            const float l = __ldg(a.tables[kind].levels + threadIdx.x / 2);
+            const float l = a.tables[kind].levels[threadIdx.x / 2];
             values[kind][threadIdx.x] = threadIdx.x % 2 ? -l : l;
         }
     __syncthreads();
@@ -390,21 +396,23 @@ __global__ void __launch_bounds__(kRowThreads) cache_read_kernel(const __grid_co
     constexpr int kRows = kRowThreads / kLanes;
     const uint32_t rows = (uint32_t)(a.tokens * a.shape.heads);
     const int lane = threadIdx.x % kLanes, d = lane * kEach, page_size = 1 << a.shape.page_shift;
+    const int64_t* const slots = fresh(a.slots);
+    const uint32_t* const pages = fresh(a.pages);
     for (uint32_t r = blockIdx.x * kRows + threadIdx.x / kLanes; r < rows; r += gridDim.x * kRows) {
-        Place p = place_of(r, a.shape.heads, a.by_head, a.slots);
+        Place p = place_of(r, a.shape.heads, a.by_head, slots);
         if (p.slot >= a.num_slots) { p.slot = -1; if (lane == 0) atomicOr(a.flags, LQ_CACHE_BAD_SLOT); }
         const int place = (int)p.slot & (page_size - 1);
-        const uint32_t* base = a.pages + (int64_t)((uint32_t)p.slot >> a.shape.page_shift) * a.shape.page_words + p.head * a.shape.head_words;
+        const uint32_t* base = pages + (int64_t)((uint32_t)p.slot >> a.shape.page_shift) * a.shape.page_words + p.head * a.shape.head_words;
         uint2 w[2] = {};
         float norm[2] = {0.0f, 0.0f};
         if (p.slot >= 0) {
 #pragma unroll
             for (int kind = 0; kind < 2; ++kind) {
                 const uint32_t* codes = base + (kind ? page_size * a.shape.row_words[0] : 0) + place * a.shape.row_words[kind];
-                norm[kind] = __ldg(reinterpret_cast<const float*>(base + page_size * (a.shape.row_words[0] + a.shape.row_words[1])) +
-                                   kind * page_size + place);
-                if (a.shape.sym_bits[kind] == 4) w[kind].x = __ldg(codes + lane);
-                else w[kind] = __ldg(reinterpret_cast<const uint2*>(codes) + lane);
+                norm[kind] = __ldca(reinterpret_cast<const float*>(base + page_size * (a.shape.row_words[0] + a.shape.row_words[1])) +
+                                    kind * page_size + place);
+                if (a.shape.sym_bits[kind] == 4) w[kind].x = __ldca(codes + lane);
+                else w[kind] = __ldca(reinterpret_cast<const uint2*>(codes) + lane);
             }
         }
 #pragma unroll
