@@ -441,6 +441,7 @@ struct Query {
         for (int i = 0; i < P / 32; ++i) {
             const int d = lane + 32 * i;
             x[i] = live && d < a.shape.dim ? raw(row, d) : 0;
+            y[i] = 0; c[i] = s[i] = 0.0f;       // (a place without a query holds zeros: its scores vote with the others')
             if (r.table && live && !lost && d < r.dim) {
                 const int p = r.interleaved ? d / 2 : d < half ? d : d - half;
                 c[i] = angles[p]; s[i] = angles[half + p];

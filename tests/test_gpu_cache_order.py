@@ -52,3 +52,64 @@ def test_rows_pages_and_sums_of_the_call_before(heads, dim, page, bits, kind, ro
     assert a.lq_cache_status() == 0 and b.lq_cache_status() == 0
     # the rounds do differ
     assert not torch.equal(want[0][0], want[0][1]) and not torch.equal(want[3][0], want[3][1])
+
+
+@pytest.mark.parametrize("dim,group,kind", [(128, 1, "bf16"), (128, 3, "fp32"), (128, 5, "bf16"), (64, 7, "fp32"), (64, 3, "fp16"), (256, 5, "bf16"), (256, 9, "fp16"), (41, 2, "fp32")])
+def test_the_same_call_gives_the_same_bits(dim, group, kind):
+    """Rotated queries in blocks that they do not fill, whatever ran before: the places without a query have no say in when the running
+    references move, by which weights are rounded."""
+    import paper_2505_14371_b200 as lq
+    gen = torch.Generator("cuda").manual_seed(dim + group)
+    heads, tokens, page = 2, 4001, 32
+    c = lq.Cache(1, heads, dim, page, (3, 7), 0, 7)
+    num = -(-tokens // page)
+    # scores that grow along the sequence: references move all the way
+    grow = torch.linspace(0.1, 8.0, num * page, device="cuda").view(-1, 1, 1)
+    k, v = (torch.randn((num * page, heads, dim), generator=gen, device="cuda") for _ in range(2))
+    pages = c.empty_pages(num)
+    c.lq_cache_write(0, k * grow, v, torch.arange(num * page, device="cuda"), pages)
+    table = torch.arange(num, dtype=torch.int32, device="cuda").view(1, num)
+    length = torch.tensor([tokens], dtype=torch.int32, device="cuda")
+    q = torch.randn((1, heads * group, dim), generator=gen, device="cuda").to(TYPES[kind])
+    angles = lq.lq_rotary_table(tokens, dim // 2 * 2)
+    first = None
+    others = [lambda: None, lambda: torch.randn(1 << 22, generator=gen, device="cuda").mul_(1e30).exp_(),
+              lambda: torch.full((4096, 4096), 3e38, device="cuda") @ torch.ones((4096, 4096), device="cuda"),
+              lambda: (torch.randn((2048, 2048), generator=gen, device="cuda").half() * 100) @ torch.randn((2048, 2048), generator=gen, device="cuda").half(),
+              lambda: torch.randint(-2 ** 31, 2 ** 31 - 1, (1 << 22,), generator=gen, device="cuda").sort(),
+              lambda: c.lq_cache_read(0, pages, torch.arange(64, device="cuda"), torch.empty_like(k[:64]), torch.empty_like(k[:64])),
+              lambda: torch.randn((64, 64, 64), generator=gen, device="cuda", dtype=torch.float64).cumsum(0)]
+    for i in range(6 * len(others)):
+        others[i % len(others)]()
+        out, lse = torch.empty_like(q), torch.empty((1, heads * group), device="cuda")
+        c.lq_cache_attend(0, q, pages, table, length, out, lse=lse, rotary=angles)
+        assert torch.isfinite(out).all() and torch.isfinite(lse).all()
+        first = first or (out, lse)
+        assert torch.equal(out, first[0]) and torch.equal(lse, first[1]), i
+
+
+@pytest.mark.parametrize("dim,group,kind,bits", [(128, 1, "bf16", (3, 3)), (128, 5, "bf16", (7, 7)), (64, 3, "fp32", (3, 7)), (64, 7, "fp16", (3, 3)), (256, 5, "fp32", (3, 3)),
+                                                 (256, 2, "bf16", (7, 3))])
+def test_other_sequences_of_a_batch_leave_no_trace(dim, group, kind, bits):
+    """The queries of every second sequence are other ones: the bits of those between them stay (lengths, and with them the split, are the same)."""
+    import paper_2505_14371_b200 as lq
+    gen = torch.Generator("cuda").manual_seed(dim + group)
+    heads, page, batch, most = 3, 16, 400, 700
+    c = lq.Cache(1, heads, dim, page, bits, 0, 7)
+    per = most // page + 1
+    grow = torch.linspace(0.1, 8.0, per * page, device="cuda").repeat(4).view(-1, 1, 1)
+    k, v = (torch.randn((4 * per * page, heads, dim), generator=gen, device="cuda") for _ in range(2))
+    pages = c.empty_pages(4 * per)
+    c.lq_cache_write(0, k * grow, v * torch.randn_like(v[:, :1, :1]).mul_(3).exp_(), torch.arange(4 * per * page, device="cuda"), pages)
+    table = (torch.arange(batch, device="cuda")[:, None] % 4 * per + torch.arange(per, device="cuda")).to(torch.int32)
+    lengths = torch.randint(1, most, (batch,), generator=gen, device="cuda", dtype=torch.int32)
+    q = torch.randn((batch, heads * group, dim), generator=gen, device="cuda").to(TYPES[kind])
+    angles = lq.lq_rotary_table(most, dim // 2 * 2)
+    first = None
+    for factor in (1.0, 50.0, 0.0, -3.0):
+        mine = q.clone()
+        mine[1::2] *= factor
+        out, lse = torch.empty_like(q), torch.empty((batch, heads * group), device="cuda")
+        c.lq_cache_attend(0, mine, pages, table, lengths, out, lse=lse, rotary=angles)
+        first = first or (out[::2].clone(), lse[::2].clone())
+        assert torch.equal(out[::2], first[0]) and torch.equal(lse[::2], first[1]), factor
