@@ -2,10 +2,11 @@
 //
 // Mathematics.  A row of the cache is N * level[symbol] with sign.  The keys' norm is a factor of the score and the values'
 // norm one of the weight, so the two products run on bare signed levels, which are fp16 numbers as they stand:
-//   s_j = (scale N_j) (q . level(K_j)),  w_j = exp2(s_j + log2 M_j - ref'),  out = sum_j w_j level(V_j) / sum_j p_j * 2^(ref' - ref)
-// with p_j = exp2(s_j - ref).  Weights and denominator have running references of their own (ref' of s + log2 M, ref of s), so
-// that no spread of the values' norms costs a weight its bits; a reference moves only when a score passes it by more than
-// kSlack, which the threads of a warp vote on, and sums are rescaled then.  Scores, p, w and all sums are fp32.  Roundings to
+//   s_j = (scale N_j) (q . level(K_j)),  w_j = exp2((s_j - ref) + (log2 M_j - k)),  out = 2^k sum_j w_j level(V_j) / sum_j p_j
+// with p_j = exp2(s_j - ref).  Weights have a scale 2^k beside the running reference of the scores, so that no spread of the values'
+// norms costs a weight its bits; k is a whole number and s_j - ref is formed first, so that neither large scores nor large logarithms
+// round the sum.  Reference and scale move only when an exponent passes kSlack, which the threads of a warp vote on, and sums are
+// rescaled then.  Scores, p, w and all sums are fp32.  Roundings to
 // fewer bits: q as fp16 after a power of two per query (exact for fp16 and bf16 queries; rotated and fp32 ones are taken as
 // a sum of two fp16 numbers, 22 bits), and w as fp16, 11 bits, for the second product (with fp32 outputs as a sum of two as
 // well, and with fp16 ones of up to 4 queries a head): the rounding of a weight is at most an eighth of the output's own for
@@ -48,6 +49,8 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <type_traits>
+
 #include "lq_cache.cuh"
 #include "lq_internal.cuh"
 
@@ -64,9 +67,11 @@ constexpr int kTableBytes = 256 * 256;  // entry e: 32 copies for the keys, 32 f
 // system's; the last one that a CTA can have is left free, so that the places below hold wherever in the first the kernel's own begins.)
 constexpr int kTableAt = 1 << 16, kSystemBytes = 1 << 10, kEnd = (227 << 10);
 constexpr int kStart = 2;               // what a segment costs beside its units, in units
-constexpr float kLow = -1e30f;          // a reference before its first score
+constexpr float kLow = -1e30f;          // the reference of a warp or team without a score
 constexpr float kSlack = 8.0f;          // how far (log2) a score may pass its reference
-constexpr float kLift = 6.0f;           // weights are 2^kLift at their reference: at most 2^14 as fp16, and exact down to 2^-20
+constexpr float kLift = 6.0f;           // weights are 2^kLift at their scale: at most 2^14 as fp16 (2^15 times a significand), and exact down to 2^-20
+template <bool kFloat>
+constexpr float kLiftOf = kFloat ? 0.0f : kLift;    // ... of it in the exponent (otherwise in the significand)
 
 // Workspace: a record for every team, then two partials of kCacheRecordBytes a team (sums; reference, reference of the weights,
 // denominator, unused).
@@ -118,6 +123,34 @@ constexpr int smem_bytes() { return Stage<P, WK, WV>::kTeamsAt + Stage<P, WK, WV
 
 __device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 __device__ __forceinline__ float lg2(float x) { float y; asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+
+// The values' norm of a token, 2^x m: for fp32 outputs its exponent and significand (with 2^kLift), so that a weight is as exact for
+// norms of 1e-12 as for 1 (the logarithm's error grows with its size: 6e-6 at 1e12); for others x = log2 and m is not used.
+// What is not a positive normal number becomes its logarithm in both: 0 a weight of 0, NaN NaN.
+template <bool kFloat>
+__device__ __forceinline__ void norm_parts(float norm, float& x, float& m)
+{
+    x = lg2(norm);
+    if constexpr (kFloat) {
+        const uint32_t bits = __float_as_uint(norm);
+        const float exponent = __uint_as_float(0x4b000000u | bits >> 23) - (8388608.0f + 127.0f);
+        if (bits - 0x00800000u < 0x7f000000u) x = exponent;
+        m = __uint_as_float((bits & 0x007fffffu) | (127u + (uint32_t)kLift) << 23);
+    }
+}
+
+// A scale as a whole number, so that its differences from exponents are exact.  (The bound takes the place of -infinity; what is
+// that far below the largest p adds nothing to an fp32 output.)
+__device__ __forceinline__ float whole_scale(float v) { return ceilf(fmaxf(v, -1000.0f)); }
+
+// What the sum of weighted values is multiplied by in the end: 2^scale / total, the power in two factors that are normal numbers.
+template <bool kFloat>
+__device__ __forceinline__ float out_factor(float scale, float total)
+{
+    const int n = max((int)scale - (kFloat ? (int)kLift : 0), -252), half = n >> 1;
+    const float f = 1.0f / total * __uint_as_float((uint32_t)(127 + half) << 23) * __uint_as_float((uint32_t)(127 + n - half) << 23);
+    return total != 0.0f ? f : 0.0f;
+}
 
 __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
@@ -317,13 +350,12 @@ constexpr int kPlain = 0, kTwo = 1, kTwoBoth = 2, kBeside = 3, kBesideBoth = 4, 
 template <int P>
 struct Sums {
     float acc[P / 16][4];
-    float ref[2], ref_w[2], total[2];   // of queries 2t and 2t + 1
+    float ref[2], scale[2], total[2];   // of queries 2t and 2t + 1; the scale is a whole number
     __device__ __forceinline__ void clear()
     {
 #pragma unroll
         for (int i = 0; i < P / 16; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.0f;
-        ref[0] = ref[1] = ref_w[0] = ref_w[1] = kLow;
-        total[0] = total[1] = 0.0f;
+        ref[0] = ref[1] = scale[0] = scale[1] = total[0] = total[1] = 0.0f;
     }
 };
 
@@ -583,8 +615,8 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
         }
         team_sync(team);
         int sequence = (int)sh.words[16];
-        Extent x = extent_of(a, sequence);
-        int64_t units = x.template units<X::kUnit>();
+        Extent extent = extent_of(a, sequence);
+        int64_t units = extent.template units<X::kUnit>();
         const int64_t offset = begin - sh.words[17];
         int hb = offset < 1 << 30 ? (int)((uint32_t)offset / (uint32_t)(units + kStart)) : (int)(offset / (units + kStart));
         int64_t chunk = offset - hb * (units + kStart) - kStart, at = begin;      // below 0: what comes before the segment's first unit
@@ -607,7 +639,7 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
             const int head = hb / a.group_blocks, block = hb - head * a.group_blocks;
             // ---- the first copies: this warp's tiles are kPair of every unit
             const int32_t* pages = a.table + (int64_t)sequence * a.table_width;
-            const int tile0 = x.tile0 + (int)chunk * X::kUnit + warp * X::kPair, stop = min(x.tile1, x.tile0 + ((int)chunk + count) * X::kUnit);
+            const int tile0 = extent.tile0 + (int)chunk * X::kUnit + warp * X::kPair, stop = min(extent.tile1, extent.tile0 + ((int)chunk + count) * X::kUnit);
             const int rounds = stop > tile0 ? (stop - tile0 + X::kUnit - 1) / X::kUnit : 0;
             const uint32_t head_at = (uint32_t)(head * a.shape.head_words) * 4;
             auto tile_of = [&](int n) { return tile0 + n / X::kPair * X::kUnit + n % X::kPair; };      // of the warp's n-th tile
@@ -616,7 +648,7 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
             auto page_of = [&](int n) { const int tile = tile_of(n); return tile < stop ? pages[tile >> tile_shift] : -1; };
             const int first_pages = page_of(lane);
             Query<P, kFloat> query_raw;
-            query_raw.fetch(a, sequence, head, block * kQueries + (kRests ? warp % 4 : warp), lane, x.length);
+            query_raw.fetch(a, sequence, head, block * kQueries + (kRests ? warp % 4 : warp), lane, extent.length);
             auto start = [&](int round, int stage) {
                 if (round < rounds) {
                     if (round * X::kPair % 32 == 0) {
@@ -654,6 +686,7 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
 
             Sums<P> S;
             S.clear();
+            bool begun = false;                                         // the reference is a score's
             int stage = 0, ahead = X::kStages - X::kPair;
             for (int j = 0; j < rounds; ++j) {
                 __syncwarp();                                           // every lane has read the stages that are filled next
@@ -666,7 +699,8 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
                 if ((ahead += X::kPair) == X::kStages) ahead = 0;
                 if (gone == (1u << X::kPair) - 1) continue;
 
-                float s[X::kPair][4], w[X::kPair][4];
+                // exponents of p and of the weights; the values' norms as 2^x m
+                float d[X::kPair][4], w[X::kPair][4], m[X::kPair][2];
 #pragma unroll
                 for (int h = 0; h < X::kPair; ++h) {
                     T cur;
@@ -677,54 +711,97 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
 #pragma unroll
                         for (int i = 0; i < 4; ++i) c[i] += __shfl_xor_sync(0xffffffffu, c[i], 2);
                     const char* n = norms + place + h * X::kBytes;
-                    const float nk0 = *reinterpret_cast<const float*>(n), nk1 = *reinterpret_cast<const float*>(n + 8);
-                    s[h][0] = c[0] * (f0 * nk0); s[h][1] = c[1] * (f1 * nk0); s[h][2] = c[2] * (f0 * nk1); s[h][3] = c[3] * (f1 * nk1);
-                    w[h][0] = w[h][1] = lg2(*reinterpret_cast<const float*>(n + 64));
-                    w[h][2] = w[h][3] = lg2(*reinterpret_cast<const float*>(n + 72));
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) {
+                        const float nk = *reinterpret_cast<const float*>(n + 8 * r);
+                        float x;
+                        norm_parts<kFloat>(*reinterpret_cast<const float*>(n + 64 + 8 * r), x, m[h][r]);
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            d[h][2 * r + i] = fmaf(c[2 * r + i] * (i ? f1 : f0), nk, -S.ref[i]);
+                            w[h][2 * r + i] = d[h][2 * r + i] + (x - S.scale[i]);
+                        }
+                    }
                 }
                 const uint32_t first = (uint32_t)(tile0 + j * X::kUnit) * kTile;
-                if (gone || first < x.first || first + X::kPair * kTile > x.length) {       // the ends of what is seen
+                if (gone || first < extent.first || first + X::kPair * kTile > extent.length) {     // the ends of what is seen
 #pragma unroll
                     for (int h = 0; h < X::kPair; ++h)
 #pragma unroll
                         for (int i = 0; i < 4; i += 2) {
                             const uint32_t token = first + h * kTile + row + i;
-                            if ((gone >> h & 1) || token < x.first || token >= x.length) s[h][i] = s[h][i + 1] = w[h][i] = w[h][i + 1] = -INFINITY;
+                            if ((gone >> h & 1) || token < extent.first || token >= extent.length) d[h][i] = d[h][i + 1] = w[h][i] = w[h][i + 1] = -INFINITY;
                         }
                 }
                 T values;                       // the first tile's before what the scores go through (1 to 2 % where there are two)
                 take_values(values, even + place, odd + place);
-                float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};        // of s, of w
+                float top_d = -INFINITY, top_w = -INFINITY;
 #pragma unroll
                 for (int h = 0; h < X::kPair; ++h)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        w[h][i] += s[h][i];
-                        top[i & 1] = fmaxf(top[i & 1], s[h][i]);
-                        top[2 + (i & 1)] = fmaxf(top[2 + (i & 1)], w[h][i]);
-                    }
-                const bool passed = top[0] > S.ref[0] + kSlack || top[1] > S.ref[1] + kSlack || top[2] > S.ref_w[0] + kSlack || top[3] > S.ref_w[1] + kSlack;
-                if (__any_sync(0xffffffffu, passed)) {
+                    for (int i = 0; i < 4; ++i) { top_d = fmaxf(top_d, d[h][i]); top_w = fmaxf(top_w, w[h][i]); }
+                if (__any_sync(0xffffffffu, top_d > kSlack || top_w > kSlack + kLiftOf<kFloat> || !begun)) {
+                    float x[X::kPair][2];
 #pragma unroll
-                    for (int o = 4; o < 32; o *= 2)
+                    for (int h = 0; h < X::kPair; ++h)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], o));
+                        for (int r = 0; r < 2; ++r) {   // (once more, so that they need not be kept)
+                            float unused;
+                            norm_parts<kFloat>(*reinterpret_cast<const volatile float*>(norms + place + h * X::kBytes + 64 + 8 * r), x[h][r], unused);
+                        }
+                    float step[2], moved[2], scale[2];
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
-                        const float r = fmaxf(S.ref[i], top[i]), rw = fmaxf(S.ref_w[i], top[2 + i]);
-                        S.total[i] *= ex2(S.ref[i] - r);
-                        const float f = ex2(S.ref_w[i] - rw);
-                        S.ref[i] = r; S.ref_w[i] = rw;
+                        step[i] = begun ? 0.0f : -INFINITY; scale[i] = -INFINITY;
 #pragma unroll
-                        for (int k = 0; k < P / 16; ++k) { S.acc[k][i] *= f; S.acc[k][2 + i] *= f; }
+                        for (int h = 0; h < X::kPair; ++h) step[i] = fmaxf(step[i], fmaxf(d[h][i], d[h][2 + i]));
                     }
+                    auto over_tokens = [](float (&v)[2]) {              // the largest of the lanes with the same queries
+#pragma unroll
+                        for (int o = 4; o < 32; o *= 2)
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) v[i] = fmaxf(v[i], __shfl_xor_sync(0xffffffffu, v[i], o));
+                    };
+                    over_tokens(step);
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const float ref = step[i] > -INFINITY ? S.ref[i] + step[i] : S.ref[i];
+                        moved[i] = S.ref[i] - ref;
+                        S.ref[i] = ref;
+#pragma unroll
+                        for (int h = 0; h < X::kPair; ++h)
+#pragma unroll
+                            for (int r = 0; r < 2; ++r) {
+                                d[h][2 * r + i] += moved[i];
+                                scale[i] = fmaxf(scale[i], d[h][2 * r + i] == -INFINITY ? -INFINITY : d[h][2 * r + i] + x[h][r]);
+                            }
+                    }
+                    over_tokens(scale);
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const float k = whole_scale(begun ? fmaxf(S.scale[i] + moved[i], scale[i] - kLiftOf<kFloat>) : scale[i] - kLiftOf<kFloat>);
+#pragma unroll
+                        for (int h = 0; h < X::kPair; ++h)
+#pragma unroll
+                            for (int r = 0; r < 2; ++r)
+                                w[h][2 * r + i] = d[h][2 * r + i] == -INFINITY ? -INFINITY : d[h][2 * r + i] + (x[h][r] - k);
+                        if (begun) {
+                            S.total[i] *= ex2(moved[i]);
+                            const float f = ex2(moved[i] + (S.scale[i] - k));
+#pragma unroll
+                            for (int m = 0; m < P / 16; ++m) { S.acc[m][i] *= f; S.acc[m][2 + i] *= f; }
+                        }
+                        S.scale[i] = k;
+                    }
+                    begun = true;
                 }
 #pragma unroll
                 for (int h = 0; h < X::kPair; ++h) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        S.total[i & 1] += ex2(s[h][i] - S.ref[i & 1]);
-                        w[h][i] = ex2(w[h][i] - (S.ref_w[i & 1] - kLift));
+                        S.total[i & 1] += ex2(d[h][i]);
+                        w[h][i] = ex2(w[h][i]);
+                        if constexpr (kFloat) w[h][i] *= m[h][i >> 1];
                     }
                     uint32_t h0 = halves(w[h][0], w[h][1]), h1 = halves(w[h][2], w[h][3]);
                     if constexpr (kRestsBoth) {
@@ -753,7 +830,7 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     float* st = sh.stats[warp][2 * t + i];
-                    st[0] = S.ref[i]; st[1] = S.ref_w[i]; st[2] = S.total[i];
+                    st[0] = begun ? S.ref[i] : kLow; st[1] = S.scale[i]; st[2] = S.total[i];
                 }
             }
             wait_copies<0>();
@@ -770,19 +847,22 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
             const bool starts = chunk == 0, whole = starts && count == units;
             const int slot = 2 * me + starts;
             if (tid < kQueries) {
-                float r = kLow, rw = kLow, total = 0.0f;
-                for (int w = 0; w < kTeamWarps; ++w) { r = fmaxf(r, sh.stats[w][tid][0]); rw = fmaxf(rw, sh.stats[w][tid][1]); }
+                float r = kLow, scale = -INFINITY, total = 0.0f;
+                for (int w = 0; w < kTeamWarps; ++w) r = fmaxf(r, sh.stats[w][tid][0]);
+                for (int w = 0; w < kTeamWarps; ++w) scale = fmaxf(scale, sh.stats[w][tid][1] + (sh.stats[w][tid][0] - r));
+                scale = whole_scale(scale);
                 for (int w = 0; w < kTeamWarps; ++w) {
-                    total += sh.stats[w][tid][2] * ex2(sh.stats[w][tid][0] - r);
-                    sh.share[tid][w] = ex2(sh.stats[w][tid][1] - rw);
+                    const float moved = sh.stats[w][tid][0] - r;
+                    total += sh.stats[w][tid][2] * ex2(moved);
+                    sh.share[tid][w] = ex2(moved + (sh.stats[w][tid][1] - scale));
                 }
                 if (whole) {                    // the segment's own: what is left to multiply by, and the logarithm
-                    sh.share[tid][kTeamWarps] = total != 0.0f ? ex2(rw - r - kLift) / total : 0.0f;
+                    sh.share[tid][kTeamWarps] = out_factor<kFloat>(scale, total);
                     if (a.lse && block * kQueries + tid < a.group)
                         a.lse[(int64_t)sequence * a.shape.heads * a.group + head * a.group + block * kQueries + tid] =
                             total != 0.0f ? (r + log2f(total)) * 0.693147180559945309f : -INFINITY;
                 } else {
-                    *reinterpret_cast<float4*>(partials + slot * kPartial<P> + tid * (P + 4) + P) = make_float4(r, rw, total, 0.0f);
+                    *reinterpret_cast<float4*>(partials + slot * kPartial<P> + tid * (P + 4) + P) = make_float4(r, scale, total, 0.0f);
                 }
             }
             team_sync(team);
@@ -823,7 +903,7 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
             chunk = -kStart;
             if (at < end && ++hb == head_blocks) {
                 hb = 0;
-                do { x = extent_of(a, ++sequence); units = x.template units<X::kUnit>(); } while (units == 0);
+                do { extent = extent_of(a, ++sequence); units = extent.template units<X::kUnit>(); } while (units == 0);
             }
             team_sync(team);                                            // the sums have been read
         }
@@ -856,40 +936,69 @@ __global__ void __launch_bounds__(32 * kQueries* kJoinWarps) attend_join_kernel(
     const int lane = threadIdx.x & 31, q = (threadIdx.x >> 5) % kQueries, share = (threadIdx.x >> 5) / kQueries, begin = blockIdx.x;
     const float* partials = workspace + (int64_t)gridDim.x * (sizeof(Record) / 4) + q * (P + 4);
     auto part = [&](int c) { return partials + (2 * (int64_t)c + (c == begin)) * kPartial<P>; };
-    // the references move as the teams come, so that nothing is read twice or waited for
-    float r = kLow, rw = kLow, total = 0.0f;
+    // four teams' partials are read at once where there are as many; reference and scale move with each group
+    float r = kLow, scale = 0.0f, total = 0.0f;
     float4 acc[kVectors] = {};
-#pragma unroll (P == 256 ? 4 : 8)
-    for (int c = begin + share; c <= rec.last; c += kJoinWarps) {
-        const float* p = part(c);
-        const float4 st = __ldcg(reinterpret_cast<const float4*>(p + P));
-        const float r1 = fmaxf(r, st.x), rw1 = fmaxf(rw, st.y), old = ex2(rw - rw1), f = ex2(st.y - rw1);
-        total = total * ex2(r - r1) + st.z * ex2(st.x - r1);
-        r = r1; rw = rw1;
+    int c = begin + share;
+    auto take = [&](auto teams) {
+        constexpr int kTeams = decltype(teams)::value;
+        float4 st[kTeams], v[kTeams][kVectors] = {};
 #pragma unroll
-        for (int i = 0; i < kVectors; ++i) {
-            if (P >= 128 || lane < P / 4) {
-                const float4 v = __ldcg(reinterpret_cast<const float4*>(p + 4 * (lane + 32 * i)));
-                acc[i].x = acc[i].x * old + v.x * f; acc[i].y = acc[i].y * old + v.y * f;
-                acc[i].z = acc[i].z * old + v.z * f; acc[i].w = acc[i].w * old + v.w * f;
+        for (int j = 0; j < kTeams; ++j) {
+            const float* p = part(c + kJoinWarps * j);
+            st[j] = __ldcg(reinterpret_cast<const float4*>(p + P));
+#pragma unroll
+            for (int i = 0; i < kVectors; ++i)
+                if (P >= 128 || lane < P / 4) v[j][i] = __ldcg(reinterpret_cast<const float4*>(p + 4 * (lane + 32 * i)));
+        }
+        float r1 = r;
+#pragma unroll
+        for (int j = 0; j < kTeams; ++j) r1 = fmaxf(r1, st[j].x);
+        const float here = r - r1;
+        float scale1 = scale + here;
+#pragma unroll
+        for (int j = 0; j < kTeams; ++j) scale1 = fmaxf(scale1, st[j].y + (st[j].x - r1));
+        scale1 = whole_scale(scale1);
+        total *= ex2(here);
+        const float old = ex2(here + (scale - scale1));
+#pragma unroll
+        for (int i = 0; i < kVectors; ++i) { acc[i].x *= old; acc[i].y *= old; acc[i].z *= old; acc[i].w *= old; }
+#pragma unroll
+        for (int j = 0; j < kTeams; ++j) {
+            const float there = st[j].x - r1, f = ex2(there + (st[j].y - scale1));
+            total += st[j].z * ex2(there);
+#pragma unroll
+            for (int i = 0; i < kVectors; ++i) {
+                acc[i].x += v[j][i].x * f; acc[i].y += v[j][i].y * f; acc[i].z += v[j][i].z * f; acc[i].w += v[j][i].w * f;
             }
         }
-    }
+        r = r1; scale = scale1;
+        c += kJoinWarps * kTeams;
+    };
+#pragma unroll 1
+    while (c + 3 * kJoinWarps <= rec.last) take(std::integral_constant<int, 4>());
+#pragma unroll 1
+    while (c + kJoinWarps <= rec.last) take(std::integral_constant<int, 2>());
+    if (c <= rec.last) take(std::integral_constant<int, 1>());
 #pragma unroll
     for (int i = 0; i < kVectors; ++i) sums[share][q][i][lane] = acc[i];
-    if (lane == 0) stats[share][q] = make_float4(r, rw, total, 0.0f);
+    if (lane == 0) stats[share][q] = make_float4(r, scale, total, 0.0f);
     __syncthreads();
     const int head = rec.head_block / a.group_blocks, query = (rec.head_block - head * a.group_blocks) * kQueries + q;
     if (share > 0 || query >= a.group) return;
-    for (int s = 1; s < kJoinWarps; ++s) { r = fmaxf(r, stats[s][q].x); rw = fmaxf(rw, stats[s][q].y); }
+    for (int s = 1; s < kJoinWarps; ++s) r = fmaxf(r, stats[s][q].x);
+    scale = -INFINITY;
+    for (int s = 0; s < kJoinWarps; ++s) scale = fmaxf(scale, stats[s][q].y + (stats[s][q].x - r));
+    scale = whole_scale(scale);
     float f[kJoinWarps];
     total = 0.0f;
 #pragma unroll
     for (int s = 0; s < kJoinWarps; ++s) {
-        total += stats[s][q].z * ex2(stats[s][q].x - r);
-        f[s] = ex2(stats[s][q].y - rw);
+        const float moved = stats[s][q].x - r;
+        total += stats[s][q].z * ex2(moved);
+        f[s] = ex2(moved + (stats[s][q].y - scale));
     }
-    const float out = total != 0.0f ? ex2(rw - r - kLift) / total : 0.0f;
+    const float out = a.out.type == LQ_F32 ? out_factor<true>(scale, total) : out_factor<false>(scale, total);
     char* const to = row_of(a.out, rec.sequence, head * a.group + query);
 #pragma unroll
     for (int i = 0; i < kVectors; ++i) {

@@ -1,0 +1,98 @@
+"""The cache's attention where numbers are large, small or many: scores past 1e30, norms of every size, weights of a long context."""
+import numpy as np
+import pytest
+import torch
+
+import cache_reference as R
+
+pytestmark = pytest.mark.gpu
+
+TYPES = {"fp32": torch.float32, "fp16": torch.float16, "bf16": torch.bfloat16}
+
+
+def in_order(heads, dim, k, v, page=16, bits=(3, 3), q=0):
+    """A cache whose slots 0, 1, ... hold k and v [tokens][heads][dim], its pages, and the table of the one sequence that they are."""
+    import paper_2505_14371_b200 as lq
+    c = lq.Cache(1, heads, dim, page, bits, q, 7)
+    num = -(-k.shape[0] // page)
+    pages = c.empty_pages(num)
+    c.lq_cache_write(0, k, v, torch.arange(k.shape[0], device="cuda"), pages)
+    assert c.lq_cache_status() == 0
+    return c, pages, torch.arange(num, dtype=torch.int32, device="cuda").view(1, num)
+
+
+def kept(c, pages, tokens):
+    """What the cache holds of its first tokens, in 64 bits: keys and values [heads][tokens][dim]."""
+    sec = R.head_sections(pages.cpu().numpy().view(np.uint32), c.kv_heads, c.head_dim, c.page_size, c.bits)
+    got = [R.values_of(sec[i], sec[2 + i], c.lq_cache_get_levels(0, n))[..., : c.head_dim] for i, n in ((0, "keys"), (1, "values"))]
+    return [np.moveaxis(x, 0, 1).reshape(c.kv_heads, -1, c.head_dim)[:, :tokens] for x in got]
+
+
+def attended(c, pages, table, q, tokens, **more):
+    out, lse = torch.empty_like(q), torch.empty(q.shape[:2], device="cuda")
+    c.lq_cache_attend(0, q, pages, table, torch.tensor([tokens], dtype=torch.int32, device="cuda"), out, lse=lse, **more)
+    assert c.lq_cache_status() == 0
+    return out, lse
+
+
+@pytest.mark.parametrize("norm", [1e-30, 1e-12, 1e-6, 1.0, 1e6, 1e12, 1e30])
+@pytest.mark.parametrize("group,dim,bits", [(2, 64, (3, 3)), (6, 128, (3, 7)), (3, 200, (7, 3)), (8, 41, (7, 7))])
+def test_weights_are_as_exact_for_values_of_any_size(norm, group, dim, bits):
+    """fp32, small scores, all values' norms of one size, nothing that cancels: a factor that all weights share would show."""
+    gen = torch.Generator("cuda").manual_seed(dim)
+    tokens = 100
+    k = torch.randn((tokens, 2, dim), generator=gen, device="cuda")
+    v = (torch.rand((tokens, 2, dim), generator=gen, device="cuda") + 0.1) * (torch.rand((tokens, 2, 1), generator=gen, device="cuda") + 1) * norm
+    c, pages, table = in_order(2, dim, k, v, bits=bits)
+    q = torch.randn((1, 2 * group, dim), generator=gen, device="cuda")
+    out, lse = attended(c, pages, table, q, tokens, scale=1e-4)
+    keys, values = kept(c, pages, tokens)
+    for h in range(2 * group):
+        s = 1e-4 * (keys[h // group] @ q[0, h].double().cpu().numpy())
+        assert np.abs(s).max() < 0.01
+        p = np.exp(s - s.max())
+        want = p @ values[h // group] / p.sum()
+        # in units of 2^-24: exp2 of a weight and of p 4 each, significand 1, a weight as two numbers 2, a sum of 100 tokens in products of 16
+        # (truncated: 2 each, 2 of them a warp) and 8 warps 4 + 8 in both, the quotient 2; scores below 0.01 have errors below 1 together
+        assert np.all(np.abs(out[0, h].double().cpu().numpy() - want) <= 36 * 2.0 ** -24 * want)
+        assert abs(float(lse[0, h]) - (s.max() + np.log(p.sum()))) <= 36 * 2.0 ** -24 + 2.0 ** -23 * np.log(tokens)
+
+
+@pytest.mark.parametrize("kind", ["fp32", "fp16", "bf16"])
+@pytest.mark.parametrize("group,dim,bits", [(4, 128, (3, 3)), (6, 64, (7, 3)), (16, 256, (3, 7))])
+@pytest.mark.parametrize("size", [30.0, 1e3, 1e5, 1e7])
+def test_large_scores_leave_the_values_norms_alone(kind, group, dim, bits, size):
+    """All tokens have the same key, so the same score, however large: the output is the mean of values of many sizes."""
+    gen = torch.Generator("cuda").manual_seed(dim)
+    tokens = 333
+    k = torch.randn((1, 1, dim), generator=gen, device="cuda").expand(tokens, 1, dim)
+    v = (torch.rand((tokens, 1, dim), generator=gen, device="cuda") + 0.1) * torch.randn((tokens, 1, 1), generator=gen, device="cuda").exp_()
+    c, pages, table = in_order(1, dim, k, v, bits=bits)
+    q = torch.randn((1, group, dim), generator=gen, device="cuda").to(TYPES[kind])
+    keys, values = kept(c, pages, tokens)
+    # every query's score about `size`, with either sign
+    raw = q[0].double().cpu().numpy() @ keys[0, 0]
+    want = values[0].mean(0)
+    for sign in (1, -1):
+        scale = sign * size / float(np.abs(raw).max())
+        out, lse = attended(c, pages, table, q, tokens, scale=scale)
+        got = out[0].double().cpu().numpy()
+        # weights: a logarithm and an exponential of 2^-21 each, then 11 bits (two of them for fp32); sums of 333 tokens; the output's rounding
+        half = torch.finfo(TYPES[kind]).eps / 2
+        assert np.all(np.abs(got - want) <= (2.0 ** -18 + (0 if kind == "fp32" else 2.0 ** -11 + half)) * want)
+        s = scale * raw
+        assert np.all(np.abs(lse[0].double().cpu().numpy() - (s + np.log(tokens))) <= 2.0 ** -18 * (np.abs(s) + abs(scale) * np.abs(q[0].double().cpu().numpy()) @ np.abs(keys[0, 0]) + 6))
+
+
+def test_a_score_of_nothing_times_a_large_norm():
+    """Queries of 2^100 and keys' norms of 2^50 whose products are all with the level 0: scores are 0, not 0 times infinity."""
+    k = torch.zeros((50, 1, 64), device="cuda")
+    k[..., 1:] = 2.0 ** 50
+    v = torch.rand((50, 1, 64), generator=torch.Generator("cuda").manual_seed(3), device="cuda") + 0.1
+    c, pages, table = in_order(1, 64, k, v)
+    q = torch.zeros((1, 3, 64), device="cuda")
+    q[..., 0] = 2.0 ** 100
+    out, lse = attended(c, pages, table, q, 50)
+    want = kept(c, pages, 50)[1][0].mean(0)
+    assert np.all(np.abs(out[0].double().cpu().numpy() - want) <= 2.0 ** -18 * want)
+    assert np.all(np.abs(lse.double().cpu().numpy() - np.log(50)) <= 2.0 ** -20)
