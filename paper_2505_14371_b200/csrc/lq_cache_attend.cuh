@@ -67,7 +67,7 @@ constexpr int kTableBytes = 256 * 256;  // entry e: 32 copies for the keys, 32 f
 // system's; the last one that a CTA can have is left free, so that the places below hold wherever in the first the kernel's own begins.)
 constexpr int kTableAt = 1 << 16, kSystemBytes = 1 << 10, kEnd = (227 << 10);
 constexpr int kStart = 2;               // what a segment costs beside its units, in units
-constexpr float kLow = -1e30f;          // the reference of a warp or team without a score
+constexpr float kLow = -3.402823466e38f;    // the reference of a warp or team without a score: below every finite score's
 constexpr float kSlack = 8.0f;          // how far (log2) a score may pass its reference
 constexpr float kLift = 6.0f;           // weights are 2^kLift at their scale: at most 2^14 as fp16 (2^15 times a significand), and exact down to 2^-20
 template <bool kFloat>

@@ -96,3 +96,26 @@ def test_a_score_of_nothing_times_a_large_norm():
     want = kept(c, pages, 50)[1][0].mean(0)
     assert np.all(np.abs(out[0].double().cpu().numpy() - want) <= 2.0 ** -18 * want)
     assert np.all(np.abs(lse.double().cpu().numpy() - np.log(50)) <= 2.0 ** -20)
+
+
+@pytest.mark.parametrize("tokens", [5, 40, 3000])
+@pytest.mark.parametrize("sign", [-1, 1])
+def test_scores_of_any_finite_size(tokens, sign):
+    """Scores of 1e35 times 1, 2, 3, ...: the softmax is one at the largest, also where all are below -1e30."""
+    dim = 64
+    u = torch.zeros((tokens, 1, dim), device="cuda")
+    size = torch.arange(1, tokens + 1, device="cuda", dtype=torch.float32).view(-1, 1, 1)
+    order = torch.randperm(tokens, generator=torch.Generator("cuda").manual_seed(1), device="cuda")
+    u[..., 0] = 1e15
+    v = torch.randn((tokens, 1, dim), generator=torch.Generator("cuda").manual_seed(tokens), device="cuda")
+    c, pages, table = in_order(1, dim, (u * size)[order], v)
+    q = torch.zeros((1, 2, dim), device="cuda")
+    q[..., 0] = sign * 1e20 / tokens
+    out, lse = attended(c, pages, table, q, tokens, scale=1.0)
+    keys, values = kept(c, pages, tokens)
+    scores = keys[0] @ q[0, 0].double().cpu().numpy()
+    top = scores.argmax()
+    assert np.abs(scores).max() < 3e38 and abs(np.sort(scores)[-1]) > 1e30
+    # the one weight is 1, as a sum of two numbers of 11 bits exactly; the sum of weights is 1
+    assert np.all(np.abs(out[0].double().cpu().numpy() - values[0, top]) <= 2.0 ** -20 * np.abs(values[0, top]))
+    assert np.all(np.abs(lse.double().cpu().numpy() - scores[top]) <= 2.0 ** -20 * abs(scores[top]))
