@@ -8,9 +8,9 @@
 // round the sum.  Reference and scale move only when an exponent passes kSlack, which the threads of a warp vote on, and sums are
 // rescaled then.  Scores, p, w and all sums are fp32.  Roundings to
 // fewer bits: q as fp16 after a power of two per query (exact for fp16 and bf16 queries; rotated and fp32 ones are taken as
-// a sum of two fp16 numbers, 22 bits), and w as fp16, 11 bits, for the second product (with fp32 outputs as a sum of two as
-// well, and with fp16 ones of up to 4 queries a head): the rounding of a weight is at most an eighth of the output's own for
-// bf16 and equal to it for fp16, and independent from token to token.
+// a sum of two fp16 numbers, 22 bits), and w as fp16, 11 bits, for the second product of bf16
+// outputs (at most an eighth of the output's own rounding, and independent from token to token), as a sum of two, 22 bits, for fp16
+// and fp32 ones.
 //
 // Work.  A warp takes 16 tokens of one head at a time: the keys are the A operand (16 tokens x 16 coordinates) of
 // mma.m16n8k16, 8 queries the B operand; the scores' fragment, transposed by two movmatrix, is the B operand of the second
@@ -340,12 +340,14 @@ __device__ __forceinline__ void take_values(Tile<P, WK, WV>& t, const char* even
                                      (r & 1 ? odd : even) + (r >> 1) * 2 * Stage<P, WK, WV>::kRowV + 8 * c * X::kValueChunk);
 }
 
-// How queries and weights are rounded to fp16.  kPlain: a query is one number (exactly, for fp16 and bf16 that are not rotated);
-// kTwo: a sum of two, with a second product for the rest; kTwoBoth: and the weights are.  With up to 4 queries a head the rests
-// take columns 4 to 7 of the same product (kBeside: of queries, kBesideBoth: of queries and weights), which costs neither
-// registers nor products: 32 sequences of 8192 tokens, rows of 128, rotated bf16 queries 92 -> 82 us, fp32 100 -> 82.
-// fp16 outputs take that for their weights too (kBesideHalf: kBesideBoth for rows of 16 bits).
-constexpr int kPlain = 0, kTwo = 1, kTwoBoth = 2, kBeside = 3, kBesideBoth = 4, kBesideHalf = 5;
+// How queries and weights are rounded to fp16.  kPlain: a query is one number (exactly, for fp16 and bf16 that are not rotated), a
+// weight one of 11 bits.  kTwo: a query is a sum of two, with a second product for the rest; kWeights: a weight is; kTwoBoth,
+// kTwoBothHalf: both are.  With up to 4 queries a head the rests take columns 4 to 7 of the same product (kBeside: of queries,
+// kBesideBoth, kBesideHalf: of queries and weights), which costs neither registers nor products: 32 sequences of 8192 tokens, rows of
+// 128, rotated bf16 queries 92 -> 82 us, fp32 100 -> 82.  (Both: rows of 32 bits, half: of 16.)
+// One number is a weight of bf16 outputs: its rounding adds 1 % to the error of the output's own, and two cost 1 to 10 % of the time
+// (rows of 128 in 4 bits, 8 queries a head: 75.9 us, 83.8 with two).  With fp16 outputs it would add 39 %.
+constexpr int kPlain = 0, kTwo = 1, kTwoBoth = 2, kBeside = 3, kBesideBoth = 4, kBesideHalf = 5, kWeights = 6, kTwoBothHalf = 7;
 
 template <int P>
 struct Sums {
@@ -526,8 +528,8 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
 {
     using X = Stage<P, WK, WV>;
     using T = Tile<P, WK, WV>;
-    constexpr bool kSecond = kMode == kTwo || kMode == kTwoBoth, kRestsBoth = kMode == kBesideBoth || kMode == kBesideHalf;
-    constexpr bool kRests = kMode == kBeside || kRestsBoth;
+    constexpr bool kSecond = kMode == kTwo || kMode == kTwoBoth || kMode == kTwoBothHalf, kRestsBoth = kMode == kBesideBoth || kMode == kBesideHalf;
+    constexpr bool kRests = kMode == kBeside || kRestsBoth, kWeighTwo = kMode == kTwoBoth || kMode == kTwoBothHalf || kMode == kWeights;
     constexpr bool kFloat = kMode == kTwoBoth || kMode == kBesideBoth;
     extern __shared__ __align__(128) char smem[];
     char* const shared = smem - __cvta_generic_to_shared(smem);         // shared address 0
@@ -810,13 +812,13 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
                     }
                     const uint32_t b[2] = {transposed(h0), transposed(h1)};
                     uint32_t b2[2] = {0, 0};
-                    if constexpr (kMode == kTwoBoth) {
+                    if constexpr (kWeighTwo) {
                         const float2 r0 = rest_of(h0, w[h][0], w[h][1]), r1 = rest_of(h1, w[h][2], w[h][3]);
                         b2[0] = transposed(halves(r0.x, r0.y));
                         b2[1] = transposed(halves(r1.x, r1.y));
                     }
                     if (h > 0) take_values(values, even + place + h * X::kBytes, odd + place + h * X::kBytes);
-                    weigh<P, WK, WV, (kMode == kTwoBoth)>(S.acc, values, b, b2, base_v);
+                    weigh<P, WK, WV, kWeighTwo>(S.acc, values, b, b2, base_v);
                 }
             }
 
@@ -1036,7 +1038,10 @@ cudaError_t launch_mode(const CacheAttendArgs& a, cudaStream_t s)
 {
     const bool beside = a.group <= 4;
     if (a.queries.type == LQ_F32) return beside ? launch_as<P, WK, WV, kBesideBoth>(a, s) : launch_as<P, WK, WV, kTwoBoth>(a, s);
-    if (beside && a.queries.type == LQ_F16) return launch_as<P, WK, WV, kBesideHalf>(a, s);
+    if (a.queries.type == LQ_F16) {
+        if (beside) return launch_as<P, WK, WV, kBesideHalf>(a, s);
+        return a.rotary.table ? launch_as<P, WK, WV, kTwoBothHalf>(a, s) : launch_as<P, WK, WV, kWeights>(a, s);
+    }
     if (a.rotary.table) return beside ? launch_as<P, WK, WV, kBeside>(a, s) : launch_as<P, WK, WV, kTwo>(a, s);
     return launch_as<P, WK, WV, kPlain>(a, s);
 }

@@ -119,3 +119,38 @@ def test_scores_of_any_finite_size(tokens, sign):
     # the one weight is 1, as a sum of two numbers of 11 bits exactly; the sum of weights is 1
     assert np.all(np.abs(out[0].double().cpu().numpy() - values[0, top]) <= 2.0 ** -20 * np.abs(values[0, top]))
     assert np.all(np.abs(lse.double().cpu().numpy() - scores[top]) <= 2.0 ** -20 * abs(scores[top]))
+
+
+@pytest.mark.parametrize("group,dim,bits,rot", [(1, 128, (3, 3), 0), (4, 64, (3, 7), 0), (4, 128, (3, 3), 128), (3, 256, (7, 7), 0), (6, 128, (7, 7), 0), (8, 128, (3, 3), 0),
+                                                (8, 64, (7, 3), 64), (16, 256, (3, 7), 0), (7, 200, (3, 3), 100), (5, 41, (7, 7), 0)])
+def test_fp16_outputs_are_off_by_their_own_rounding_alone(group, dim, bits, rot):
+    """Over many short sequences, the error against 64 bits is that of rounding the exact output to fp16.  (Weights of 11 bits add a fifth
+    and more.)"""
+    import paper_2505_14371_b200 as lq
+    gen = torch.Generator("cuda").manual_seed(dim + group)
+    heads, batch, tokens = 2, 300, 5
+    k, v = (torch.randn((16 * batch, heads, dim), generator=gen, device="cuda") for _ in range(2))
+    c, pages, _ = in_order(heads, dim, k, v * torch.randn((16 * batch, heads, 1), generator=gen, device="cuda").exp_(), bits=bits)
+    table = torch.arange(batch, dtype=torch.int32, device="cuda").view(batch, 1)
+    q = torch.randn((batch, heads * group, dim), generator=gen, device="cuda").half()
+    out = torch.empty_like(q)
+    angles = lq.lq_rotary_table(tokens, rot) if rot else None
+    scale = 0.2 / dim
+    c.lq_cache_attend(0, q, pages, table, torch.full((batch,), tokens, dtype=torch.int32, device="cuda"), out, scale=scale, rotary=angles)
+    keys, values = (x.reshape(heads, batch, 16, dim)[:, :, :tokens] for x in kept(c, pages, 16 * batch))
+    x = q.float().cpu().numpy()
+    if rot:
+        x = R.rotate(x, np.repeat(angles[tokens - 1:].cpu().numpy(), batch, 0), False)
+    x = x.astype(np.float64).reshape(batch, heads, group, dim)
+    s = scale * np.einsum("bhgd,hbtd->bhgt", x, keys)
+    assert (scale * np.einsum("bhgd,hbtd->bhgt", np.abs(x), np.abs(keys))).max() < 0.5
+    p = np.exp(s)
+    p /= p.sum(-1, keepdims=True)
+    want = np.einsum("bhgt,hbtd->bhgd", p, values).reshape(out.shape)
+    own = np.linalg.norm(torch.from_numpy(want).half().double().numpy() - want)
+    # before the rounding, in units of 2^-24 of sum p |v|: exp2 twice 8, the norm's logarithm (below 8 in size) 22 and its sum 1, two numbers 2,
+    # one product of 16 tokens 2, the quotient 2, scores whose terms add up to 0.5 at most: 18 * 2 * 0.5 twice.  A rounding that
+    # tips over because of it is off by twice as much more.
+    before = 73 * 2.0 ** -24 * np.linalg.norm(np.einsum("bhgt,hbtd->bhgd", p, np.abs(values)))
+    assert before < 0.06 * own
+    assert np.linalg.norm(out.double().cpu().numpy() - want) <= own + 2 * before
