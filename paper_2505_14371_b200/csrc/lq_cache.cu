@@ -344,7 +344,7 @@ int lq_cache_status(lq_cache* cache, uint32_t* flags)
     LQ_ON_DEVICE(cache);
     LQ_CUDA(cudaDeviceSynchronize());
     LQ_CUDA(cudaMemcpy(flags, cache->flags, sizeof *flags, cudaMemcpyDeviceToHost));
-    LQ_CUDA(cudaMemset(cache->flags, 0, sizeof *flags));
+    if (*flags) LQ_CUDA(launch_cache_clear(cache->flags, *flags));      // what another thread's call sets meanwhile stays
     LQ_CUDA(cudaDeviceSynchronize());
     return LQ_OK;
 }

@@ -118,6 +118,7 @@ struct CacheAttendArgs {
 
 cudaError_t launch_cache_write(const CacheWriteArgs& a, cudaStream_t s);
 cudaError_t launch_cache_read(const CacheReadArgs& a, cudaStream_t s);
+cudaError_t launch_cache_clear(uint32_t* flags, uint32_t seen);        // on the default stream
 
 // One of each per padded head size (lq_cache_attend_<size>.cu).
 cudaError_t launch_cache_attend_64(const CacheAttendArgs& a, cudaStream_t s);

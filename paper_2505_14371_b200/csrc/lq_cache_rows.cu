@@ -434,6 +434,8 @@ __global__ void __launch_bounds__(kRowThreads) cache_read_kernel(const __grid_co
     }
 }
 
+__global__ void cache_clear_kernel(uint32_t* flags, uint32_t seen) { atomicAnd(flags, ~seen); }
+
 // CTAs: as many as the rows need with `each` coordinates a lane, at most as the GPU holds at once (`resident` an SM).
 template <typename Args, typename Go>
 cudaError_t by_type_and_size(const Args& a, int each, int resident, Go go)
@@ -459,6 +461,11 @@ cudaError_t launch_cache_write(const CacheWriteArgs& a, cudaStream_t s)
         return a.unbiased ? launch(cache_write_kernel<T, P, true>, grid, kRowThreads, 0, s, a)
                           : launch(cache_write_kernel<T, P, false>, grid, kRowThreads, 0, s, a);
     });
+}
+
+cudaError_t launch_cache_clear(uint32_t* flags, uint32_t seen)
+{
+    return launch_as(false, cache_clear_kernel, 1, 1, 0, 1, nullptr, flags, seen);
 }
 
 cudaError_t launch_cache_read(const CacheReadArgs& a, cudaStream_t s)

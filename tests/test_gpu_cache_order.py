@@ -113,3 +113,46 @@ def test_other_sequences_of_a_batch_leave_no_trace(dim, group, kind, bits):
         c.lq_cache_attend(0, mine, pages, table, lengths, out, lse=lse, rotary=angles)
         first = first or (out[::2].clone(), lse[::2].clone())
         assert torch.equal(out[::2], first[0]) and torch.equal(lse[::2], first[1]), factor
+
+
+def test_no_flag_is_lost_to_another_threads_status():
+    """One thread makes calls that set a flag, each after the last flag was seen; another asks for the flags all the time.  (A flag that is set
+    between their copy and their clearing has to stay.)"""
+    import random
+    import threading
+    import time
+    import paper_2505_14371_b200 as lq
+    c = lq.Cache(1, 1, 64, 16, 3, 0, 7)
+    pages = c.empty_pages(1)
+    k, bad = torch.ones((1, 1, 64), device="cuda"), torch.tensor([1000], device="cuda")
+    seen, stop, failed = [0], threading.Event(), []
+
+    def ask():
+        try:
+            while not stop.is_set():
+                if c.lq_cache_status() & lq.CACHE_BAD_SLOT:
+                    seen[0] += 1
+        except Exception as e:                      # (reported by the test's thread)
+            failed.append(e)
+
+    asking = threading.Thread(target=ask)
+    torch.cuda.synchronize()
+    asking.start()
+    try:
+        rng, stream, lost = random.Random(1), torch.cuda.Stream(), None
+        with torch.cuda.stream(stream):
+            for i in range(1500):
+                before, until = seen[0], time.perf_counter() + rng.random() * 60e-6
+                while time.perf_counter() < until:
+                    pass
+                c.lq_cache_write(0, k, k, bad, pages)
+                until = time.perf_counter() + 1.0
+                while seen[0] == before and not failed and time.perf_counter() < until:
+                    time.sleep(0)
+                if seen[0] == before:
+                    lost = i
+                    break
+    finally:
+        stop.set()
+        asking.join()
+    assert not failed and lost is None, (failed, lost)
