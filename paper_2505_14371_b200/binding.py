@@ -378,7 +378,8 @@ class Plan:
 
 class Cache:
     """Owns one lq_cache: a key-value cache in the framework's quantised form (include/lq.h).  Methods carry the names of the C entry
-    points; tensors have to be on the device that was current when the cache was made, and calls run on its current stream."""
+    points; tensors have to be on the device that was current when the cache was made, and calls run on its current stream.  No gradient
+    passes: keys and values are kept as numbers, and queries and outputs that require one are refused while gradients are recorded."""
 
     _KINDS = {"keys": 0, "values": 1}
     _LAYOUTS = {"half": False, "interleaved": True}

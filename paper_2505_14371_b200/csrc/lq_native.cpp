@@ -5,6 +5,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <ATen/core/grad_mode.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -204,6 +205,13 @@ bool wrong(const char* name, const char* what)
     return false;
 }
 
+// Outputs of these calls carry no gradient: a tensor that one would have to pass through is refused, not cut off silently.
+bool no_gradient(PyObject* o, const char* name)
+{
+    if (!THPVariable_Check(o) || !at::GradMode::is_enabled() || !THPVariable_Unpack(o).requires_grad()) return true;
+    return wrong(name, "a tensor without a gradient (detach it, or call under torch.no_grad())");
+}
+
 // [tokens][heads][head_dim] rows with the coordinates side by side; heads 0: any number.
 bool rows_of(PyObject* o, const CacheInfo& c, const char* name, int64_t tokens, int64_t heads, lq_rows* out)
 {
@@ -295,7 +303,7 @@ PyObject* cache_read(PyObject*, PyObject* const* a, Py_ssize_t n)
     CacheInfo c; lq_rows k, v; int64_t *slots, pages; uint32_t* p; int32_t layer; const at::Tensor* t;
     if (!arity(n, 6) || !cache_of(a[0], &c) || !int_of(a[1], &layer) || !pages_of(a[2], c, &p, &pages) ||
         !array_of(a[3], c, "slots", at::kLong, 1, &slots, &t) || !rows_of(a[4], c, "keys", t->numel(), c.heads, &k) ||
-        !rows_of(a[5], c, "values", t->numel(), c.heads, &v)) return nullptr;
+        !rows_of(a[5], c, "values", t->numel(), c.heads, &v) || !no_gradient(a[4], "keys") || !no_gradient(a[5], "values")) return nullptr;
     return call_on(c, [&](void* s) { return lq_cache_read(c.cache, layer, p, pages, t->numel(), slots, &k, &v, s); });
 }
 
@@ -312,6 +320,7 @@ PyObject* cache_attend(PyObject*, PyObject* const* a, Py_ssize_t n)
     if (!pages_of(a[3], c, &p, &pages) || !array_of(a[4], c, "table", at::kInt, 2, &table, &t)) return nullptr;
     if (t->size(0) != batch) { wrong("table", "a row a sequence"); return nullptr; }
     if (!rows_of(a[6], c, "out", batch, heads, &o)) return nullptr;
+    if (!no_gradient(a[2], "queries") || !no_gradient(a[6], "out") || !no_gradient(a[7], "lse")) return nullptr;
     if (a[7] != Py_None) {
         const at::Tensor* e;
         if (!array_of(a[7], c, "lse", at::kFloat, 2, &lse, &e)) return nullptr;

@@ -156,3 +156,33 @@ def test_no_flag_is_lost_to_another_threads_status():
         stop.set()
         asking.join()
     assert not failed and lost is None, (failed, lost)
+
+
+def test_gradients_are_not_cut_off_silently():
+    import paper_2505_14371_b200 as lq
+    c = lq.Cache(1, 2, 64, 16, 3, 0, 7)
+    pages = c.empty_pages(1)
+    k, q, slots = torch.randn((4, 2, 64), device="cuda"), torch.randn((1, 4, 64), device="cuda"), torch.arange(4, device="cuda")
+    table, n = torch.zeros((1, 1), dtype=torch.int32, device="cuda"), torch.tensor([4], dtype=torch.int32, device="cuda")
+    kept = k.clone().requires_grad_()
+    c.lq_cache_write(0, kept, kept * 2, slots, pages)               # what is stored is numbers
+    out, lse = torch.empty_like(q), torch.empty((1, 4), device="cuda")
+    c.lq_cache_attend(0, q, pages, table, n, out, lse=lse)
+    want = q.clone().requires_grad_()
+    for mine in (want, want * 1.0):
+        with pytest.raises(lq.LqError, match="queries.*gradient"):
+            c.lq_cache_attend(0, mine, pages, table, n, out)
+    with pytest.raises(lq.LqError, match="out.*gradient"):
+        c.lq_cache_attend(0, q, pages, table, n, out.clone().requires_grad_())
+    with pytest.raises(lq.LqError, match="lse.*gradient"):
+        c.lq_cache_attend(0, q, pages, table, n, out, lse=lse.clone().requires_grad_())
+    with pytest.raises(lq.LqError, match="keys.*gradient"):
+        c.lq_cache_read(0, pages, slots, kept, k.clone())
+    with pytest.raises(lq.LqError, match="values.*gradient"):
+        c.lq_cache_read(0, pages, slots, k.clone(), kept)
+    other = torch.empty_like(out)
+    with torch.no_grad():
+        c.lq_cache_attend(0, want, pages, table, n, other)
+    assert torch.equal(other, out)
+    c.lq_cache_attend(0, want.detach(), pages, table, n, other)
+    assert torch.equal(other, out) and c.lq_cache_status() == 0
