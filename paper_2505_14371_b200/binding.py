@@ -384,6 +384,13 @@ class Cache:
     _KINDS = {"keys": 0, "values": 1}
     _LAYOUTS = {"half": False, "interleaved": True}
 
+    @staticmethod
+    def _one_of(what: str, names: dict, name):
+        try:
+            return names[name]
+        except (KeyError, TypeError):
+            raise LqError(f"{what} {name!r} is not one of {', '.join(names)}") from None
+
     def __init__(self, num_layers: int, kv_heads: int, head_dim: int, page_size: int = 64, bits=(3, 3), q: int = 0, seed: int = 0):
         L = load_library()
         self.bits = (int(bits), int(bits)) if isinstance(bits, int) else (int(bits[0]), int(bits[1]))
@@ -416,12 +423,13 @@ class Cache:
     def lq_cache_set_levels(self, layer: int, kind: str, levels) -> None:
         """Level set of the layer's "keys" or "values", rounded to numbers of 11 bits."""
         arr = (C.c_float * len(levels))(*[float(x) for x in levels])
-        _check(load_library().lq_cache_set_levels(self._h, layer, self._KINDS[kind], arr, len(levels)))
+        _check(load_library().lq_cache_set_levels(self._h, layer, self._one_of("kind", self._KINDS, kind), arr, len(levels)))
 
     def lq_cache_get_levels(self, layer: int, kind: str) -> List[float]:
-        n = 1 << self.bits[self._KINDS[kind]]
+        at = self._one_of("kind", self._KINDS, kind)
+        n = 1 << self.bits[at]
         arr = (C.c_float * n)()
-        _check(load_library().lq_cache_get_levels(self._h, layer, self._KINDS[kind], arr, n))
+        _check(load_library().lq_cache_get_levels(self._h, layer, at, arr, n))
         return list(arr)
 
     def lq_cache_status(self) -> int:
@@ -438,7 +446,7 @@ class Cache:
         if step is not None and step < 0:
             raise LqError(f"step {step} is negative")
         _native.lq_cache_write(self._addr, layer, keys, values, slots, pages, -1 if step is None else step, rotary, positions,
-                               self._LAYOUTS[layout])
+                               self._one_of("layout", self._LAYOUTS, layout))
 
     def lq_cache_read(self, layer: int, pages, slots, keys, values) -> None:
         """The rows of slots [tokens] into keys and values [tokens][kv_heads][head_dim]; zeros for a negative slot."""
@@ -450,4 +458,4 @@ class Cache:
         and lengths [batch] int32, lse [batch][heads] fp32.  scale: 1 / sqrt(head_dim) unless given; window: how many of the last
         tokens are seen (0: all); rotary: the queries are turned first, at positions [batch] or each sequence's last one."""
         _native.lq_cache_attend(self._addr, layer, queries, pages, table, lengths, out, lse,
-                                self.head_dim ** -0.5 if scale is None else scale, window, rotary, positions, self._LAYOUTS[layout])
+                                self.head_dim ** -0.5 if scale is None else scale, window, rotary, positions, self._one_of("layout", self._LAYOUTS, layout))
