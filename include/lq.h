@@ -419,7 +419,8 @@ const char* lq_last_error(void);
 
 typedef struct lq_cache lq_cache;
 
-/* Rows [tokens][heads][head_dim] in device memory; strides in elements; the coordinates of a row side by side. */
+/* Rows [tokens][heads][head_dim] in device memory; strides in elements, below 2^31 bytes each (LQ_EINVAL otherwise); the coordinates
+ * of a row side by side.  Inputs may have strides of 0; rows of an output must not share memory (a stride of 0 is refused). */
 typedef struct {
     void* data;
     int64_t token_stride, head_stride;
