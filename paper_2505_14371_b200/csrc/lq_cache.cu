@@ -408,7 +408,8 @@ int lq_cache_attend(lq_cache* cache, int32_t layer, const lq_rows* queries, int6
     if (table_width < 0 || table_width > INT32_MAX) return lq_set_error(LQ_EINVAL, "table_width = %lld out of range", (long long)table_width);
     if (batch > 0 && (!lengths || (table_width > 0 && !table))) return lq_set_error(LQ_EINVAL, "table or lengths is NULL");
     if (!aligned(table, 4) || !aligned(lengths, 4) || !aligned(lse, 4)) return lq_set_error(LQ_EINVAL, "table, lengths and lse must be 4-byte aligned");
-    if (!std::isfinite(scale)) return lq_set_error(LQ_EINVAL, "scale is not a finite number");
+    a.scale = scale * 1.44269504088896341f;
+    if (!std::isfinite(a.scale)) return lq_set_error(LQ_EINVAL, "scale is not a finite number (or above 2^127, where its base-2 form is none)");
     if (window < 0) return lq_set_error(LQ_EINVAL, "window = %lld is negative", (long long)window);
     LQ_TRY(take_rotary(rotary, s, false, &a.rotary));
     const int64_t needed = workspace_of(cache, table_width, window);
@@ -423,7 +424,6 @@ int lq_cache_attend(lq_cache* cache, int32_t layer, const lq_rows* queries, int6
     a.shape = s; a.tables = cache->tables + (size_t)layer * 2;
     a.pages = pages; a.table = table; a.lengths = lengths; a.lse = lse; a.partial = needed > 0 ? static_cast<float*>(workspace) : nullptr; a.flags = cache->flags;
     a.num_pages = num_pages; a.table_width = table_width; a.window = window;
-    a.scale = scale * 1.44269504088896341f;
     a.batch = (int32_t)batch;
     a.sms = cache->sms;
     LQ_ON_DEVICE(cache);

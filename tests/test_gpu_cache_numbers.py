@@ -154,3 +154,21 @@ def test_fp16_outputs_are_off_by_their_own_rounding_alone(group, dim, bits, rot)
     before = 73 * 2.0 ** -24 * np.linalg.norm(np.einsum("bhgt,hbtd->bhgd", p, np.abs(values)))
     assert before < 0.06 * own
     assert np.linalg.norm(out.double().cpu().numpy() - want) <= own + 2 * before
+
+
+def test_scales_at_the_end_of_fp32():
+    """2^126 is a scale; above 2^127 the factor of base 2 would be infinite, and a score of 0 no number."""
+    import paper_2505_14371_b200 as lq
+    k = torch.zeros((20, 1, 64), device="cuda")
+    k[..., 1:] = 1.0
+    v = torch.rand((20, 1, 64), generator=torch.Generator("cuda").manual_seed(3), device="cuda") + 0.1
+    c, pages, table = in_order(1, 64, k, v)
+    q = torch.zeros((1, 3, 64), device="cuda")
+    q[..., 0] = 1.0
+    want = kept(c, pages, 20)[1][0].mean(0)
+    for scale in (2.0 ** 126, -(2.0 ** 126)):
+        out, _ = attended(c, pages, table, q, 20, scale=scale)
+        assert np.all(np.abs(out[0].double().cpu().numpy() - want) <= 2.0 ** -18 * want)
+    for scale in (3e38, -3e38, float("inf"), 1e300):
+        with pytest.raises(lq.LqError, match="scale"):
+            attended(c, pages, table, q, 20, scale=scale)
