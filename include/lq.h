@@ -448,7 +448,8 @@ int64_t lq_cache_page_words(const lq_cache* cache);
 int lq_cache_info(const lq_cache* cache, int32_t* kv_heads, int32_t* head_dim, int32_t* page_size, int32_t* device);
 
 /* Level set of (layer, kind), kind = LQ_KEYS or LQ_VALUES: n = 2^bits values from 0 to 1, strictly increasing also after
- * rounding to fp16 (else LQ_EINVAL); a set of lq_fit_levels can be taken as it is where that holds.  Rows written before
+ * rounding to fp16 (else LQ_EINVAL); a set of lq_fit_levels can be taken as it is where that holds.  (In bucket scope its samples are
+ * normalised by buckets of 128 coordinates: the cache's own norms where head_dim is 128, others where it is not.)  Rows written before
  * a set are read with the new levels.  set synchronises the device; get returns the rounded set. */
 int lq_cache_set_levels(lq_cache* cache, int32_t layer, int32_t kind, const float* host_levels, int32_t n);
 int lq_cache_get_levels(const lq_cache* cache, int32_t layer, int32_t kind, float* host_levels, int32_t n);
@@ -471,7 +472,8 @@ int lq_cache_read(lq_cache* cache, int32_t layer, const uint32_t* pages, int64_t
  * heads h * heads/kv_heads and on belong to head h of the cache)
  *   s_j = scale * q . k_j,  out = sum_j softmax(s)_j v_j,  lse = log sum_j exp(s_j)
  * over the tokens max(0, length - window) <= j < length (window 0: all).  Token j sits in page table[b][j / page_size] at
- * place j % page_size.  A sequence with nothing to see gives zeros and lse = -infinity.  Sums and softmax are in fp32.
+ * place j % page_size.  A sequence with nothing to see gives zeros and lse = -infinity.  Sums and softmax are in fp32;
+ * rotated and fp32 queries are taken with 22 bits, and so are the weights of the values for fp16 and fp32 outputs, for bf16 ones with 11.
  *   queries, out [batch][heads][head_dim] of one type; table dev [batch][table_width]; lengths dev [batch]; lse dev
  *   [batch][heads] or NULL; rotary: NULL, or the queries are rotated first, without rounding them to their type.
  *   workspace: dev, 16-byte aligned, of the bytes that lq_cache_workspace() says for this table_width and window (0: NULL will do);

@@ -6,11 +6,10 @@
 // with p_j = exp2(s_j - ref).  Weights have a scale 2^k beside the running reference of the scores, so that no spread of the values'
 // norms costs a weight its bits; k is a whole number and s_j - ref is formed first, so that neither large scores nor large logarithms
 // round the sum.  Reference and scale move only when an exponent passes kSlack, which the threads of a warp vote on, and sums are
-// rescaled then.  Scores, p, w and all sums are fp32.  Roundings to
-// fewer bits: q as fp16 after a power of two per query (exact for fp16 and bf16 queries; rotated and fp32 ones are taken as
-// a sum of two fp16 numbers, 22 bits), and w as fp16, 11 bits, for the second product of bf16
-// outputs (at most an eighth of the output's own rounding, and independent from token to token), as a sum of two, 22 bits, for fp16
-// and fp32 ones.
+// rescaled then.  Scores, p, w and all sums are fp32.  Roundings to fewer bits: q as fp16 after a power of two per query (exact for
+// fp16 and bf16 queries; rotated and fp32 ones are taken as a sum of two fp16 numbers, 22 bits), and w, for the second product of bf16
+// outputs as fp16, 11 bits (at most an eighth of the output's own rounding, and independent from token to token), of fp16 and fp32
+// ones as a sum of two, 22 bits (of a weight down to 2^-9 of the scale; below, 2^-31 of the scale).
 //
 // Work.  A warp takes 16 tokens of one head at a time: the keys are the A operand (16 tokens x 16 coordinates) of
 // mma.m16n8k16, 8 queries the B operand; the scores' fragment, transposed by two movmatrix, is the B operand of the second
@@ -33,17 +32,17 @@
 // Split.  Units of 128 tokens (8 warps x 16; 256 where a warp takes two tiles at a time) of all (sequence, head, 8 queries) in a
 // row are dealt out evenly to teams of 8 warps, as many as the GPU holds at once (two a CTA, which share the look-up table;
 // one for rows of 256); every team finds its share from the lengths, on the device.  The start of a segment (sequence, head,
-// 8 queries) counts as two units more: 64 sequences of 250 to 16384 tokens 140 -> 102 us.  A team that has all of a segment writes its
+// 8 queries) counts as two units more: 64 sequences of 250 to 16384 tokens 110 -> 89 us.  A team that has all of a segment writes its
 // output; the others leave partial sums in the workspace, at most two a team, and the team where a segment begins leaves a
 // record of it, from which a second kernel joins them in the order of the teams, so that the same call gives the same bits.
 //
 // Loads.  Both kernels start beside their predecessor, which may be what writes the lengths, pages, queries or partial sums: what is
 // read behind pdl_wait is read by ordinary loads, by cp.async, or by intrinsics on a pointer from fresh().
 //
-// What bounds it: the instructions that load from shared memory (98 a tile of 16 tokens and 128 coordinates at one a cycle and SM,
-// where DRAM would need 93 cycles), of which 60 % of the cycles are used, as the 16 warps of an SM wait for one another's
-// results; 32 sequences of 8192 tokens, 8 heads of 128 in 4 bits: 80 us, where the copy bandwidth would take 43.6.  Short
-// sequences: a segment's chain of page, copy, products, sum and output, some 4 us.
+// What bounds it: shared memory, which a tile of 16 tokens and 128 coordinates of 4 bits keeps busy for 108 cycles (88 of loads, 64 of
+// them look-ups, and 20 of copies and sums written), where DRAM would need 93; 63 % of its cycles are used, and 62 % of the issue slots, as
+// the 16 warps of an SM wait for their own results.  64 sequences of 250 to 16384 tokens, 8 heads of 128 in 4 bits: 89 us, where the copy
+// bandwidth would take 45.6.  Short sequences: a segment's chain of page, copy, products, sum and output, some 4 us.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -344,7 +343,7 @@ __device__ __forceinline__ void take_values(Tile<P, WK, WV>& t, const char* even
 // weight one of 11 bits.  kTwo: a query is a sum of two, with a second product for the rest; kWeights: a weight is; kTwoBoth,
 // kTwoBothHalf: both are.  With up to 4 queries a head the rests take columns 4 to 7 of the same product (kBeside: of queries,
 // kBesideBoth, kBesideHalf: of queries and weights), which costs neither registers nor products: 32 sequences of 8192 tokens, rows of
-// 128, rotated bf16 queries 92 -> 82 us, fp32 100 -> 82.  (Both: rows of 32 bits, half: of 16.)
+// 128 in 4 bits, 4 queries a head: rotated bf16 87 -> 77 us, fp16 82 -> 77, fp32 93 -> 81.  (Both: rows of 32 bits, half: of 16.)
 // One number is a weight of bf16 outputs: its rounding adds 1 % to the error of the output's own, and two cost 1 to 10 % of the time
 // (rows of 128 in 4 bits, 8 queries a head: 75.9 us, 83.8 with two).  With fp16 outputs it would add 39 %.
 constexpr int kPlain = 0, kTwo = 1, kTwoBoth = 2, kBeside = 3, kBesideBoth = 4, kBesideHalf = 5, kWeights = 6, kTwoBothHalf = 7;

@@ -3,11 +3,11 @@
 // A lane takes 8 coordinates of a row (token, head, keys or values) at a time: 16 bytes of fp16 or bf16 in one load or store, one
 // 32-bit word of 4-bit symbols (or two of 8-bit ones), two Philox blocks.  The writing kernel gives a lane two such parts of rows of 128
 // and 256 (lane i those from 8 i and from padded / 2 + 8 i): with one, what a row costs besides its coordinates was a third of the
-// instructions (16384 tokens of 8 heads of 128 54 us, 44 with two); rows of 64 have one (9600 tokens of 10 heads of 41, unbiased: 36 us, 39 with two).
+// instructions (16384 tokens of 8 heads of 128 65 us, 42 with two); rows of 64 have one (9600 tokens of 10 heads of 41, unbiased: 36 us, 38 with two).
 // A row's norm is an all-reduce over its lanes, its symbols are found by one look-up each (CacheSearch).
 //
-// What bounds them.  Writing: instructions, some 33 a coordinate (rotation 15 of a key's, look-up and packing 14, norm 4), at 70 %
-// of the issue slots; 76 MB read and 9 MB written in 44 us.  Reading: its writes, 3.7 TB/s beside 1 TB/s of reads (100 003 tokens in
+// What bounds them.  Writing: instructions, some 32 a coordinate (rotation 15 of a key's, look-up and packing 14, norm 4), at 70 %
+// of the issue slots; 76 MB read and 18 MB written in 42 us.  Reading: its writes, 3.7 TB/s beside 1 TB/s of reads (100 003 tokens in
 // 112 us; a plain fill writes 3.9 TB/s).  Few tokens: latency of slot -> row -> norm -> store, and the host.
 //
 // Both kernels start beside their predecessor, which may be what writes their slots, rows, positions or pages (a row is read back right
