@@ -9,7 +9,7 @@
 // rescaled then.  Scores, p, w and all sums are fp32.  Roundings to fewer bits: q as fp16 after a power of two per query (exact for
 // fp16 and bf16 queries; rotated and fp32 ones are taken as a sum of two fp16 numbers, 22 bits), and w, for the second product of bf16
 // outputs as fp16, 11 bits (at most an eighth of the output's own rounding, and independent from token to token), of fp16 and fp32
-// ones as a sum of two, 22 bits (of a weight down to 2^-9 of the scale; below, 2^-31 of the scale).
+// ones as a sum of two, 22 bits (of a weight down to 2^-9 of the largest; below, to 2^-31 of the largest).
 //
 // Work.  A warp takes 16 tokens of one head at a time: the keys are the A operand (16 tokens x 16 coordinates) of
 // mma.m16n8k16, 8 queries the B operand; the scores' fragment, transposed by two movmatrix, is the B operand of the second
@@ -68,7 +68,7 @@ constexpr int kTableAt = 1 << 16, kSystemBytes = 1 << 10, kEnd = (227 << 10);
 constexpr int kStart = 2;               // what a segment costs beside its units, in units
 constexpr float kLow = -3.402823466e38f;    // the reference of a warp or team without a score: below every finite score's
 constexpr float kSlack = 8.0f;          // how far (log2) a score may pass its reference
-constexpr float kLift = 6.0f;           // weights are 2^kLift at their scale: at most 2^14 as fp16 (2^15 times a significand), and exact down to 2^-20
+constexpr float kLift = 6.0f;           // weights are 2^kLift at their scale: at most 2^14 as fp16 (2^15 times a significand), with all bits down to 2^-20 of it
 template <bool kFloat>
 constexpr float kLiftOf = kFloat ? 0.0f : kLift;    // ... of it in the exponent (otherwise in the significand)
 
@@ -138,9 +138,9 @@ __device__ __forceinline__ void norm_parts(float norm, float& x, float& m)
     }
 }
 
-// A scale as a whole number, so that its differences from exponents are exact.  (The bound takes the place of -infinity; what is
-// that far below the largest p adds nothing to an fp32 output.)
-__device__ __forceinline__ float whole_scale(float v) { return ceilf(fmaxf(v, -1000.0f)); }
+// A scale as a whole number, so that its differences from exponents are exact; rounded down, so that the largest weight is 2^kLift or more.
+// (The bound takes the place of -infinity; what is that far below the largest p adds nothing to an fp32 output.)
+__device__ __forceinline__ float whole_scale(float v) { return floorf(fmaxf(v, -1000.0f)); }
 
 // What the sum of weighted values is multiplied by in the end: 2^scale / total, the power in two factors that are normal numbers.
 template <bool kFloat>

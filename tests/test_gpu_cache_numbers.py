@@ -172,3 +172,30 @@ def test_scales_at_the_end_of_fp32():
     for scale in (3e38, -3e38, float("inf"), 1e300):
         with pytest.raises(lq.LqError, match="scale"):
             attended(c, pages, table, q, 20, scale=scale)
+
+
+@pytest.mark.parametrize("group,dim", [(4, 64), (8, 128), (2, 256)])
+def test_small_weights_keep_their_bits_down_to_the_bound(group, dim):
+    """Two tokens whose values share no coordinate, fp16: what the second adds is off by 2^-31 of the first's weight beside the output's own
+    rounding, wherever the first's norm lies between two powers of two."""
+    batch = 64
+    k, v = torch.zeros((16 * batch, 1, dim), device="cuda"), torch.zeros((16 * batch, 1, dim), device="cuda")
+    norm = 2.0 ** torch.linspace(14.0, 15.5, batch, device="cuda")
+    k[::16, 0, 0] = 1.0
+    v[::16, 0, 0] = norm
+    v[1::16, 0, 1] = norm
+    c, pages, _ = in_order(1, dim, k, v)
+    table = torch.arange(batch, dtype=torch.int32, device="cuda").view(batch, 1)
+    q = torch.zeros((batch, group, dim), device="cuda")
+    q[..., 0] = torch.linspace(8, 20, batch * group, device="cuda")[torch.randperm(batch * group, generator=torch.Generator("cuda").manual_seed(5), device="cuda")].view(batch, group)
+    q = q.half()
+    out = torch.empty_like(q)
+    c.lq_cache_attend(0, q, pages, table, torch.full((batch,), 2, dtype=torch.int32, device="cuda"), out, scale=1.0)
+    p = np.exp(-q[..., 0].double().cpu().numpy())
+    values = kept(c, pages, 16 * batch)[1][0].reshape(batch, 16, dim)
+    big, small = values[:, 0, 0][:, None], values[:, 1, 1][:, None]
+    got = out.double().cpu().numpy()
+    # a weight's exponent: a score below 20 as one product (2^-20), exp2 and log2 below 16 in size (2^-18)
+    for at, want in ((0, big / (1 + p)), (1, small * p / (1 + p))):
+        assert np.all(np.abs(got[..., at] - want) <= want * (2.0 ** -11 + 2.0 ** -17) + 2.0 ** -31 * big + 2.0 ** -25)
+    assert not got[..., 2:].any()
