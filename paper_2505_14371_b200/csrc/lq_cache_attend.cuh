@@ -67,12 +67,12 @@ constexpr int kTableBytes = 256 * 256;  // entry e: 32 copies for the keys, 32 f
 constexpr int kTableAt = 1 << 16, kSystemBytes = 1 << 10, kEnd = (227 << 10);
 constexpr int kStart = 2;               // what a segment costs beside its units, in units
 constexpr float kLow = -3.402823466e38f;    // the reference of a warp or team without a score: below every finite score's
-constexpr float kSlack = 8.0f;          // how far (log2) a score may pass its reference
+constexpr float kSlack = 8.0f;          // how far (log2) a score may pass its reference, a weight its scale
 constexpr float kLift = 6.0f;           // weights are 2^kLift at their scale: at most 2^14 as fp16 (2^15 times a significand), with all bits down to 2^-20 of it
 template <bool kFloat>
 constexpr float kLiftOf = kFloat ? 0.0f : kLift;    // ... of it in the exponent (otherwise in the significand)
 
-// Workspace: a record for every team, then two partials of kCacheRecordBytes a team (sums; reference, reference of the weights,
+// Workspace: a record for every team, then two partials of kCacheRecordBytes a team (sums; reference, scale of the weights,
 // denominator, unused).
 struct Record { int32_t sequence, head_block, last, pad; };
 static_assert(sizeof(Record) == kCacheRecordBytes && kQueries == 8, "the workspace is sized by lq_cache.cuh");
@@ -84,7 +84,7 @@ struct TeamShared {
     int64_t words[18];                  // schedule
     float factor[kQueries];             // scale * log2(e) / the query's power of two
     float stats[kTeamWarps][kQueries][3];
-    float share[kQueries][kTeamWarps + 4];      // factor of each warp's sums; then ref, ref_w, total
+    float share[kQueries][kTeamWarps + 4];      // factor of each warp's sums; then that of the whole segment's
     alignas(16) __half q[2][kQueries][P + 8];   // the queries, and what their rounding left
 };
 template <int P>
@@ -928,7 +928,7 @@ __global__ void __launch_bounds__(32 * kQueries* kJoinWarps) attend_join_kernel(
 {
     constexpr int kVectors = P / 128 > 0 ? P / 128 : 1;                 // of 4 coordinates a lane
     __shared__ float4 sums[kJoinWarps][kQueries][kVectors][32];
-    __shared__ float4 stats[kJoinWarps][kQueries];      // reference, reference of the weights, denominator
+    __shared__ float4 stats[kJoinWarps][kQueries];      // reference, scale of the weights, denominator
     pdl_wait();
     pdl_launch_next();
     const float* const workspace = fresh(a.partial);
