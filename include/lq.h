@@ -416,6 +416,7 @@ const char* lq_last_error(void);
 #define LQ_CACHE_BAD_POSITION  4u  /* a position outside the rotary table: token not written; NaN from attention */
 #define LQ_CACHE_BAD_PAGE      8u  /* a page number outside [0, num_pages) inside a sequence: its tokens are left out */
 #define LQ_CACHE_BAD_LENGTH   16u  /* a negative length (taken as 0), or one past its table (taken as the table's tokens) */
+#define LQ_CACHE_GAVE_UP      32u  /* lq_cache_attend_shared waited in vain on the GPU: its outputs are not valid */
 
 typedef struct lq_cache lq_cache;
 
@@ -483,6 +484,52 @@ int lq_cache_attend(lq_cache* cache, int32_t layer, const lq_rows* queries, int6
                     const uint32_t* pages, int64_t num_pages, const int32_t* table, int64_t table_width,
                     const int32_t* lengths, float scale, int64_t window, const lq_rotary* rotary, const lq_rows* out,
                     float* lse, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* The same for sequences that share a prefix: each sees the tokens j < *prefix_length of the pages prefix[prefix_width] (dev), then the first
+ * lengths[b] of its own pages table[b].  The prefix is read once for all of them.  prefix_length: dev [1].  Without rotary->at a query stands
+ * at its sequence's last position, *prefix_length + lengths[b] - 1.  Either part may be empty; no window.  Roundings as above; the prefix's sums of up to
+ * 1024 tokens (fp32 outputs; else of a split) are those of the matrix unit.  batch * heads up to 2^26.  Between calls nothing is kept: the
+ * workspace holds what a call's kernels hand on.  (`type`: that of queries and out.) */
+int64_t lq_cache_shared_workspace(const lq_cache* cache, int64_t batch, int32_t heads, int64_t prefix_width, int64_t table_width, int32_t type);
+int lq_cache_attend_shared(lq_cache* cache, int32_t layer, const lq_rows* queries, int64_t batch, int32_t heads,
+                           const uint32_t* pages, int64_t num_pages, const int32_t* prefix, int64_t prefix_width,
+                           const int32_t* prefix_length, const int32_t* table, int64_t table_width, const int32_t* lengths, float scale,
+                           const lq_rotary* rotary, const lq_rows* out, float* lse, void* workspace, int64_t workspace_bytes,
+                           void* stream);
+
+/* Bounds of the keys of whole pages: upper_d and lower_d, whole numbers of 8 bits, and a scale.  With N the largest norm of a page's keys
+ * (of one head), v the values that lq_cache_read would give in fp32 and inv = fl(127 fl(1 / N)),
+ *   upper_d = ceil(fl(max v_d * inv)), lower_d = floor(fl(min v_d * inv)), both within [-127, 127], scale = fl(N fl(1 / 127));
+ * zeros and scale 0 where N is below 2^-100 or a norm is not finite.  All page_size tokens count, written or not.
+ * A page's bounds are lq_cache_bounds_words() 32-bit words: for each head `padded` bytes of upper and `padded` bytes of lower bounds, then
+ * the heads' scales (fp32), to a multiple of 16 bytes.  bounds [num_pages][words] (dev, 16-byte aligned); which: dev [count] page numbers,
+ * those below 0 are skipped; bounds of other pages stay. */
+int64_t lq_cache_bounds_words(const lq_cache* cache);
+int lq_cache_bounds(lq_cache* cache, int32_t layer, const uint32_t* pages, int64_t num_pages, const int32_t* which, int64_t count,
+                    uint32_t* bounds, void* stream);
+
+/* Which pages each sequence's queries look at.  A query (rotated first, if rotary is given) becomes whole numbers i_d = rint(fl(q_d * fl(127 fl(1 / Q))))
+ * with the scale fl(Q fl(1 / 127)), Q its largest coordinate (below 2^-100 or not finite: zeros); a page's score is
+ *   fl(fl(sum_d max(i_d upper_d, i_d lower_d) * query's scale) * page's scale),
+ * the largest over the queries of a head of the cache.  Of a sequence's pages, as many as its length fills or begins, the first `first` and the last
+ * `last` are kept always, of the others those with the highest scores, of equal scores the ones that come first: `keep` in all, or all
+ * where there are no more.  chosen: dev [batch][kv_heads][keep], page numbers in the sequence's order, -1 behind the last; seen: dev
+ * [batch][kv_heads], the tokens that they hold (only the sequence's last page may be filled in part).  first >= 0, last >= 1 (the bounds of a
+ * page that is still being filled are not looked at), first + last <= keep.  A page number outside [0, num_pages) scores below every other.
+ * batch * kv_heads up to 2^24.  workspace as above; 0 bytes where table_width is 12288 or less. */
+int64_t lq_cache_choose_workspace(const lq_cache* cache, int64_t batch, int64_t table_width);
+int lq_cache_choose(lq_cache* cache, const lq_rows* queries, int64_t batch, int32_t heads, const uint32_t* bounds, int64_t num_pages,
+                    const int32_t* table, int64_t table_width, const int32_t* lengths, int32_t first, int32_t last,
+                    const lq_rotary* rotary, int32_t* chosen, int32_t keep, int32_t* seen, void* workspace, int64_t workspace_bytes,
+                    void* stream);
+
+/* lq_cache_attend with a table and a length for every (sequence, head of the cache): chosen dev [batch][kv_heads][keep], seen dev
+ * [batch][kv_heads], as lq_cache_choose leaves them or made otherwise.  rotary: NULL, or with positions (at), which the lengths here do not tell.
+ * workspace: lq_cache_workspace(cache, keep, 0) bytes.  batch * kv_heads up to 2^24. */
+int lq_cache_attend_chosen(lq_cache* cache, int32_t layer, const lq_rows* queries, int64_t batch, int32_t heads,
+                           const uint32_t* pages, int64_t num_pages, const int32_t* chosen, int64_t keep, const int32_t* seen,
+                           float scale, const lq_rotary* rotary, const lq_rows* out, float* lse, void* workspace,
+                           int64_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -27,6 +27,7 @@ CACHE_BAD_SLOT = 2              # a slot past the last page
 CACHE_BAD_POSITION = 4          # a position outside the rotary table
 CACHE_BAD_PAGE = 8              # a page number outside the pages
 CACHE_BAD_LENGTH = 16           # a length below 0 or past its table
+CACHE_GAVE_UP = 32              # lq_cache_attend_shared waited in vain on the GPU
 CODE_BROKEN = 1                 # a decode met an invalid stream
 CODE_GAVE_UP = 2                # an encode waited in vain
 STEP_AUTO = 0xFFFFFFFF          # lq_quantize_pack: take the step index from the plan's device-side iteration counter
@@ -40,6 +41,8 @@ EXPORTS = ["lq_plan_create", "lq_plan_destroy", "lq_plan_padded_elems", "lq_plan
            "lq_profile_read",
            "lq_cache_create", "lq_cache_destroy", "lq_cache_page_words", "lq_cache_info", "lq_cache_set_levels", "lq_cache_get_levels",
            "lq_cache_status", "lq_cache_write", "lq_cache_read", "lq_cache_workspace", "lq_cache_attend",
+           "lq_cache_shared_workspace", "lq_cache_attend_shared", "lq_cache_bounds_words", "lq_cache_bounds", "lq_cache_choose_workspace",
+           "lq_cache_choose", "lq_cache_attend_chosen",
            "lq_error_string", "lq_last_error"]
 KERNEL_NAMES = ["norm_partial", "norm_finalize", "quantize_pack", "stat_finalize", "qoda_scalars",
                 "decode", "fit", "alt_finalize", "average", "block_live"]
@@ -127,6 +130,13 @@ def load_library() -> C.CDLL:
     L.lq_cache_write.argtypes = [vp, i32, rows, rows, i64, vp, vp, i64, i64, rotary, vp]
     L.lq_cache_read.argtypes = [vp, i32, vp, i64, i64, vp, rows, rows, vp]
     L.lq_cache_attend.argtypes = [vp, i32, rows, i64, i32, vp, i64, vp, i64, vp, C.c_float, i64, rotary, rows, vp, vp, i64, vp]
+    L.lq_cache_shared_workspace.argtypes = [vp, i64, i32, i64, i64, i32]; L.lq_cache_shared_workspace.restype = i64
+    L.lq_cache_attend_shared.argtypes = [vp, i32, rows, i64, i32, vp, i64, vp, i64, vp, vp, i64, vp, C.c_float, rotary, rows, vp, vp, i64, vp]
+    L.lq_cache_bounds_words.argtypes = [vp]; L.lq_cache_bounds_words.restype = i64
+    L.lq_cache_bounds.argtypes = [vp, i32, vp, i64, vp, i64, vp, vp]
+    L.lq_cache_choose_workspace.argtypes = [vp, i64, i64]; L.lq_cache_choose_workspace.restype = i64
+    L.lq_cache_choose.argtypes = [vp, rows, i64, i32, vp, i64, vp, i64, vp, i32, i32, rotary, vp, i32, vp, vp, i64, vp]
+    L.lq_cache_attend_chosen.argtypes = [vp, i32, rows, i64, i32, vp, i64, vp, i64, vp, C.c_float, rotary, rows, vp, vp, i64, vp]
     L.lq_error_string.argtypes = [C.c_int]; L.lq_error_string.restype = C.c_char_p
     L.lq_last_error.argtypes = []; L.lq_last_error.restype = C.c_char_p
     for name in EXPORTS:
@@ -400,7 +410,7 @@ class Cache:
         _check(L.lq_cache_create(C.byref(h), self.num_layers, self.kv_heads, self.head_dim, self.page_size, *self.bits, self.q,
                                  C.c_uint64(self.seed)))
         self._h, self._addr = h, h.value
-        self.page_words = int(L.lq_cache_page_words(h))
+        self.page_words, self.bounds_words = int(L.lq_cache_page_words(h)), int(L.lq_cache_bounds_words(h))
         device = C.c_int32()
         _check(L.lq_cache_info(h, None, None, None, C.byref(device)))
         self.device = torch.device("cuda", device.value)
@@ -419,6 +429,10 @@ class Cache:
     def empty_pages(self, num_pages: int) -> torch.Tensor:
         """[num_pages][page_words] pages of one layer; a slot that was not written yet holds zeros."""
         return torch.zeros((num_pages, self.page_words), dtype=torch.int32, device=self.device)
+
+    def empty_bounds(self, num_pages: int) -> torch.Tensor:
+        """[num_pages][bounds_words] bounds of the keys of one layer's pages; zeros for a page whose bounds were not asked for yet."""
+        return torch.zeros((num_pages, self.bounds_words), dtype=torch.int32, device=self.device)
 
     def lq_cache_set_levels(self, layer: int, kind: str, levels) -> None:
         """Level set of the layer's "keys" or "values", rounded to numbers of 11 bits."""
@@ -459,3 +473,31 @@ class Cache:
         tokens are seen (0: all); rotary: the queries are turned first, at positions [batch] or each sequence's last one."""
         _native.lq_cache_attend(self._addr, layer, queries, pages, table, lengths, out, lse,
                                 self.head_dim ** -0.5 if scale is None else scale, window, rotary, positions, self._one_of("layout", self._LAYOUTS, layout))
+
+    def lq_cache_attend_shared(self, layer: int, queries, pages, prefix, prefix_length, table, lengths, out, lse=None,
+                               scale: Optional[float] = None, rotary=None, positions=None, layout: str = "half") -> None:
+        """lq_cache_attend for sequences that share a prefix, which is read once for all of them: each sees the prefix_length (int32, one
+        number on the device) tokens of pages prefix [pages of the prefix], then its own.  Without positions a query is turned at its
+        sequence's last one, prefix_length + length - 1."""
+        _native.lq_cache_attend_shared(self._addr, layer, queries, pages, prefix, prefix_length, table, lengths, out, lse,
+                                       self.head_dim ** -0.5 if scale is None else scale, rotary, positions, self._one_of("layout", self._LAYOUTS, layout))
+
+    def lq_cache_bounds(self, layer: int, pages, which, bounds) -> None:
+        """Bounds of the keys of pages which [count] (int32; negative: skipped), all of whose tokens have been written, into their rows of
+        bounds (empty_bounds of as many pages)."""
+        _native.lq_cache_bounds(self._addr, layer, pages, which, bounds)
+
+    def lq_cache_choose(self, queries, bounds, table, lengths, chosen, seen, first: int = 1, last: int = 1, rotary=None, positions=None,
+                        layout: str = "half") -> None:
+        """The pages that each sequence's queries look at, for every head of the cache: chosen [batch][kv_heads][keep] int32 (-1 behind the last
+        one) and how many tokens they hold, seen [batch][kv_heads] int32.  Kept are the first and last pages of a sequence and those
+        whose bounds give the highest scores; the queries are turned first if rotary is given, as in lq_cache_attend."""
+        _native.lq_cache_choose(self._addr, queries, bounds, table, lengths, chosen, seen, first, last, rotary, positions,
+                                self._one_of("layout", self._LAYOUTS, layout))
+
+    def lq_cache_attend_chosen(self, layer: int, queries, pages, chosen, seen, out, lse=None, scale: Optional[float] = None, rotary=None,
+                               positions=None, layout: str = "half") -> None:
+        """lq_cache_attend with a table and a length of its own for every head of the cache, as lq_cache_choose leaves them.  rotary needs
+        positions [batch], which are the sequences' (their lengths less 1), not those of what is seen."""
+        _native.lq_cache_attend_chosen(self._addr, layer, queries, pages, chosen, seen, out, lse,
+                                       self.head_dim ** -0.5 if scale is None else scale, rotary, positions, self._one_of("layout", self._LAYOUTS, layout))

@@ -206,6 +206,100 @@ int64_t workspace_of(const lq_cache* c, int64_t table_width, int64_t window)
 
 #define LQ_TRY(expr) do { const int c_ = (expr); if (c_ != LQ_OK) return c_; } while (0)
 
+int check_batch(const lq_cache* c, int64_t batch, int heads)
+{
+    if (batch < 0 || batch > 1 << 24) return lq_set_error(LQ_EINVAL, "batch = %lld out of [0, 2^24]", (long long)batch);
+    if (heads < c->shape.heads || heads % c->shape.heads || heads > 1 << 16)
+        return lq_set_error(LQ_EINVAL, "query heads (%d) have to be a multiple of the cache's %d, at most 65536", heads, c->shape.heads);
+    return LQ_OK;
+}
+
+// Where every (sequence, head of the cache) has a table of its own.
+int check_heads(const lq_cache* c, int64_t batch)
+{
+    if (batch < 0 || batch * c->shape.heads > 1 << 24)
+        return lq_set_error(LQ_EINVAL, "batch = %lld: batch * kv_heads has to be in [0, 2^24]", (long long)batch);
+    return LQ_OK;
+}
+
+int check_bounds(const void* bounds, int64_t num_pages)
+{
+    if (num_pages > 0 && !bounds) return lq_set_error(LQ_EINVAL, "bounds is NULL");
+    if (!aligned(bounds, 16)) return lq_set_error(LQ_EINVAL, "bounds must be 16-byte aligned");
+    return LQ_OK;
+}
+
+// What the calls of attention have in common: queries, outputs, pages, and a table with its lengths, which a call has names for.
+int take_attend(const lq_cache* c, int32_t layer, const lq_rows* queries, int64_t batch, int heads, const uint32_t* pages, int64_t num_pages,
+                const char* table_name, const int32_t* table, int64_t table_width, const char* lengths_name, const int32_t* lengths, const lq_rows* out,
+                float* lse, CacheAttendArgs* a)
+{
+    const CacheShape& s = c->shape;
+    LQ_TRY(check_pages(c, layer, pages, num_pages));
+    LQ_TRY(check_batch(c, batch, heads));
+    LQ_TRY(take_rows("queries", queries, batch, heads, false, &a->queries));
+    LQ_TRY(take_rows("out", out, batch, heads, true, &a->out));
+    if (queries->type != out->type) return lq_set_error(LQ_EINVAL, "queries and out have to be of one type");
+    if (table_width < 0 || table_width > INT32_MAX) return lq_set_error(LQ_EINVAL, "%s: a width of %lld is out of range", table_name, (long long)table_width);
+    if (batch > 0 && (!lengths || (table_width > 0 && !table))) return lq_set_error(LQ_EINVAL, "%s or %s is NULL", table_name, lengths_name);
+    if (!aligned(table, 4) || !aligned(lengths, 4) || !aligned(lse, 4))
+        return lq_set_error(LQ_EINVAL, "%s, %s and lse must be 4-byte aligned", table_name, lengths_name);
+    a->shape = s; a->tables = c->tables + (size_t)layer * 2;
+    a->pages = pages; a->table = table; a->lengths = lengths; a->lse = lse; a->flags = c->flags;
+    a->num_pages = num_pages; a->table_width = table_width;
+    a->batch = (int32_t)batch; a->group = heads / s.heads; a->group_blocks = (a->group + 7) / 8; a->row_heads = s.heads;
+    a->sms = c->sms;
+    return LQ_OK;
+}
+
+int take_scale(float scale, float* out)
+{
+    *out = scale * 1.44269504088896341f;
+    if (!std::isfinite(*out)) return lq_set_error(LQ_EINVAL, "scale is not a finite number (or above 2^127, where its base-2 form is none)");
+    return LQ_OK;
+}
+
+int take_workspace(void* workspace, int64_t bytes, int64_t needed, float** out)
+{
+    if (needed > 0 && (!workspace || !aligned(workspace, 16) || bytes < needed))
+        return lq_set_error(LQ_EINVAL, "workspace has to be 16-byte aligned and of %lld bytes or more", (long long)needed);
+    *out = needed > 0 ? static_cast<float*>(workspace) : nullptr;
+    return LQ_OK;
+}
+
+// The dealing out of work multiplies its units with the grid in 64 bits.
+int check_units(const lq_cache* c, const CacheAttendArgs& a, int64_t batch)
+{
+    const double tokens = (double)std::min<int64_t>(a.table_width << c->shape.page_shift, INT32_MAX);
+    if ((tokens / 128 + 1) * (double)batch * c->shape.heads * a.group_blocks * c->sms * 2 > 4e18)
+        return lq_set_error(LQ_EINVAL, "batch, heads and table_width are too large together");
+    return LQ_OK;
+}
+
+cudaError_t launch_attend(const CacheAttendArgs& a, cudaStream_t s)
+{
+    return a.shape.padded == 64 ? launch_cache_attend_64(a, s) : a.shape.padded == 128 ? launch_cache_attend_128(a, s) : launch_cache_attend_256(a, s);
+}
+
+constexpr int64_t kMostRows = (int64_t)1 << 26;        // (sequence, query head) pairs of a shared prefix
+int64_t most_tokens(const lq_cache* c, int64_t width) { return std::min<int64_t>(width << c->shape.page_shift, INT32_MAX); }
+
+// The workspace of attention with a shared prefix, in floats from its start: parts of the prefix, parts of the sequences' own tokens, and what
+// lq_cache_attend needs for those (-1: nothing).
+struct SharedSpace { int splits; int64_t parts, own, partial, bytes; };
+SharedSpace shared_space(const lq_cache* c, int64_t batch, int heads, int64_t prefix_width, int64_t table_width, int type)
+{
+    const CacheShape& s = c->shape;
+    const int64_t rows = batch * heads, part = cache_part_floats(s.padded);
+    SharedSpace x{};
+    x.splits = batch > 0 ? cache_shared_splits(s, batch * (heads / s.heads), most_tokens(c, prefix_width), type == LQ_F32, c->sms) : 0;
+    x.own = x.splits * cache_shared_slots(s.padded) * rows * part;
+    const int64_t partial = x.own + (table_width > 0 ? rows * part : 0), bytes = workspace_of(c, table_width, 0);
+    x.partial = bytes > 0 ? partial : -1;
+    x.bytes = partial * 4 + bytes;
+    return x;
+}
+
 }  // namespace
 
 extern "C" {
@@ -396,39 +490,150 @@ int lq_cache_attend(lq_cache* cache, int32_t layer, const lq_rows* queries, int6
                     const lq_rotary* rotary, const lq_rows* out, float* lse, void* workspace, int64_t workspace_bytes, void* stream)
 {
     if (!cache) return lq_set_error(LQ_EINVAL, "cache is NULL");
+    CacheAttendArgs a{};
+    LQ_TRY(take_attend(cache, layer, queries, batch, heads, pages, num_pages, "table", table, table_width, "lengths", lengths, out, lse, &a));
+    LQ_TRY(take_scale(scale, &a.scale));
+    if (window < 0) return lq_set_error(LQ_EINVAL, "window = %lld is negative", (long long)window);
+    a.window = window;
+    LQ_TRY(take_rotary(rotary, cache->shape, false, &a.rotary));
+    LQ_TRY(take_workspace(workspace, workspace_bytes, workspace_of(cache, table_width, window), &a.partial));
+    LQ_TRY(check_units(cache, a, batch));
+    if (batch == 0) return LQ_OK;
+    LQ_ON_DEVICE(cache);
+    LQ_CUDA(launch_attend(a, (cudaStream_t)stream));
+    return LQ_OK;
+}
+
+int lq_cache_attend_chosen(lq_cache* cache, int32_t layer, const lq_rows* queries, int64_t batch, int32_t heads, const uint32_t* pages,
+                           int64_t num_pages, const int32_t* chosen, int64_t keep, const int32_t* seen, float scale, const lq_rotary* rotary,
+                           const lq_rows* out, float* lse, void* workspace, int64_t workspace_bytes, void* stream)
+{
+    if (!cache) return lq_set_error(LQ_EINVAL, "cache is NULL");
+    CacheAttendArgs a{};
+    LQ_TRY(take_attend(cache, layer, queries, batch, heads, pages, num_pages, "chosen", chosen, keep, "seen", seen, out, lse, &a));
+    LQ_TRY(check_heads(cache, batch));
+    LQ_TRY(take_scale(scale, &a.scale));
+    LQ_TRY(take_rotary(rotary, cache->shape, batch > 0, &a.rotary));
+    LQ_TRY(take_workspace(workspace, workspace_bytes, workspace_of(cache, keep, 0), &a.partial));
+    LQ_TRY(check_units(cache, a, batch));
+    if (batch == 0) return LQ_OK;
+    a.batch = (int32_t)batch * cache->shape.heads;
+    a.row_heads = 1;
+    LQ_ON_DEVICE(cache);
+    LQ_CUDA(launch_attend(a, (cudaStream_t)stream));
+    return LQ_OK;
+}
+
+int64_t lq_cache_shared_workspace(const lq_cache* cache, int64_t batch, int32_t heads, int64_t prefix_width, int64_t table_width, int32_t type)
+{
+    if (!cache) return lq_set_error(LQ_EINVAL, "cache is NULL");
+    LQ_TRY(check_batch(cache, batch, heads));
+    if (batch * heads > kMostRows) return lq_set_error(LQ_EINVAL, "batch * heads = %lld: at most 2^26", (long long)(batch * heads));
+    if (prefix_width < 0 || prefix_width > INT32_MAX || table_width < 0 || table_width > INT32_MAX)
+        return lq_set_error(LQ_EINVAL, "prefix_width or table_width out of range");
+    if (type != LQ_F32 && type != LQ_F16 && type != LQ_BF16) return lq_set_error(LQ_EINVAL, "type %d is not one of LQ_F32, LQ_F16, LQ_BF16", type);
+    return shared_space(cache, batch, heads, prefix_width, table_width, type).bytes;
+}
+
+int lq_cache_attend_shared(lq_cache* cache, int32_t layer, const lq_rows* queries, int64_t batch, int32_t heads, const uint32_t* pages,
+                           int64_t num_pages, const int32_t* prefix, int64_t prefix_width, const int32_t* prefix_length,
+                           const int32_t* table, int64_t table_width, const int32_t* lengths, float scale, const lq_rotary* rotary,
+                           const lq_rows* out, float* lse, void* workspace, int64_t workspace_bytes, void* stream)
+{
+    if (!cache) return lq_set_error(LQ_EINVAL, "cache is NULL");
     const CacheShape& s = cache->shape;
     CacheAttendArgs a{};
+    LQ_TRY(take_attend(cache, layer, queries, batch, heads, pages, num_pages, "table", table, table_width, "lengths", lengths, out, lse, &a));
+    if (batch * heads > kMostRows) return lq_set_error(LQ_EINVAL, "batch * heads = %lld: at most 2^26", (long long)(batch * heads));
+    if (prefix_width < 0 || prefix_width > INT32_MAX) return lq_set_error(LQ_EINVAL, "prefix_width = %lld out of range", (long long)prefix_width);
+    if (batch > 0 && (!prefix_length || (prefix_width > 0 && !prefix))) return lq_set_error(LQ_EINVAL, "prefix or prefix_length is NULL");
+    if (!aligned(prefix, 4) || !aligned(prefix_length, 4)) return lq_set_error(LQ_EINVAL, "prefix and prefix_length must be 4-byte aligned");
+    LQ_TRY(take_scale(scale, &a.scale));
+    LQ_TRY(take_rotary(rotary, s, false, &a.rotary));
+    const SharedSpace space = shared_space(cache, batch, heads, prefix_width, table_width, queries->type);
+    float* base = nullptr;
+    LQ_TRY(take_workspace(workspace, workspace_bytes, space.bytes, &base));
+    LQ_TRY(check_units(cache, a, batch));
+    const int64_t row_blocks = (batch * a.group + 127) / 128;
+    if (row_blocks * s.heads * std::max(space.splits, 1) > INT32_MAX)
+        return lq_set_error(LQ_EINVAL, "batch, heads and prefix_width are too large together");
+    if (batch == 0) return LQ_OK;
+    CacheSharedArgs b{};
+    b.shape = s; b.tables = a.tables; b.queries = a.queries; b.out = a.out; b.rotary = a.rotary; b.pages = pages;
+    b.prefix = prefix; b.prefix_length = prefix_length; b.lengths = lengths; b.lse = lse; b.flags = cache->flags;
+    b.num_pages = num_pages; b.prefix_width = prefix_width; b.prefix_most = most_tokens(cache, prefix_width); b.own_most = most_tokens(cache, table_width);
+    b.scale = a.scale; b.batch = a.batch; b.group = a.group; b.splits = space.splits;
+    b.two_queries = queries->type == LQ_F32 || rotary != nullptr;
+    b.parts = base + space.parts; b.own = base + space.own;
+    a.partial = space.partial < 0 ? nullptr : base + space.partial;
+    a.sums = b.own; a.before = prefix_length; a.before_most = b.prefix_most; a.lse = nullptr;
+    LQ_ON_DEVICE(cache);
+    if (space.splits > 0) LQ_CUDA(launch_cache_shared_prefix(b, (cudaStream_t)stream));
+    if (table_width > 0) LQ_CUDA(launch_attend(a, (cudaStream_t)stream));
+    LQ_CUDA(launch_cache_shared_join(b, (cudaStream_t)stream));
+    return LQ_OK;
+}
+
+int64_t lq_cache_bounds_words(const lq_cache* cache)
+{
+    return cache ? (int64_t)cache_bounds_words(cache->shape.heads, cache->shape.padded) : (int64_t)lq_set_error(LQ_EINVAL, "cache is NULL");
+}
+
+int lq_cache_bounds(lq_cache* cache, int32_t layer, const uint32_t* pages, int64_t num_pages, const int32_t* which, int64_t count,
+                    uint32_t* bounds, void* stream)
+{
+    if (!cache) return lq_set_error(LQ_EINVAL, "cache is NULL");
     LQ_TRY(check_pages(cache, layer, pages, num_pages));
-    if (batch < 0 || batch > 1 << 24) return lq_set_error(LQ_EINVAL, "batch = %lld out of [0, 2^24]", (long long)batch);
-    if (heads < s.heads || heads % s.heads || heads > 1 << 16)
-        return lq_set_error(LQ_EINVAL, "query heads (%d) have to be a multiple of the cache's %d, at most 65536", heads, s.heads);
+    if (count < 0 || count > INT32_MAX) return lq_set_error(LQ_EINVAL, "count = %lld out of [0, 2^31)", (long long)count);
+    if (count > 0 && !which) return lq_set_error(LQ_EINVAL, "which is NULL");
+    if (!aligned(which, 4)) return lq_set_error(LQ_EINVAL, "which must be 4-byte aligned");
+    LQ_TRY(check_bounds(bounds, num_pages));
+    if (count == 0) return LQ_OK;
+    CacheBoundsArgs a{};
+    a.shape = cache->shape; a.tables = cache->tables + (size_t)layer * 2; a.pages = pages; a.which = which; a.bounds = bounds; a.flags = cache->flags;
+    a.num_pages = num_pages; a.count = count;
+    LQ_ON_DEVICE(cache);
+    LQ_CUDA(launch_cache_bounds(a, (cudaStream_t)stream));
+    return LQ_OK;
+}
+
+int64_t lq_cache_choose_workspace(const lq_cache* cache, int64_t batch, int64_t table_width)
+{
+    if (!cache) return lq_set_error(LQ_EINVAL, "cache is NULL");
+    if (table_width < 0 || table_width > INT32_MAX) return lq_set_error(LQ_EINVAL, "table_width out of range");
+    LQ_TRY(check_heads(cache, batch));
+    return table_width > kCacheChooseKeys ? batch * cache->shape.heads * table_width * 4 : 0;
+}
+
+int lq_cache_choose(lq_cache* cache, const lq_rows* queries, int64_t batch, int32_t heads, const uint32_t* bounds, int64_t num_pages,
+                    const int32_t* table, int64_t table_width, const int32_t* lengths, int32_t first, int32_t last, const lq_rotary* rotary,
+                    int32_t* chosen, int32_t keep, int32_t* seen, void* workspace, int64_t workspace_bytes, void* stream)
+{
+    if (!cache) return lq_set_error(LQ_EINVAL, "cache is NULL");
+    const CacheShape& s = cache->shape;
+    CacheChooseArgs a{};
+    LQ_TRY(check_batch(cache, batch, heads));
+    LQ_TRY(check_heads(cache, batch));
     LQ_TRY(take_rows("queries", queries, batch, heads, false, &a.queries));
-    LQ_TRY(take_rows("out", out, batch, heads, true, &a.out));
-    if (queries->type != out->type) return lq_set_error(LQ_EINVAL, "queries and out have to be of one type");
+    if (num_pages < 0 || num_pages > INT32_MAX) return lq_set_error(LQ_EINVAL, "num_pages = %lld out of range", (long long)num_pages);
+    LQ_TRY(check_bounds(bounds, num_pages));
     if (table_width < 0 || table_width > INT32_MAX) return lq_set_error(LQ_EINVAL, "table_width = %lld out of range", (long long)table_width);
     if (batch > 0 && (!lengths || (table_width > 0 && !table))) return lq_set_error(LQ_EINVAL, "table or lengths is NULL");
-    if (!aligned(table, 4) || !aligned(lengths, 4) || !aligned(lse, 4)) return lq_set_error(LQ_EINVAL, "table, lengths and lse must be 4-byte aligned");
-    a.scale = scale * 1.44269504088896341f;
-    if (!std::isfinite(a.scale)) return lq_set_error(LQ_EINVAL, "scale is not a finite number (or above 2^127, where its base-2 form is none)");
-    if (window < 0) return lq_set_error(LQ_EINVAL, "window = %lld is negative", (long long)window);
+    if (batch > 0 && (!chosen || !seen)) return lq_set_error(LQ_EINVAL, "chosen or seen is NULL");
+    if (!aligned(table, 4) || !aligned(lengths, 4) || !aligned(chosen, 4) || !aligned(seen, 4))
+        return lq_set_error(LQ_EINVAL, "table, lengths, chosen and seen must be 4-byte aligned");
+    if (first < 0 || last < 1 || (int64_t)first + last > keep)
+        return lq_set_error(LQ_EINVAL, "first = %d, last = %d, keep = %d: first >= 0, last >= 1 and first + last <= keep are wanted", first, last, keep);
     LQ_TRY(take_rotary(rotary, s, false, &a.rotary));
-    const int64_t needed = workspace_of(cache, table_width, window);
-    if (needed > 0 && (!workspace || !aligned(workspace, 16) || workspace_bytes < needed))
-        return lq_set_error(LQ_EINVAL, "workspace has to be 16-byte aligned and of %lld bytes or more", (long long)needed);
-    a.group = heads / s.heads; a.group_blocks = (a.group + 7) / 8;
-    // the dealing out of work multiplies its units with the grid in 64 bits
-    const double tokens = (double)std::min<int64_t>(table_width << s.page_shift, INT32_MAX);
-    if ((tokens / 128 + 1) * (double)batch * s.heads * a.group_blocks * cache->sms * 2 > 4e18)
-        return lq_set_error(LQ_EINVAL, "batch, heads and table_width are too large together");
+    float* scores = nullptr;
+    const int64_t needed = table_width > kCacheChooseKeys ? batch * s.heads * table_width * 4 : 0;
+    LQ_TRY(take_workspace(workspace, workspace_bytes, needed, &scores));
     if (batch == 0) return LQ_OK;
-    a.shape = s; a.tables = cache->tables + (size_t)layer * 2;
-    a.pages = pages; a.table = table; a.lengths = lengths; a.lse = lse; a.partial = needed > 0 ? static_cast<float*>(workspace) : nullptr; a.flags = cache->flags;
-    a.num_pages = num_pages; a.table_width = table_width; a.window = window;
-    a.batch = (int32_t)batch;
-    a.sms = cache->sms;
+    a.shape = s; a.bounds = bounds; a.table = table; a.lengths = lengths; a.chosen = chosen; a.seen = seen; a.scores = reinterpret_cast<uint32_t*>(scores);
+    a.flags = cache->flags; a.num_pages = num_pages; a.table_width = table_width; a.batch = (int32_t)batch; a.group = heads / s.heads;
+    a.first = first; a.last = last; a.keep = keep; a.sms = cache->sms;
     LQ_ON_DEVICE(cache);
-    LQ_CUDA(s.padded == 64 ? launch_cache_attend_64(a, (cudaStream_t)stream)
-            : s.padded == 128 ? launch_cache_attend_128(a, (cudaStream_t)stream) : launch_cache_attend_256(a, (cudaStream_t)stream));
+    LQ_CUDA(launch_cache_choose(a, (cudaStream_t)stream));
     return LQ_OK;
 }
 

@@ -105,16 +105,66 @@ struct CacheAttendArgs {
     CacheRows queries, out;
     CacheRotary rotary;
     const uint32_t* pages;
-    const int32_t* table;               // [batch][table_width] page numbers
+    const int32_t* table;               // [batch][table_width] page numbers; [batch * heads][table_width] where every head has its own
     const int32_t* lengths;
     float* lse;                         // [batch][heads * group] or NULL
     float* partial;                     // workspace, see lq_cache_attend.cuh; NULL: no sequence can be split
     uint32_t* flags;
-    int64_t num_pages, table_width, window;
+    const int32_t* before;              // NULL, or how many tokens stand before each sequence's own: its last position is so much higher
+    float* sums;                        // NULL, or [batch][heads * group] parts (cache_part_floats) that take the place of out and lse
+    int64_t num_pages, table_width, window, before_most;        // before_most: tokens that *before can mean
     float scale;                        // of the scores, times log2(e)
-    int32_t batch, group, group_blocks; // queries a head, and their blocks of 8
+    int32_t batch, group, group_blocks; // rows of the table; queries a head, and their blocks of 8
+    int32_t row_heads;                  // heads that a row of the table serves: all, or 1
     int32_t sms;                        // CTAs
 };
+
+// A prefix that all sequences of a batch share (lq_cache_shared.cu), and how what it and the sequences' own tokens give is joined.
+struct CacheSharedArgs {
+    CacheShape shape;
+    const CacheTable* tables;
+    CacheRows queries, out;
+    CacheRotary rotary;
+    const uint32_t* pages;
+    const int32_t* prefix;              // [prefix_width] page numbers
+    const int32_t* prefix_length;       // dev [1]
+    const int32_t* lengths;             // dev [batch]: the sequences' own tokens
+    float* lse;
+    float* parts;                       // [splits][batch][heads * group] parts of the prefix (cache_part_floats)
+    float* own;                         // [batch][heads * group] parts of the sequences' own tokens
+    uint32_t* flags;
+    int64_t num_pages, prefix_width, prefix_most, own_most;     // tokens that the lengths can mean
+    float scale;
+    int32_t batch, group, splits;
+    int32_t two_queries;                // queries are sums of two fp16 numbers
+};
+
+// Which pages a sequence's queries look at (lq_cache_choose.cu).
+struct CacheBoundsArgs {
+    CacheShape shape;
+    const CacheTable* tables;
+    const uint32_t* pages;
+    const int32_t* which;               // [count] page numbers
+    uint32_t* bounds;
+    uint32_t* flags;
+    int64_t num_pages, count;
+};
+struct CacheChooseArgs {
+    CacheShape shape;
+    CacheRows queries;
+    CacheRotary rotary;
+    const uint32_t* bounds;
+    const int32_t* table;
+    const int32_t* lengths;
+    int32_t* chosen;                    // [batch][heads][keep]
+    int32_t* seen;                      // [batch][heads]
+    uint32_t* scores;                   // [batch][heads][table_width]
+    uint32_t* flags;
+    int64_t num_pages, table_width;
+    int32_t batch, group, first, last, keep, sms;
+};
+// Words of a page's bounds: for each head `padded` upper and `padded` lower bounds of a byte, then a scale a head, to a multiple of 16 bytes.
+__host__ __device__ constexpr int cache_bounds_words(int heads, int padded) { return (heads * (padded / 2 + 1) + 3) / 4 * 4; }
 
 cudaError_t launch_cache_write(const CacheWriteArgs& a, cudaStream_t s);
 cudaError_t launch_cache_read(const CacheReadArgs& a, cudaStream_t s);
@@ -124,6 +174,13 @@ cudaError_t launch_cache_clear(uint32_t* flags, uint32_t seen);        // on the
 cudaError_t launch_cache_attend_64(const CacheAttendArgs& a, cudaStream_t s);
 cudaError_t launch_cache_attend_128(const CacheAttendArgs& a, cudaStream_t s);
 cudaError_t launch_cache_attend_256(const CacheAttendArgs& a, cudaStream_t s);
+cudaError_t launch_cache_bounds(const CacheBoundsArgs& a, cudaStream_t s);
+cudaError_t launch_cache_choose(const CacheChooseArgs& a, cudaStream_t s);
+cudaError_t launch_cache_shared_prefix(const CacheSharedArgs& a, cudaStream_t s);
+cudaError_t launch_cache_shared_join(const CacheSharedArgs& a, cudaStream_t s);
+// Into how many parts the prefix's tokens are split, and how many parts a query may leave (a CTA of rows of 64 and 128 leaves two, see there).
+int cache_shared_splits(const CacheShape& shape, int64_t rows, int64_t prefix_tokens, bool exact, int sms);
+__host__ __device__ constexpr int cache_shared_slots(int padded) { return padded == 256 ? 1 : 2; }
 // Teams of 8 warps that share an SM in the attention kernel (its registers: rows of 256 need twice as many a thread), and what
 // each may leave in the workspace: a record, then two partial sums of 8 queries.
 __host__ __device__ constexpr int cache_attend_teams(int padded) { return padded == 256 ? 1 : 2; }
@@ -131,7 +188,11 @@ __host__ __device__ constexpr int cache_attend_teams(int padded) { return padded
 // in 4 bits: one sequence of 130 001 tokens 47.0 us with one, 45.4 with two, of 200 tokens 8.8 and 6.3).
 __host__ __device__ constexpr int cache_attend_pair(int padded, int bits_k, int bits_v) { return padded * (bits_k + bits_v) <= 1024 ? 2 : 1; }
 __host__ __device__ constexpr int cache_attend_unit(int padded, int bits_k, int bits_v) { return 8 * cache_attend_pair(padded, bits_k, bits_v); }
+constexpr int kCacheChooseKeys = 12288; // scores that a choosing CTA keeps in its shared memory; more are kept in the workspace
 constexpr int kCacheRecordBytes = 16;
-constexpr int cache_partial_floats(int padded) { return 8 * (padded + 4); }
+// What is left of one query over some of its tokens: sums of `padded` weighted values; reference of the scores, scale of the weights (both as
+// base-2 exponents), denominator, unused.
+__host__ __device__ constexpr int cache_part_floats(int padded) { return padded + 4; }
+constexpr int cache_partial_floats(int padded) { return 8 * cache_part_floats(padded); }
 
 }  // namespace lq

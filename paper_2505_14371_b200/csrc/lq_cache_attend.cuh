@@ -232,7 +232,16 @@ __device__ __forceinline__ void store_four(const CacheRows& r, char* row, int d,
     for (int k = 0; k < 4; ++k) if (d + k < dim) store_any(r.type, row, d + k, o[k]);
 }
 
-// What a sequence has to be read of: tokens [first, length), as tiles [tile0, tile1).
+// Whose queries a segment has: a row of the table serves all heads of a sequence, or (row_heads = 1) one.
+struct Owner { int sequence, head; };
+__device__ __forceinline__ Owner owner_of(const CacheAttendArgs& a, int row, int head)
+{
+    if (a.row_heads == a.shape.heads) return {row, head};
+    const int sequence = row / a.shape.heads;
+    return {sequence, row - sequence * a.shape.heads};
+}
+
+// What a row of the table has to be read of: tokens [first, length), as tiles [tile0, tile1).
 struct Extent {
     uint32_t first, length;             // (a tile's last token may be just past 2^31)
     int32_t tile0, tile1;
@@ -465,7 +474,7 @@ struct Query {
         const float* angles = r.table;
         const int half = r.dim / 2;
         if (r.table && live) {
-            const int64_t at = r.at ? r.at[sequence] : (length > 0 ? (int64_t)length - 1 : 0);
+            const int64_t last = (int64_t)length + (a.before ? min((int64_t)max(*a.before, 0), a.before_most) : 0), at = r.at ? r.at[sequence] : (last > 0 ? last - 1 : 0);
             lost = at < 0 || at >= r.positions;
             if (lost) { if (lane == 0) atomicOr(a.flags, LQ_CACHE_BAD_POSITION); }
             else angles += at * r.dim;
@@ -551,7 +560,7 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
     pdl_launch_next();
 
     // ---- this team's share of all units
-    const int head_blocks = a.shape.heads * a.group_blocks, me = blockIdx.x * X::kTeams + team, teams = gridDim.x * X::kTeams;
+    const int head_blocks = a.row_heads * a.group_blocks, me = blockIdx.x * X::kTeams + team, teams = gridDim.x * X::kTeams;
     // what the segments of sequence `b` cost: units, and kStart for each segment that has any
     auto units_of = [&](int b) -> int64_t {
         const int64_t u = b < a.batch ? extent_of(a, b).template units<X::kUnit>() : 0;
@@ -637,7 +646,9 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
             const int count = (int)(ours + min(chunk, (int64_t)0));     // units of this segment that are ours
             if (count <= 0) break;                                      // (the end of our share)
             if (chunk < 0) chunk = 0;
-            const int head = hb / a.group_blocks, block = hb - head * a.group_blocks;
+            const int row_head = hb / a.group_blocks, block = hb - row_head * a.group_blocks;
+            const Owner owner = owner_of(a, sequence, row_head);
+            const int head = owner.head;
             // ---- the first copies: this warp's tiles are kPair of every unit
             const int32_t* pages = a.table + (int64_t)sequence * a.table_width;
             const int tile0 = extent.tile0 + (int)chunk * X::kUnit + warp * X::kPair, stop = min(extent.tile1, extent.tile0 + ((int)chunk + count) * X::kUnit);
@@ -649,7 +660,7 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
             auto page_of = [&](int n) { const int tile = tile_of(n); return tile < stop ? pages[tile >> tile_shift] : -1; };
             const int first_pages = page_of(lane);
             Query<P, kFloat> query_raw;
-            query_raw.fetch(a, sequence, head, block * kQueries + (kRests ? warp % 4 : warp), lane, extent.length);
+            query_raw.fetch(a, owner.sequence, head, block * kQueries + (kRests ? warp % 4 : warp), lane, extent.length);
             auto start = [&](int round, int stage) {
                 if (round < rounds) {
                     if (round * X::kPair % 32 == 0) {
@@ -845,8 +856,11 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
                         make_float4(S.acc[m][i], S.acc[m][2 + i], S.acc[m + 1][i], S.acc[m + 1][2 + i]);
             }
             team_sync(team);
-            const bool starts = chunk == 0, whole = starts && count == units;
+            const bool starts = chunk == 0, whole = starts && count == units, done = whole && !a.sums;
             const int slot = 2 * me + starts;
+            const int64_t first_query = (int64_t)owner.sequence * a.shape.heads * a.group + head * a.group + block * kQueries;
+            float* const left = whole ? a.sums + first_query * cache_part_floats(P) : partials + slot * kPartial<P>;     // (where it is not done)
+            const int lefts = whole ? a.group - block * kQueries : kQueries;            // a query that is not there has no part
             if (tid < kQueries) {
                 float r = kLow, scale = -INFINITY, total = 0.0f;
                 for (int w = 0; w < kTeamWarps; ++w) r = fmaxf(r, sh.stats[w][tid][0]);
@@ -857,13 +871,12 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
                     total += sh.stats[w][tid][2] * ex2(moved);
                     sh.share[tid][w] = ex2(moved + (sh.stats[w][tid][1] - scale));
                 }
-                if (whole) {                    // the segment's own: what is left to multiply by, and the logarithm
+                if (done) {                     // the segment's own: what is left to multiply by, and the logarithm
                     sh.share[tid][kTeamWarps] = out_factor<kFloat>(scale, total);
                     if (a.lse && block * kQueries + tid < a.group)
-                        a.lse[(int64_t)sequence * a.shape.heads * a.group + head * a.group + block * kQueries + tid] =
-                            total != 0.0f ? (r + log2f(total)) * 0.693147180559945309f : -INFINITY;
-                } else {
-                    *reinterpret_cast<float4*>(partials + slot * kPartial<P> + tid * (P + 4) + P) = make_float4(r, scale, total, 0.0f);
+                        a.lse[first_query + tid] = total != 0.0f ? (r + log2f(total)) * 0.693147180559945309f : -INFINITY;
+                } else if (tid < lefts) {
+                    *reinterpret_cast<float4*>(left + tid * (P + 4) + P) = make_float4(r, whole && kFloat ? scale - kLift : scale, total, 0.0f);
                 }
             }
             team_sync(team);
@@ -883,14 +896,14 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
                     }
                     sum4.x += v.x * f; sum4.y += v.y * f; sum4.z += v.z * f; sum4.w += v.w * f;
                 }
-                if (whole) {
+                if (done) {
                     if (block * kQueries + query < a.group) {
                         const float f = share[kTeamWarps];
-                        store_four<kFloat>(a.out, row_of(a.out, sequence, head * a.group + block * kQueries + query), d, a.shape.dim,
+                        store_four<kFloat>(a.out, row_of(a.out, owner.sequence, head * a.group + block * kQueries + query), d, a.shape.dim,
                                            make_float4(sum4.x * f, sum4.y * f, sum4.z * f, sum4.w * f));
                     }
-                } else {
-                    *reinterpret_cast<float4*>(partials + slot * kPartial<P> + query * (P + 4) + d) = sum4;
+                } else if (query < lefts) {
+                    *reinterpret_cast<float4*>(left + query * (P + 4) + d) = sum4;
                 }
             }
             if (starts && !whole && tid == 0) {
@@ -910,13 +923,16 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
         }
     }
 
-    // sequences without a token to see
-    for (int b = me; b < a.batch; b += teams) {
+    // rows without a token to see (where parts are asked for, the join leaves them out)
+    for (int b = a.sums ? a.batch : me; b < a.batch; b += teams) {
         if (extent_of(a, b).template units<X::kUnit>() > 0) continue;
-        const int queries = a.shape.heads * a.group;
+        const int queries = a.row_heads * a.group;
+        const Owner owner = owner_of(a, b, 0);
         for (int64_t i = tid; i < (int64_t)queries * a.shape.dim; i += kTeam)
-            store_any(a.out.type, row_of(a.out, b, (int)(i / a.shape.dim)), (int)(i % a.shape.dim), 0.0f);
-        if (a.lse) for (int i = tid; i < queries; i += kTeam) a.lse[(int64_t)b * queries + i] = -INFINITY;
+            store_any(a.out.type, row_of(a.out, owner.sequence, owner.head * a.group + (int)(i / a.shape.dim)), (int)(i % a.shape.dim), 0.0f);
+        if (a.lse)
+            for (int i = tid; i < queries; i += kTeam)
+                a.lse[((int64_t)owner.sequence * a.shape.heads + owner.head) * a.group + i] = -INFINITY;
     }
 }
 
@@ -985,7 +1001,9 @@ __global__ void __launch_bounds__(32 * kQueries* kJoinWarps) attend_join_kernel(
     for (int i = 0; i < kVectors; ++i) sums[share][q][i][lane] = acc[i];
     if (lane == 0) stats[share][q] = make_float4(r, scale, total, 0.0f);
     __syncthreads();
-    const int head = rec.head_block / a.group_blocks, query = (rec.head_block - head * a.group_blocks) * kQueries + q;
+    const int row_head = rec.head_block / a.group_blocks, query = (rec.head_block - row_head * a.group_blocks) * kQueries + q;
+    const Owner owner = owner_of(a, rec.sequence, row_head);
+    const int head = owner.head;
     if (share > 0 || query >= a.group) return;
     for (int s = 1; s < kJoinWarps; ++s) r = fmaxf(r, stats[s][q].x);
     scale = -INFINITY;
@@ -1000,7 +1018,8 @@ __global__ void __launch_bounds__(32 * kQueries* kJoinWarps) attend_join_kernel(
         f[s] = ex2(moved + (stats[s][q].y - scale));
     }
     const float out = a.out.type == LQ_F32 ? out_factor<true>(scale, total) : out_factor<false>(scale, total);
-    char* const to = row_of(a.out, rec.sequence, head * a.group + query);
+    const int64_t row = ((int64_t)owner.sequence * a.shape.heads + head) * a.group + query;
+    char* const to = a.sums ? nullptr : row_of(a.out, owner.sequence, head * a.group + query);
 #pragma unroll
     for (int i = 0; i < kVectors; ++i) {
         float4 v = make_float4(0, 0, 0, 0);
@@ -1009,14 +1028,20 @@ __global__ void __launch_bounds__(32 * kQueries* kJoinWarps) attend_join_kernel(
             const float4 u = sums[s][q][i][lane];
             v.x += u.x * f[s]; v.y += u.y * f[s]; v.z += u.z * f[s]; v.w += u.w * f[s];
         }
-        const float o[4] = {v.x * out, v.y * out, v.z * out, v.w * out};
         const int d = 4 * (lane + 32 * i);
+        if (a.sums) {
+            if (d < P) *reinterpret_cast<float4*>(a.sums + row * cache_part_floats(P) + d) = v;
+            continue;
+        }
+        const float o[4] = {v.x * out, v.y * out, v.z * out, v.w * out};
 #pragma unroll
         for (int k = 0; k < 4; ++k) if (d + k < a.shape.dim) store_any(a.out.type, to, d + k, o[k]);
     }
-    if (lane == 0 && a.lse)
-        a.lse[(int64_t)rec.sequence * a.shape.heads * a.group + head * a.group + query] =
-            total != 0.0f ? (r + log2f(total)) * 0.693147180559945309f : -INFINITY;
+    if (lane == 0 && a.sums)
+        *reinterpret_cast<float4*>(a.sums + row * cache_part_floats(P) + P) =
+            make_float4(r, a.out.type == LQ_F32 ? scale - kLift : scale, total, 0.0f);
+    else if (lane == 0 && a.lse)
+        a.lse[row] = total != 0.0f ? (r + log2f(total)) * 0.693147180559945309f : -INFINITY;
 }
 
 template <int P, int WK, int WV, int kMode>

@@ -338,6 +338,119 @@ PyObject* cache_attend(PyObject*, PyObject* const* a, Py_ssize_t n)
     });
 }
 
+// What the calls of attention have in common: queries and outputs of `batch` sequences, and their logarithms.
+bool attended_of(PyObject* queries, PyObject* out, PyObject* lse, const CacheInfo& c, int64_t batch, lq_rows* q, lq_rows* o, int64_t* heads, float** l)
+{
+    if (!rows_of(queries, c, "queries", batch, 0, q)) return false;
+    *heads = THPVariable_Unpack(queries).size(1);
+    if (*heads > INT32_MAX) return wrong("queries", "at most 65536 heads");
+    if (!rows_of(out, c, "out", batch, *heads, o)) return false;
+    if (!no_gradient(queries, "queries") || !no_gradient(out, "out") || !no_gradient(lse, "lse")) return false;
+    *l = nullptr;
+    if (lse == Py_None) return true;
+    const at::Tensor* e;
+    if (!array_of(lse, c, "lse", at::kFloat, 2, l, &e)) return false;
+    return (e->size(0) == batch && e->size(1) == *heads) || wrong("lse", "[batch][heads]");
+}
+
+// From torch's allocator, on the stream that the call runs on: a workspace of its own for every call, also in a graph.
+at::Tensor space_of(int64_t bytes, const at::Tensor& beside)
+{
+    return bytes > 0 ? at::empty({bytes}, beside.options().dtype(at::kByte)) : at::Tensor();
+}
+
+// cache, layer, queries, pages, prefix, prefix_length, table, lengths, out, lse, scale, rotary, positions, interleaved
+PyObject* cache_attend_shared(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    CacheInfo c; lq_rows q, o; int64_t pages, heads; uint32_t* p; int32_t layer, *prefix, *prefix_length, *table, *lengths; lq_rotary r; bool turned;
+    const at::Tensor *f, *fl, *t, *l; float* lse;
+    if (!arity(n, 14) || !cache_of(a[0], &c) || !int_of(a[1], &layer) || !array_of(a[7], c, "lengths", at::kInt, 1, &lengths, &l)) return nullptr;
+    const int64_t batch = l->numel();
+    if (!pages_of(a[3], c, &p, &pages) || !array_of(a[4], c, "prefix", at::kInt, 1, &prefix, &f) ||
+        !array_of(a[5], c, "prefix_length", at::kInt, 0, &prefix_length, &fl) || !array_of(a[6], c, "table", at::kInt, 2, &table, &t)) return nullptr;
+    if (fl->numel() != 1) { wrong("prefix_length", "one number"); return nullptr; }
+    if (t->size(0) != batch) { wrong("table", "a row a sequence"); return nullptr; }
+    if (!attended_of(a[2], a[8], a[9], c, batch, &q, &o, &heads, &lse)) return nullptr;
+    const double scale = PyFloat_AsDouble(a[10]);
+    if (PyErr_Occurred() || !rotary_of(a[11], a[12], a[13], c, batch, &r, &turned)) return nullptr;
+    const int64_t bytes = lq_cache_shared_workspace(c.cache, batch, static_cast<int32_t>(heads), f->numel(), t->size(1), q.type);
+    if (bytes < 0) return done(static_cast<int>(bytes));
+    const at::Tensor space = space_of(bytes, *l);
+    return call_on(c, [&](void* s) {
+        return lq_cache_attend_shared(c.cache, layer, &q, batch, static_cast<int32_t>(heads), p, pages, prefix, f->numel(), prefix_length, table,
+                                      t->size(1), lengths, static_cast<float>(scale), turned ? &r : nullptr, &o, lse,
+                                      bytes > 0 ? space.data_ptr() : nullptr, bytes, s);
+    });
+}
+
+// [num_pages][words] bounds
+bool bounds_of(PyObject* o, const CacheInfo& c, uint32_t** bounds, int64_t* num)
+{
+    const at::Tensor* t;
+    if (!array_of(o, c, "bounds", at::kInt, 2, bounds, &t)) return false;
+    *num = t->size(0);
+    return t->size(1) == lq_cache_bounds_words(c.cache) || wrong("bounds", "[num_pages][bounds_words]");
+}
+
+// cache, layer, pages, which, bounds
+PyObject* cache_bounds(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    CacheInfo c; int64_t pages, bounded; uint32_t *p, *b; int32_t layer, *which; const at::Tensor* t;
+    if (!arity(n, 5) || !cache_of(a[0], &c) || !int_of(a[1], &layer) || !pages_of(a[2], c, &p, &pages) ||
+        !array_of(a[3], c, "which", at::kInt, 1, &which, &t) || !bounds_of(a[4], c, &b, &bounded)) return nullptr;
+    if (bounded != pages) { wrong("bounds", "a row a page"); return nullptr; }
+    return call_on(c, [&](void* s) { return lq_cache_bounds(c.cache, layer, p, pages, which, t->numel(), b, s); });
+}
+
+// [batch][kv_heads][keep] pages of every (sequence, head), and [batch][kv_heads] tokens
+bool chosen_of(PyObject* chosen, PyObject* seen, const CacheInfo& c, int64_t* batch, int64_t* keep, int32_t** pages, int32_t** tokens, const at::Tensor** t)
+{
+    const at::Tensor* s;
+    if (!array_of(chosen, c, "chosen", at::kInt, 0, pages, t) || !array_of(seen, c, "seen", at::kInt, 2, tokens, &s)) return false;
+    if ((*t)->dim() != 3 || (*t)->size(1) != c.heads) return wrong("chosen", "[batch][kv_heads][keep]");
+    *batch = (*t)->size(0);
+    *keep = (*t)->size(2);
+    return (s->size(0) == *batch && s->size(1) == c.heads) || wrong("seen", "[batch][kv_heads]");
+}
+
+// cache, queries, bounds, table, lengths, chosen, seen, first, last, rotary, positions, interleaved
+PyObject* cache_choose(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    CacheInfo c; lq_rows q; int64_t pages, batch, keep; uint32_t* b; int32_t *table, *lengths, *chosen, *seen, first, last; lq_rotary r; bool turned;
+    const at::Tensor *t, *l, *k;
+    if (!arity(n, 12) || !cache_of(a[0], &c) || !chosen_of(a[5], a[6], c, &batch, &keep, &chosen, &seen, &k) || !rows_of(a[1], c, "queries", batch, 0, &q) ||
+        !no_gradient(a[1], "queries") || !bounds_of(a[2], c, &b, &pages) || !array_of(a[3], c, "table", at::kInt, 2, &table, &t) ||
+        !array_of(a[4], c, "lengths", at::kInt, 1, &lengths, &l) || !int_of(a[7], &first) || !int_of(a[8], &last)) return nullptr;
+    const int64_t heads = THPVariable_Unpack(a[1]).size(1);
+    if (heads > INT32_MAX || keep > INT32_MAX) { wrong("queries", "at most 65536 heads, and 2^31 - 1 pages kept"); return nullptr; }
+    if (t->size(0) != batch || l->numel() != batch) { wrong("table and lengths", "a row a sequence"); return nullptr; }
+    if (!rotary_of(a[9], a[10], a[11], c, batch, &r, &turned)) return nullptr;
+    const int64_t bytes = lq_cache_choose_workspace(c.cache, batch, t->size(1));
+    if (bytes < 0) return done(static_cast<int>(bytes));
+    const at::Tensor space = space_of(bytes, *l);
+    return call_on(c, [&](void* s) {
+        return lq_cache_choose(c.cache, &q, batch, static_cast<int32_t>(heads), b, pages, table, t->size(1), lengths, first, last,
+                               turned ? &r : nullptr, chosen, static_cast<int32_t>(keep), seen, bytes > 0 ? space.data_ptr() : nullptr, bytes, s);
+    });
+}
+
+// cache, layer, queries, pages, chosen, seen, out, lse, scale, rotary, positions, interleaved
+PyObject* cache_attend_chosen(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    CacheInfo c; lq_rows q, o; int64_t pages, heads, batch, keep; uint32_t* p; int32_t layer, *chosen, *seen; lq_rotary r; bool turned;
+    const at::Tensor* k; float* lse;
+    if (!arity(n, 12) || !cache_of(a[0], &c) || !int_of(a[1], &layer) || !chosen_of(a[4], a[5], c, &batch, &keep, &chosen, &seen, &k) ||
+        !pages_of(a[3], c, &p, &pages) || !attended_of(a[2], a[6], a[7], c, batch, &q, &o, &heads, &lse)) return nullptr;
+    const double scale = PyFloat_AsDouble(a[8]);
+    if (PyErr_Occurred() || !rotary_of(a[9], a[10], a[11], c, batch, &r, &turned)) return nullptr;
+    const int64_t bytes = lq_cache_workspace(c.cache, keep, 0);
+    const at::Tensor space = space_of(bytes, *k);
+    return call_on(c, [&](void* s) {
+        return lq_cache_attend_chosen(c.cache, layer, &q, batch, static_cast<int32_t>(heads), p, pages, chosen, keep, seen, static_cast<float>(scale),
+                                      turned ? &r : nullptr, &o, lse, bytes > 0 ? space.data_ptr() : nullptr, bytes, s);
+    });
+}
+
 PyObject* register_error(PyObject*, PyObject* cls)
 {
     Py_INCREF(cls);
@@ -364,6 +477,8 @@ PyMethodDef methods[] = {LQ_FAST("lq_quantize_pack", quantize_pack), LQ_FAST("qo
                          LQ_FAST("lq_entropy_decode", entropy_decode),
                          LQ_FAST("lq_vector_norm_static", vector_norm_static), LQ_FAST("lq_cache_write", cache_write),
                          LQ_FAST("lq_cache_read", cache_read), LQ_FAST("lq_cache_attend", cache_attend),
+                         LQ_FAST("lq_cache_attend_shared", cache_attend_shared), LQ_FAST("lq_cache_bounds", cache_bounds),
+                         LQ_FAST("lq_cache_choose", cache_choose), LQ_FAST("lq_cache_attend_chosen", cache_attend_chosen),
                          {"register_error", register_error, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 #undef LQ_FAST
 
