@@ -284,16 +284,17 @@ cudaError_t launch_attend(const CacheAttendArgs& a, cudaStream_t s)
 constexpr int64_t kMostRows = (int64_t)1 << 26;        // (sequence, query head) pairs of a shared prefix
 int64_t most_tokens(const lq_cache* c, int64_t width) { return std::min<int64_t>(width << c->shape.page_shift, INT32_MAX); }
 
-// The workspace of attention with a shared prefix, in floats from its start: parts of the prefix, parts of the sequences' own tokens, and what
+// The workspace of attention with a shared prefix, in floats from its start: the queries, parts of the prefix, parts of the sequences' own tokens, and what
 // lq_cache_attend needs for those (-1: nothing).
-struct SharedSpace { int splits; int64_t parts, own, partial, bytes; };
+struct SharedSpace { int splits; int64_t rows, parts, own, partial, bytes; };
 SharedSpace shared_space(const lq_cache* c, int64_t batch, int heads, int64_t prefix_width, int64_t table_width, int type)
 {
     const CacheShape& s = c->shape;
     const int64_t rows = batch * heads, part = cache_part_floats(s.padded);
     SharedSpace x{};
     x.splits = batch > 0 ? cache_shared_splits(s, batch * (heads / s.heads), most_tokens(c, prefix_width), type == LQ_F32, c->sms) : 0;
-    x.own = x.splits * cache_shared_slots(s.padded) * rows * part;
+    x.parts = x.splits > 0 ? (batch * (heads / s.heads) + 127) / 128 * s.heads * (cache_shared_block_bytes(s.padded) / 4) : 0;
+    x.own = x.parts + x.splits * cache_shared_slots(s.padded) * rows * part;
     const int64_t partial = x.own + (table_width > 0 ? rows * part : 0), bytes = workspace_of(c, table_width, 0);
     x.partial = bytes > 0 ? partial : -1;
     x.bytes = partial * 4 + bytes;
@@ -564,11 +565,14 @@ int lq_cache_attend_shared(lq_cache* cache, int32_t layer, const lq_rows* querie
     b.num_pages = num_pages; b.prefix_width = prefix_width; b.prefix_most = most_tokens(cache, prefix_width); b.own_most = most_tokens(cache, table_width);
     b.scale = a.scale; b.batch = a.batch; b.group = a.group; b.splits = space.splits;
     b.two_queries = queries->type == LQ_F32 || rotary != nullptr;
-    b.parts = base + space.parts; b.own = base + space.own;
+    b.rows = reinterpret_cast<char*>(base + space.rows); b.parts = base + space.parts; b.own = base + space.own;
     a.partial = space.partial < 0 ? nullptr : base + space.partial;
     a.sums = b.own; a.before = prefix_length; a.before_most = b.prefix_most; a.lse = nullptr;
     LQ_ON_DEVICE(cache);
-    if (space.splits > 0) LQ_CUDA(launch_cache_shared_prefix(b, (cudaStream_t)stream));
+    if (space.splits > 0) {
+        LQ_CUDA(launch_cache_shared_rows(b, (cudaStream_t)stream));
+        LQ_CUDA(launch_cache_shared_prefix(b, (cudaStream_t)stream));
+    }
     if (table_width > 0) LQ_CUDA(launch_attend(a, (cudaStream_t)stream));
     LQ_CUDA(launch_cache_shared_join(b, (cudaStream_t)stream));
     return LQ_OK;

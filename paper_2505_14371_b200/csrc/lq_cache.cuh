@@ -130,6 +130,7 @@ struct CacheSharedArgs {
     const int32_t* prefix_length;       // dev [1]
     const int32_t* lengths;             // dev [batch]: the sequences' own tokens
     float* lse;
+    char* rows;                         // the queries as the matrix unit reads them (cache_shared_rows_bytes), see lq_cache_shared.cu
     float* parts;                       // [splits][batch][heads * group] parts of the prefix (cache_part_floats)
     float* own;                         // [batch][heads * group] parts of the sequences' own tokens
     uint32_t* flags;
@@ -176,11 +177,14 @@ cudaError_t launch_cache_attend_128(const CacheAttendArgs& a, cudaStream_t s);
 cudaError_t launch_cache_attend_256(const CacheAttendArgs& a, cudaStream_t s);
 cudaError_t launch_cache_bounds(const CacheBoundsArgs& a, cudaStream_t s);
 cudaError_t launch_cache_choose(const CacheChooseArgs& a, cudaStream_t s);
+cudaError_t launch_cache_shared_rows(const CacheSharedArgs& a, cudaStream_t s);
 cudaError_t launch_cache_shared_prefix(const CacheSharedArgs& a, cudaStream_t s);
 cudaError_t launch_cache_shared_join(const CacheSharedArgs& a, cudaStream_t s);
 // Into how many parts the prefix's tokens are split, and how many parts a query may leave (a CTA of rows of 64 and 128 leaves two, see there).
 int cache_shared_splits(const CacheShape& shape, int64_t rows, int64_t prefix_tokens, bool exact, int sms);
 __host__ __device__ constexpr int cache_shared_slots(int padded) { return padded == 256 ? 1 : 2; }
+// Workspace for a head's block of 128 rows: fp16 numbers, what their rounding left, a factor for each row.
+__host__ __device__ constexpr int cache_shared_block_bytes(int padded) { return 128 * (4 * padded + 4); }
 // Teams of 8 warps that share an SM in the attention kernel (its registers: rows of 256 need twice as many a thread), and what
 // each may leave in the workspace: a record, then two partial sums of 8 queries.
 __host__ __device__ constexpr int cache_attend_teams(int padded) { return padded == 256 ? 1 : 2; }

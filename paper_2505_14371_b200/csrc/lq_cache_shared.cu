@@ -3,7 +3,7 @@
 // Mathematics: that of lq_cache_attend.cuh.  With c_j = (2^e q) . level(K_j) and f = scale log2(e) / 2^e
 //   d_j = (c_j f) N_j - ref,  p_j = exp2(d_j),  w_j = p_j M_j 2^(6 - k),  out = 2^(k - 6) sum_j w_j level(V_j) / sum_j p_j,
 // N and M the keys' and values' norms, ref a running reference of the scores and k a whole number, the running scale of the weights: both
-// move, and the sums with them, only when a score passes its reference by 8 powers of two, or a weight its scale.  Scores, p, w and all
+// move, and the sums with them, only when a tile's p add up to 2^16 or a weight passes 2^14.  Scores, p, w and all
 // sums are fp32.  Levels are fp16 as they stand.  Roundings to fewer bits: q as fp16 after a power of two (exact for fp16 and bf16;
 // rotated and fp32 ones as a sum of two, 22 bits); w as fp16 for bf16 outputs (11 bits, an eighth of the output's own rounding), as a sum of
 // two for fp16 and fp32 ones (22 bits).
@@ -38,7 +38,7 @@ constexpr int kTableAt = 1 << 16, kTableBytes = 256 * 256, kSystemBytes = 1 << 1
 constexpr int kHighAt = kTableAt + kTableBytes;
 constexpr int kPanelQ = kRows * 128, kPanel = kTile * 128;      // bytes of 64 coordinates of a block's rows, of a tile's
 constexpr float kLow = -3.402823466e38f;
-constexpr float kSlack = 8.0f;
+constexpr float kRoom = 65536.0f, kMostWeight = 16384.0f;
 constexpr int kLift = 6;
 constexpr int kColumns = 512;           // of tensor memory: all (one CTA an SM)
 
@@ -47,8 +47,11 @@ template <int P>
 struct Layout {
     static constexpr int kSlots = cache_shared_slots(P), kPanels = P / 64, kPiece = P * 128;
     static constexpr int kStages = P == 256 ? 1 : 2;
-    static constexpr int kThreads = 128 * kSlots + kDecode + 32;
-    static constexpr int kDecodeAt = 4 * kSlots, kIssuer = kDecodeAt + kDecodeWarps;    // warps
+    static constexpr int kThreads = 128 * kSlots + kDecode + 128;
+    static constexpr int kDecodeAt = 4 * kSlots, kIssuer = kDecodeAt + kDecodeWarps;    // warps (three behind the issuer have nothing to do)
+    // Registers a thread at launch, and as they are dealt out to softmax, decoding and products: no more than all threads had.
+    static constexpr int kRegisters = kSlots == 2 ? 96 : 128, kSoftmax = kSlots == 2 ? 144 : 208, kDecoding = kSlots == 2 ? 72 : 120, kProducts = 40;
+    static_assert(128 * kSlots * kSoftmax + kDecode * kDecoding + 128 * kProducts <= kThreads * kRegisters && kThreads * kRegisters <= 65536, "registers");
     static constexpr int kQueries = kSlots * kPanels * kPanelQ;
     static constexpr int kLowPieces = P == 64 ? 4 : P == 128 ? 3 : 1;
     static constexpr int kSmallAt = kSystemBytes + kLowPieces * kPiece;
@@ -58,20 +61,15 @@ struct Layout {
         return i < kLowPieces ? kSystemBytes + i * kPiece : kHighAt + kQueries + (i - kLowPieces) * kPiece;
     }
     static __device__ __forceinline__ uint32_t queries(int slot, int panel) { return kHighAt + (slot * kPanels + panel) * kPanelQ; }
-    // what the queries' rounding leaves, before it goes to tensor memory: in the pieces' place
-    static __device__ __forceinline__ uint32_t rests(int slot, int panel)
-    {
-        const int at = (slot * kPanels + panel) * kPanelQ;
-        return piece(at / kPiece) + at % kPiece;
-    }
     // tensor memory, columns of a slot
     static constexpr int kScores = 0, kSums = kTile, kRests = kTile + P, kSlotColumns = kTile + P + P / 2;
-    static_assert(kSlots * kSlotColumns <= kColumns && kEnd <= 227 << 10 && kSlots * kPanels * kPanelQ <= 2 * kStages * kPiece, "places");
+    static_assert(kSlots * kSlotColumns <= kColumns && kEnd <= 227 << 10, "places");
 };
 
 struct Small {
     uint64_t full[2], empty[2];         // a stage holds a tile; has been read
     uint64_t scored[2], weighed[2], summed[2];          // of a slot: its scores are there, its weights, its sums
+    uint64_t brought;                   // the queries are there
     uint64_t drained;
     uint32_t tensor;                    // address of tensor memory
     uint32_t failed;
@@ -79,7 +77,6 @@ struct Small {
     int32_t exponent[2];                // of a stage: what the values' norms are divided by
     alignas(16) float keys[2][kTile];   // norms
     alignas(16) float values[2][kTile];
-    float factor[2 * kRows];
 };
 
 // ---- instructions ----------------------------------------------------------------------------------------------
@@ -123,7 +120,8 @@ __device__ __forceinline__ void loaded() { asm volatile("tcgen05.wait::ld.sync.a
 __device__ __forceinline__ void stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void commit(uint64_t* b)
 {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" :: "r"(address_of(b)) : "memory");
+    asm volatile("{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\t"
+                 "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" :: "r"(address_of(b)) : "memory");
 }
 
 // 32 columns of this warp's 32 lanes.
@@ -137,6 +135,14 @@ __device__ __forceinline__ void tensor_load32(uint32_t (&v)[32], uint32_t at)
                    "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
                  : "r"(at) : "memory");
 }
+// 32 columns of 16 lanes, by 8: registers 4 j and 4 j + 1 of lane l hold columns 8 j + 2 (l % 4) and the next of lane l / 4, the two behind those of lane l / 4 + 8.
+__device__ __forceinline__ void tensor_load_rows(uint32_t (&v)[16], uint32_t at)
+{
+    asm volatile("tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]),
+                   "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+                 : "r"(at) : "memory");
+}
 __device__ __forceinline__ void tensor_store32(uint32_t at, const uint32_t (&v)[32])
 {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,"
@@ -147,6 +153,13 @@ __device__ __forceinline__ void tensor_store32(uint32_t at, const uint32_t (&v)[
                     "r"(v[30]), "r"(v[31])
                  : "memory");
 }
+
+// The products and their commits are given by a whole warp, whose elected lane (always the same one) issues them: what they are given is then the
+// same in all lanes.
+template <int kRegisters>
+__device__ __forceinline__ void give_up_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(kRegisters)); }
+template <int kRegisters>
+__device__ __forceinline__ void take_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" :: "n"(kRegisters)); }
 
 // Operand in shared memory, swizzled by 128 bytes.  K along the rows of 128 bytes: rows in groups of 8, 1024 bytes apart.  N along them
 // (tokens outermost): the next 64 coordinates are a panel further, the next 8 tokens 1024 bytes.
@@ -159,12 +172,14 @@ __host__ __device__ constexpr uint32_t instruction(int n, bool n_outermost) { re
 
 __device__ __forceinline__ void multiply(uint32_t sums, uint64_t a, uint64_t b, uint32_t how, bool add)
 {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+    asm volatile("{\n\t.reg .pred p, q;\n\telect.sync _|q, 0xffffffff;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+                 "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
                  :: "r"(sums), "l"(a), "l"(b), "r"(how), "r"((uint32_t)add) : "memory");
 }
 __device__ __forceinline__ void multiply_tensor(uint32_t sums, uint32_t a, uint64_t b, uint32_t how, bool add)
 {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+    asm volatile("{\n\t.reg .pred p, q;\n\telect.sync _|q, 0xffffffff;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+                 "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
                  :: "r"(sums), "r"(a), "l"(b), "r"(how), "r"((uint32_t)add) : "memory");
 }
 
@@ -194,13 +209,105 @@ __device__ __forceinline__ void store16(uint32_t at, uint32_t a, uint32_t b, uin
 {
     asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" :: "r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
-__device__ __forceinline__ void store2(uint32_t at, __half v)
+
+// ---- the queries -----------------------------------------------------------------------------------------------
+
+// Row i of a head's block b is query r % group of sequence r / group, r = 128 b + i.  The queries go to the workspace first, once for all CTAs that
+// take them: turned, times a power of two, as fp16 in the place that the matrix unit expects (panels of 64 coordinates, swizzled), what that
+// rounding left in rows, and the factors.  (Each CTA for itself: 300 instructions a row, 18 us for two blocks.)  Rows without a query are zeros.
+template <int P>
+__device__ __forceinline__ char* block_at(const CacheSharedArgs& a, int head, int block)
 {
-    asm volatile("st.shared.b16 [%0], %1;" :: "r"(at), "h"(__half_as_ushort(v)) : "memory");
+    const int64_t blocks = ((int64_t)a.batch * a.group + kRows - 1) / kRows;
+    return a.rows + (head * blocks + block) * cache_shared_block_bytes(P);
 }
 
-// Where coordinate d of row r stands in a panel of rows of 128 bytes.
+// Where chunk `chunk` of 16 bytes of row r stands in a panel of rows of 128 bytes.
 __device__ __forceinline__ uint32_t swizzled(int r, int chunk) { return (uint32_t)(r * 128 + ((chunk ^ (r & 7)) << 4)); }
+
+constexpr int kRowWarps = 8;
+
+template <int P, bool kFloat>
+__global__ void __launch_bounds__(32 * kRowWarps) shared_rows_kernel(const __grid_constant__ CacheSharedArgs a)
+{
+    constexpr int kEach = P / 32;                               // coordinates of a lane, side by side
+    pdl_wait();
+    pdl_launch_next();
+    const int lane = threadIdx.x & 31, d0 = lane * kEach, all = a.batch * a.group, padded = (all + kRows - 1) / kRows * kRows;      // (at most 2^26)
+    const int64_t item = (int64_t)blockIdx.x * kRowWarps + (threadIdx.x >> 5);
+    const int head = (int)(item / padded), row = (int)(item - (int64_t)head * padded);
+    if (head >= a.shape.heads) return;
+    const bool live = row < all;
+    const int sequence = live ? row / a.group : 0, query = live ? row - sequence * a.group : 0;
+    const CacheRotary& r = a.rotary;
+    const int half = r.dim / 2;
+    const float* angles = r.table;
+    bool lost = false;
+    if (r.table && live) {
+        int64_t at;
+        if (r.at) {
+            at = r.at[sequence];
+        } else {
+            const int64_t before = min((int64_t)max(*a.prefix_length, 0), a.prefix_most), own = min((int64_t)max(a.lengths[sequence], 0), a.own_most);
+            at = max(before + own - 1, (int64_t)0);
+        }
+        lost = at < 0 || at >= r.positions;
+        if (lost) { if (lane == 0) atomicOr(a.flags, LQ_CACHE_BAD_POSITION); }
+        else angles += at * r.dim;
+    }
+    const char* const from = static_cast<const char*>(a.queries.data) + (int64_t)sequence * a.queries.token_bytes + (int64_t)(head * a.group + query) * a.queries.head_bytes;
+    using Raw = std::conditional_t<kFloat, float, unsigned short>;      // (what its bits mean is looked at when all loads are under way)
+    Raw x[kEach], u[kEach];
+    float c[kEach], t[kEach];
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+        const int d = d0 + e;
+        const bool there = live && d < a.shape.dim, turned = there && r.table && !lost && d < r.dim;
+        const int other = r.interleaved ? d ^ 1 : d < half ? d + half : d - half, p = r.interleaved ? d >> 1 : d < half ? d : d - half;
+        x[e] = there ? reinterpret_cast<const Raw*>(from)[d] : (Raw)0;
+        u[e] = turned ? reinterpret_cast<const Raw*>(from)[other] : (Raw)0;
+        c[e] = turned ? angles[p] : 1.0f;
+        t[e] = turned ? angles[half + p] : 0.0f;
+    }
+    auto number = [&](Raw v) -> float {
+        if constexpr (kFloat) return v;
+        else return a.queries.type == LQ_BF16 ? __uint_as_float((uint32_t)v << 16) : __half2float(__ushort_as_half(v));
+    };
+    float y[kEach];
+    uint32_t top = 0;
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+        const int d = d0 + e;
+        y[e] = number(x[e]);
+        if (live && r.table && !lost && d < min(r.dim, a.shape.dim)) {
+            const bool lower = r.interleaved ? d % 2 == 0 : d < half;
+            const float z = number(u[e]);
+            y[e] = lower ? __fsub_rn(__fmul_rn(y[e], c[e]), __fmul_rn(z, t[e])) : __fadd_rn(__fmul_rn(y[e], c[e]), __fmul_rn(z, t[e]));
+        }
+        if (lost) y[e] = __uint_as_float(0x7fffffffu);
+        top = max(top, __float_as_uint(y[e]) & 0x7fffffffu);
+    }
+    top = __reduce_max_sync(0xffffffffu, top);
+    // 2^e brings the largest coordinate to [2^14, 2^15); Inf and NaN stay what they are
+    const int up = min(top >= 0x7f800000u || top == 0 ? 0 : 141 - (int)(top >> 23), 120);
+    uint32_t h[kEach / 2], rest[kEach / 2];
+#pragma unroll
+    for (int e = 0; e < kEach; e += 2) {
+        const float z = y[e] * power(up), w = y[e + 1] * power(up);
+        h[e / 2] = halves(z, w);
+        rest[e / 2] = rest_of(h[e / 2], z, w);
+    }
+    char* const to = block_at<P>(a, head, row / kRows);
+    const int place = row % kRows;
+    auto store = [&](char* at, const uint32_t (&v)[kEach / 2]) {
+        if constexpr (kEach == 2) *reinterpret_cast<uint32_t*>(at) = v[0];
+        else if constexpr (kEach == 4) *reinterpret_cast<uint2*>(at) = make_uint2(v[0], v[1]);
+        else *reinterpret_cast<uint4*>(at) = make_uint4(v[0], v[1], v[2], v[3]);
+    };
+    store(to + (d0 >> 6) * kPanelQ + swizzled(place, (d0 & 63) >> 3) + (d0 & 7) * 2, h);
+    store(to + 2 * P * kRows + place * 2 * P + d0 * 2, rest);
+    if (lane == 0) reinterpret_cast<float*>(to + 4 * P * kRows)[place] = a.scale * power(-up);
+}
 
 // ---- a CTA's share ---------------------------------------------------------------------------------------------
 
@@ -223,166 +330,129 @@ __device__ __forceinline__ Share share_of(const CacheSharedArgs& a)
     s.pair = kSlots == 2 && s.block + 1 < blocks;
     const int given = *a.prefix_length;
     s.length = given < 0 ? 0 : given > a.prefix_most ? a.prefix_most : given;
-    if (given != s.length && blockIdx.x == 0 && threadIdx.x == 0) atomicOr(a.flags, LQ_CACHE_BAD_LENGTH);
     const int64_t all = (s.length + kTile - 1) / kTile;
     s.tile0 = (int)(all * split / a.splits);
     s.tiles = (int)(all * (split + 1) / a.splits) - s.tile0;
     return s;
 }
 
-// Row `row` of a head: query row % group of sequence row / group.  A warp brings it into shared memory: times its power of two, as fp16 and the rest.
-template <int P>
-__device__ __forceinline__ void bring_query(const CacheSharedArgs& a, const Share& s, Small& sm, int slot, int place, int lane)
-{
-    using L = Layout<P>;
-    const int64_t row = (int64_t)(s.block + slot) * kRows + place;
-    const bool live = row < (int64_t)a.batch * a.group;
-    float x[P / 32];
-    bool lost = false;
-#pragma unroll
-    for (int i = 0; i < P / 32; ++i) x[i] = 0.0f;
-    if (live) {
-        const int sequence = (int)(row / a.group), query = (int)(row - (int64_t)sequence * a.group);
-        const char* from = static_cast<const char*>(a.queries.data) + (int64_t)sequence * a.queries.token_bytes +
-                           (int64_t)(s.head * a.group + query) * a.queries.head_bytes;
-        auto number = [&](int d) -> float {
-            if (a.queries.type == LQ_F32) return reinterpret_cast<const float*>(from)[d];
-            if (a.queries.type == LQ_F16) return __half2float(reinterpret_cast<const __half*>(from)[d]);
-            return __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(from)[d]);
-        };
-        const CacheRotary& r = a.rotary;
-        const float* angles = r.table;
-        if (r.table) {
-            int64_t at;
-            if (r.at) {
-                at = r.at[sequence];
-            } else {
-                const int n = a.lengths[sequence];
-                const int64_t last = s.length + (n < 0 ? 0 : n > a.own_most ? a.own_most : n);
-                at = last > 0 ? last - 1 : 0;
-            }
-            lost = at < 0 || at >= r.positions;
-            if (lost) { if (lane == 0) atomicOr(a.flags, LQ_CACHE_BAD_POSITION); }
-            else angles += at * r.dim;
-        }
-        const int half = r.dim / 2;
-#pragma unroll
-        for (int i = 0; i < P / 32; ++i) {
-            const int d = lane + 32 * i;
-            x[i] = d < a.shape.dim ? number(d) : 0.0f;
-            if (r.table && !lost && d < r.dim) {
-                const bool lower = r.interleaved ? d % 2 == 0 : d < half;
-                const int p = r.interleaved ? d / 2 : d < half ? d : d - half;
-                const float u = number(r.interleaved ? d ^ 1 : lower ? d + half : d - half), c = angles[p], t = angles[half + p];
-                x[i] = lower ? __fsub_rn(__fmul_rn(x[i], c), __fmul_rn(u, t)) : __fadd_rn(__fmul_rn(x[i], c), __fmul_rn(u, t));
-            }
-            if (lost) x[i] = __uint_as_float(0x7fffffffu);
-        }
-    }
-    uint32_t top = 0;
-#pragma unroll
-    for (int i = 0; i < P / 32; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
-    top = __reduce_max_sync(0xffffffffu, top);
-    // 2^e brings the largest coordinate to [2^14, 2^15); Inf and NaN stay what they are
-    const int e = min(top >= 0x7f800000u || top == 0 ? 0 : 141 - (int)(top >> 23), 120);
-#pragma unroll
-    for (int i = 0; i < P / 32; ++i) {
-        const int d = lane + 32 * i;
-        const float y = x[i] * power(e);
-        const __half h = __float2half_rn(y);
-        const uint32_t at = swizzled(place, (d & 63) >> 3) + (d & 7) * 2;
-        store2(L::queries(slot, d >> 6) + at, h);
-        if (a.two_queries) store2(L::rests(slot, d >> 6) + at, __float2half_rn(y - __half2float(h)));
-    }
-    if (lane == 0) sm.factor[slot * kRows + place] = a.scale * power(-e);
-}
-
 // ---- decoding --------------------------------------------------------------------------------------------------
 
-// Symbols of 8 coordinates of a thread's rows of a tile, and what one warp brings of its norms.
+// A thread decodes 64 coordinates of a token at a time, a row of 128 bytes of a panel: lanes have tokens in a row, so that their stores, swizzled, meet
+// every bank.  A warp's are all keys or all values.
 template <int P>
 struct Codes {
-    static constexpr int kEach = kTile * (P / 8) / kDecode;     // rows (of keys, and of values) that a thread has 8 coordinates of
-    uint2 w[2][kEach];
-    float keys[2], values[2];
+    static constexpr int kItems = 2 * (P / 64) * (kTile / 32);          // of 32 tokens
+    static constexpr int kEach = (kItems + kDecodeWarps - 1) / kDecodeWarps;
+    uint32_t w[kEach][16];              // (symbols of 4 bits: 8 words)
+    float keys[2], values[2];           // norms, brought by one warp
     uint32_t seen;                      // bit i: the tile's i-th 16 tokens are on a page that is there
 };
 
-// The page of 16 of a tile's tokens, by lanes 0 to 3; -1 past the end.
+template <int P>
+__device__ __forceinline__ void item_of(int i, int& kind, int& panel, int& token)
+{
+    kind = i / (Codes<P>::kItems / 2);
+    panel = i / (kTile / 32) % (P / 64);
+    token = i % (kTile / 32) * 32;
+}
+
+// The page of 16 of a tile's tokens, by lanes 0 to 3, as the table has it (no look is taken at it before it is used).
 __device__ __forceinline__ int page_of(const CacheSharedArgs& a, const Share& s, int tile, bool inside, int lane)
 {
     const int64_t token = (int64_t)(s.tile0 + tile) * kTile + 16 * lane;
-    if (!inside || lane >= kTile / 16 || token >= s.length) return -1;
-    const int page = a.prefix[token >> a.shape.page_shift];
-    if (page < 0 || page >= a.num_pages) {
-        atomicOr(a.flags, LQ_CACHE_BAD_PAGE);
-        return -1;
-    }
-    return page;
+    return inside && lane < kTile / 16 && token < s.length ? a.prefix[token >> a.shape.page_shift] : -1;
 }
 
-template <int P>
-__device__ __forceinline__ void fetch(Codes<P>& c, const CacheSharedArgs& a, const Share& s, int tile, int page, int tid)
+__device__ __forceinline__ void load32(uint32_t* v, const char* from)
 {
-    const int lane = tid & 31, mask = (1 << a.shape.page_shift) - 1;
-    const int64_t first = (int64_t)(s.tile0 + tile) * kTile;
-    c.seen = __ballot_sync(0xffffffffu, page >= 0) & 15u;
+    asm volatile("ld.global.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "l"(from) : "memory");
+    asm volatile("ld.global.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]) : "l"(from + 16) : "memory");
+}
+
+// Where there is no page, the level tables are read instead (any numbers will do: the token is not seen): nothing then waits for a load here.
+template <int P>
+__device__ __forceinline__ void fetch(Codes<P>& c, const CacheSharedArgs& a, const Share& s, int tile, int page, int warp, int lane)
+{
+    const int mask = (1 << a.shape.page_shift) - 1;
+    const int row0 = (s.tile0 + tile) * kTile & mask;
+    const bool there = (uint32_t)page < (uint32_t)a.num_pages;
+    c.seen = __ballot_sync(0xffffffffu, there) & 15u;
+    if (c.seen != 15u && lane < kTile / 16 && !there && (int64_t)(s.tile0 + tile) * kTile + 16 * lane < s.length) atomicOr(a.flags, LQ_CACHE_BAD_PAGE);
     const uint32_t values_at = (uint32_t)a.shape.row_words[0] << a.shape.page_shift, norms_at = values_at + ((uint32_t)a.shape.row_words[1] << a.shape.page_shift);
-    auto head_of = [&](int p) { return a.pages + (int64_t)p * a.shape.page_words + (int64_t)s.head * a.shape.head_words; };
+    const char* const pages = reinterpret_cast<const char*>(a.pages + (int64_t)s.head * a.shape.head_words);
+    const uint32_t page_bytes = 4u * (uint32_t)a.shape.page_words;
 #pragma unroll
     for (int k = 0; k < Codes<P>::kEach; ++k) {
-        const int unit = tid + kDecode * k, token = unit / (P / 8), col = unit % (P / 8);
-        const int p = __shfl_sync(0xffffffffu, page, token >> 4);
-        c.w[0][k] = c.w[1][k] = make_uint2(0, 0);
-        if (p >= 0) {
-            const uint32_t* base = head_of(p);
-            const int row = (int)((first + token) & mask);
-            const uint32_t* keys = base + row * a.shape.row_words[0];
-            const uint32_t* values = base + values_at + row * a.shape.row_words[1];
-            if (a.shape.sym_bits[0] == 8) c.w[0][k] = reinterpret_cast<const uint2*>(keys)[col]; else c.w[0][k].x = keys[col];
-            if (a.shape.sym_bits[1] == 8) c.w[1][k] = reinterpret_cast<const uint2*>(values)[col]; else c.w[1][k].x = values[col];
-        }
+        const int i = warp + kDecodeWarps * k;
+        if (i >= Codes<P>::kItems) break;
+        int kind, panel, token;
+        item_of<P>(i, kind, panel, token);
+        token += lane;
+        const int p = __shfl_sync(0xffffffffu, page, token >> 4), bits = kind ? a.shape.sym_bits[1] : a.shape.sym_bits[0];
+        const uint32_t words = kind ? a.shape.row_words[1] : a.shape.row_words[0];
+        const uint32_t at = 4u * ((kind ? values_at : 0u) + (uint32_t)((row0 + token) & mask) * words) + (uint32_t)(panel * 8 * bits);
+        const char* from = pages + (uint64_t)(uint32_t)p * page_bytes + at;
+        from = (uint32_t)p < (uint32_t)a.num_pages ? from : reinterpret_cast<const char*>(a.tables);
+        load32(c.w[k], from);
+        if (bits == 8) load32(c.w[k] + 8, from + 32);
     }
-    if (tid < 32) {
+    if (warp == kDecodeWarps - 1) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const int token = lane + 32 * i, p = __shfl_sync(0xffffffffu, page, token >> 4);
-            c.keys[i] = c.values[i] = 0.0f;
-            if (p >= 0) {
-                const float* norms = reinterpret_cast<const float*>(head_of(p) + norms_at) + ((first + token) & mask);
-                c.keys[i] = norms[0];
-                c.values[i] = norms[mask + 1];
-            }
+            const float* norms = reinterpret_cast<const float*>(pages + (uint64_t)(uint32_t)p * page_bytes) + norms_at + ((row0 + token) & mask);
+            norms = (uint32_t)p < (uint32_t)a.num_pages ? norms : a.tables->levels;
+            c.keys[i] = norms[0];
+            c.values[i] = norms[(uint32_t)p < (uint32_t)a.num_pages ? mask + 1 : 0];
         }
     }
 }
 
 template <int P>
-__device__ __forceinline__ void decode(const Codes<P>& c, const CacheSharedArgs& a, const Share& s, Small& sm, int tile, int stage, int tid)
+__device__ __forceinline__ void decode(const Codes<P>& c, const CacheSharedArgs& a, const Share& s, Small& sm, int tile, int stage, int warp, int lane)
 {
     using L = Layout<P>;
-    const int lane = tid & 31;
-    const uint32_t base = kTableAt + 4 * lane;
 #pragma unroll
-    for (int kind = 0; kind < 2; ++kind) {
-        const uint32_t piece = L::piece(2 * stage + kind), copies = base + 128 * kind;
-        const bool fine = a.shape.sym_bits[kind] == 8;
+    for (int k = 0; k < Codes<P>::kEach; ++k) {
+        const int i = warp + kDecodeWarps * k;
+        if (i >= Codes<P>::kItems) break;
+        int kind, panel, token;
+        item_of<P>(i, kind, panel, token);
+        token += lane;
+        const uint32_t row = L::piece(2 * stage + kind) + panel * kPanel + token * 128, copies = kTableAt + 4 * lane + 128 * kind;
+        const uint32_t turn = (token & 7) << 4;
+        const uint32_t (&w)[16] = c.w[k];
+        // (16 look-ups before their stores: the compiler moves no load of shared memory above a store)
+        if ((kind ? a.shape.sym_bits[1] : a.shape.sym_bits[0]) == 8) {
+            auto two = [](uint32_t x, uint32_t y) { return __byte_perm(x, y, 0x5410); };
 #pragma unroll
-        for (int k = 0; k < Codes<P>::kEach; ++k) {
-            const int unit = tid + kDecode * k, token = unit / (P / 8), col = unit % (P / 8);
-            const uint2 w = c.w[kind][k];
-            uint32_t v[4];
-            if (fine) {
-                auto two = [](uint32_t x, uint32_t y) { return __byte_perm(x, y, 0x5410); };
-                v[0] = two(look<0>(w.x, copies), look<1>(w.x, copies)); v[1] = two(look<2>(w.x, copies), look<3>(w.x, copies));
-                v[2] = two(look<0>(w.y, copies), look<1>(w.y, copies)); v[3] = two(look<2>(w.y, copies), look<3>(w.y, copies));
-            } else {
-                v[0] = look<0>(w.x, copies); v[1] = look<1>(w.x, copies); v[2] = look<2>(w.x, copies); v[3] = look<3>(w.x, copies);
+            for (int j = 0; j < 8; j += 2) {
+                uint32_t v[8];
+#pragma unroll
+                for (int m = 0; m < 4; ++m) {
+                    const uint32_t x = w[2 * j + m];
+                    v[2 * m] = two(look<0>(x, copies), look<1>(x, copies));
+                    v[2 * m + 1] = two(look<2>(x, copies), look<3>(x, copies));
+                }
+                store16(row + ((16 * j) ^ turn), v[0], v[1], v[2], v[3]);
+                store16(row + ((16 * j + 16) ^ turn), v[4], v[5], v[6], v[7]);
             }
-            store16(piece + (col >> 3) * kPanel + swizzled(token, col & 7), v[0], v[1], v[2], v[3]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; j += 4) {
+                uint32_t v[4][4];
+#pragma unroll
+                for (int m = 0; m < 4; ++m) {
+                    v[m][0] = look<0>(w[j + m], copies); v[m][1] = look<1>(w[j + m], copies);
+                    v[m][2] = look<2>(w[j + m], copies); v[m][3] = look<3>(w[j + m], copies);
+                }
+#pragma unroll
+                for (int m = 0; m < 4; ++m) store16(row + ((16 * (j + m)) ^ turn), v[m][0], v[m][1], v[m][2], v[m][3]);
+            }
         }
     }
-    if (tid < 32) {
+    if (warp == kDecodeWarps - 1) {
         const int64_t first = (int64_t)(s.tile0 + tile) * kTile;
         uint32_t seen[2];
         int most = -127;
@@ -427,108 +497,190 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
     return v;
 }
 
-// The scores of a tile become weights, in their place.  `sums`: this slot's, moved where reference or scale moves; `none`: there are none yet.
+// 32 of a tile's scores of this row become distances from the reference (base-2 exponents); those not seen -infinity.
+__device__ __forceinline__ void distances(float (&d)[32], const uint32_t (&v)[32], const Row& row, const Small& sm, int stage, int half, bool whole)
+{
+    const uint64_t f2 = pair_of(row.f, row.f), minus = pair_of(-row.ref, -row.ref);
+#pragma unroll
+    for (int j = 0; j < 32; j += 4) {
+        const float4 n = *reinterpret_cast<const float4*>(&sm.keys[stage][32 * half + j]);
+        parted(fma2(mul2(pair_of(__uint_as_float(v[j]), __uint_as_float(v[j + 1])), f2), pair_of(n.x, n.y), minus), d[j], d[j + 1]);
+        parted(fma2(mul2(pair_of(__uint_as_float(v[j + 2]), __uint_as_float(v[j + 3])), f2), pair_of(n.z, n.w), minus), d[j + 2], d[j + 3]);
+    }
+    if (!whole) {
+        const uint32_t seen = sm.seen[stage][half];
+#pragma unroll
+        for (int j = 0; j < 32; ++j) if (!(seen >> j & 1)) d[j] = -INFINITY;
+    }
+}
+
+// Reference and scale of the rows of a warp as this tile wants them, and the sums moved along (`none`: there are none yet).
+template <int P>
+__device__ __noinline__ Row moved_row(Row row, const Small& sm, int stage, uint32_t scores, uint32_t sums, bool none, bool whole)
+{
+    float most = -INFINITY;
+    bool none_such = false;             // a score that is not a number: nothing is gained by waiting for a better one
+#pragma unroll 1
+    for (int half = 0; half < 2; ++half) {
+        uint32_t v[32];
+        float d[32];
+        tensor_load32(v, scores + 32 * half);
+        loaded();
+        distances(d, v, row, sm, stage, half, whole);
+#pragma unroll
+        for (int j = 0; j < 32; ++j) { most = fmaxf(most, d[j]); none_such = none_such || d[j] != d[j]; }
+    }
+    const float step = row.begun ? fmaxf(most, 0.0f) : most;
+    float moved = 0.0f;
+    if (step > -INFINITY) {
+        const float ref = row.ref + step;
+        moved = row.ref - ref;
+        row.ref = ref;
+        if (row.begun) row.total *= ex2(moved);
+    }
+    float heavy = 0.0f;
+#pragma unroll 1
+    for (int half = 0; half < 2; ++half) {
+        uint32_t v[32];
+        float d[32];
+        tensor_load32(v, scores + 32 * half);
+        loaded();
+        distances(d, v, row, sm, stage, half, whole);
+#pragma unroll
+        for (int j = 0; j < 32; ++j) heavy = fmaxf(heavy, ex2(d[j]) * sm.values[stage][32 * half + j]);
+    }
+    // the largest weight is 2^(exponent + e) or up to twice that; the scale's fraction, where the reference moved by one, is left to the factor
+    const int exponent = sm.exponent[stage], e = exponent_of(heavy);
+    int scale = max(exponent + e, exponent - 114);
+    if (row.begun) scale = max(scale, (int)floorf(fmaxf((float)row.scale + moved, -1000.0f)));
+    const float factor = row.begun ? ex2(moved + (float)(row.scale - scale)) : 0.0f;
+    row.scale = scale;
+    row.begun = row.begun || most > -INFINITY || none_such;
+    if (!none) {
+#pragma unroll 1
+        for (int c = 0; c < P; c += 32) {
+            uint32_t v[32];
+            tensor_load32(v, sums + c);
+            loaded();
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * factor);
+            tensor_store32(sums + c, v);
+        }
+        stored();
+    }
+    return row;
+}
+
+// The scores of a tile become weights, in their place: in one pass with reference and scale as they are, and once more if that shows that they have to move
+// (p is fp32 and has room: its sum may grow to 2^kRoom; a weight is fp16, up to 2^(kSlack + kLift)).
 template <int P, bool kTwo>
 __device__ __forceinline__ void weigh_tile(Row& row, const Small& sm, int stage, uint32_t scores, uint32_t sums, bool none)
 {
-    float d[kTile];
-    {
-        uint32_t (&lo)[32] = *reinterpret_cast<uint32_t (*)[32]>(&d[0]);
-        uint32_t (&hi)[32] = *reinterpret_cast<uint32_t (*)[32]>(&d[32]);
-        tensor_load32(lo, scores);
-        tensor_load32(hi, scores + 32);
-        loaded();
-    }
-    const uint64_t f2 = pair_of(row.f, row.f), minus = pair_of(-row.ref, -row.ref);
-#pragma unroll
-    for (int j = 0; j < kTile; j += 4) {
-        const float4 n = *reinterpret_cast<const float4*>(&sm.keys[stage][j]);
-        parted(fma2(mul2(pair_of(d[j], d[j + 1]), f2), pair_of(n.x, n.y), minus), d[j], d[j + 1]);
-        parted(fma2(mul2(pair_of(d[j + 2], d[j + 3]), f2), pair_of(n.z, n.w), minus), d[j + 2], d[j + 3]);
-    }
-    const uint32_t seen0 = sm.seen[stage][0], seen1 = sm.seen[stage][1];
-    if ((seen0 & seen1) != 0xffffffffu) {
-#pragma unroll
-        for (int j = 0; j < 32; ++j) {
-            if (!(seen0 >> j & 1)) d[j] = -INFINITY;
-            if (!(seen1 >> j & 1)) d[32 + j] = -INFINITY;
-        }
-    }
-    float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-    for (int j = 0; j < kTile; j += 8)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) top[i] = fmaxf(top[i], fmaxf(d[j + i], d[j + 4 + i]));
-    const float most = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
-    float moved = 0.0f;
-    if (__any_sync(0xffffffffu, most > kSlack || !row.begun)) {
-        const float step = row.begun ? fmaxf(most, 0.0f) : most;
-        if (step > -INFINITY) {
-            const float ref = row.ref + step;
-            moved = row.ref - ref;
-            row.ref = ref;
-#pragma unroll
-            for (int j = 0; j < kTile; ++j) d[j] += moved;
-            if (row.begun) row.total *= ex2(moved);
-        }
-    }
-    uint64_t total[2] = {0, 0};
-    float heavy[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-    for (int j = 0; j < kTile; j += 4) {
-        const float4 m = *reinterpret_cast<const float4*>(&sm.values[stage][j]);
-        const uint64_t p = pair_of(ex2(d[j]), ex2(d[j + 1])), q = pair_of(ex2(d[j + 2]), ex2(d[j + 3]));
-        total[0] = add2(total[0], p);
-        total[1] = add2(total[1], q);
-        parted(mul2(p, pair_of(m.x, m.y)), d[j], d[j + 1]);
-        parted(mul2(q, pair_of(m.z, m.w)), d[j + 2], d[j + 3]);
-        heavy[0] = fmaxf(heavy[0], fmaxf(d[j], d[j + 1]));
-        heavy[1] = fmaxf(heavy[1], fmaxf(d[j + 2], d[j + 3]));
-    }
-    {
-        float x, y;
-        parted(add2(total[0], total[1]), x, y);
-        row.total += x + y;
-    }
-    // the largest weight is 2^(exponent + e) or twice that
-    const int exponent = sm.exponent[stage], e = exponent_of(fmaxf(heavy[0], heavy[1]));
-    const bool over = exponent + e >= row.scale + (int)kSlack || exponent - row.scale > 114 || !row.begun;
-    if (__any_sync(0xffffffffu, over || moved != 0.0f)) {
-        // (an exponent's difference is whole but for `moved`, whose fraction the scale's rounding down leaves to the factor)
-        float factor = 1.0f;
-        if (over || moved != 0.0f) {
-            int scale = max(exponent + e, exponent - 114);
-            if (row.begun) scale = max(scale, (int)floorf(fmaxf((float)row.scale + moved, -1000.0f)));
-            factor = row.begun ? ex2(moved + (float)(row.scale - scale)) : 0.0f;
-            row.scale = scale;
-            row.begun = row.begun || most > -INFINITY;
-        }
-        if (!none) {
+    const bool whole = (sm.seen[stage][0] & sm.seen[stage][1]) == 0xffffffffu;
+    if (__any_sync(0xffffffffu, !row.begun)) row = moved_row<P>(row, sm, stage, scores, sums, none, whole);
+    uint32_t w[32], rest[kTwo ? 32 : 1];
+    float sum;
 #pragma unroll 1
-            for (int c = 0; c < P; c += 32) {
-                uint32_t v[32];
-                tensor_load32(v, sums + c);
-                loaded();
+    for (int tries = 0;; ++tries) {
+        // (a scale far below the tile's norms would be no power of two: then it moves)
+        const int up = sm.exponent[stage] - row.scale + kLift;
+        const float lift = power(max(-126, min(127, up)));
+        const uint64_t lift2 = pair_of(lift, lift);
+        uint64_t total[2] = {0, 0};
+        __half2 heavy = __half2half2(__ushort_as_half(0));
+        uint32_t v[2][32];
+        tensor_load32(v[0], scores);
+        tensor_load32(v[1], scores + 32);
+        loaded();
 #pragma unroll
-                for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * factor);
-                tensor_store32(sums + c, v);
+        for (int half = 0; half < 2; ++half) {
+            float d[32];
+            distances(d, v[half], row, sm, stage, half, whole);
+#pragma unroll
+            for (int j = 0; j < 32; j += 4) {
+                const float4 m = *reinterpret_cast<const float4*>(&sm.values[stage][32 * half + j]);
+                const uint64_t p = pair_of(ex2(d[j]), ex2(d[j + 1])), q = pair_of(ex2(d[j + 2]), ex2(d[j + 3]));
+                total[0] = add2(total[0], p);
+                total[1] = add2(total[1], q);
+                float x, y, z, u;
+                parted(mul2(mul2(p, lift2), pair_of(m.x, m.y)), x, y);
+                parted(mul2(mul2(q, lift2), pair_of(m.z, m.w)), z, u);
+                const int at = 16 * half + j / 2;
+                w[at] = halves(x, y);
+                w[at + 1] = halves(z, u);
+                if constexpr (kTwo) { rest[at] = rest_of(w[at], x, y); rest[at + 1] = rest_of(w[at + 1], z, u); }
+                heavy = __hmax2(heavy, __hmax2(reinterpret_cast<const __half2&>(w[at]), reinterpret_cast<const __half2&>(w[at + 1])));
             }
         }
-    }
-    const float lift = power(max(-126, min(127, exponent - row.scale + kLift)));
-    const uint64_t lift2 = pair_of(lift, lift);
-    uint32_t w[32];
-    uint32_t rest[kTwo ? 32 : 1];
-#pragma unroll
-    for (int j = 0; j < 32; ++j) {
         float x, y;
-        parted(mul2(pair_of(d[2 * j], d[2 * j + 1]), lift2), x, y);
-        w[j] = halves(x, y);
-        if constexpr (kTwo) rest[j] = rest_of(w[j], x, y);
+        parted(add2(total[0], total[1]), x, y);
+        sum = x + y;
+        const float largest = __half2float(__hmax(__low2half(heavy), __high2half(heavy)));
+        const bool over = sum > kRoom || largest >= kMostWeight || up > 120;
+        if (tries > 0 || !__any_sync(0xffffffffu, over)) break;
+        row = moved_row<P>(row, sm, stage, scores, sums, none, whole);
     }
+    row.total += sum;
     tensor_store32(scores, w);
     if constexpr (kTwo) tensor_store32(scores + 32, rest);
     stored();
+}
+
+// ---- products ------------------------------------------------------------------------------------------------
+
+// By one warp: scores of a use (a tile and a slot), and `slots` uses later its weighted values.
+template <int P, bool kTwo>
+__device__ __forceinline__ void issue_products(const CacheSharedArgs& a, const Share& s, Small& sm, uint32_t tensor, int uses)
+{
+    using L = Layout<P>;
+    constexpr int slots = L::kSlots;
+    constexpr uint32_t score = instruction(kTile, false), weigh = instruction(P, true);
+    const int shift = a.two_queries;                                   // (the first phase of `weighed` is that of the queries' rests)
+    bool ok = wait(&sm.brought, 0, sm, a.flags);
+    for (int w = 0; a.two_queries && w < slots; ++w) ok = wait(&sm.weighed[w], 0, sm, a.flags) && ok;
+    ok = __all_sync(0xffffffffu, ok);
+    fence_after();
+    for (int v = 0; ok && v < uses + slots; ++v) {
+        if (v >= slots) {
+            const int use = v - slots, w = use % slots, tile = s.pair ? use >> 1 : use, stage = tile % L::kStages;
+            ok = __all_sync(0xffffffffu, wait(&sm.weighed[w], (use / slots + shift) & 1, sm, a.flags));
+            if (!ok) break;
+            fence_after();
+            const uint32_t at = tensor + w * L::kSlotColumns;
+            const uint64_t values = operand(L::piece(2 * stage + 1), kPanel);
+#pragma unroll
+            for (int rest = 0; rest < (kTwo ? 2 : 1); ++rest)
+#pragma unroll
+                for (int k = 0; k < kTile / 16; ++k)
+                    multiply_tensor(at + L::kSums, at + L::kScores + 32 * rest + 8 * k, values + k * (2048 >> 4), weigh, use >= slots || rest > 0 || k > 0);
+            commit(&sm.summed[w]);
+            if (!s.pair || w == slots - 1) commit(&sm.empty[stage]);
+        }
+        if (v < uses) {
+            const int w = v % slots, tile = s.pair ? v >> 1 : v, stage = tile % L::kStages;
+            ok = wait(&sm.full[stage], (tile / L::kStages) & 1, sm, a.flags);
+            if (v >= slots) ok = wait(&sm.summed[w], (v / slots - 1) & 1, sm, a.flags) && ok;           // (weights stand where the scores come)
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            fence_after();
+            const uint32_t at = tensor + w * L::kSlotColumns;
+            const uint64_t keys = operand(L::piece(2 * stage), 16), queries = operand(L::queries(s.pair ? w : 0, 0), 16);
+            // (the rests first: each step cuts the sum's last bit off, which is worth nothing while the sum is small)
+            if (a.two_queries)
+#pragma unroll
+                for (int k = 0; k < P / 16; ++k)
+                    multiply_tensor(at + L::kScores, at + L::kRests + 8 * k, keys + (k / 4 * kPanel + k % 4 * 32 >> 4), score, k > 0);
+#pragma unroll
+            for (int k = 0; k < P / 16; ++k)
+                multiply(at + L::kScores, queries + (k / 4 * kPanelQ + k % 4 * 32 >> 4), keys + (k / 4 * kPanel + k % 4 * 32 >> 4), score, a.two_queries || k > 0);
+            commit(&sm.scored[w]);
+        }
+    }
+    if (!ok) {                                                          // what is under way ends before tensor memory and shared memory are given back
+        commit(&sm.drained);
+        const long long start = clock64();
+        while (!(passed(&sm.drained, 0) && passed(&sm.brought, 0)) && clock64() - start < 1ll << 32) {}
+    }
 }
 
 // ---- the kernel ------------------------------------------------------------------------------------------------
@@ -555,6 +707,7 @@ __global__ void __launch_bounds__(Layout<P>::kThreads, 1) shared_prefix_kernel(c
                 barrier_init(&sm.full[i], kDecode); barrier_init(&sm.empty[i], 1);
                 barrier_init(&sm.scored[i], 1); barrier_init(&sm.weighed[i], 128); barrier_init(&sm.summed[i], 1);
             }
+            barrier_init(&sm.brought, 1);
             barrier_init(&sm.drained, 1);
             sm.failed = 0;
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -566,44 +719,40 @@ __global__ void __launch_bounds__(Layout<P>::kThreads, 1) shared_prefix_kernel(c
     pdl_wait();
     pdl_launch_next();
     const Share s = share_of<P>(a);
-    const int rows = s.pair ? 2 * kRows : kRows;
-    for (int r = warp; r < rows; r += L::kThreads / 32) bring_query<P>(a, s, sm, r / kRows, r % kRows, lane);
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     fence_before();
     __syncthreads();
     fence_after();
     const uint32_t tensor = sm.tensor;
     // slot s of a use: pairs of blocks take every tile twice
-    const int slots = L::kSlots, uses = s.pair ? 2 * s.tiles : s.tiles;
+    constexpr int slots = L::kSlots;
+    const int uses = s.pair ? 2 * s.tiles : s.tiles;
     auto tile_of = [&](int use) { return s.pair ? use >> 1 : use; };
 
     const int slot = warp >> 2;                                         // (of the softmax's warps)
     const int64_t my_row = (int64_t)(s.block + (s.pair ? slot : 0)) * kRows + (tid & 127);
     const uint32_t lanes = tensor + ((uint32_t)(32 * (warp & 3)) << 16), mine = lanes + slot * L::kSlotColumns;
-    if (warp < L::kDecodeAt && a.two_queries) {                         // what the queries' rounding left goes to tensor memory
-        const int from = s.pair ? slot : 0, r = tid & 127;
-#pragma unroll 1
-        for (int p = 0; p < L::kPanels; ++p) {
-            uint32_t v[32];
-#pragma unroll
-            for (int c = 0; c < 8; ++c) {
-                const uint4 x = *reinterpret_cast<const uint4*>(shared + L::rests(from, p) + swizzled(r, c));
-                v[4 * c] = x.x; v[4 * c + 1] = x.y; v[4 * c + 2] = x.z; v[4 * c + 3] = x.w;
-            }
-            tensor_store32(mine + L::kRests + 32 * p, v);
-        }
-        stored();
-        fence_before();
-    }
-    if (a.two_queries) {
-        __syncthreads();
-        fence_after();
-    }
-
     if (warp < L::kDecodeAt) {
         // ---- softmax: a thread has a row
+        take_registers<L::kSoftmax>();
+        const char* const queries = block_at<P>(a, s.head, s.block + (s.pair ? slot : 0));
         Row row;
-        row.f = sm.factor[(s.pair ? slot : 0) * kRows + (tid & 127)];
+        row.f = reinterpret_cast<const float*>(queries + 4 * P * kRows)[tid & 127];
+        if (a.two_queries) {                                            // what the queries' rounding left goes to tensor memory
+            const uint4* from = reinterpret_cast<const uint4*>(queries + 2 * P * kRows + (tid & 127) * 2 * P);
+#pragma unroll 1
+            for (int p = 0; p < L::kPanels; ++p) {
+                uint32_t v[32];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const uint4 x = from[8 * p + i];
+                    v[4 * i] = x.x; v[4 * i + 1] = x.y; v[4 * i + 2] = x.z; v[4 * i + 3] = x.w;
+                }
+                tensor_store32(mine + L::kRests + 32 * p, v);
+            }
+            stored();
+            fence_before();
+            arrive(&sm.weighed[slot]);                                  // (its first phase: what comes before the first scores)
+        }
         const bool live = __any_sync(0xffffffffu, my_row < (int64_t)a.batch * a.group);
         int n = 0;
         bool ok = true;
@@ -623,86 +772,66 @@ __global__ void __launch_bounds__(Layout<P>::kThreads, 1) shared_prefix_kernel(c
             // ---- what is left of this row; of a block that is alone, one part of even tiles and one of odd ones
             const int part = blockIdx.x % a.splits + (slot == 1 && !s.pair ? a.splits : 0);
             const int64_t all_rows = (int64_t)a.batch * a.shape.heads * a.group;
-            const int sequence = (int)(my_row / a.group);
-            const bool there = my_row < (int64_t)a.batch * a.group;
-            float* const to = a.parts + (part * all_rows + (int64_t)sequence * a.shape.heads * a.group + s.head * a.group +
-                                         (my_row - (int64_t)sequence * a.group)) * cache_part_floats(P);
+            const int all = a.batch * a.group;
+            auto part_of = [&](int r) {
+                const int sequence = r / a.group;
+                return a.parts + (part * all_rows + (int64_t)sequence * a.shape.heads * a.group + s.head * a.group + (r - sequence * a.group)) * cache_part_floats(P);
+            };
             if (n > 0 && ok) {
+                // four lanes have 32 bytes of a row side by side: lane l those of rows l / 4, + 8, + 16 and + 24
+                const int row0 = (int)my_row - lane + lane / 4;
+                float* to[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) to[i] = row0 + 8 * i < all ? part_of(row0 + 8 * i) + 2 * (lane & 3) : nullptr;
 #pragma unroll 1
                 for (int c = 0; c < P; c += 32) {
-                    uint32_t v[32];
-                    tensor_load32(v, mine + L::kSums + c);
+                    uint32_t v[2][16];
+                    tensor_load_rows(v[0], mine + L::kSums + c);
+                    tensor_load_rows(v[1], mine + L::kSums + c + (16u << 16));
                     loaded();
-                    if (there)
 #pragma unroll
-                        for (int i = 0; i < 32; i += 4) *reinterpret_cast<uint4*>(to + c + i) = make_uint4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+                    for (int i = 0; i < 4; ++i)
+                        if (to[i])
+#pragma unroll
+                            for (int j = 0; j < 4; ++j)
+                                *reinterpret_cast<uint2*>(to[i] + c + 8 * j) = make_uint2(v[i / 2][4 * j + 2 * (i & 1)], v[i / 2][4 * j + 2 * (i & 1) + 1]);
                 }
             }
-            if (there)
-                *reinterpret_cast<float4*>(to + P) = make_float4(row.begun ? row.ref : kLow, (float)(row.scale - kLift), n > 0 && ok ? row.total : 0.0f, 0.0f);
+            if (my_row < all)
+                *reinterpret_cast<float4*>(part_of((int)my_row) + P) = make_float4(row.begun ? row.ref : kLow, (float)(row.scale - kLift), n > 0 && ok ? row.total : 0.0f, 0.0f);
         }
         fence_before();
     } else if (warp < L::kIssuer) {
-        // ---- decoding: codes a tile ahead, pages two
-        const int t = tid - 32 * L::kDecodeAt;
+        // ---- decoding: codes a tile ahead, page numbers three
+        give_up_registers<L::kDecoding>();
+        const int t = warp - L::kDecodeAt;
         Codes<P> codes;
-        int page = page_of(a, s, 0, s.tiles > 0, lane);
-        if (s.tiles > 0) fetch<P>(codes, a, s, 0, page, t);
-        page = page_of(a, s, 1, s.tiles > 1, lane);
+        const int page = page_of(a, s, 0, s.tiles > 0, lane);
+        int next = page_of(a, s, 1, s.tiles > 1, lane), after = page_of(a, s, 2, s.tiles > 2, lane);
+        if (s.tiles > 0) fetch<P>(codes, a, s, 0, page, t, lane);
         for (int tile = 0; tile < s.tiles; ++tile) {
             const int stage = tile % L::kStages;
             const Codes<P> now = codes;
-            if (tile + 1 < s.tiles) fetch<P>(codes, a, s, tile + 1, page, t);
-            page = page_of(a, s, tile + 2, tile + 2 < s.tiles, lane);
+            if (tile + 1 < s.tiles) fetch<P>(codes, a, s, tile + 1, next, t, lane);
+            next = after;
+            after = page_of(a, s, tile + 3, tile + 3 < s.tiles, lane);
             if (!__all_sync(0xffffffffu, wait(&sm.empty[stage], (tile / L::kStages & 1) ^ 1, sm, a.flags))) break;
-            decode<P>(now, a, s, sm, tile, stage, t);
+            decode<P>(now, a, s, sm, tile, stage, t, lane);
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             arrive(&sm.full[stage]);
         }
-    } else if (lane == 0) {
-        // ---- the products, by one thread
-        bool ok = true;
-        for (int v = 0; v < uses + slots && ok; ++v) {
-            if (v >= slots) {
-                const int use = v - slots, w = use % slots, tile = tile_of(use), stage = tile % L::kStages;
-                ok = wait(&sm.weighed[w], (use / slots) & 1, sm, a.flags);
-                if (!ok) break;
-                fence_after();
-                const uint32_t at = tensor + w * L::kSlotColumns, values = L::piece(2 * stage + 1);
-                constexpr uint32_t how = instruction(P, true);
-#pragma unroll
-                for (int rest = 0; rest < (kTwo ? 2 : 1); ++rest)
-#pragma unroll
-                    for (int k = 0; k < kTile / 16; ++k)
-                        multiply_tensor(at + L::kSums, at + L::kScores + 32 * rest + 8 * k, operand(values + k * 2048, kPanel), how,
-                                        use >= slots || rest > 0 || k > 0);
-                commit(&sm.summed[w]);
-                if (!s.pair || w == slots - 1) commit(&sm.empty[stage]);
+    } else {
+        give_up_registers<L::kProducts>();
+        if (warp == L::kIssuer) {
+            const int there = s.pair ? 2 : 1;
+            if (lane == 0) {
+                asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" :: "r"(address_of(&sm.brought)), "r"(there * L::kPanels * kPanelQ) : "memory");
+                for (int i = 0; i < there; ++i)
+                    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                                 :: "r"(L::queries(i, 0)), "l"(block_at<P>(a, s.head, s.block + i)), "r"(L::kPanels * kPanelQ), "r"(address_of(&sm.brought)) : "memory");
             }
-            if (v < uses) {
-                const int w = v % slots, tile = tile_of(v), stage = tile % L::kStages;
-                ok = wait(&sm.full[stage], (tile / L::kStages) & 1, sm, a.flags);
-                if (ok && v >= slots) ok = wait(&sm.summed[w], (v / slots - 1) & 1, sm, a.flags);       // (weights stand where the scores come)
-                if (!ok) break;
-                fence_after();
-                const uint32_t at = tensor + w * L::kSlotColumns, keys = L::piece(2 * stage);
-                constexpr uint32_t how = instruction(kTile, false);
-                // (the rests first: each step cuts the sum's last bit off, which is worth nothing while the sum is small)
-                if (a.two_queries)
-#pragma unroll
-                    for (int k = 0; k < P / 16; ++k)
-                        multiply_tensor(at + L::kScores, at + L::kRests + 8 * k, operand(keys + k / 4 * kPanel + (k % 4) * 32, 16), how, k > 0);
-#pragma unroll
-                for (int k = 0; k < P / 16; ++k)
-                    multiply(at + L::kScores, operand(L::queries(s.pair ? w : 0, k / 4) + (k % 4) * 32, 16), operand(keys + k / 4 * kPanel + (k % 4) * 32, 16),
-                             how, a.two_queries || k > 0);
-                commit(&sm.scored[w]);
-            }
-        }
-        if (!ok) {                                                      // what is under way ends before tensor memory is given back
-            commit(&sm.drained);
-            const long long start = clock64();
-            while (!passed(&sm.drained, 0) && clock64() - start < 1ll << 32) {}
+            __syncwarp();
+            issue_products<P, kTwo>(a, s, sm, __shfl_sync(0xffffffffu, tensor, 0), uses);
         }
     }
     __syncthreads();
@@ -714,36 +843,43 @@ __global__ void __launch_bounds__(Layout<P>::kThreads, 1) shared_prefix_kernel(c
 
 // ---- the join --------------------------------------------------------------------------------------------------
 
-// A warp for a row: what its parts of the prefix and of its own tokens give, in their order.
-constexpr int kJoinThreads = 128;
+// What a row's parts of the prefix and of its own tokens give, in an order that goes by their number alone: `share` warps a row, each with some of the parts, of
+// which all that has to be read is asked for before anything waits; then their sums in order.
+constexpr int kJoinWarps = 8;
 
 template <int P>
-__global__ void __launch_bounds__(kJoinThreads) shared_join_kernel(const __grid_constant__ CacheSharedArgs a)
+__global__ void __launch_bounds__(32 * kJoinWarps) shared_join_kernel(const __grid_constant__ CacheSharedArgs a, int share)
 {
     constexpr int kVectors = P / 128 > 0 ? P / 128 : 1;
+    __shared__ float4 sums[kJoinWarps][kVectors][32];
     pdl_wait();
     pdl_launch_next();
-    const int lane = threadIdx.x & 31;
-    const int64_t all_rows = (int64_t)a.batch * a.shape.heads * a.group, row = (int64_t)blockIdx.x * (kJoinThreads / 32) + (threadIdx.x >> 5);
-    if (row >= all_rows) return;
-    const int heads = a.shape.heads * a.group, sequence = (int)(row / heads), head = (int)(row - (int64_t)sequence * heads);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, mine = warp % share;
+    const int64_t all_rows = (int64_t)a.batch * a.shape.heads * a.group, row = (int64_t)blockIdx.x * (kJoinWarps / share) + warp / share;
+    const bool there = row < all_rows;
+    if (blockIdx.x == 0 && threadIdx.x == 0 && (*a.prefix_length < 0 || *a.prefix_length > a.prefix_most)) atomicOr(a.flags, LQ_CACHE_BAD_LENGTH);
+    const int heads = a.shape.heads * a.group, sequence = there ? (int)(row / heads) : 0, head = there ? (int)(row - (int64_t)sequence * heads) : 0;
     const int64_t in_head = (int64_t)sequence * a.group + head % a.group;
     const int blocks = (int)(((int64_t)a.batch * a.group + kRows - 1) / kRows), block = (int)(in_head / kRows);
     const bool alone = cache_shared_slots(P) == 2 && blocks % 2 == 1 && block == blocks - 1;
-    const int before = a.splits * (alone ? 2 : 1), parts = before + (a.own_most > 0 && a.lengths[sequence] > 0);
+    const int before = a.splits * (alone ? 2 : 1), parts = there ? before + (a.own_most > 0 && a.lengths[sequence] > 0) : 0;
     const float* const prefix = fresh(a.parts);
     const float* const own = fresh(a.own);
     auto part = [&](int i) { return (i < before ? prefix + (i * all_rows + row) * cache_part_floats(P) : own + row * cache_part_floats(P)); };
     auto stats = [&](int i) { return __ldcg(reinterpret_cast<const float4*>(part(i) + P)); };
-    float r = kLow, scale = -1000.0f, total = 0.0f;
-    for (int i = lane; i < parts; i += 32) r = fmaxf(r, stats(i).x);
+    // every warp of a row looks at all parts' references, scales and denominators
+    float4 t0 = lane < parts ? stats(lane) : make_float4(kLow, 0.0f, 0.0f, 0.0f);
+    float r = t0.x;
+    for (int i = lane + 32; i < parts; i += 32) r = fmaxf(r, stats(i).x);
 #pragma unroll
     for (int o = 16; o > 0; o /= 2) r = fmaxf(r, __shfl_xor_sync(0xffffffffu, r, o));
-    for (int i = lane; i < parts; i += 32) {
-        const float4 t = stats(i);
+    float scale = -1000.0f, total = 0.0f;
+    auto count = [&](const float4& t) {
         if (t.z != 0.0f) scale = fmaxf(scale, t.y + (t.x - r));
         total += t.z * ex2(t.x - r);
-    }
+    };
+    count(t0);
+    for (int i = lane + 32; i < parts; i += 32) count(stats(i));
 #pragma unroll
     for (int o = 16; o > 0; o /= 2) {
         scale = fmaxf(scale, __shfl_xor_sync(0xffffffffu, scale, o));
@@ -752,8 +888,8 @@ __global__ void __launch_bounds__(kJoinThreads) shared_join_kernel(const __grid_
     scale = floorf(scale);
     float4 acc[kVectors] = {};
 #pragma unroll 4
-    for (int i = 0; i < parts; ++i) {
-        const float4 t = stats(i);
+    for (int i = mine; i < parts; i += share) {
+        const float4 t = i < 32 ? make_float4(__shfl_sync(0xffffffffu, t0.x, i & 31), __shfl_sync(0xffffffffu, t0.y, i & 31), __shfl_sync(0xffffffffu, t0.z, i & 31), 0.0f) : stats(i);
         if (t.z == 0.0f) continue;                              // (nothing seen, and nothing written)
         const float f = ex2((t.x - r) + (t.y - scale));
 #pragma unroll
@@ -763,6 +899,19 @@ __global__ void __launch_bounds__(kJoinThreads) shared_join_kernel(const __grid_
                 acc[k].x += v.x * f; acc[k].y += v.y * f; acc[k].z += v.z * f; acc[k].w += v.w * f;
             }
     }
+    if (share > 1) {
+#pragma unroll
+        for (int k = 0; k < kVectors; ++k) sums[warp][k][lane] = acc[k];
+        __syncthreads();
+        if (mine > 0) return;
+        for (int w = 1; w < share; ++w)
+#pragma unroll
+            for (int k = 0; k < kVectors; ++k) {
+                const float4 v = sums[warp + w][k][lane];
+                acc[k].x += v.x; acc[k].y += v.y; acc[k].z += v.z; acc[k].w += v.w;
+            }
+    }
+    if (!there) return;
     // 2^scale / total, the power in two factors that are normal numbers
     const int n = min(max((int)scale, -252), 254), half = n >> 1;
     const float out = total != 0.0f ? 1.0f / total * power(half) * power(n - half) : 0.0f;
@@ -788,16 +937,33 @@ cudaError_t launch_prefix(const CacheSharedArgs& a, cudaStream_t s)
     using L = Layout<P>;
     static std::atomic<uint64_t> configured{0};
     cudaError_t e = opt_in_shared_memory(configured, L::kEnd, shared_prefix_kernel<P, kTwo>);
+    // registers are dealt out anew in the kernel: it must have been given as many as that counts on
+    static std::atomic<int> registers{0};
+    if (e == cudaSuccess && !registers.load(std::memory_order_relaxed)) {
+        cudaFuncAttributes at;
+        e = cudaFuncGetAttributes(&at, shared_prefix_kernel<P, kTwo>);
+        if (e == cudaSuccess && at.numRegs != L::kRegisters) e = cudaErrorLaunchOutOfResources;
+        if (e == cudaSuccess) registers.store(at.numRegs, std::memory_order_relaxed);
+    }
     const int64_t blocks = ((int64_t)a.batch * a.group + kRows - 1) / kRows, items = a.shape.heads * ((blocks + L::kSlots - 1) / L::kSlots);
     if (e == cudaSuccess) e = launch(shared_prefix_kernel<P, kTwo>, (unsigned)(items * a.splits), L::kThreads, L::kEnd, s, a);
     return e;
 }
 
 template <int P>
+cudaError_t launch_rows(const CacheSharedArgs& a, cudaStream_t s)
+{
+    const int64_t rows = ((int64_t)a.batch * a.group + kRows - 1) / kRows * kRows * a.shape.heads;
+    const unsigned grid = (unsigned)((rows + kRowWarps - 1) / kRowWarps);
+    return a.queries.type == LQ_F32 ? launch(shared_rows_kernel<P, true>, grid, 32 * kRowWarps, 0, s, a) : launch(shared_rows_kernel<P, false>, grid, 32 * kRowWarps, 0, s, a);
+}
+
+template <int P>
 cudaError_t launch_join(const CacheSharedArgs& a, cudaStream_t s)
 {
     const int64_t rows = (int64_t)a.batch * a.shape.heads * a.group;
-    return launch(shared_join_kernel<P>, (unsigned)((rows + kJoinThreads / 32 - 1) / (kJoinThreads / 32)), kJoinThreads, 0, s, a);
+    const int share = rows <= 1184 ? 8 : 2, per = kJoinWarps / share;
+    return launch(shared_join_kernel<P>, (unsigned)((rows + per - 1) / per), 32 * kJoinWarps, 0, s, a, share);
 }
 
 }  // namespace
@@ -817,6 +983,11 @@ int cache_shared_splits(const CacheShape& shape, int64_t rows, int64_t prefix_to
         if (n >= 64 && n * items > 2 * sms) break;
     }
     return (int)best;
+}
+
+cudaError_t launch_cache_shared_rows(const CacheSharedArgs& a, cudaStream_t s)
+{
+    return a.shape.padded == 64 ? launch_rows<64>(a, s) : a.shape.padded == 128 ? launch_rows<128>(a, s) : launch_rows<256>(a, s);
 }
 
 cudaError_t launch_cache_shared_prefix(const CacheSharedArgs& a, cudaStream_t s)
