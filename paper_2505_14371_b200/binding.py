@@ -130,7 +130,7 @@ def load_library() -> C.CDLL:
     L.lq_cache_write.argtypes = [vp, i32, rows, rows, i64, vp, vp, i64, i64, rotary, vp]
     L.lq_cache_read.argtypes = [vp, i32, vp, i64, i64, vp, rows, rows, vp]
     L.lq_cache_attend.argtypes = [vp, i32, rows, i64, i32, vp, i64, vp, i64, vp, C.c_float, i64, rotary, rows, vp, vp, i64, vp]
-    L.lq_cache_shared_workspace.argtypes = [vp, i64, i32, i64, i64, i32]; L.lq_cache_shared_workspace.restype = i64
+    L.lq_cache_shared_workspace.argtypes = [vp, i64, i32, i64, i64, i32, i32]; L.lq_cache_shared_workspace.restype = i64
     L.lq_cache_attend_shared.argtypes = [vp, i32, rows, i64, i32, vp, i64, vp, i64, vp, vp, i64, vp, C.c_float, rotary, rows, vp, vp, i64, vp]
     L.lq_cache_bounds_words.argtypes = [vp]; L.lq_cache_bounds_words.restype = i64
     L.lq_cache_bounds.argtypes = [vp, i32, vp, i64, vp, i64, vp, vp]

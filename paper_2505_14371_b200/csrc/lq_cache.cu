@@ -286,15 +286,18 @@ int64_t most_tokens(const lq_cache* c, int64_t width) { return std::min<int64_t>
 
 // The workspace of attention with a shared prefix, in floats from its start: the queries, parts of the prefix, parts of the sequences' own tokens, and what
 // lq_cache_attend needs for those (-1: nothing).
-struct SharedSpace { int splits; int64_t rows, parts, own, partial, bytes; };
-SharedSpace shared_space(const lq_cache* c, int64_t batch, int heads, int64_t prefix_width, int64_t table_width, int type)
+struct SharedSpace { int splits, slots; bool rests; int64_t rows, parts, own, partial, bytes; };
+SharedSpace shared_space(const lq_cache* c, int64_t batch, int heads, int64_t prefix_width, int64_t table_width, int type, bool turned)
 {
     const CacheShape& s = c->shape;
     const int64_t rows = batch * heads, part = cache_part_floats(s.padded);
     SharedSpace x{};
-    x.splits = batch > 0 ? cache_shared_splits(s, batch * (heads / s.heads), most_tokens(c, prefix_width), type == LQ_F32, c->sms) : 0;
+    // fp32 queries, and turned ones of fp16 outputs, are sums of two fp16 numbers; turned ones of bf16 outputs are one, see lq_cache_shared.cu
+    x.rests = type == LQ_F32 || (type == LQ_F16 && turned);
+    x.slots = cache_shared_slots(s.padded, x.rests);
+    x.splits = batch > 0 ? cache_shared_splits(s.heads, x.slots, batch * (heads / s.heads), most_tokens(c, prefix_width), type == LQ_F32, c->sms) : 0;
     x.parts = x.splits > 0 ? (batch * (heads / s.heads) + 127) / 128 * s.heads * (cache_shared_block_bytes(s.padded) / 4) : 0;
-    x.own = x.parts + x.splits * cache_shared_slots(s.padded) * rows * part;
+    x.own = x.parts + x.splits * (int64_t)x.slots * rows * part;
     const int64_t partial = x.own + (table_width > 0 ? rows * part : 0), bytes = workspace_of(c, table_width, 0);
     x.partial = bytes > 0 ? partial : -1;
     x.bytes = partial * 4 + bytes;
@@ -525,7 +528,7 @@ int lq_cache_attend_chosen(lq_cache* cache, int32_t layer, const lq_rows* querie
     return LQ_OK;
 }
 
-int64_t lq_cache_shared_workspace(const lq_cache* cache, int64_t batch, int32_t heads, int64_t prefix_width, int64_t table_width, int32_t type)
+int64_t lq_cache_shared_workspace(const lq_cache* cache, int64_t batch, int32_t heads, int64_t prefix_width, int64_t table_width, int32_t type, int32_t turned)
 {
     if (!cache) return lq_set_error(LQ_EINVAL, "cache is NULL");
     LQ_TRY(check_batch(cache, batch, heads));
@@ -533,7 +536,7 @@ int64_t lq_cache_shared_workspace(const lq_cache* cache, int64_t batch, int32_t 
     if (prefix_width < 0 || prefix_width > INT32_MAX || table_width < 0 || table_width > INT32_MAX)
         return lq_set_error(LQ_EINVAL, "prefix_width or table_width out of range");
     if (type != LQ_F32 && type != LQ_F16 && type != LQ_BF16) return lq_set_error(LQ_EINVAL, "type %d is not one of LQ_F32, LQ_F16, LQ_BF16", type);
-    return shared_space(cache, batch, heads, prefix_width, table_width, type).bytes;
+    return shared_space(cache, batch, heads, prefix_width, table_width, type, turned != 0).bytes;
 }
 
 int lq_cache_attend_shared(lq_cache* cache, int32_t layer, const lq_rows* queries, int64_t batch, int32_t heads, const uint32_t* pages,
@@ -551,7 +554,7 @@ int lq_cache_attend_shared(lq_cache* cache, int32_t layer, const lq_rows* querie
     if (!aligned(prefix, 4) || !aligned(prefix_length, 4)) return lq_set_error(LQ_EINVAL, "prefix and prefix_length must be 4-byte aligned");
     LQ_TRY(take_scale(scale, &a.scale));
     LQ_TRY(take_rotary(rotary, s, false, &a.rotary));
-    const SharedSpace space = shared_space(cache, batch, heads, prefix_width, table_width, queries->type);
+    const SharedSpace space = shared_space(cache, batch, heads, prefix_width, table_width, queries->type, rotary != nullptr);
     float* base = nullptr;
     LQ_TRY(take_workspace(workspace, workspace_bytes, space.bytes, &base));
     LQ_TRY(check_units(cache, a, batch));
@@ -564,7 +567,7 @@ int lq_cache_attend_shared(lq_cache* cache, int32_t layer, const lq_rows* querie
     b.prefix = prefix; b.prefix_length = prefix_length; b.lengths = lengths; b.lse = lse; b.flags = cache->flags;
     b.num_pages = num_pages; b.prefix_width = prefix_width; b.prefix_most = most_tokens(cache, prefix_width); b.own_most = most_tokens(cache, table_width);
     b.scale = a.scale; b.batch = a.batch; b.group = a.group; b.splits = space.splits;
-    b.two_queries = queries->type == LQ_F32 || rotary != nullptr;
+    b.rests = space.rests; b.slots = space.slots;
     b.rows = reinterpret_cast<char*>(base + space.rows); b.parts = base + space.parts; b.own = base + space.own;
     a.partial = space.partial < 0 ? nullptr : base + space.partial;
     a.sums = b.own; a.before = prefix_length; a.before_most = b.prefix_most; a.lse = nullptr;

@@ -137,7 +137,7 @@ struct CacheSharedArgs {
     int64_t num_pages, prefix_width, prefix_most, own_most;     // tokens that the lengths can mean
     float scale;
     int32_t batch, group, splits;
-    int32_t two_queries;                // queries are sums of two fp16 numbers
+    int32_t rests, slots;               // queries are sums of two fp16 numbers; blocks of rows that a CTA takes at a time
 };
 
 // Which pages a sequence's queries look at (lq_cache_choose.cu).
@@ -180,9 +180,9 @@ cudaError_t launch_cache_choose(const CacheChooseArgs& a, cudaStream_t s);
 cudaError_t launch_cache_shared_rows(const CacheSharedArgs& a, cudaStream_t s);
 cudaError_t launch_cache_shared_prefix(const CacheSharedArgs& a, cudaStream_t s);
 cudaError_t launch_cache_shared_join(const CacheSharedArgs& a, cudaStream_t s);
-// Into how many parts the prefix's tokens are split, and how many parts a query may leave (a CTA of rows of 64 and 128 leaves two, see there).
-int cache_shared_splits(const CacheShape& shape, int64_t rows, int64_t prefix_tokens, bool exact, int sms);
-__host__ __device__ constexpr int cache_shared_slots(int padded) { return padded == 256 ? 1 : 2; }
+// Into how many parts the prefix's tokens are split, and how many parts a query may leave of each (blocks of rows that tensor memory holds at a time).
+int cache_shared_splits(int heads, int slots, int64_t rows, int64_t prefix_tokens, bool exact, int sms);
+__host__ __device__ constexpr int cache_shared_slots(int padded, bool rests) { return padded == 256 || (padded == 128 && rests) ? 1 : 2; }
 // Workspace for a head's block of 128 rows: fp16 numbers, what their rounding left, a factor for each row.
 __host__ __device__ constexpr int cache_shared_block_bytes(int padded) { return 128 * (4 * padded + 4); }
 // Teams of 8 warps that share an SM in the attention kernel (its registers: rows of 256 need twice as many a thread), and what

@@ -2,8 +2,8 @@
 //
 // Mathematics: that of lq_cache_attend.cuh.  With c_j = (2^e q) . level(K_j) and f = scale log2(e) / 2^e
 //   d_j = (c_j f) N_j - ref,  p_j = exp2(d_j),  w_j = p_j M_j 2^(6 - k),  out = 2^(k - 6) sum_j w_j level(V_j) / sum_j p_j,
-// N and M the keys' and values' norms, ref a running reference of the scores and k a whole number, the running scale of the weights: both
-// move, and the sums with them, only when a tile's p add up to 2^16 or a weight passes 2^14.  Scores, p, w and all
+// N and M the keys' and values' norms, ref and k whole numbers, the running reference of the scores and the running scale of the weights: both
+// move, and the sums with them (by powers of two), only when p add up to 2^16 or a weight passes 2^14.  Scores, p, w and all
 // sums are fp32.  Levels are fp16 as they stand.  Roundings to fewer bits: q as fp16 after a power of two (exact for fp16 and bf16;
 // rotated and fp32 ones as a sum of two, 22 bits); w as fp16 for bf16 outputs (11 bits, an eighth of the output's own rounding), as a sum of
 // two for fp16 and fp32 ones (22 bits).
@@ -11,7 +11,7 @@
 // Work.  All sequences' queries of one head of the cache are the rows of a matrix, 128 of them a block: both products are dense, and
 // run on tcgen05: S = Q K^T (128 x 64 tokens, Q and K in shared memory) and O += W V (W in tensor memory, where the scores stood; V in
 // shared memory, tokens outermost).  What q's rounding left is a second operand in tensor memory, what w's left stands beside W.
-// A CTA has two slots (one for rows of 256), each with scores, sums and four warps of its own, so that one slot's scores go through the
+// A CTA has two slots (one for rows of 256), each with scores, weights, sums and four warps of its own, so that one slot's scores go through the
 // softmax while the other's products run: two blocks of rows over the same tiles of 64 tokens or, where a block is alone, that
 // block over even and odd tiles.  Eight warps decode: a byte of a row is looked up in a table of shared memory that has a copy in each lane's bank
 // (as in lq_cache_attend.cuh), 8 coordinates are 16 bytes of a tile, swizzled by 128 bytes as the matrix unit reads it.
@@ -38,45 +38,45 @@ constexpr int kTableAt = 1 << 16, kTableBytes = 256 * 256, kSystemBytes = 1 << 1
 constexpr int kHighAt = kTableAt + kTableBytes;
 constexpr int kPanelQ = kRows * 128, kPanel = kTile * 128;      // bytes of 64 coordinates of a block's rows, of a tile's
 constexpr float kLow = -3.402823466e38f;
-constexpr float kRoom = 65536.0f, kMostWeight = 16384.0f;
+constexpr float kRoom = 65536.0f, kMostWeight = 16384.0f, kLeastWeight = 4.0f;
 constexpr int kLift = 6;
 constexpr int kColumns = 512;           // of tensor memory: all (one CTA an SM)
 
 // Shared memory, by address.  Below the table: pieces (a tile's keys or values), then what is small; behind it: the queries, then pieces.
-template <int P>
+template <int P, bool kRests>
 struct Layout {
-    static constexpr int kSlots = cache_shared_slots(P), kPanels = P / 64, kPiece = P * 128;
-    static constexpr int kStages = P == 256 ? 1 : 2;
-    static constexpr int kThreads = 128 * kSlots + kDecode + 128;
-    static constexpr int kDecodeAt = 4 * kSlots, kIssuer = kDecodeAt + kDecodeWarps;    // warps (three behind the issuer have nothing to do)
+    static constexpr int kSlots = cache_shared_slots(P, kRests), kPanels = P / 64, kPiece = P * 128;
+    static constexpr int kKeys = P == 64 ? 3 : P == 128 ? 2 : 1, kValues = P == 64 ? 4 : P == 128 ? 3 : 1;      // tiles of keys and of values at a time
+    static constexpr int kSoftmaxWarps = 4;                             // of a slot: a thread has a row
+    static constexpr int kThreads = 32 * kSoftmaxWarps * kSlots + kDecode + 128;
+    static constexpr int kDecodeAt = kSoftmaxWarps * kSlots, kIssuer = kDecodeAt + kDecodeWarps;        // warps (three behind the issuer have nothing to do)
     // Registers a thread at launch, and as they are dealt out to softmax, decoding and products: no more than all threads had.
     static constexpr int kRegisters = kSlots == 2 ? 96 : 128, kSoftmax = kSlots == 2 ? 144 : 208, kDecoding = kSlots == 2 ? 72 : 120, kProducts = 40;
-    static_assert(128 * kSlots * kSoftmax + kDecode * kDecoding + 128 * kProducts <= kThreads * kRegisters && kThreads * kRegisters <= 65536, "registers");
+    static_assert(32 * kSoftmaxWarps * kSlots * kSoftmax + kDecode * kDecoding + 128 * kProducts <= kThreads * kRegisters && kThreads * kRegisters <= 65536, "registers");
     static constexpr int kQueries = kSlots * kPanels * kPanelQ;
-    static constexpr int kLowPieces = P == 64 ? 4 : P == 128 ? 3 : 1;
+    static constexpr int kLowPieces = P == 64 ? 7 : P == 128 ? 3 : 1;
     static constexpr int kSmallAt = kSystemBytes + kLowPieces * kPiece;
-    static constexpr int kEnd = kHighAt + kQueries + (2 * kStages - kLowPieces) * kPiece;
-    static __device__ __forceinline__ uint32_t piece(int i)     // 2 * stage + (0: keys, 1: values)
-    {
-        return i < kLowPieces ? kSystemBytes + i * kPiece : kHighAt + kQueries + (i - kLowPieces) * kPiece;
-    }
+    static constexpr int kEnd = kHighAt + kQueries + (kKeys + kValues - kLowPieces) * kPiece;
+    static __device__ __forceinline__ uint32_t piece(int i) { return i < kLowPieces ? kSystemBytes + i * kPiece : kHighAt + kQueries + (i - kLowPieces) * kPiece; }
+    static __device__ __forceinline__ uint32_t keys(int stage) { return piece(stage); }
+    static __device__ __forceinline__ uint32_t values(int stage) { return piece(kKeys + stage); }
     static __device__ __forceinline__ uint32_t queries(int slot, int panel) { return kHighAt + (slot * kPanels + panel) * kPanelQ; }
-    // tensor memory, columns of a slot
-    static constexpr int kScores = 0, kSums = kTile, kRests = kTile + P, kSlotColumns = kTile + P + P / 2;
+    // tensor memory, columns of a slot: scores, weights (and what their rounding left), sums, what the queries' rounding left
+    static constexpr int kScores = 0, kWeights = kTile, kSums = 2 * kTile, kRest = 2 * kTile + P, kSlotColumns = kRest + (kRests ? P / 2 : 0);
     static_assert(kSlots * kSlotColumns <= kColumns && kEnd <= 227 << 10, "places");
 };
 
 struct Small {
-    uint64_t full[2], empty[2];         // a stage holds a tile; has been read
-    uint64_t scored[2], weighed[2], summed[2];          // of a slot: its scores are there, its weights, its sums
+    uint64_t key_full[4], key_empty[4], value_full[4], value_empty[4];  // a place holds a tile's keys or values; they have been read
+    uint64_t scored[2], taken[2], weighed[2], summed[2];        // of a slot: its scores are there; have been taken; its weights are there, its sums
     uint64_t brought;                   // the queries are there
-    uint64_t drained;
+    uint64_t drained[4];
     uint32_t tensor;                    // address of tensor memory
     uint32_t failed;
-    uint32_t seen[2][2];                // of a stage: bit per token
-    int32_t exponent[2];                // of a stage: what the values' norms are divided by
-    alignas(16) float keys[2][kTile];   // norms
-    alignas(16) float values[2][kTile];
+    uint32_t seen[4][2];                // of a tile, beside its values: bit per token
+    int32_t exponent[4];                // what the values' norms are divided by
+    alignas(16) float keys[4][kTile];   // norms
+    alignas(16) float values[4][kTile];
 };
 
 // ---- instructions ----------------------------------------------------------------------------------------------
@@ -134,6 +134,17 @@ __device__ __forceinline__ void tensor_load32(uint32_t (&v)[32], uint32_t at)
                    "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]), "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]),
                    "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
                  : "r"(at) : "memory");
+}
+__device__ __forceinline__ void tensor_load16(uint32_t (&v)[16], uint32_t at)
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+                 : "r"(at) : "memory");
+}
+__device__ __forceinline__ void tensor_store16(uint32_t at, const uint32_t (&v)[16])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+                 :: "r"(at), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]) : "memory");
 }
 // 32 columns of 16 lanes, by 8: registers 4 j and 4 j + 1 of lane l hold columns 8 j + 2 (l % 4) and the next of lane l / 4, the two behind those of lane l / 4 + 8.
 __device__ __forceinline__ void tensor_load_rows(uint32_t (&v)[16], uint32_t at)
@@ -318,16 +329,22 @@ struct Share {
     bool pair;                          // two blocks of rows; else (two slots) even and odd tiles
 };
 
-template <int P>
+// The pair of blocks that this CTA takes, and whether it is one.
+template <int kSlots>
+__device__ __forceinline__ bool pair_of_blocks(const CacheSharedArgs& a, int* head = nullptr, int* block = nullptr)
+{
+    const int blocks = (a.batch * a.group + kRows - 1) / kRows, pairs = (blocks + kSlots - 1) / kSlots;
+    const int item = blockIdx.x / a.splits, h = item / pairs, b = (item - h * pairs) * kSlots;
+    if (head) { *head = h; *block = b; }
+    return kSlots == 2 && b + 1 < blocks;
+}
+
+template <int kSlots>
 __device__ __forceinline__ Share share_of(const CacheSharedArgs& a)
 {
-    constexpr int kSlots = cache_shared_slots(P);
     Share s;
-    const int blocks = (int)(((int64_t)a.batch * a.group + kRows - 1) / kRows), pairs = (blocks + kSlots - 1) / kSlots;
-    const int split = blockIdx.x % a.splits, item = blockIdx.x / a.splits;
-    s.head = item / pairs;
-    s.block = (item - s.head * pairs) * kSlots;
-    s.pair = kSlots == 2 && s.block + 1 < blocks;
+    s.pair = pair_of_blocks<kSlots>(a, &s.head, &s.block);
+    const int split = blockIdx.x % a.splits;
     const int given = *a.prefix_length;
     s.length = given < 0 ? 0 : given > a.prefix_most ? a.prefix_most : given;
     const int64_t all = (s.length + kTile - 1) / kTile;
@@ -344,6 +361,7 @@ template <int P>
 struct Codes {
     static constexpr int kItems = 2 * (P / 64) * (kTile / 32);          // of 32 tokens
     static constexpr int kEach = (kItems + kDecodeWarps - 1) / kDecodeWarps;
+    static constexpr int kNorms = (kItems - 1) % kDecodeWarps;          // the warp that brings the norms: one that has values
     uint32_t w[kEach][16];              // (symbols of 4 bits: 8 words)
     float keys[2], values[2];           // norms, brought by one warp
     uint32_t seen;                      // bit i: the tile's i-th 16 tokens are on a page that is there
@@ -397,7 +415,7 @@ __device__ __forceinline__ void fetch(Codes<P>& c, const CacheSharedArgs& a, con
         load32(c.w[k], from);
         if (bits == 8) load32(c.w[k] + 8, from + 32);
     }
-    if (warp == kDecodeWarps - 1) {
+    if (warp == Codes<P>::kNorms) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const int token = lane + 32 * i, p = __shfl_sync(0xffffffffu, page, token >> 4);
@@ -409,18 +427,15 @@ __device__ __forceinline__ void fetch(Codes<P>& c, const CacheSharedArgs& a, con
     }
 }
 
+// A warp's k-th item into its piece.
 template <int P>
-__device__ __forceinline__ void decode(const Codes<P>& c, const CacheSharedArgs& a, const Share& s, Small& sm, int tile, int stage, int warp, int lane)
+__device__ __forceinline__ void decode(const Codes<P>& c, int k, const CacheSharedArgs& a, uint32_t piece, int warp, int lane)
 {
-    using L = Layout<P>;
-#pragma unroll
-    for (int k = 0; k < Codes<P>::kEach; ++k) {
-        const int i = warp + kDecodeWarps * k;
-        if (i >= Codes<P>::kItems) break;
-        int kind, panel, token;
-        item_of<P>(i, kind, panel, token);
-        token += lane;
-        const uint32_t row = L::piece(2 * stage + kind) + panel * kPanel + token * 128, copies = kTableAt + 4 * lane + 128 * kind;
+    int kind, panel, token;
+    item_of<P>(warp + kDecodeWarps * k, kind, panel, token);
+    token += lane;
+    {
+        const uint32_t row = piece + panel * kPanel + token * 128, copies = kTableAt + 4 * lane + 128 * kind;
         const uint32_t turn = (token & 7) << 4;
         const uint32_t (&w)[16] = c.w[k];
         // (16 look-ups before their stores: the compiler moves no load of shared memory above a store)
@@ -452,7 +467,13 @@ __device__ __forceinline__ void decode(const Codes<P>& c, const CacheSharedArgs&
             }
         }
     }
-    if (warp == kDecodeWarps - 1) {
+}
+
+// ... and the norms beside its values, by one warp.
+template <int P>
+__device__ __forceinline__ void place_norms(const Codes<P>& c, const Share& s, Small& sm, int tile, int stage, int lane)
+{
+    {
         const int64_t first = (int64_t)(s.tile0 + tile) * kTile;
         uint32_t seen[2];
         int most = -127;
@@ -497,40 +518,25 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
     return v;
 }
 
-// 32 of a tile's scores of this row become distances from the reference (base-2 exponents); those not seen -infinity.
-__device__ __forceinline__ void distances(float (&d)[32], const uint32_t (&v)[32], const Row& row, const Small& sm, int stage, int half, bool whole)
-{
-    const uint64_t f2 = pair_of(row.f, row.f), minus = pair_of(-row.ref, -row.ref);
-#pragma unroll
-    for (int j = 0; j < 32; j += 4) {
-        const float4 n = *reinterpret_cast<const float4*>(&sm.keys[stage][32 * half + j]);
-        parted(fma2(mul2(pair_of(__uint_as_float(v[j]), __uint_as_float(v[j + 1])), f2), pair_of(n.x, n.y), minus), d[j], d[j + 1]);
-        parted(fma2(mul2(pair_of(__uint_as_float(v[j + 2]), __uint_as_float(v[j + 3])), f2), pair_of(n.z, n.w), minus), d[j + 2], d[j + 3]);
-    }
-    if (!whole) {
-        const uint32_t seen = sm.seen[stage][half];
-#pragma unroll
-        for (int j = 0; j < 32; ++j) if (!(seen >> j & 1)) d[j] = -INFINITY;
-    }
-}
+constexpr int kFar = 100;               // a weight's factor 2^up is between 2^-kFar (and then 0 as fp16) and 2^kFar
 
-// Reference and scale of the rows of a warp as this tile wants them, and the sums moved along (`none`: there are none yet).
+// Reference and scale of a warp's rows as a tile of scores `v` wants them, the denominators and the sums (`summed`: a barrier's phase that they wait for; NULL:
+// there are none yet) moved along.  Both numbers are whole, so that what has been summed is multiplied by powers of two.  (Not inline: it is
+// rare, and what it wants to keep in registers crowds out what the usual way needs.)
 template <int P>
-__device__ __noinline__ Row moved_row(Row row, const Small& sm, int stage, uint32_t scores, uint32_t sums, bool none, bool whole)
+__device__ __noinline__ Row moved_row(Row row, Small& sm, const uint32_t* v, int stage, uint64_t* summed, uint32_t parity, uint32_t sums, uint32_t* flags)
 {
+    const float* const keys = sm.keys[stage];
+    const uint32_t seen[2] = {sm.seen[stage][0], sm.seen[stage][1]};
     float most = -INFINITY;
-    bool none_such = false;             // a score that is not a number: nothing is gained by waiting for a better one
-#pragma unroll 1
-    for (int half = 0; half < 2; ++half) {
-        uint32_t v[32];
-        float d[32];
-        tensor_load32(v, scores + 32 * half);
-        loaded();
-        distances(d, v, row, sm, stage, half, whole);
-#pragma unroll
-        for (int j = 0; j < 32; ++j) { most = fmaxf(most, d[j]); none_such = none_such || d[j] != d[j]; }
+    bool none_such = false;         // a score that is not a number: nothing is gained by waiting for a better one
+#pragma unroll 8
+    for (int j = 0; j < kTile; ++j) {
+        const float d = seen[j / 32] >> (j % 32) & 1 ? fmaf(__uint_as_float(v[j]) * row.f, keys[j], -row.ref) : -INFINITY;
+        most = fmaxf(most, d);
+        none_such = none_such || d != d;
     }
-    const float step = row.begun ? fmaxf(most, 0.0f) : most;
+    const float step = ceilf(row.begun ? fmaxf(most, 0.0f) : most);
     float moved = 0.0f;
     if (step > -INFINITY) {
         const float ref = row.ref + step;
@@ -539,156 +545,214 @@ __device__ __noinline__ Row moved_row(Row row, const Small& sm, int stage, uint3
         if (row.begun) row.total *= ex2(moved);
     }
     float heavy = 0.0f;
-#pragma unroll 1
-    for (int half = 0; half < 2; ++half) {
-        uint32_t v[32];
-        float d[32];
-        tensor_load32(v, scores + 32 * half);
-        loaded();
-        distances(d, v, row, sm, stage, half, whole);
-#pragma unroll
-        for (int j = 0; j < 32; ++j) heavy = fmaxf(heavy, ex2(d[j]) * sm.values[stage][32 * half + j]);
-    }
-    // the largest weight is 2^(exponent + e) or up to twice that; the scale's fraction, where the reference moved by one, is left to the factor
-    const int exponent = sm.exponent[stage], e = exponent_of(heavy);
-    int scale = max(exponent + e, exponent - 114);
-    if (row.begun) scale = max(scale, (int)floorf(fmaxf((float)row.scale + moved, -1000.0f)));
-    const float factor = row.begun ? ex2(moved + (float)(row.scale - scale)) : 0.0f;
+#pragma unroll 8
+    for (int j = 0; j < kTile; ++j)
+        if (seen[j / 32] >> (j % 32) & 1) heavy = fmaxf(heavy, ex2(fmaf(__uint_as_float(v[j]) * row.f, keys[j], -row.ref)) * sm.values[stage][j]);
+    // the largest weight is 2^(exponent + e) or up to twice that
+    const int exponent = sm.exponent[stage], e = exponent_of(heavy), by = (int)fmaxf(moved, -4000.0f);
+    int scale = max(exponent + e, exponent + kLift - kFar + 6);
+    if (row.begun) scale = max(scale, max(row.scale + by, -4000));
+    const int down = row.begun ? by + row.scale - scale : -4000;   // (at most 0)
+    const float factor = down < -126 ? 0.0f : power(down);
     row.scale = scale;
     row.begun = row.begun || most > -INFINITY || none_such;
-    if (!none) {
+    if (summed) {
+        wait(summed, parity, sm, flags);        // (a failure is met by the next wait, too)
+        __syncwarp();
+        fence_after();
 #pragma unroll 1
-        for (int c = 0; c < P; c += 32) {
-            uint32_t v[32];
-            tensor_load32(v, sums + c);
+        for (int c = 0; c < P; c += 16) {
+            uint32_t x[16];
+            tensor_load16(x, sums + c);
             loaded();
 #pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * factor);
-            tensor_store32(sums + c, v);
+            for (int i = 0; i < 16; ++i) x[i] = __float_as_uint(__uint_as_float(x[i]) * factor);
+            tensor_store16(sums + c, x);
         }
         stored();
     }
     return row;
 }
 
-// The scores of a tile become weights, in their place: in one pass with reference and scale as they are, and once more if that shows that they have to move
-// (p is fp32 and has room: its sum may grow to 2^kRoom; a weight is fp16, up to 2^(kSlack + kLift)).
-template <int P, bool kTwo>
-__device__ __forceinline__ void weigh_tile(Row& row, const Small& sm, int stage, uint32_t scores, uint32_t sums, bool none)
+// Barrier of all softmax warps; whether any says so.
+template <int kWidth>
+__device__ __forceinline__ bool any_of_slots(bool v)
 {
-    const bool whole = (sm.seen[stage][0] & sm.seen[stage][1]) == 0xffffffffu;
-    if (__any_sync(0xffffffffu, !row.begun)) row = moved_row<P>(row, sm, stage, scores, sums, none, whole);
-    uint32_t w[32], rest[kTwo ? 32 : 1];
-    float sum;
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, 1, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                 : "=r"(r) : "r"((uint32_t)v), "n"(kWidth) : "memory");
+    return r;
+}
+
+// The softmax of a slot's uses.  A row's scores become weights in one pass with reference and scale as they are, and once more if that shows that these have to
+// move (p is fp32 and has room: a tile's may add up to kRoom; a weight is fp16, up to kMostWeight).  The scale of the weights is part of p's exponent,
+// and taken out of the denominator again.
+template <int P, bool kTwo, bool kRests>
+struct Softmax {
+    using L = Layout<P, kRests>;
+    Row row;
+    int slot;
+    uint32_t columns;                   // of tensor memory, this slot's
+
+    // A row's first tile: the reference is its largest score, the scale that of a weight of 1 at the tile's largest norm (if that is far too high,
+    // the pass shows it).
+    __device__ __forceinline__ void begin(Small& sm, int stage)
+    {
+        float most = -INFINITY;
+        bool none_such = false;         // a score that is not a number: nothing is gained by waiting for a better one
 #pragma unroll 1
-    for (int tries = 0;; ++tries) {
-        // (a scale far below the tile's norms would be no power of two: then it moves)
-        const int up = sm.exponent[stage] - row.scale + kLift;
-        const float lift = power(max(-126, min(127, up)));
-        const uint64_t lift2 = pair_of(lift, lift);
-        uint64_t total[2] = {0, 0};
-        __half2 heavy = __half2half2(__ushort_as_half(0));
-        uint32_t v[2][32];
-        tensor_load32(v[0], scores);
-        tensor_load32(v[1], scores + 32);
-        loaded();
+        for (int c = 0; c < kTile; c += 16) {
+            uint32_t x[16];
+            tensor_load16(x, columns + L::kScores + c);
+            loaded();
+            const uint32_t seen = sm.seen[stage][c / 32] >> (c % 32);
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            float d[32];
-            distances(d, v[half], row, sm, stage, half, whole);
-#pragma unroll
-            for (int j = 0; j < 32; j += 4) {
-                const float4 m = *reinterpret_cast<const float4*>(&sm.values[stage][32 * half + j]);
-                const uint64_t p = pair_of(ex2(d[j]), ex2(d[j + 1])), q = pair_of(ex2(d[j + 2]), ex2(d[j + 3]));
-                total[0] = add2(total[0], p);
-                total[1] = add2(total[1], q);
-                float x, y, z, u;
-                parted(mul2(mul2(p, lift2), pair_of(m.x, m.y)), x, y);
-                parted(mul2(mul2(q, lift2), pair_of(m.z, m.w)), z, u);
-                const int at = 16 * half + j / 2;
-                w[at] = halves(x, y);
-                w[at + 1] = halves(z, u);
-                if constexpr (kTwo) { rest[at] = rest_of(w[at], x, y); rest[at + 1] = rest_of(w[at + 1], z, u); }
-                heavy = __hmax2(heavy, __hmax2(reinterpret_cast<const __half2&>(w[at]), reinterpret_cast<const __half2&>(w[at + 1])));
+            for (int j = 0; j < 16; ++j) {
+                const float d = seen >> j & 1 ? __uint_as_float(x[j]) * row.f * sm.keys[stage][c + j] : -INFINITY;
+                most = fmaxf(most, d);
+                none_such = none_such || d != d;
             }
         }
-        float x, y;
-        parted(add2(total[0], total[1]), x, y);
-        sum = x + y;
-        const float largest = __half2float(__hmax(__low2half(heavy), __high2half(heavy)));
-        const bool over = sum > kRoom || largest >= kMostWeight || up > 120;
-        if (tries > 0 || !__any_sync(0xffffffffu, over)) break;
-        row = moved_row<P>(row, sm, stage, scores, sums, none, whole);
+        if (row.begun) return;
+        if (most > -INFINITY) row.ref = ceilf(most);
+        row.scale = sm.exponent[stage];
+        row.begun = most > -INFINITY || none_such;
     }
-    row.total += sum;
-    tensor_store32(scores, w);
-    if constexpr (kTwo) tensor_store32(scores + 32, rest);
-    stored();
-}
+
+    // The n-th tile of this slot, whose norms are at `stage`.
+    __device__ __forceinline__ void tile(Small& sm, int stage, int n, uint32_t* flags)
+    {
+        const int exponent = sm.exponent[stage];
+        const uint32_t seen[2] = {sm.seen[stage][0], sm.seen[stage][1]};
+        const bool fresh = !row.begun;
+        if (__any_sync(0xffffffffu, fresh)) begin(sm, stage);
+        uint32_t v[kTile], w[kTile / 2], rest[kTwo ? kTile / 2 : 1];
+        tensor_load32(reinterpret_cast<uint32_t (&)[32]>(v[0]), columns + L::kScores);
+        tensor_load32(reinterpret_cast<uint32_t (&)[32]>(v[32]), columns + L::kScores + 32);
+        loaded();
+        fence_before();
+        arrive(&sm.taken[slot]);        // (the next tile's scores may come)
+        float sum;
+#pragma unroll 1
+        for (int tries = 0;; ++tries) {
+            const int wanted = exponent - row.scale + kLift, up = max(-kFar, min(kFar, wanted));
+            const float offset = (float)up - row.ref;
+            const uint64_t f2 = pair_of(row.f, row.f), offset2 = pair_of(offset, offset);
+            uint64_t total[2] = {0, 0};
+            __half2 heavy = __half2half2(__ushort_as_half(0));
+            auto pass = [&](auto all) {
+#pragma unroll
+                for (int j = 0; j < kTile; j += 4) {
+                    const float4 k = *reinterpret_cast<const float4*>(&sm.keys[stage][j]), m = *reinterpret_cast<const float4*>(&sm.values[stage][j]);
+                    float x, y, z, u;
+                    parted(fma2(mul2(pair_of(__uint_as_float(v[j]), __uint_as_float(v[j + 1])), f2), pair_of(k.x, k.y), offset2), x, y);
+                    parted(fma2(mul2(pair_of(__uint_as_float(v[j + 2]), __uint_as_float(v[j + 3])), f2), pair_of(k.z, k.w), offset2), z, u);
+                    if constexpr (!decltype(all)::value) {
+                        const uint32_t bits = seen[j / 32] >> (j % 32);
+                        x = bits & 1 ? x : -INFINITY; y = bits & 2 ? y : -INFINITY; z = bits & 4 ? z : -INFINITY; u = bits & 8 ? u : -INFINITY;
+                    }
+                    const uint64_t p = pair_of(ex2(x), ex2(y)), q = pair_of(ex2(z), ex2(u));
+                    total[0] = add2(total[0], p);
+                    total[1] = add2(total[1], q);
+                    parted(mul2(p, pair_of(m.x, m.y)), x, y);
+                    parted(mul2(q, pair_of(m.z, m.w)), z, u);
+                    w[j / 2] = halves(x, y);
+                    w[j / 2 + 1] = halves(z, u);
+                    if constexpr (kTwo) { rest[j / 2] = rest_of(w[j / 2], x, y); rest[j / 2 + 1] = rest_of(w[j / 2 + 1], z, u); }
+                    heavy = __hmax2(heavy, __hmax2(reinterpret_cast<const __half2&>(w[j / 2]), reinterpret_cast<const __half2&>(w[j / 2 + 1])));
+                }
+            };
+            if ((seen[0] & seen[1]) == 0xffffffffu) pass(std::true_type()); else pass(std::false_type());
+            float x, y;
+            parted(add2(total[0], total[1]), x, y);
+            sum = (x + y) * power(-up);
+            const float largest = __half2float(__hmax(__low2half(heavy), __high2half(heavy)));
+            const bool over = sum > kRoom || largest >= kMostWeight || wanted > kFar || (fresh && row.begun && largest < kLeastWeight);
+            if (tries > 0 || !__any_sync(0xffffffffu, over)) break;
+            if (fresh) row.begun = false;
+            uint32_t kept[kTile];
+#pragma unroll
+            for (int j = 0; j < kTile; ++j) kept[j] = v[j];
+            row = moved_row<P>(row, sm, kept, stage, n > 0 ? &sm.summed[slot] : nullptr, (n - 1) & 1, columns + L::kSums, flags);
+        }
+        row.total += sum;
+        if (n > 0) {                    // the weights before have been used
+            wait(&sm.summed[slot], (n - 1) & 1, sm, flags);
+            __syncwarp();
+            fence_after();
+        }
+        tensor_store32(columns + L::kWeights, w);
+        if constexpr (kTwo) tensor_store32(columns + L::kWeights + 32, rest);
+        stored();
+    }
+};
 
 // ---- products ------------------------------------------------------------------------------------------------
 
-// By one warp: scores of a use (a tile and a slot), and `slots` uses later its weighted values.
-template <int P, bool kTwo>
-__device__ __forceinline__ void issue_products(const CacheSharedArgs& a, const Share& s, Small& sm, uint32_t tensor, int uses)
+// Scores of a slot's uses, by one warp, and weighted values by another: each waits only for what its own products need.
+template <int P, bool kTwo, bool kRests>
+__device__ __forceinline__ bool issue_scores(const CacheSharedArgs& a, const Share& s, Small& sm, uint32_t tensor, int slot)
 {
-    using L = Layout<P>;
-    constexpr int slots = L::kSlots;
-    constexpr uint32_t score = instruction(kTile, false), weigh = instruction(P, true);
-    const int shift = a.two_queries;                                   // (the first phase of `weighed` is that of the queries' rests)
+    using L = Layout<P, kRests>;
+    constexpr uint32_t how = instruction(kTile, false);
+    const uint32_t at = tensor + slot * L::kSlotColumns;
     bool ok = wait(&sm.brought, 0, sm, a.flags);
-    for (int w = 0; a.two_queries && w < slots; ++w) ok = wait(&sm.weighed[w], 0, sm, a.flags) && ok;
-    ok = __all_sync(0xffffffffu, ok);
-    fence_after();
-    for (int v = 0; ok && v < uses + slots; ++v) {
-        if (v >= slots) {
-            const int use = v - slots, w = use % slots, tile = s.pair ? use >> 1 : use, stage = tile % L::kStages;
-            ok = __all_sync(0xffffffffu, wait(&sm.weighed[w], (use / slots + shift) & 1, sm, a.flags));
-            if (!ok) break;
-            fence_after();
-            const uint32_t at = tensor + w * L::kSlotColumns;
-            const uint64_t values = operand(L::piece(2 * stage + 1), kPanel);
-#pragma unroll
-            for (int rest = 0; rest < (kTwo ? 2 : 1); ++rest)
-#pragma unroll
-                for (int k = 0; k < kTile / 16; ++k)
-                    multiply_tensor(at + L::kSums, at + L::kScores + 32 * rest + 8 * k, values + k * (2048 >> 4), weigh, use >= slots || rest > 0 || k > 0);
-            commit(&sm.summed[w]);
-            if (!s.pair || w == slots - 1) commit(&sm.empty[stage]);
-        }
-        if (v < uses) {
-            const int w = v % slots, tile = s.pair ? v >> 1 : v, stage = tile % L::kStages;
-            ok = wait(&sm.full[stage], (tile / L::kStages) & 1, sm, a.flags);
-            if (v >= slots) ok = wait(&sm.summed[w], (v / slots - 1) & 1, sm, a.flags) && ok;           // (weights stand where the scores come)
-            ok = __all_sync(0xffffffffu, ok);
-            if (!ok) break;
-            fence_after();
-            const uint32_t at = tensor + w * L::kSlotColumns;
-            const uint64_t keys = operand(L::piece(2 * stage), 16), queries = operand(L::queries(s.pair ? w : 0, 0), 16);
-            // (the rests first: each step cuts the sum's last bit off, which is worth nothing while the sum is small)
-            if (a.two_queries)
-#pragma unroll
-                for (int k = 0; k < P / 16; ++k)
-                    multiply_tensor(at + L::kScores, at + L::kRests + 8 * k, keys + (k / 4 * kPanel + k % 4 * 32 >> 4), score, k > 0);
+    if constexpr (kRests) ok = wait(&sm.weighed[slot], 0, sm, a.flags) && ok;
+    const uint64_t queries = operand(L::queries(s.pair ? slot : 0, 0), 16);
+    for (int tile = s.pair ? 0 : slot, n = 0; tile < s.tiles; tile += s.pair ? 1 : L::kSlots, ++n) {
+        const int stage = tile % L::kKeys;
+        ok = wait(&sm.key_full[stage], (tile / L::kKeys) & 1, sm, a.flags) && ok;
+        if (n > 0) ok = wait(&sm.taken[slot], (n - 1) & 1, sm, a.flags) && ok;
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        fence_after();
+        const uint64_t keys = operand(L::keys(stage), 16);
+        // (the rests first: each step cuts the sum's last bit off, which is worth nothing while the sum is small)
+        if constexpr (kRests)
 #pragma unroll
             for (int k = 0; k < P / 16; ++k)
-                multiply(at + L::kScores, queries + (k / 4 * kPanelQ + k % 4 * 32 >> 4), keys + (k / 4 * kPanel + k % 4 * 32 >> 4), score, a.two_queries || k > 0);
-            commit(&sm.scored[w]);
-        }
+                multiply_tensor(at + L::kScores, at + L::kRest + 8 * k, keys + (k / 4 * kPanel + k % 4 * 32 >> 4), how, k > 0);
+#pragma unroll
+        for (int k = 0; k < P / 16; ++k)
+            multiply(at + L::kScores, queries + (k / 4 * kPanelQ + k % 4 * 32 >> 4), keys + (k / 4 * kPanel + k % 4 * 32 >> 4), how, kRests || k > 0);
+        commit(&sm.scored[slot]);
+        commit(&sm.key_empty[stage]);
     }
-    if (!ok) {                                                          // what is under way ends before tensor memory and shared memory are given back
-        commit(&sm.drained);
-        const long long start = clock64();
-        while (!(passed(&sm.drained, 0) && passed(&sm.brought, 0)) && clock64() - start < 1ll << 32) {}
+    return ok;
+}
+
+template <int P, bool kTwo, bool kRests>
+__device__ __forceinline__ bool issue_sums(const CacheSharedArgs& a, const Share& s, Small& sm, uint32_t tensor, int slot)
+{
+    using L = Layout<P, kRests>;
+    constexpr uint32_t how = instruction(P, true);
+    const uint32_t at = tensor + slot * L::kSlotColumns;
+    bool ok = !kRests || wait(&sm.weighed[slot], 0, sm, a.flags);       // (its first phase is that of the queries' rests)
+    for (int tile = s.pair ? 0 : slot, n = 0; tile < s.tiles; tile += s.pair ? 1 : L::kSlots, ++n) {
+        const int stage = tile % L::kValues;
+        ok = wait(&sm.value_full[stage], (tile / L::kValues) & 1, sm, a.flags) && ok;
+        ok = wait(&sm.weighed[slot], (n + kRests) & 1, sm, a.flags) && ok;
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        fence_after();
+        const uint64_t values = operand(L::values(stage), kPanel);
+#pragma unroll
+        for (int rest = 0; rest < (kTwo ? 2 : 1); ++rest)
+#pragma unroll
+            for (int k = 0; k < kTile / 16; ++k)
+                multiply_tensor(at + L::kSums, at + L::kWeights + 32 * rest + 8 * k, values + k * (2048 >> 4), how, n > 0 || rest > 0 || k > 0);
+        commit(&sm.summed[slot]);
+        commit(&sm.value_empty[stage]);
     }
+    return ok;
 }
 
 // ---- the kernel ------------------------------------------------------------------------------------------------
 
-template <int P, bool kTwo>
-__global__ void __launch_bounds__(Layout<P>::kThreads, 1) shared_prefix_kernel(const __grid_constant__ CacheSharedArgs a)
+template <int P, bool kTwo, bool kRests>
+__global__ void __launch_bounds__(Layout<P, kRests>::kThreads, 1) shared_prefix_kernel(const __grid_constant__ CacheSharedArgs a)
 {
-    using L = Layout<P>;
+    using L = Layout<P, kRests>;
     extern __shared__ __align__(1024) char smem[];
     char* const shared = smem - __cvta_generic_to_shared(smem);         // shared address 0
     Small& sm = *reinterpret_cast<Small*>(shared + L::kSmallAt);
@@ -703,12 +767,18 @@ __global__ void __launch_bounds__(Layout<P>::kThreads, 1) shared_prefix_kernel(c
     }
     if (warp == L::kIssuer) {
         if (lane == 0) {
+            constexpr int kItems = Codes<P>::kItems / 2;                // warps that bring a tile's keys, or values
+            const int readers = pair_of_blocks<L::kSlots>(a) ? 2 : 1;   // slots that read them
+            for (int i = 0; i < 4; ++i) {
+                barrier_init(&sm.key_full[i], 32 * kItems); barrier_init(&sm.key_empty[i], readers);
+                barrier_init(&sm.value_full[i], 32 * kItems); barrier_init(&sm.value_empty[i], readers);
+            }
             for (int i = 0; i < 2; ++i) {
-                barrier_init(&sm.full[i], kDecode); barrier_init(&sm.empty[i], 1);
-                barrier_init(&sm.scored[i], 1); barrier_init(&sm.weighed[i], 128); barrier_init(&sm.summed[i], 1);
+                barrier_init(&sm.scored[i], 1); barrier_init(&sm.taken[i], 32 * L::kSoftmaxWarps);
+                barrier_init(&sm.weighed[i], 32 * L::kSoftmaxWarps); barrier_init(&sm.summed[i], 1);
             }
             barrier_init(&sm.brought, 1);
-            barrier_init(&sm.drained, 1);
+            for (int i = 0; i < 4; ++i) barrier_init(&sm.drained[i], 1);
             sm.failed = 0;
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         }
@@ -718,7 +788,7 @@ __global__ void __launch_bounds__(Layout<P>::kThreads, 1) shared_prefix_kernel(c
     }
     pdl_wait();
     pdl_launch_next();
-    const Share s = share_of<P>(a);
+    const Share s = share_of<L::kSlots>(a);
     fence_before();
     __syncthreads();
     fence_after();
@@ -728,17 +798,19 @@ __global__ void __launch_bounds__(Layout<P>::kThreads, 1) shared_prefix_kernel(c
     const int uses = s.pair ? 2 * s.tiles : s.tiles;
     auto tile_of = [&](int use) { return s.pair ? use >> 1 : use; };
 
-    const int slot = warp >> 2;                                         // (of the softmax's warps)
-    const int64_t my_row = (int64_t)(s.block + (s.pair ? slot : 0)) * kRows + (tid & 127);
+    const int slot = warp / L::kSoftmaxWarps, place = tid & 127;        // of the softmax's warps: the slot; the thread's row of the block
+    const int64_t my_row = (int64_t)(s.block + (s.pair ? slot : 0)) * kRows + place;
     const uint32_t lanes = tensor + ((uint32_t)(32 * (warp & 3)) << 16), mine = lanes + slot * L::kSlotColumns;
     if (warp < L::kDecodeAt) {
         // ---- softmax: a thread has a row
         take_registers<L::kSoftmax>();
         const char* const queries = block_at<P>(a, s.head, s.block + (s.pair ? slot : 0));
-        Row row;
-        row.f = reinterpret_cast<const float*>(queries + 4 * P * kRows)[tid & 127];
-        if (a.two_queries) {                                            // what the queries' rounding left goes to tensor memory
-            const uint4* from = reinterpret_cast<const uint4*>(queries + 2 * P * kRows + (tid & 127) * 2 * P);
+        Softmax<P, kTwo, kRests> softmax;
+        softmax.slot = slot; softmax.columns = mine;
+        Row& row = softmax.row;
+        row.f = reinterpret_cast<const float*>(queries + 4 * P * kRows)[place];
+        if constexpr (kRests) {                                         // what the queries' rounding left goes to tensor memory
+            const uint4* from = reinterpret_cast<const uint4*>(queries + 2 * P * kRows + place * 2 * P);
 #pragma unroll 1
             for (int p = 0; p < L::kPanels; ++p) {
                 uint32_t v[32];
@@ -747,7 +819,7 @@ __global__ void __launch_bounds__(Layout<P>::kThreads, 1) shared_prefix_kernel(c
                     const uint4 x = from[8 * p + i];
                     v[4 * i] = x.x; v[4 * i + 1] = x.y; v[4 * i + 2] = x.z; v[4 * i + 3] = x.w;
                 }
-                tensor_store32(mine + L::kRests + 32 * p, v);
+                tensor_store32(mine + L::kRest + 32 * p, v);
             }
             stored();
             fence_before();
@@ -757,12 +829,14 @@ __global__ void __launch_bounds__(Layout<P>::kThreads, 1) shared_prefix_kernel(c
         int n = 0;
         bool ok = true;
         for (int use = slot; use < uses && ok; use += slots, ++n) {
-            const int tile = tile_of(use), stage = tile % L::kStages;
-            ok = wait(&sm.full[stage], (tile / L::kStages) & 1, sm, a.flags) && wait(&sm.scored[slot], n & 1, sm, a.flags);
-            ok = __all_sync(0xffffffffu, ok);
+            const int tile = tile_of(use), stage = tile % L::kValues;
+            ok = wait(&sm.value_full[stage], (tile / L::kValues) & 1, sm, a.flags) && wait(&sm.scored[slot], n & 1, sm, a.flags);
+            // (two slots with the same tiles stay in step: out of step, each fetches the 600 instructions of a tile for itself)
+            ok = s.pair ? !any_of_slots<32 * L::kSoftmaxWarps * L::kSlots>(!ok) : __all_sync(0xffffffffu, ok);
             if (!ok) break;
             fence_after();
-            if (live) weigh_tile<P, kTwo>(row, sm, stage, mine + L::kScores, mine + L::kSums, n == 0);
+            if (live) softmax.tile(sm, stage, n, a.flags);
+            else arrive(&sm.taken[slot]);
             fence_before();
             arrive(&sm.weighed[slot]);
         }
@@ -809,20 +883,31 @@ __global__ void __launch_bounds__(Layout<P>::kThreads, 1) shared_prefix_kernel(c
         const int page = page_of(a, s, 0, s.tiles > 0, lane);
         int next = page_of(a, s, 1, s.tiles > 1, lane), after = page_of(a, s, 2, s.tiles > 2, lane);
         if (s.tiles > 0) fetch<P>(codes, a, s, 0, page, t, lane);
-        for (int tile = 0; tile < s.tiles; ++tile) {
-            const int stage = tile % L::kStages;
+        for (int tile = 0; tile < s.tiles && t < Codes<P>::kItems; ++tile) {
             const Codes<P> now = codes;
             if (tile + 1 < s.tiles) fetch<P>(codes, a, s, tile + 1, next, t, lane);
             next = after;
             after = page_of(a, s, tile + 3, tile + 3 < s.tiles, lane);
-            if (!__all_sync(0xffffffffu, wait(&sm.empty[stage], (tile / L::kStages & 1) ^ 1, sm, a.flags))) break;
-            decode<P>(now, a, s, sm, tile, stage, t, lane);
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            arrive(&sm.full[stage]);
+            bool ok = true;
+#pragma unroll
+            for (int k = 0; k < Codes<P>::kEach && ok; ++k) {
+                int kind, panel, token;
+                item_of<P>(t + kDecodeWarps * k, kind, panel, token);
+                const int stage = kind ? tile % L::kValues : tile % L::kKeys, round = kind ? tile / L::kValues : tile / L::kKeys;
+                ok = __all_sync(0xffffffffu, wait(kind ? &sm.value_empty[stage] : &sm.key_empty[stage], (round & 1) ^ 1, sm, a.flags));
+                if (!ok) break;
+                if (kind && t == Codes<P>::kNorms) place_norms<P>(now, s, sm, tile, stage, lane);
+                decode<P>(now, k, a, kind ? L::values(stage) : L::keys(stage), t, lane);
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                arrive(kind ? &sm.value_full[stage] : &sm.key_full[stage]);
+            }
+            if (!ok) break;
         }
     } else {
         give_up_registers<L::kProducts>();
-        if (warp == L::kIssuer) {
+        // ---- products: of each slot, a warp for the scores and one for the sums; the first of all brings the queries
+        const int me = warp - L::kIssuer, slot_of = me >> 1;
+        if (me == 0) {
             const int there = s.pair ? 2 : 1;
             if (lane == 0) {
                 asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" :: "r"(address_of(&sm.brought)), "r"(there * L::kPanels * kPanelQ) : "memory");
@@ -831,7 +916,15 @@ __global__ void __launch_bounds__(Layout<P>::kThreads, 1) shared_prefix_kernel(c
                                  :: "r"(L::queries(i, 0)), "l"(block_at<P>(a, s.head, s.block + i)), "r"(L::kPanels * kPanelQ), "r"(address_of(&sm.brought)) : "memory");
             }
             __syncwarp();
-            issue_products<P, kTwo>(a, s, sm, __shfl_sync(0xffffffffu, tensor, 0), uses);
+        }
+        if (slot_of < L::kSlots) {
+            const uint32_t at = __shfl_sync(0xffffffffu, tensor, 0);
+            const bool ok = me & 1 ? issue_sums<P, kTwo, kRests>(a, s, sm, at, slot_of) : issue_scores<P, kTwo, kRests>(a, s, sm, at, slot_of);
+            if (!ok || me == 0) {       // what is under way ends before tensor memory and shared memory are given back
+                if (!ok) commit(&sm.drained[me]);
+                const long long start = clock64();
+                while (!((ok || passed(&sm.drained[me], 0)) && passed(&sm.brought, 0)) && clock64() - start < 1ll << 32) {}
+            }
         }
     }
     __syncthreads();
@@ -861,7 +954,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) shared_join_kernel(const __gr
     const int heads = a.shape.heads * a.group, sequence = there ? (int)(row / heads) : 0, head = there ? (int)(row - (int64_t)sequence * heads) : 0;
     const int64_t in_head = (int64_t)sequence * a.group + head % a.group;
     const int blocks = (int)(((int64_t)a.batch * a.group + kRows - 1) / kRows), block = (int)(in_head / kRows);
-    const bool alone = cache_shared_slots(P) == 2 && blocks % 2 == 1 && block == blocks - 1;
+    const bool alone = a.slots == 2 && blocks % 2 == 1 && block == blocks - 1;
     const int before = a.splits * (alone ? 2 : 1), parts = there ? before + (a.own_most > 0 && a.lengths[sequence] > 0) : 0;
     const float* const prefix = fresh(a.parts);
     const float* const own = fresh(a.own);
@@ -931,23 +1024,30 @@ __global__ void __launch_bounds__(32 * kJoinWarps) shared_join_kernel(const __gr
     if (lane == 0 && a.lse) a.lse[row] = total != 0.0f ? (r + log2f(total)) * 0.693147180559945309f : -INFINITY;
 }
 
-template <int P, bool kTwo>
+template <int P, bool kTwo, bool kRests>
 cudaError_t launch_prefix(const CacheSharedArgs& a, cudaStream_t s)
 {
-    using L = Layout<P>;
+    using L = Layout<P, kRests>;
     static std::atomic<uint64_t> configured{0};
-    cudaError_t e = opt_in_shared_memory(configured, L::kEnd, shared_prefix_kernel<P, kTwo>);
+    cudaError_t e = opt_in_shared_memory(configured, L::kEnd, shared_prefix_kernel<P, kTwo, kRests>);
     // registers are dealt out anew in the kernel: it must have been given as many as that counts on
     static std::atomic<int> registers{0};
     if (e == cudaSuccess && !registers.load(std::memory_order_relaxed)) {
         cudaFuncAttributes at;
-        e = cudaFuncGetAttributes(&at, shared_prefix_kernel<P, kTwo>);
+        e = cudaFuncGetAttributes(&at, shared_prefix_kernel<P, kTwo, kRests>);
         if (e == cudaSuccess && at.numRegs != L::kRegisters) e = cudaErrorLaunchOutOfResources;
         if (e == cudaSuccess) registers.store(at.numRegs, std::memory_order_relaxed);
     }
     const int64_t blocks = ((int64_t)a.batch * a.group + kRows - 1) / kRows, items = a.shape.heads * ((blocks + L::kSlots - 1) / L::kSlots);
-    if (e == cudaSuccess) e = launch(shared_prefix_kernel<P, kTwo>, (unsigned)(items * a.splits), L::kThreads, L::kEnd, s, a);
+    if (e == cudaSuccess) e = launch(shared_prefix_kernel<P, kTwo, kRests>, (unsigned)(items * a.splits), L::kThreads, L::kEnd, s, a);
     return e;
+}
+
+template <int P>
+cudaError_t launch_prefix_of(const CacheSharedArgs& a, cudaStream_t s)
+{
+    if (a.queries.type == LQ_BF16) return launch_prefix<P, false, false>(a, s);
+    return a.rests ? launch_prefix<P, true, true>(a, s) : launch_prefix<P, true, false>(a, s);
 }
 
 template <int P>
@@ -968,10 +1068,9 @@ cudaError_t launch_join(const CacheSharedArgs& a, cudaStream_t s)
 
 }  // namespace
 
-int cache_shared_splits(const CacheShape& shape, int64_t rows, int64_t prefix_tokens, bool exact, int sms)
+int cache_shared_splits(int heads, int slots, int64_t rows, int64_t prefix_tokens, bool exact, int sms)
 {
-    const int slots = cache_shared_slots(shape.padded);
-    const int64_t blocks = (rows + kRows - 1) / kRows, items = shape.heads * ((blocks + slots - 1) / slots), tiles = (prefix_tokens + kTile - 1) / kTile;
+    const int64_t blocks = (rows + kRows - 1) / kRows, items = heads * ((blocks + slots - 1) / slots), tiles = (prefix_tokens + kTile - 1) / kTile;
     if (tiles == 0) return 0;
     // a tile of two blocks takes twice as long as one of a block alone; what a CTA takes besides is some 8 of those
     const int64_t each = blocks > 1 && slots == 2 ? 2 : 1;
@@ -992,10 +1091,7 @@ cudaError_t launch_cache_shared_rows(const CacheSharedArgs& a, cudaStream_t s)
 
 cudaError_t launch_cache_shared_prefix(const CacheSharedArgs& a, cudaStream_t s)
 {
-    const bool two = a.queries.type != LQ_BF16;
-    if (a.shape.padded == 64) return two ? launch_prefix<64, true>(a, s) : launch_prefix<64, false>(a, s);
-    if (a.shape.padded == 128) return two ? launch_prefix<128, true>(a, s) : launch_prefix<128, false>(a, s);
-    return two ? launch_prefix<256, true>(a, s) : launch_prefix<256, false>(a, s);
+    return a.shape.padded == 64 ? launch_prefix_of<64>(a, s) : a.shape.padded == 128 ? launch_prefix_of<128>(a, s) : launch_prefix_of<256>(a, s);
 }
 
 cudaError_t launch_cache_shared_join(const CacheSharedArgs& a, cudaStream_t s)

@@ -373,7 +373,7 @@ PyObject* cache_attend_shared(PyObject*, PyObject* const* a, Py_ssize_t n)
     if (!attended_of(a[2], a[8], a[9], c, batch, &q, &o, &heads, &lse)) return nullptr;
     const double scale = PyFloat_AsDouble(a[10]);
     if (PyErr_Occurred() || !rotary_of(a[11], a[12], a[13], c, batch, &r, &turned)) return nullptr;
-    const int64_t bytes = lq_cache_shared_workspace(c.cache, batch, static_cast<int32_t>(heads), f->numel(), t->size(1), q.type);
+    const int64_t bytes = lq_cache_shared_workspace(c.cache, batch, static_cast<int32_t>(heads), f->numel(), t->size(1), q.type, turned);
     if (bytes < 0) return done(static_cast<int>(bytes));
     const at::Tensor space = space_of(bytes, *l);
     return call_on(c, [&](void* s) {

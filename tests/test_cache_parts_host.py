@@ -8,7 +8,7 @@ def test_calls_without_a_cache():
     import paper_2505_14371_b200 as lq
     lib = lq.load_library()
     assert lib.lq_cache_bounds_words(None) == -1 and lib.lq_cache_choose_workspace(None, 1, 1) == -1
-    assert lib.lq_cache_shared_workspace(None, 1, 1, 1, 1, 0) == -1
+    assert lib.lq_cache_shared_workspace(None, 1, 1, 1, 1, 0, 0) == -1
     assert lib.lq_cache_bounds(None, 0, None, 0, None, 0, None, None) == -1
     assert lib.lq_cache_choose(None, None, 0, 1, None, 0, None, 0, None, 0, 1, None, None, 1, None, None, 0, None) == -1
     assert lib.lq_cache_attend_chosen(None, 0, None, 0, 1, None, 0, None, 0, None, 1.0, None, None, None, None, 0, None) == -1
