@@ -114,6 +114,13 @@ __device__ __forceinline__ bool wait(uint64_t* b, uint32_t parity, Small& sm, ui
     return true;
 }
 
+// Two of them, looked at together.
+__device__ __forceinline__ bool wait(uint64_t* b, uint32_t parity, uint64_t* c, uint32_t other, Small& sm, uint32_t* flags)
+{
+    const bool x = passed(b, parity), y = passed(c, other);
+    return (x || wait(b, parity, sm, flags)) && (y || wait(c, other, sm, flags));
+}
+
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void loaded() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
@@ -574,16 +581,6 @@ __device__ __noinline__ Row moved_row(Row row, Small& sm, const uint32_t* v, int
     return row;
 }
 
-// Barrier of all softmax warps; whether any says so.
-template <int kWidth>
-__device__ __forceinline__ bool any_of_slots(bool v)
-{
-    uint32_t r;
-    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, 1, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
-                 : "=r"(r) : "r"((uint32_t)v), "n"(kWidth) : "memory");
-    return r;
-}
-
 // The softmax of a slot's uses.  A row's scores become weights in one pass with reference and scale as they are, and once more if that shows that these have to
 // move (p is fp32 and has room: a tile's may add up to kRoom; a weight is fp16, up to kMostWeight).  The scale of the weights is part of p's exponent,
 // and taken out of the denominator again.
@@ -701,8 +698,7 @@ __device__ __forceinline__ bool issue_scores(const CacheSharedArgs& a, const Sha
     const uint64_t queries = operand(L::queries(s.pair ? slot : 0, 0), 16);
     for (int tile = s.pair ? 0 : slot, n = 0; tile < s.tiles; tile += s.pair ? 1 : L::kSlots, ++n) {
         const int stage = tile % L::kKeys;
-        ok = wait(&sm.key_full[stage], (tile / L::kKeys) & 1, sm, a.flags) && ok;
-        if (n > 0) ok = wait(&sm.taken[slot], (n - 1) & 1, sm, a.flags) && ok;
+        ok = wait(&sm.key_full[stage], (tile / L::kKeys) & 1, &sm.taken[slot], (n - 1) & 1, sm, a.flags) && ok;         // (there is no phase before the first to wait for)
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         fence_after();
@@ -730,8 +726,7 @@ __device__ __forceinline__ bool issue_sums(const CacheSharedArgs& a, const Share
     bool ok = !kRests || wait(&sm.weighed[slot], 0, sm, a.flags);       // (its first phase is that of the queries' rests)
     for (int tile = s.pair ? 0 : slot, n = 0; tile < s.tiles; tile += s.pair ? 1 : L::kSlots, ++n) {
         const int stage = tile % L::kValues;
-        ok = wait(&sm.value_full[stage], (tile / L::kValues) & 1, sm, a.flags) && ok;
-        ok = wait(&sm.weighed[slot], (n + kRests) & 1, sm, a.flags) && ok;
+        ok = wait(&sm.value_full[stage], (tile / L::kValues) & 1, &sm.weighed[slot], (n + kRests) & 1, sm, a.flags) && ok;
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         fence_after();
@@ -830,9 +825,8 @@ __global__ void __launch_bounds__(Layout<P, kRests>::kThreads, 1) shared_prefix_
         bool ok = true;
         for (int use = slot; use < uses && ok; use += slots, ++n) {
             const int tile = tile_of(use), stage = tile % L::kValues;
-            ok = wait(&sm.value_full[stage], (tile / L::kValues) & 1, sm, a.flags) && wait(&sm.scored[slot], n & 1, sm, a.flags);
-            // (two slots with the same tiles stay in step: out of step, each fetches the 600 instructions of a tile for itself)
-            ok = s.pair ? !any_of_slots<32 * L::kSoftmaxWarps * L::kSlots>(!ok) : __all_sync(0xffffffffu, ok);
+            ok = wait(&sm.value_full[stage], (tile / L::kValues) & 1, &sm.scored[slot], n & 1, sm, a.flags);
+            ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
             fence_after();
             if (live) softmax.tile(sm, stage, n, a.flags);
