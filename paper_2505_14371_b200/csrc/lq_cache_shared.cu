@@ -955,36 +955,58 @@ __global__ void __launch_bounds__(32 * kJoinWarps) shared_join_kernel(const __gr
     auto part = [&](int i) { return (i < before ? prefix + (i * all_rows + row) * cache_part_floats(P) : own + row * cache_part_floats(P)); };
     auto stats = [&](int i) { return __ldcg(reinterpret_cast<const float4*>(part(i) + P)); };
     // every warp of a row looks at all parts' references, scales and denominators
-    float4 t0 = lane < parts ? stats(lane) : make_float4(kLow, 0.0f, 0.0f, 0.0f);
-    float r = t0.x;
-    for (int i = lane + 32; i < parts; i += 32) r = fmaxf(r, stats(i).x);
+    float r = kLow, scale = -1000.0f, total = 0.0f;
+    for (int i = lane; i < parts; i += 32) {
+        const float4 t = stats(i);
+        const float r1 = fmaxf(r, t.x), old = r - r1, there = t.x - r1;
+        total = total * ex2(old) + t.z * ex2(there);
+        scale = fmaxf(scale + old, t.z != 0.0f ? t.y + there : -INFINITY);
+        r = r1;
+    }
+    {
+        float most = r;
 #pragma unroll
-    for (int o = 16; o > 0; o /= 2) r = fmaxf(r, __shfl_xor_sync(0xffffffffu, r, o));
-    float scale = -1000.0f, total = 0.0f;
-    auto count = [&](const float4& t) {
-        if (t.z != 0.0f) scale = fmaxf(scale, t.y + (t.x - r));
-        total += t.z * ex2(t.x - r);
-    };
-    count(t0);
-    for (int i = lane + 32; i < parts; i += 32) count(stats(i));
+        for (int o = 16; o > 0; o /= 2) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+        total *= ex2(r - most);
+        scale += r - most;
+        r = most;
+    }
 #pragma unroll
     for (int o = 16; o > 0; o /= 2) {
         scale = fmaxf(scale, __shfl_xor_sync(0xffffffffu, scale, o));
         total += __shfl_xor_sync(0xffffffffu, total, o);
     }
-    scale = floorf(scale);
+    scale = floorf(fmaxf(scale, -1000.0f));
     float4 acc[kVectors] = {};
-#pragma unroll 4
-    for (int i = mine; i < parts; i += share) {
-        const float4 t = i < 32 ? make_float4(__shfl_sync(0xffffffffu, t0.x, i & 31), __shfl_sync(0xffffffffu, t0.y, i & 31), __shfl_sync(0xffffffffu, t0.z, i & 31), 0.0f) : stats(i);
-        if (t.z == 0.0f) continue;                              // (nothing seen, and nothing written)
-        const float f = ex2((t.x - r) + (t.y - scale));
+    for (int base = mine; base < parts; base += 32 * share) {
+        // lane l: the factor of this warp's l-th part from here; 0 where nothing was seen (and nothing written)
+        const int i = base + share * lane;
+        float f = 0.0f;
+        if (i < parts) {
+            const float4 t = stats(i);
+            if (t.z != 0.0f) f = ex2((t.x - r) + (t.y - scale));
+        }
+        const int here = min(32, (parts - base + share - 1) / share);
+        for (int l = 0; l < here; l += 4) {
+            float4 v[4][kVectors];
+            float g[4];
 #pragma unroll
-        for (int k = 0; k < kVectors; ++k)
-            if (P >= 128 || lane < P / 4) {
-                const float4 v = __ldcg(reinterpret_cast<const float4*>(part(i) + 4 * (lane + 32 * k)));
-                acc[k].x += v.x * f; acc[k].y += v.y * f; acc[k].z += v.z * f; acc[k].w += v.w * f;
+            for (int j = 0; j < 4; ++j) {
+                g[j] = __shfl_sync(0xffffffffu, f, (l + j) & 31);
+                const bool some = l + j < here && g[j] != 0.0f;
+                if (!some) g[j] = 0.0f;
+#pragma unroll
+                for (int k = 0; k < kVectors; ++k)
+                    v[j][k] = some && (P >= 128 || lane < P / 4) ? __ldcg(reinterpret_cast<const float4*>(part(base + share * (l + j)) + 4 * (lane + 32 * k)))
+                                                                 : make_float4(0, 0, 0, 0);
             }
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int k = 0; k < kVectors; ++k) {
+                    acc[k].x += v[j][k].x * g[j]; acc[k].y += v[j][k].y * g[j]; acc[k].z += v[j][k].z * g[j]; acc[k].w += v[j][k].w * g[j];
+                }
+        }
     }
     if (share > 1) {
 #pragma unroll
@@ -1056,7 +1078,8 @@ template <int P>
 cudaError_t launch_join(const CacheSharedArgs& a, cudaStream_t s)
 {
     const int64_t rows = (int64_t)a.batch * a.shape.heads * a.group;
-    const int share = rows <= 1184 ? 8 : 2, per = kJoinWarps / share;
+    // as many warps a row as the GPU holds at once
+    const int share = rows <= 1184 ? 8 : rows <= 2368 ? 4 : 2, per = kJoinWarps / share;
     return launch(shared_join_kernel<P>, (unsigned)((rows + per - 1) / per), 32 * kJoinWarps, 0, s, a, share);
 }
 
