@@ -598,7 +598,7 @@ int lq_cache_bounds(lq_cache* cache, int32_t layer, const uint32_t* pages, int64
     if (count == 0) return LQ_OK;
     CacheBoundsArgs a{};
     a.shape = cache->shape; a.tables = cache->tables + (size_t)layer * 2; a.pages = pages; a.which = which; a.bounds = bounds; a.flags = cache->flags;
-    a.num_pages = num_pages; a.count = count;
+    a.num_pages = num_pages; a.count = count; a.sms = cache->sms;
     LQ_ON_DEVICE(cache);
     LQ_CUDA(launch_cache_bounds(a, (cudaStream_t)stream));
     return LQ_OK;

@@ -149,6 +149,7 @@ struct CacheBoundsArgs {
     uint32_t* bounds;
     uint32_t* flags;
     int64_t num_pages, count;
+    int32_t sms;
 };
 struct CacheChooseArgs {
     CacheShape shape;

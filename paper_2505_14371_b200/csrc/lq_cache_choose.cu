@@ -29,29 +29,35 @@ __device__ __forceinline__ bool counts(float largest) { return largest >= kLeast
 
 // ---- bounds --------------------------------------------------------------------------------------------------
 
-// `split` warps take a page's rows of one head; a lane has 8 coordinates of every row of its own.  The signed levels stand in shared memory
-// 32 times, each lane's copy in its own bank.
+// `split` warps take a page's rows of one head; a lane has 8 coordinates of every row of its own.  What a byte of a row stands for is looked up in shared
+// memory, the two signed levels of symbols of 4 bits at once; a lane's copy of the table is in banks of its own (16 copies of two levels, 32 of one).
+// Few pages are split over more warps, for their latency; many are not, as what a warp does behind its rows is half of what it does for 16 of them.
 template <int P, int WK>
 __global__ void __launch_bounds__(kThreads) bounds_kernel(const __grid_constant__ CacheBoundsArgs a, int split)
 {
-    constexpr int kLanes = P / 8, kRows = 32 / kLanes, kSymbols = 1 << WK;
+    constexpr int kLanes = P / 8, kRows = 32 / kLanes;
     extern __shared__ __align__(16) char smem[];
-    float* const values = reinterpret_cast<float*>(smem);       // [kSymbols][32]
-    float* const most = values + kSymbols * 32;                  // [kWarps][P], then least, then the norms
+    float* const values = reinterpret_cast<float*>(smem);       // [256][32]
+    float* const most = values + 256 * 32;                      // [kWarps][P], then least, then the norms
     float* const least = most + kWarps * P;
     float* const norms = least + kWarps * P;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    for (int i = threadIdx.x; i < kSymbols * 8; i += kThreads) {
-        const float v = a.tables[LQ_KEYS].levels[i >> 4], w = (i >> 3) & 1 ? -v : v;
-        reinterpret_cast<float4*>(values)[i] = make_float4(w, w, w, w);
+    {
+        auto level = [&](int symbol) { const float v = a.tables[LQ_KEYS].levels[symbol >> 1]; return symbol & 1 ? -v : v; };
+        const int e = threadIdx.x;                              // a thread fills an entry, a warp's lanes at different banks
+        const float x = level(WK == 4 ? e & 15 : e), y = WK == 4 ? level(e >> 4) : x;
+        float4* row = reinterpret_cast<float4*>(values + 32 * e);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) row[(j + lane) & 7] = make_float4(x, y, x, y);
     }
+    static_assert(kThreads == 256, "a thread an entry");
     pdl_wait();
     pdl_launch_next();
     __syncthreads();
     const int per = kWarps / split, part = warp % split, page_size = 1 << a.shape.page_shift;
     const int row0 = lane / kLanes, col = lane % kLanes;
     const int64_t items = a.count * a.shape.heads;
-    const char* const mine = reinterpret_cast<const char*>(values + lane);
+    const char* const mine = reinterpret_cast<const char*>(values) + (WK == 4 ? (lane & 15) * 8 : lane * 4);
     for (int64_t first = (int64_t)blockIdx.x * per; first < items; first += (int64_t)gridDim.x * per) {
         const int64_t item = first + warp / split;
         int page = -1, head = 0;
@@ -83,14 +89,24 @@ __global__ void __launch_bounds__(kThreads) bounds_kernel(const __grid_constant_
                 }
                 const float norm = row_norms[r];
                 n = norm >= 0.0f ? fmaxf(n, norm) : INFINITY;   // (NaN: no bounds)
+                if constexpr (WK == 8) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    uint32_t at;                                // symbol * 128
-                    if constexpr (WK == 8) at = __byte_perm(w[i / 4], 0, 0x4440 + i % 4) << 7;
-                    else at = (i == 0 ? w[0] << 7 : i == 1 ? w[0] << 3 : w[0] >> (4 * i - 7)) & (15u << 7);
-                    const float v = __fmul_rn(norm, *reinterpret_cast<const float*>(mine + at));
-                    up[i] = fmaxf(up[i], v);
-                    down[i] = fminf(down[i], v);
+                    for (int i = 0; i < 8; ++i) {
+                        const float v = __fmul_rn(norm, *reinterpret_cast<const float*>(mine + (__byte_perm(w[i / 4], 0, 0x4440 + i % 4) << 7)));
+                        up[i] = fmaxf(up[i], v);
+                        down[i] = fminf(down[i], v);
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const uint32_t at = (i == 0 ? w[0] << 7 : w[0] >> (8 * i - 7)) & (255u << 7);
+                        const float2 l = *reinterpret_cast<const float2*>(mine + at);
+                        const float x = __fmul_rn(norm, l.x), y = __fmul_rn(norm, l.y);
+                        up[2 * i] = fmaxf(up[2 * i], x);
+                        down[2 * i] = fminf(down[2 * i], x);
+                        up[2 * i + 1] = fmaxf(up[2 * i + 1], y);
+                        down[2 * i + 1] = fminf(down[2 * i + 1], y);
+                    }
                 }
             }
         }
@@ -146,13 +162,16 @@ __global__ void __launch_bounds__(kThreads) bounds_kernel(const __grid_constant_
 template <int P, int WK>
 cudaError_t launch_bounds(const CacheBoundsArgs& a, cudaStream_t s)
 {
-    constexpr int kBytes = 4 * ((1 << WK) * 32 + kWarps * (2 * P + 1));
+    constexpr int kBytes = 4 * (256 * 32 + kWarps * (2 * P + 1));
     static std::atomic<uint64_t> configured{0};
     cudaError_t e = opt_in_shared_memory(configured, kBytes, bounds_kernel<P, WK>);
-    // 16 rows a warp: pages of 64 then take half a CTA
-    const int split = a.shape.page_shift >= 7 ? kWarps : 1 << (a.shape.page_shift - 4), per = kWarps / split;
-    const int64_t groups = (a.count * a.shape.heads + per - 1) / per;
-    if (e == cudaSuccess) e = launch(bounds_kernel<P, WK>, (unsigned)(groups < 65535 ? groups : 65535), kThreads, kBytes, s, a, split);
+    // 16 rows a warp at least, and as few warps a page as keep the GPU's SMs busy
+    const int64_t items = a.count * a.shape.heads;
+    int split = 1;
+    while (split < kWarps && split < 1 << (a.shape.page_shift - 4) && items * split < (int64_t)a.sms * 2 * kWarps) split *= 2;
+    const int per = kWarps / split;
+    const int64_t groups = (items + per - 1) / per, most = (int64_t)a.sms * 4;
+    if (e == cudaSuccess) e = launch(bounds_kernel<P, WK>, (unsigned)(groups < most ? groups : most), kThreads, kBytes, s, a, split);
     return e;
 }
 
@@ -174,11 +193,18 @@ struct ChooseShared {
     uint32_t keys[1];                   // kKeys or the table's pages, whichever is less
 };
 
-__device__ __forceinline__ float number(const char* row, int type, int d)
+// A query's coordinate as it is stored, and as a number: what its bits mean is looked at when all loads are under way.
+template <bool kFloat>
+__device__ __forceinline__ uint32_t raw(const char* row, int d)
 {
-    if (type == LQ_F32) return reinterpret_cast<const float*>(row)[d];
-    if (type == LQ_F16) return __half2float(reinterpret_cast<const __half*>(row)[d]);
-    return __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(row)[d]);
+    if constexpr (kFloat) return reinterpret_cast<const uint32_t*>(row)[d];
+    else return reinterpret_cast<const unsigned short*>(row)[d];
+}
+template <bool kFloat>
+__device__ __forceinline__ float number(uint32_t v, int type)
+{
+    if constexpr (kFloat) return __uint_as_float(v);
+    else return type == LQ_BF16 ? __uint_as_float(v << 16) : __half2float(__ushort_as_half((unsigned short)v));
 }
 
 // A score as a number whose order is the scores' (0 is kept for pages that are not there).
@@ -205,7 +231,7 @@ __device__ __forceinline__ uint2 block_scan(uint2 v, uint2* sums)
 }
 
 // A cluster of CTAs takes one (sequence, head): each scores its share of the pages, the first one chooses.
-template <int P>
+template <int P, bool kFloat>
 __global__ void __launch_bounds__(kThreads) choose_kernel(const __grid_constant__ CacheChooseArgs a)
 {
     constexpr int kLanes = P / 16, kGroups = kThreads / kLanes;
@@ -238,8 +264,30 @@ __global__ void __launch_bounds__(kThreads) choose_kernel(const __grid_constant_
     const int share = (middle + ranks - 1) / ranks, begin = min(rank * share, middle), end = min(begin + share, middle);
     const int group = tid / kLanes, col = tid % kLanes;
     const int64_t page_words = cache_bounds_words(a.shape.heads, P);
+    // bounds of kAhead pages of this thread's group of lanes: asked for before the queries are looked at
+    uint4 up[kAhead], down[kAhead];
+    float scale[kAhead];
+    bool there[kAhead];
+    auto fetch = [&](int base) {
+        int page[kAhead];
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) { const int i = base + j * kGroups + group; page[j] = i < end ? table[a.first + i] : -1; }
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            there[j] = page[j] >= 0 && page[j] < a.num_pages;
+            up[j] = down[j] = make_uint4(0, 0, 0, 0);
+            scale[j] = 0.0f;
+            if (there[j]) {
+                const uint32_t* from = a.bounds + page[j] * page_words;
+                up[j] = *reinterpret_cast<const uint4*>(from + head * (P / 2) + 4 * col);
+                down[j] = *reinterpret_cast<const uint4*>(from + head * (P / 2) + P / 4 + 4 * col);
+                scale[j] = reinterpret_cast<const float*>(from)[a.shape.heads * (P / 2) + head];
+            }
+        }
+    };
     for (int block = 0; block < a.group; block += kBlock) {
         const int queries = min(kBlock, a.group - block);
+        fetch(begin);
         __syncthreads();
         for (int q = warp; q < queries; q += kWarps) {          // the queries as whole numbers
             const char* const row = static_cast<const char*>(a.queries.data) + (int64_t)sequence * a.queries.token_bytes +
@@ -253,17 +301,27 @@ __global__ void __launch_bounds__(kThreads) choose_kernel(const __grid_constant_
                 if (lost) { if (lane == 0) atomicOr(a.flags, LQ_CACHE_BAD_POSITION); }
                 else angles += at * r.dim;
             }
-            float x[P / 32], top = 0.0f;
+            uint32_t bits[P / 32], other[P / 32];
+            float x[P / 32], c[P / 32], t[P / 32], top = 0.0f;
+            const int half = r.dim / 2;
 #pragma unroll
             for (int i = 0; i < P / 32; ++i) {
-                const int d = lane + 32 * i, half = r.dim / 2;
-                x[i] = d < a.shape.dim ? number(row, a.queries.type, d) : 0.0f;
+                const int d = lane + 32 * i;
+                const bool turned = r.table && !lost && d < r.dim;
+                bits[i] = d < a.shape.dim ? raw<kFloat>(row, d) : 0;
+                other[i] = turned ? raw<kFloat>(row, r.interleaved ? d ^ 1 : d < half ? d + half : d - half) : 0;
+                const int p = r.interleaved ? d / 2 : d < half ? d : d - half;
+                c[i] = turned ? angles[p] : 1.0f;
+                t[i] = turned ? angles[half + p] : 0.0f;
+            }
+#pragma unroll
+            for (int i = 0; i < P / 32; ++i) {
+                const int d = lane + 32 * i;
+                x[i] = number<kFloat>(bits[i], a.queries.type);
                 if (r.table && !lost && d < r.dim) {
-                    const int p = r.interleaved ? d / 2 : d < half ? d : d - half;
                     const bool lower = r.interleaved ? d % 2 == 0 : d < half;
-                    const float u = number(row, a.queries.type, r.interleaved ? d ^ 1 : lower ? d + half : d - half);
-                    const float c = angles[p], s = angles[half + p];
-                    x[i] = lower ? __fsub_rn(__fmul_rn(x[i], c), __fmul_rn(u, s)) : __fadd_rn(__fmul_rn(x[i], c), __fmul_rn(u, s));
+                    const float u = number<kFloat>(other[i], a.queries.type);
+                    x[i] = lower ? __fsub_rn(__fmul_rn(x[i], c[i]), __fmul_rn(u, t[i])) : __fadd_rn(__fmul_rn(x[i], c[i]), __fmul_rn(u, t[i]));
                 }
                 top = fabsf(x[i]) <= top ? top : fabsf(x[i]);   // (keeps NaN)
                 if (x[i] != x[i]) top = INFINITY;
@@ -281,23 +339,10 @@ __global__ void __launch_bounds__(kThreads) choose_kernel(const __grid_constant_
         }
         __syncthreads();
         for (int base = begin; base < end; base += kGroups * kAhead) {
-            uint4 up[kAhead], down[kAhead];
-            float scale[kAhead], best[kAhead];
-            bool there[kAhead];
+            float best[kAhead];
 #pragma unroll
-            for (int j = 0; j < kAhead; ++j) {
-                const int i = base + j * kGroups + group;
-                const int page = i < end ? table[a.first + i] : -1;
-                there[j] = page >= 0 && page < a.num_pages;
-                up[j] = down[j] = make_uint4(0, 0, 0, 0);
-                scale[j] = 0.0f; best[j] = -INFINITY;
-                if (there[j]) {
-                    const uint32_t* from = a.bounds + page * page_words;
-                    up[j] = *reinterpret_cast<const uint4*>(from + head * (P / 2) + 4 * col);
-                    down[j] = *reinterpret_cast<const uint4*>(from + head * (P / 2) + P / 4 + 4 * col);
-                    scale[j] = reinterpret_cast<const float*>(from)[a.shape.heads * (P / 2) + head];
-                }
-            }
+            for (int j = 0; j < kAhead; ++j) best[j] = -INFINITY;
+            if (base > begin) fetch(base);
             for (int q = 0; q < queries; ++q) {
                 const uint4 p = *reinterpret_cast<const uint4*>(&sh.positive[q][16 * col]);
                 const uint4 n = *reinterpret_cast<const uint4*>(&sh.negative[q][16 * col]);
@@ -330,8 +375,28 @@ __global__ void __launch_bounds__(kThreads) choose_kernel(const __grid_constant_
     if (ranks > 1) cluster.sync(); else __syncthreads();
     if (rank > 0) return;
 
-    // ---- the `wanted` largest keys: bins over the range that is left, until the last one is taken whole or is one number
     const uint32_t* const mine = inside ? sh.keys : keys;
+    auto ends = [&]() {                                         // the pages that are always kept
+        for (int i = tid; i < a.first + a.last; i += kThreads)
+            if (i < a.first) chosen[i] = table[i];
+            else chosen[a.keep - a.last + (i - a.first)] = table[pages - a.last + (i - a.first)];
+    };
+    if (middle <= kThreads) {                                   // ---- a thread a page: how many stand before it (57 pages: 3 us less than by bins)
+        const uint32_t k = tid < middle ? mine[tid] : 0;
+        int before = 0;
+#pragma unroll 4
+        for (int i = 0; i < middle; ++i) { const uint32_t other = mine[i]; before += other > k || (other == k && i < tid); }
+        const bool taken = tid < middle && before < wanted;
+        const uint32_t votes = __ballot_sync(0xffffffffu, taken);
+        if (lane == 0) sh.low[warp] = __popc(votes);
+        __syncthreads();
+        int at = __popc(votes & ((1u << lane) - 1));
+        for (int w = 0; w < warp; ++w) at += sh.low[w];
+        if (taken) chosen[a.first + at] = table[a.first + tid];
+        ends();
+        return;
+    }
+    // ---- the `wanted` largest keys: bins over the range that is left, until the last one is taken whole or is one number
     uint32_t low = 0xffffffffu, high = 0;
     for (int i = tid; i < middle; i += kThreads) { const uint32_t k = mine[i]; low = min(low, k); high = max(high, k); }
     low = __reduce_min_sync(0xffffffffu, low);
@@ -386,13 +451,11 @@ __global__ void __launch_bounds__(kThreads) choose_kernel(const __grid_constant_
         sure += above;
         even += level;
     }
-    for (int i = tid; i < a.first + a.last; i += kThreads)
-        if (i < a.first) chosen[i] = table[i];
-        else chosen[a.keep - a.last + (i - a.first)] = table[pages - a.last + (i - a.first)];
+    ends();
 }
 
-template <int P>
-cudaError_t launch_choose(const CacheChooseArgs& a, cudaStream_t s)
+template <int P, bool kFloat>
+cudaError_t launch_choose_as(const CacheChooseArgs& a, cudaStream_t s)
 {
     const int64_t items = (int64_t)a.batch * a.shape.heads;
     // more CTAs an item while the GPU has room for them and each has pages to score
@@ -400,9 +463,15 @@ cudaError_t launch_choose(const CacheChooseArgs& a, cudaStream_t s)
     while (ranks < 8 && items * ranks * 2 <= a.sms && (int64_t)ranks * 128 <= a.table_width) ranks *= 2;
     const int keys = (int)(a.table_width < kKeys ? a.table_width : kKeys), bytes = (int)sizeof(ChooseShared<P>) + 4 * keys;
     static std::atomic<uint64_t> configured{0};
-    cudaError_t e = opt_in_shared_memory(configured, (int)sizeof(ChooseShared<P>) + 4 * kKeys, choose_kernel<P>);
-    if (e == cudaSuccess) e = launch_cluster(choose_kernel<P>, (unsigned)(items * ranks), kThreads, bytes, ranks, s, a);
+    cudaError_t e = opt_in_shared_memory(configured, (int)sizeof(ChooseShared<P>) + 4 * kKeys, choose_kernel<P, kFloat>);
+    if (e == cudaSuccess) e = launch_cluster(choose_kernel<P, kFloat>, (unsigned)(items * ranks), kThreads, bytes, ranks, s, a);
     return e;
+}
+
+template <int P>
+cudaError_t launch_choose(const CacheChooseArgs& a, cudaStream_t s)
+{
+    return a.queries.type == LQ_F32 ? launch_choose_as<P, true>(a, s) : launch_choose_as<P, false>(a, s);
 }
 
 }  // namespace
