@@ -247,7 +247,7 @@ int take_attend(const lq_cache* c, int32_t layer, const lq_rows* queries, int64_
     a->shape = s; a->tables = c->tables + (size_t)layer * 2;
     a->pages = pages; a->table = table; a->lengths = lengths; a->lse = lse; a->flags = c->flags;
     a->num_pages = num_pages; a->table_width = table_width;
-    a->batch = (int32_t)batch; a->group = heads / s.heads; a->group_blocks = (a->group + 7) / 8; a->row_heads = s.heads;
+    a->batch = (int32_t)batch; a->group = heads / s.heads; a->group_blocks = (a->group + 7) / 8; a->row_heads = s.heads; a->sequence_rows = 1; a->by_rows = rows_of(1);
     a->sms = c->sms;
     return LQ_OK;
 }
@@ -522,7 +522,7 @@ int lq_cache_attend_chosen(lq_cache* cache, int32_t layer, const lq_rows* querie
     LQ_TRY(check_units(cache, a, batch));
     if (batch == 0) return LQ_OK;
     a.batch = (int32_t)batch * cache->shape.heads;
-    a.row_heads = 1;
+    a.row_heads = 1; a.sequence_rows = cache->shape.heads; a.by_rows = rows_of(cache->shape.heads);
     LQ_ON_DEVICE(cache);
     LQ_CUDA(launch_attend(a, (cudaStream_t)stream));
     return LQ_OK;

@@ -115,7 +115,8 @@ struct CacheAttendArgs {
     int64_t num_pages, table_width, window, before_most;        // before_most: tokens that *before can mean
     float scale;                        // of the scores, times log2(e)
     int32_t batch, group, group_blocks; // rows of the table; queries a head, and their blocks of 8
-    int32_t row_heads;                  // heads that a row of the table serves: all, or 1
+    int32_t row_heads, sequence_rows;   // heads that a row of the table serves: all, or 1; rows of a sequence: 1, or as many as there are heads
+    CacheRowsOf by_rows;
     int32_t sms;                        // CTAs
 };
 

@@ -236,9 +236,8 @@ __device__ __forceinline__ void store_four(const CacheRows& r, char* row, int d,
 struct Owner { int sequence, head; };
 __device__ __forceinline__ Owner owner_of(const CacheAttendArgs& a, int row, int head)
 {
-    if (a.row_heads == a.shape.heads) return {row, head};
-    const int sequence = row / a.shape.heads;
-    return {sequence, row - sequence * a.shape.heads};
+    const int sequence = (int)(__umulhi(2u * (uint32_t)row, a.by_rows.factor) >> a.by_rows.shift);      // row / (rows of a sequence)
+    return {sequence, head + row - sequence * a.sequence_rows};
 }
 
 // What a row of the table has to be read of: tokens [first, length), as tiles [tile0, tile1).
@@ -647,20 +646,19 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
             if (count <= 0) break;                                      // (the end of our share)
             if (chunk < 0) chunk = 0;
             const int row_head = hb / a.group_blocks, block = hb - row_head * a.group_blocks;
-            const Owner owner = owner_of(a, sequence, row_head);
-            const int head = owner.head;
+            const Owner asked = owner_of(a, sequence, row_head);
             // ---- the first copies: this warp's tiles are kPair of every unit
             const int32_t* pages = a.table + (int64_t)sequence * a.table_width;
             const int tile0 = extent.tile0 + (int)chunk * X::kUnit + warp * X::kPair, stop = min(extent.tile1, extent.tile0 + ((int)chunk + count) * X::kUnit);
             const int rounds = stop > tile0 ? (stop - tile0 + X::kUnit - 1) / X::kUnit : 0;
-            const uint32_t head_at = (uint32_t)(head * a.shape.head_words) * 4;
+            const uint32_t head_at = (uint32_t)(asked.head * a.shape.head_words) * 4;
             auto tile_of = [&](int n) { return tile0 + n / X::kPair * X::kUnit + n % X::kPair; };      // of the warp's n-th tile
             uint32_t missing = 0;                                       // bit s: stage s holds no tile: past the end, or on a page that is not there
             int page = -1;                                              // lane l: of the warp's tile 32 i + l, i as far as copies are
             auto page_of = [&](int n) { const int tile = tile_of(n); return tile < stop ? pages[tile >> tile_shift] : -1; };
             const int first_pages = page_of(lane);
             Query<P, kFloat> query_raw;
-            query_raw.fetch(a, owner.sequence, head, block * kQueries + (kRests ? warp % 4 : warp), lane, extent.length);
+            query_raw.fetch(a, asked.sequence, asked.head, block * kQueries + (kRests ? warp % 4 : warp), lane, extent.length);
             auto start = [&](int round, int stage) {
                 if (round < rounds) {
                     if (round * X::kPair % 32 == 0) {
@@ -858,6 +856,11 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
             team_sync(team);
             const bool starts = chunk == 0, whole = starts && count == units, done = whole && !a.sums;
             const int slot = 2 * me + starts;
+            // (found again, so that it need not be kept while the tiles are gone through: 1 to 2 %)
+            int again = sequence, again_hb = hb;
+            asm volatile("" : "+r"(again), "+r"(again_hb));
+            const Owner owner = owner_of(a, again, again_hb / a.group_blocks);
+            const int head = owner.head;
             const int64_t first_query = (int64_t)owner.sequence * a.shape.heads * a.group + head * a.group + block * kQueries;
             float* const left = whole ? a.sums + first_query * cache_part_floats(P) : partials + slot * kPartial<P>;     // (where it is not done)
             const int lefts = whole ? a.group - block * kQueries : kQueries;            // a query that is not there has no part
