@@ -82,6 +82,7 @@ constexpr int64_t kPartial = cache_partial_floats(P);
 template <int P>
 struct TeamShared {
     int64_t words[18];                  // schedule
+    int32_t sequence, head;             // whose queries the segment has
     float factor[kQueries];             // scale * log2(e) / the query's power of two
     float stats[kTeamWarps][kQueries][3];
     float share[kQueries][kTeamWarps + 4];      // factor of each warp's sums; then that of the whole segment's
@@ -647,6 +648,7 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
             if (chunk < 0) chunk = 0;
             const int row_head = hb / a.group_blocks, block = hb - row_head * a.group_blocks;
             const Owner asked = owner_of(a, sequence, row_head);
+            if (tid == 0) { sh.sequence = asked.sequence; sh.head = asked.head; }   // (for the end: not to be kept in registers, 2 %)
             // ---- the first copies: this warp's tiles are kPair of every unit
             const int32_t* pages = a.table + (int64_t)sequence * a.table_width;
             const int tile0 = extent.tile0 + (int)chunk * X::kUnit + warp * X::kPair, stop = min(extent.tile1, extent.tile0 + ((int)chunk + count) * X::kUnit);
@@ -856,10 +858,7 @@ __global__ void __launch_bounds__(Stage<P, WK, WV>::kTeams* kTeam, 1) attend_ker
             team_sync(team);
             const bool starts = chunk == 0, whole = starts && count == units, done = whole && !a.sums;
             const int slot = 2 * me + starts;
-            // (found again, so that it need not be kept while the tiles are gone through: 1 to 2 %)
-            int again = sequence, again_hb = hb;
-            asm volatile("" : "+r"(again), "+r"(again_hb));
-            const Owner owner = owner_of(a, again, again_hb / a.group_blocks);
+            const Owner owner = {sh.sequence, sh.head};
             const int head = owner.head;
             const int64_t first_query = (int64_t)owner.sequence * a.shape.heads * a.group + head * a.group + block * kQueries;
             float* const left = whole ? a.sums + first_query * cache_part_floats(P) : partials + slot * kPartial<P>;     // (where it is not done)
