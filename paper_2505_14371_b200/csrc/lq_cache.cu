@@ -286,16 +286,17 @@ int64_t most_tokens(const lq_cache* c, int64_t width) { return std::min<int64_t>
 
 // The workspace of attention with a shared prefix, in floats from its start: the queries, parts of the prefix, parts of the sequences' own tokens, and what
 // lq_cache_attend needs for those (-1: nothing).
-struct SharedSpace { int splits, slots; bool rests; int64_t rows, parts, own, partial, bytes; };
+struct SharedSpace { int splits, slots; bool pairs, rests; int64_t rows, parts, own, partial, bytes; };
 SharedSpace shared_space(const lq_cache* c, int64_t batch, int heads, int64_t prefix_width, int64_t table_width, int type, bool turned)
 {
     const CacheShape& s = c->shape;
     const int64_t rows = batch * heads, part = cache_part_floats(s.padded);
     SharedSpace x{};
-    // fp32 queries, and turned ones of fp16 outputs, are sums of two fp16 numbers; turned ones of bf16 outputs are one, see lq_cache_shared.cu
-    x.rests = type == LQ_F32 || (type == LQ_F16 && turned);
-    x.slots = cache_shared_slots(s.padded, x.rests);
-    x.splits = batch > 0 ? cache_shared_splits(s.heads, x.slots, batch * (heads / s.heads), most_tokens(c, prefix_width), type == LQ_F32, c->sms) : 0;
+    const bool two = type != LQ_BF16;   // weights as sums of two fp16 numbers; queries: fp32 and turned ones
+    x.rests = type == LQ_F32 || turned;
+    x.slots = cache_shared_slots(s.padded, two, x.rests);
+    x.pairs = cache_shared_pairs(s.padded, two, x.rests);
+    x.splits = batch > 0 ? cache_shared_splits(s.heads, x.pairs, batch * (heads / s.heads), most_tokens(c, prefix_width), type == LQ_F32, c->sms) : 0;
     x.parts = x.splits > 0 ? (batch * (heads / s.heads) + 127) / 128 * s.heads * (cache_shared_block_bytes(s.padded) / 4) : 0;
     x.own = x.parts + x.splits * (int64_t)x.slots * rows * part;
     const int64_t partial = x.own + (table_width > 0 ? rows * part : 0), bytes = workspace_of(c, table_width, 0);
@@ -567,7 +568,7 @@ int lq_cache_attend_shared(lq_cache* cache, int32_t layer, const lq_rows* querie
     b.prefix = prefix; b.prefix_length = prefix_length; b.lengths = lengths; b.lse = lse; b.flags = cache->flags;
     b.num_pages = num_pages; b.prefix_width = prefix_width; b.prefix_most = most_tokens(cache, prefix_width); b.own_most = most_tokens(cache, table_width);
     b.scale = a.scale; b.batch = a.batch; b.group = a.group; b.splits = space.splits;
-    b.rests = space.rests; b.slots = space.slots;
+    b.rests = space.rests; b.slots = space.slots; b.pairs = space.pairs;
     b.rows = reinterpret_cast<char*>(base + space.rows); b.parts = base + space.parts; b.own = base + space.own;
     a.partial = space.partial < 0 ? nullptr : base + space.partial;
     a.sums = b.own; a.before = prefix_length; a.before_most = b.prefix_most; a.lse = nullptr;

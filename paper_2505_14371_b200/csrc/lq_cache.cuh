@@ -138,7 +138,7 @@ struct CacheSharedArgs {
     int64_t num_pages, prefix_width, prefix_most, own_most;     // tokens that the lengths can mean
     float scale;
     int32_t batch, group, splits;
-    int32_t rests, slots;               // queries are sums of two fp16 numbers; blocks of rows that a CTA takes at a time
+    int32_t rests, slots, pairs;        // queries are sums of two fp16 numbers; see cache_shared_slots, cache_shared_pairs
 };
 
 // Which pages a sequence's queries look at (lq_cache_choose.cu).
@@ -182,9 +182,12 @@ cudaError_t launch_cache_choose(const CacheChooseArgs& a, cudaStream_t s);
 cudaError_t launch_cache_shared_rows(const CacheSharedArgs& a, cudaStream_t s);
 cudaError_t launch_cache_shared_prefix(const CacheSharedArgs& a, cudaStream_t s);
 cudaError_t launch_cache_shared_join(const CacheSharedArgs& a, cudaStream_t s);
-// Into how many parts the prefix's tokens are split, and how many parts a query may leave of each (blocks of rows that tensor memory holds at a time).
-int cache_shared_splits(int heads, int slots, int64_t rows, int64_t prefix_tokens, bool exact, int sms);
-__host__ __device__ constexpr int cache_shared_slots(int padded, bool rests) { return padded == 256 || (padded == 128 && rests) ? 1 : 2; }
+// Into how many parts the prefix's tokens are split, and how many parts a query may leave of each (scores and sums of 128 rows that
+// tensor memory holds at a time; `two`: weights are sums of two fp16 numbers, `rests`: queries are).
+int cache_shared_splits(int heads, bool pairs, int64_t rows, int64_t prefix_tokens, bool exact, int sms);
+__host__ __device__ constexpr int cache_shared_slots(int padded, bool two, bool rests) { return padded == 256 || (padded == 128 && two && rests) ? 1 : 2; }
+// Whether a CTA takes two blocks of rows where there are two.  Rows of 128 whose queries are sums of two numbers: one, whose rests its slots share.
+__host__ __device__ constexpr bool cache_shared_pairs(int padded, bool two, bool rests) { return cache_shared_slots(padded, two, rests) == 2 && !(padded == 128 && rests); }
 // Workspace for a head's block of 128 rows: fp16 numbers, what their rounding left, a factor for each row.
 __host__ __device__ constexpr int cache_shared_block_bytes(int padded) { return 128 * (4 * padded + 4); }
 // Teams of 8 warps that share an SM in the attention kernel (its registers: rows of 256 need twice as many a thread), and what

@@ -43,9 +43,9 @@ constexpr int kLift = 6;
 constexpr int kColumns = 512;           // of tensor memory: all (one CTA an SM)
 
 // Shared memory, by address.  Below the table: pieces (a tile's keys or values), then what is small; behind it: the queries, then pieces.
-template <int P, bool kRests>
+template <int P, bool kTwo, bool kRests>
 struct Layout {
-    static constexpr int kSlots = cache_shared_slots(P, kRests), kPanels = P / 64, kPiece = P * 128;
+    static constexpr int kSlots = cache_shared_slots(P, kTwo, kRests), kPanels = P / 64, kPiece = P * 128;
     static constexpr int kKeys = P == 64 ? 3 : P == 128 ? 2 : 1, kValues = P == 64 ? 4 : P == 128 ? 3 : 1;      // tiles of keys and of values at a time
     static constexpr int kSoftmaxWarps = 4;                             // of a slot: a thread has a row
     static constexpr int kThreads = 32 * kSoftmaxWarps * kSlots + kDecode + 128;
@@ -62,8 +62,11 @@ struct Layout {
     static __device__ __forceinline__ uint32_t values(int stage) { return piece(kKeys + stage); }
     static __device__ __forceinline__ uint32_t queries(int slot, int panel) { return kHighAt + (slot * kPanels + panel) * kPanelQ; }
     // tensor memory, columns of a slot: scores, weights (and what their rounding left), sums, what the queries' rounding left
-    static constexpr int kScores = 0, kWeights = kTile, kSums = 2 * kTile, kRest = 2 * kTile + P, kSlotColumns = kRest + (kRests ? P / 2 : 0);
-    static_assert(kSlots * kSlotColumns <= kColumns && kEnd <= 227 << 10, "places");
+    static constexpr int kScores = 0, kWeights = kTile, kSums = kTile + (kTwo ? kTile : kTile / 2), kOwnColumns = kSums + P;
+    static constexpr bool kShared = kRests && kSlots == 2 && !cache_shared_pairs(P, kTwo, kRests);      // both slots have the same rows, and one copy of their rests
+    static constexpr int kSlotColumns = kOwnColumns + (kRests && !kShared ? P / 2 : 0), kAllColumns = kSlots * kSlotColumns + (kShared ? P / 2 : 0);
+    static __device__ __forceinline__ uint32_t rests(int slot) { return kShared ? kSlots * kSlotColumns : slot * kSlotColumns + kOwnColumns; }
+    static_assert(kAllColumns <= kColumns && kEnd <= 227 << 10, "places");
 };
 
 struct Small {
@@ -337,20 +340,21 @@ struct Share {
 };
 
 // The pair of blocks that this CTA takes, and whether it is one.
-template <int kSlots>
+template <int kSlots, bool kPairs>
 __device__ __forceinline__ bool pair_of_blocks(const CacheSharedArgs& a, int* head = nullptr, int* block = nullptr)
 {
-    const int blocks = (a.batch * a.group + kRows - 1) / kRows, pairs = (blocks + kSlots - 1) / kSlots;
-    const int item = blockIdx.x / a.splits, h = item / pairs, b = (item - h * pairs) * kSlots;
+    constexpr int kAtOnce = kPairs ? kSlots : 1;
+    const int blocks = (a.batch * a.group + kRows - 1) / kRows, pairs = (blocks + kAtOnce - 1) / kAtOnce;
+    const int item = blockIdx.x / a.splits, h = item / pairs, b = (item - h * pairs) * kAtOnce;
     if (head) { *head = h; *block = b; }
-    return kSlots == 2 && b + 1 < blocks;
+    return kAtOnce == 2 && b + 1 < blocks;
 }
 
-template <int kSlots>
+template <int kSlots, bool kPairs>
 __device__ __forceinline__ Share share_of(const CacheSharedArgs& a)
 {
     Share s;
-    s.pair = pair_of_blocks<kSlots>(a, &s.head, &s.block);
+    s.pair = pair_of_blocks<kSlots, kPairs>(a, &s.head, &s.block);
     const int split = blockIdx.x % a.splits;
     const int given = *a.prefix_length;
     s.length = given < 0 ? 0 : given > a.prefix_most ? a.prefix_most : given;
@@ -586,7 +590,7 @@ __device__ __noinline__ Row moved_row(Row row, Small& sm, const uint32_t* v, int
 // and taken out of the denominator again.
 template <int P, bool kTwo, bool kRests>
 struct Softmax {
-    using L = Layout<P, kRests>;
+    using L = Layout<P, kTwo, kRests>;
     Row row;
     int slot;
     uint32_t columns;                   // of tensor memory, this slot's
@@ -690,11 +694,12 @@ struct Softmax {
 template <int P, bool kTwo, bool kRests>
 __device__ __forceinline__ bool issue_scores(const CacheSharedArgs& a, const Share& s, Small& sm, uint32_t tensor, int slot)
 {
-    using L = Layout<P, kRests>;
+    using L = Layout<P, kTwo, kRests>;
     constexpr uint32_t how = instruction(kTile, false);
     const uint32_t at = tensor + slot * L::kSlotColumns;
     bool ok = wait(&sm.brought, 0, sm, a.flags);
-    if constexpr (kRests) ok = wait(&sm.weighed[slot], 0, sm, a.flags) && ok;
+    if constexpr (kRests)               // (what the queries' rounding left is there)
+        for (int w = L::kShared ? 0 : slot; w < (L::kShared ? L::kSlots : slot + 1); ++w) ok = wait(&sm.weighed[w], 0, sm, a.flags) && ok;
     const uint64_t queries = operand(L::queries(s.pair ? slot : 0, 0), 16);
     for (int tile = s.pair ? 0 : slot, n = 0; tile < s.tiles; tile += s.pair ? 1 : L::kSlots, ++n) {
         const int stage = tile % L::kKeys;
@@ -707,7 +712,7 @@ __device__ __forceinline__ bool issue_scores(const CacheSharedArgs& a, const Sha
         if constexpr (kRests)
 #pragma unroll
             for (int k = 0; k < P / 16; ++k)
-                multiply_tensor(at + L::kScores, at + L::kRest + 8 * k, keys + (k / 4 * kPanel + k % 4 * 32 >> 4), how, k > 0);
+                multiply_tensor(at + L::kScores, tensor + L::rests(slot) + 8 * k, keys + (k / 4 * kPanel + k % 4 * 32 >> 4), how, k > 0);
 #pragma unroll
         for (int k = 0; k < P / 16; ++k)
             multiply(at + L::kScores, queries + (k / 4 * kPanelQ + k % 4 * 32 >> 4), keys + (k / 4 * kPanel + k % 4 * 32 >> 4), how, kRests || k > 0);
@@ -720,7 +725,7 @@ __device__ __forceinline__ bool issue_scores(const CacheSharedArgs& a, const Sha
 template <int P, bool kTwo, bool kRests>
 __device__ __forceinline__ bool issue_sums(const CacheSharedArgs& a, const Share& s, Small& sm, uint32_t tensor, int slot)
 {
-    using L = Layout<P, kRests>;
+    using L = Layout<P, kTwo, kRests>;
     constexpr uint32_t how = instruction(P, true);
     const uint32_t at = tensor + slot * L::kSlotColumns;
     bool ok = !kRests || wait(&sm.weighed[slot], 0, sm, a.flags);       // (its first phase is that of the queries' rests)
@@ -745,9 +750,9 @@ __device__ __forceinline__ bool issue_sums(const CacheSharedArgs& a, const Share
 // ---- the kernel ------------------------------------------------------------------------------------------------
 
 template <int P, bool kTwo, bool kRests>
-__global__ void __launch_bounds__(Layout<P, kRests>::kThreads, 1) shared_prefix_kernel(const __grid_constant__ CacheSharedArgs a)
+__global__ void __launch_bounds__(Layout<P, kTwo, kRests>::kThreads, 1) shared_prefix_kernel(const __grid_constant__ CacheSharedArgs a)
 {
-    using L = Layout<P, kRests>;
+    using L = Layout<P, kTwo, kRests>;
     extern __shared__ __align__(1024) char smem[];
     char* const shared = smem - __cvta_generic_to_shared(smem);         // shared address 0
     Small& sm = *reinterpret_cast<Small*>(shared + L::kSmallAt);
@@ -763,7 +768,7 @@ __global__ void __launch_bounds__(Layout<P, kRests>::kThreads, 1) shared_prefix_
     if (warp == L::kIssuer) {
         if (lane == 0) {
             constexpr int kItems = Codes<P>::kItems / 2;                // warps that bring a tile's keys, or values
-            const int readers = pair_of_blocks<L::kSlots>(a) ? 2 : 1;   // slots that read them
+            const int readers = pair_of_blocks<L::kSlots, cache_shared_pairs(P, kTwo, kRests)>(a) ? 2 : 1;   // slots that read them
             for (int i = 0; i < 4; ++i) {
                 barrier_init(&sm.key_full[i], 32 * kItems); barrier_init(&sm.key_empty[i], readers);
                 barrier_init(&sm.value_full[i], 32 * kItems); barrier_init(&sm.value_empty[i], readers);
@@ -783,7 +788,7 @@ __global__ void __launch_bounds__(Layout<P, kRests>::kThreads, 1) shared_prefix_
     }
     pdl_wait();
     pdl_launch_next();
-    const Share s = share_of<L::kSlots>(a);
+    const Share s = share_of<L::kSlots, cache_shared_pairs(P, kTwo, kRests)>(a);
     fence_before();
     __syncthreads();
     fence_after();
@@ -807,14 +812,14 @@ __global__ void __launch_bounds__(Layout<P, kRests>::kThreads, 1) shared_prefix_
         if constexpr (kRests) {                                         // what the queries' rounding left goes to tensor memory
             const uint4* from = reinterpret_cast<const uint4*>(queries + 2 * P * kRows + place * 2 * P);
 #pragma unroll 1
-            for (int p = 0; p < L::kPanels; ++p) {
+            for (int p = L::kShared ? slot : 0; p < L::kPanels; p += L::kShared ? L::kSlots : 1) {
                 uint32_t v[32];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const uint4 x = from[8 * p + i];
                     v[4 * i] = x.x; v[4 * i + 1] = x.y; v[4 * i + 2] = x.z; v[4 * i + 3] = x.w;
                 }
-                tensor_store32(mine + L::kRest + 32 * p, v);
+                tensor_store32(lanes + L::rests(slot) + 32 * p, v);
             }
             stored();
             fence_before();
@@ -830,7 +835,10 @@ __global__ void __launch_bounds__(Layout<P, kRests>::kThreads, 1) shared_prefix_
             if (!ok) break;
             fence_after();
             if (live) softmax.tile(sm, stage, n, a.flags);
-            else arrive(&sm.taken[slot]);
+            else {                      // (its arrivals must not run ahead of the others' by a tile)
+                arrive(&sm.taken[slot]);
+                if (n > 0) wait(&sm.summed[slot], (n - 1) & 1, sm, a.flags);
+            }
             fence_before();
             arrive(&sm.weighed[slot]);
         }
@@ -948,7 +956,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) shared_join_kernel(const __gr
     const int heads = a.shape.heads * a.group, sequence = there ? (int)(row / heads) : 0, head = there ? (int)(row - (int64_t)sequence * heads) : 0;
     const int64_t in_head = (int64_t)sequence * a.group + head % a.group;
     const int blocks = (int)(((int64_t)a.batch * a.group + kRows - 1) / kRows), block = (int)(in_head / kRows);
-    const bool alone = a.slots == 2 && blocks % 2 == 1 && block == blocks - 1;
+    const bool alone = a.slots == 2 && (!a.pairs || (blocks % 2 == 1 && block == blocks - 1));
     const int before = a.splits * (alone ? 2 : 1), parts = there ? before + (a.own_most > 0 && a.lengths[sequence] > 0) : 0;
     const float* const prefix = fresh(a.parts);
     const float* const own = fresh(a.own);
@@ -1043,7 +1051,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) shared_join_kernel(const __gr
 template <int P, bool kTwo, bool kRests>
 cudaError_t launch_prefix(const CacheSharedArgs& a, cudaStream_t s)
 {
-    using L = Layout<P, kRests>;
+    using L = Layout<P, kTwo, kRests>;
     static std::atomic<uint64_t> configured{0};
     cudaError_t e = opt_in_shared_memory(configured, L::kEnd, shared_prefix_kernel<P, kTwo, kRests>);
     // registers are dealt out anew in the kernel: it must have been given as many as that counts on
@@ -1054,7 +1062,7 @@ cudaError_t launch_prefix(const CacheSharedArgs& a, cudaStream_t s)
         if (e == cudaSuccess && at.numRegs != L::kRegisters) e = cudaErrorLaunchOutOfResources;
         if (e == cudaSuccess) registers.store(at.numRegs, std::memory_order_relaxed);
     }
-    const int64_t blocks = ((int64_t)a.batch * a.group + kRows - 1) / kRows, items = a.shape.heads * ((blocks + L::kSlots - 1) / L::kSlots);
+    const int64_t blocks = ((int64_t)a.batch * a.group + kRows - 1) / kRows, items = a.shape.heads * (a.pairs ? (blocks + 1) / 2 : blocks);
     if (e == cudaSuccess) e = launch(shared_prefix_kernel<P, kTwo, kRests>, (unsigned)(items * a.splits), L::kThreads, L::kEnd, s, a);
     return e;
 }
@@ -1062,7 +1070,7 @@ cudaError_t launch_prefix(const CacheSharedArgs& a, cudaStream_t s)
 template <int P>
 cudaError_t launch_prefix_of(const CacheSharedArgs& a, cudaStream_t s)
 {
-    if (a.queries.type == LQ_BF16) return launch_prefix<P, false, false>(a, s);
+    if (a.queries.type == LQ_BF16) return a.rests ? launch_prefix<P, false, true>(a, s) : launch_prefix<P, false, false>(a, s);
     return a.rests ? launch_prefix<P, true, true>(a, s) : launch_prefix<P, true, false>(a, s);
 }
 
@@ -1085,12 +1093,12 @@ cudaError_t launch_join(const CacheSharedArgs& a, cudaStream_t s)
 
 }  // namespace
 
-int cache_shared_splits(int heads, int slots, int64_t rows, int64_t prefix_tokens, bool exact, int sms)
+int cache_shared_splits(int heads, bool pairs, int64_t rows, int64_t prefix_tokens, bool exact, int sms)
 {
-    const int64_t blocks = (rows + kRows - 1) / kRows, items = heads * ((blocks + slots - 1) / slots), tiles = (prefix_tokens + kTile - 1) / kTile;
+    const int64_t blocks = (rows + kRows - 1) / kRows, items = heads * (pairs ? (blocks + 1) / 2 : blocks), tiles = (prefix_tokens + kTile - 1) / kTile;
     if (tiles == 0) return 0;
     // a tile of two blocks takes twice as long as one of a block alone; what a CTA takes besides is some 8 of those
-    const int64_t each = blocks > 1 && slots == 2 ? 2 : 1;
+    const int64_t each = blocks > 1 && pairs ? 2 : 1;
     // fp32 outputs: sums of 1024 tokens at most, as the matrix unit cuts off what a sum's last bit does not hold
     int64_t best = 1, cost = INT64_MAX;
     for (int64_t n = exact ? (tiles + 15) / 16 : 1; n <= tiles; ++n) {
