@@ -46,14 +46,16 @@ constexpr int kColumns = 512;           // of tensor memory: all (one CTA an SM)
 template <int P, bool kTwo, bool kRests>
 struct Layout {
     static constexpr int kSlots = cache_shared_slots(P, kTwo, kRests), kPanels = P / 64, kPiece = P * 128;
-    static constexpr int kKeys = P == 64 ? 3 : P == 128 ? 2 : 1, kValues = P == 64 ? 4 : P == 128 ? 3 : 1;      // tiles of keys and of values at a time
+    static constexpr int kBlocks = cache_shared_pairs(P, kTwo, kRests) ? 2 : 1;         // of rows
+    // tiles of keys and of values at a time: as many as there is room for
+    static constexpr int kKeys = P == 64 ? 3 : P == 256 ? 1 : kBlocks == 2 ? 2 : 3, kValues = P == 64 ? 4 : P == 256 ? 1 : kBlocks == 2 ? 3 : 4;
     static constexpr int kSoftmaxWarps = 4;                             // of a slot: a thread has a row
     static constexpr int kThreads = 32 * kSoftmaxWarps * kSlots + kDecode + 128;
     static constexpr int kDecodeAt = kSoftmaxWarps * kSlots, kIssuer = kDecodeAt + kDecodeWarps;        // warps (three behind the issuer have nothing to do)
     // Registers a thread at launch, and as they are dealt out to softmax, decoding and products: no more than all threads had.
     static constexpr int kRegisters = kSlots == 2 ? 96 : 128, kSoftmax = kSlots == 2 ? 144 : 208, kDecoding = kSlots == 2 ? 72 : 120, kProducts = 40;
     static_assert(32 * kSoftmaxWarps * kSlots * kSoftmax + kDecode * kDecoding + 128 * kProducts <= kThreads * kRegisters && kThreads * kRegisters <= 65536, "registers");
-    static constexpr int kQueries = kSlots * kPanels * kPanelQ;
+    static constexpr int kQueries = kBlocks * kPanels * kPanelQ;
     static constexpr int kLowPieces = P == 64 ? 7 : P == 128 ? 3 : 1;
     static constexpr int kSmallAt = kSystemBytes + kLowPieces * kPiece;
     static constexpr int kEnd = kHighAt + kQueries + (kKeys + kValues - kLowPieces) * kPiece;
