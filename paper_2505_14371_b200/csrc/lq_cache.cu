@@ -286,14 +286,14 @@ int64_t most_tokens(const lq_cache* c, int64_t width) { return std::min<int64_t>
 
 // The workspace of attention with a shared prefix, in floats from its start: the queries, parts of the prefix, parts of the sequences' own tokens, and what
 // lq_cache_attend needs for those (-1: nothing).
-struct SharedSpace { int splits, slots; bool pairs, rests; int64_t rows, parts, own, partial, bytes; };
+struct SharedSpace { int splits, slots, rests; bool pairs; int64_t rows, parts, own, partial, bytes; };
 SharedSpace shared_space(const lq_cache* c, int64_t batch, int heads, int64_t prefix_width, int64_t table_width, int type, bool turned)
 {
     const CacheShape& s = c->shape;
     const int64_t rows = batch * heads, part = cache_part_floats(s.padded);
     SharedSpace x{};
     const bool two = type != LQ_BF16;   // weights as sums of two fp16 numbers; queries: fp32 and turned ones
-    x.rests = type == LQ_F32 || turned;
+    x.rests = !(type == LQ_F32 || turned) ? 0 : s.padded == 128 && !two && batch * (heads / s.heads) > 128 ? kRestsInPlace : kRestsBeside;
     x.slots = cache_shared_slots(s.padded, two, x.rests);
     x.pairs = cache_shared_pairs(s.padded, two, x.rests);
     x.splits = batch > 0 ? cache_shared_splits(s.heads, x.pairs, batch * (heads / s.heads), most_tokens(c, prefix_width), type == LQ_F32, c->sms) : 0;

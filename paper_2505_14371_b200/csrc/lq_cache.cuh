@@ -183,11 +183,18 @@ cudaError_t launch_cache_shared_rows(const CacheSharedArgs& a, cudaStream_t s);
 cudaError_t launch_cache_shared_prefix(const CacheSharedArgs& a, cudaStream_t s);
 cudaError_t launch_cache_shared_join(const CacheSharedArgs& a, cudaStream_t s);
 // Into how many parts the prefix's tokens are split, and how many parts a query may leave of each (scores and sums of 128 rows that
-// tensor memory holds at a time; `two`: weights are sums of two fp16 numbers, `rests`: queries are).
+// tensor memory holds at a time; `two`: weights are sums of two fp16 numbers, `rests`: see there).
 int cache_shared_splits(int heads, bool pairs, int64_t rows, int64_t prefix_tokens, bool exact, int sms);
-__host__ __device__ constexpr int cache_shared_slots(int padded, bool two, bool rests) { return padded == 256 || (padded == 128 && two && rests) ? 1 : 2; }
-// Whether a CTA takes two blocks of rows where there are two.  Rows of 128 whose queries are sums of two numbers: one, whose rests its slots share.
-__host__ __device__ constexpr bool cache_shared_pairs(int padded, bool two, bool rests) { return cache_shared_slots(padded, two, rests) == 2 && !(padded == 128 && rests); }
+// What queries' rounding leaves: nothing, numbers beside the scores and weights, or (rows of 128 with weights of 11 bits, where tensor memory has
+// no room for them and a second block's scores) numbers beside scores that give way to their weights.  128 sequences over 16384 tokens, two blocks of
+// rows a CTA: 150 us beside (one block a CTA then), 139 in place; 32 over 4096, one block: 46 us and (with an earlier form of the kernel) 49.
+constexpr int kRestsBeside = 1, kRestsInPlace = 2;
+__host__ __device__ constexpr int cache_shared_slots(int padded, bool two, int rests) { return padded == 256 || (padded == 128 && two && rests) ? 1 : 2; }
+// Whether a CTA takes two blocks of rows where there are two.
+__host__ __device__ constexpr bool cache_shared_pairs(int padded, bool two, int rests)
+{
+    return cache_shared_slots(padded, two, rests) == 2 && !(padded == 128 && rests == kRestsBeside);
+}
 // Workspace for a head's block of 128 rows: fp16 numbers, what their rounding left, a factor for each row.
 __host__ __device__ constexpr int cache_shared_block_bytes(int padded) { return 128 * (4 * padded + 4); }
 // Teams of 8 warps that share an SM in the attention kernel (its registers: rows of 256 need twice as many a thread), and what

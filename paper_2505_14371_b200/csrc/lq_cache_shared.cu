@@ -9,15 +9,24 @@
 // two for fp16 and fp32 ones (22 bits).
 //
 // Work.  All sequences' queries of one head of the cache are the rows of a matrix, 128 of them a block: both products are dense, and
-// run on tcgen05: S = Q K^T (128 x 64 tokens, Q and K in shared memory) and O += W V (W in tensor memory, where the scores stood; V in
-// shared memory, tokens outermost).  What q's rounding left is a second operand in tensor memory, what w's left stands beside W.
-// A CTA has two slots (one for rows of 256), each with scores, weights, sums and four warps of its own, so that one slot's scores go through the
-// softmax while the other's products run: two blocks of rows over the same tiles of 64 tokens or, where a block is alone, that
-// block over even and odd tiles.  Eight warps decode: a byte of a row is looked up in a table of shared memory that has a copy in each lane's bank
-// (as in lq_cache_attend.cuh), 8 coordinates are 16 bytes of a tile, swizzled by 128 bytes as the matrix unit reads it.
+// run on tcgen05: S = Q K^T (128 x 64 tokens, Q and K in shared memory) and O += W V (W in tensor memory; V in shared memory, tokens
+// outermost).  What the queries' rounding left is a second operand of the first product, in tensor memory; what the weights' left is one of the second.
+// Tensor memory holds two slots, each with scores, weights, sums and four warps of softmax (one slot where that takes more than half: rows
+// of 256, and rows of 128 with both rests).  A CTA takes two blocks of rows over the same tiles or, where a block is alone, one
+// block whose even tiles go to one slot and whose odd ones to the other; the two then share the rests of rows of 128, which leave no room else.  The scores of a tile are made while the softmax of the one before
+// runs: a slot's scores may come again once they have been taken to registers, its weights once the sums have them.
+// Eight warps decode: a byte of a row is looked up in a table of shared memory that has a copy in each lane's bank (as in lq_cache_attend.cuh), a
+// thread writes 64 coordinates of a token, swizzled by 128 bytes as the matrix unit reads them.  Two warps a slot issue products, so that each waits only for what
+// its own need.
 //
-// Split.  The prefix's tiles of a (head, pair of blocks) are dealt to several CTAs such that the GPU is full; each leaves for every row its
-// sums, reference, scale and denominator, and a second kernel joins them with those of the sequence's own tokens.
+// Split.  The prefix's tiles of a (head, block or pair of blocks) are dealt to several CTAs such that the GPU is full; each leaves for every row its
+// sums, reference, scale and denominator.  The sequences' own tokens go through lq_cache_attend's kernel, which leaves the same, and a last kernel joins them.
+//
+// What bounds it: the softmax.  Of a tile of 128 rows x 64 tokens its warps' 525 instructions each take some 2000 cycles beside decoding and waits, where the
+// special-function unit alone would need 512 and the products 640 (960 with rests): 16384 tokens for 512 rows of 8 heads of 128, 35 GFLOP, 64 us in
+// pairs of blocks without rests (550 TFLOP/s, the tensor pipe busy for 27 %), some 88 with.  Few rows or tokens: the chain of four kernels, some 24 us.
+// Measured and not kept (that case, all kernels, us, of 114 without rests): eight warps of softmax a slot 147; 16 scores at a time in a loop 146; fragments of four
+// rows a thread, whose norms then serve four scores 148; both slots in step 122.
 //
 // Waits are bounded: after some two seconds a waiting thread sets LQ_CACHE_GAVE_UP, and all leave.
 #include <cuda_bf16.h>
@@ -43,7 +52,7 @@ constexpr int kLift = 6;
 constexpr int kColumns = 512;           // of tensor memory: all (one CTA an SM)
 
 // Shared memory, by address.  Below the table: pieces (a tile's keys or values), then what is small; behind it: the queries, then pieces.
-template <int P, bool kTwo, bool kRests>
+template <int P, bool kTwo, int kRests>
 struct Layout {
     static constexpr int kSlots = cache_shared_slots(P, kTwo, kRests), kPanels = P / 64, kPiece = P * 128;
     static constexpr int kBlocks = cache_shared_pairs(P, kTwo, kRests) ? 2 : 1;         // of rows
@@ -51,7 +60,7 @@ struct Layout {
     static constexpr int kKeys = P == 64 ? 3 : P == 256 ? 1 : kBlocks == 2 ? 2 : 3, kValues = P == 64 ? 4 : P == 256 ? 1 : kBlocks == 2 ? 3 : 4;
     static constexpr int kSoftmaxWarps = 4;                             // of a slot: a thread has a row
     static constexpr int kThreads = 32 * kSoftmaxWarps * kSlots + kDecode + 128;
-    static constexpr int kDecodeAt = kSoftmaxWarps * kSlots, kIssuer = kDecodeAt + kDecodeWarps;        // warps (three behind the issuer have nothing to do)
+    static constexpr int kDecodeAt = kSoftmaxWarps * kSlots, kIssuer = kDecodeAt + kDecodeWarps;        // warps
     // Registers a thread at launch, and as they are dealt out to softmax, decoding and products: no more than all threads had.
     static constexpr int kRegisters = kSlots == 2 ? 96 : 128, kSoftmax = kSlots == 2 ? 144 : 208, kDecoding = kSlots == 2 ? 72 : 120, kProducts = 40;
     static_assert(32 * kSoftmaxWarps * kSlots * kSoftmax + kDecode * kDecoding + 128 * kProducts <= kThreads * kRegisters && kThreads * kRegisters <= 65536, "registers");
@@ -64,7 +73,8 @@ struct Layout {
     static __device__ __forceinline__ uint32_t values(int stage) { return piece(kKeys + stage); }
     static __device__ __forceinline__ uint32_t queries(int slot, int panel) { return kHighAt + (slot * kPanels + panel) * kPanelQ; }
     // tensor memory, columns of a slot: scores, weights (and what their rounding left), sums, what the queries' rounding left
-    static constexpr int kScores = 0, kWeights = kTile, kSums = kTile + (kTwo ? kTile : kTile / 2), kOwnColumns = kSums + P;
+    static constexpr bool kInPlace = kRests == kRestsInPlace;           // weights stand in the scores' place: a slot's next scores wait for its sums
+    static constexpr int kScores = 0, kWeights = kInPlace ? kScores : kTile, kSums = kInPlace ? kTile : kTile + (kTwo ? kTile : kTile / 2), kOwnColumns = kSums + P;
     static constexpr bool kShared = kRests && kSlots == 2 && !cache_shared_pairs(P, kTwo, kRests);      // both slots have the same rows, and one copy of their rests
     static constexpr int kSlotColumns = kOwnColumns + (kRests && !kShared ? P / 2 : 0), kAllColumns = kSlots * kSlotColumns + (kShared ? P / 2 : 0);
     static __device__ __forceinline__ uint32_t rests(int slot) { return kShared ? kSlots * kSlotColumns : slot * kSlotColumns + kOwnColumns; }
@@ -590,7 +600,7 @@ __device__ __noinline__ Row moved_row(Row row, Small& sm, const uint32_t* v, int
 // The softmax of a slot's uses.  A row's scores become weights in one pass with reference and scale as they are, and once more if that shows that these have to
 // move (p is fp32 and has room: a tile's may add up to kRoom; a weight is fp16, up to kMostWeight).  The scale of the weights is part of p's exponent,
 // and taken out of the denominator again.
-template <int P, bool kTwo, bool kRests>
+template <int P, bool kTwo, int kRests>
 struct Softmax {
     using L = Layout<P, kTwo, kRests>;
     Row row;
@@ -693,7 +703,7 @@ struct Softmax {
 // ---- products ------------------------------------------------------------------------------------------------
 
 // Scores of a slot's uses, by one warp, and weighted values by another: each waits only for what its own products need.
-template <int P, bool kTwo, bool kRests>
+template <int P, bool kTwo, int kRests>
 __device__ __forceinline__ bool issue_scores(const CacheSharedArgs& a, const Share& s, Small& sm, uint32_t tensor, int slot)
 {
     using L = Layout<P, kTwo, kRests>;
@@ -705,7 +715,7 @@ __device__ __forceinline__ bool issue_scores(const CacheSharedArgs& a, const Sha
     const uint64_t queries = operand(L::queries(s.pair ? slot : 0, 0), 16);
     for (int tile = s.pair ? 0 : slot, n = 0; tile < s.tiles; tile += s.pair ? 1 : L::kSlots, ++n) {
         const int stage = tile % L::kKeys;
-        ok = wait(&sm.key_full[stage], (tile / L::kKeys) & 1, &sm.taken[slot], (n - 1) & 1, sm, a.flags) && ok;         // (there is no phase before the first to wait for)
+        ok = wait(&sm.key_full[stage], (tile / L::kKeys) & 1, L::kInPlace ? &sm.summed[slot] : &sm.taken[slot], (n - 1) & 1, sm, a.flags) && ok;         // (there is no phase before the first to wait for)
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         fence_after();
@@ -717,23 +727,24 @@ __device__ __forceinline__ bool issue_scores(const CacheSharedArgs& a, const Sha
                 multiply_tensor(at + L::kScores, tensor + L::rests(slot) + 8 * k, keys + (k / 4 * kPanel + k % 4 * 32 >> 4), how, k > 0);
 #pragma unroll
         for (int k = 0; k < P / 16; ++k)
-            multiply(at + L::kScores, queries + (k / 4 * kPanelQ + k % 4 * 32 >> 4), keys + (k / 4 * kPanel + k % 4 * 32 >> 4), how, kRests || k > 0);
+            multiply(at + L::kScores, queries + (k / 4 * kPanelQ + k % 4 * 32 >> 4), keys + (k / 4 * kPanel + k % 4 * 32 >> 4), how, kRests != 0 || k > 0);
         commit(&sm.scored[slot]);
         commit(&sm.key_empty[stage]);
     }
     return ok;
 }
 
-template <int P, bool kTwo, bool kRests>
+template <int P, bool kTwo, int kRests>
 __device__ __forceinline__ bool issue_sums(const CacheSharedArgs& a, const Share& s, Small& sm, uint32_t tensor, int slot)
 {
     using L = Layout<P, kTwo, kRests>;
     constexpr uint32_t how = instruction(P, true);
     const uint32_t at = tensor + slot * L::kSlotColumns;
-    bool ok = !kRests || wait(&sm.weighed[slot], 0, sm, a.flags);       // (its first phase is that of the queries' rests)
+    constexpr int shift = kRests != 0;
+    bool ok = !shift || wait(&sm.weighed[slot], 0, sm, a.flags);       // (its first phase is that of the queries' rests)
     for (int tile = s.pair ? 0 : slot, n = 0; tile < s.tiles; tile += s.pair ? 1 : L::kSlots, ++n) {
         const int stage = tile % L::kValues;
-        ok = wait(&sm.value_full[stage], (tile / L::kValues) & 1, &sm.weighed[slot], (n + kRests) & 1, sm, a.flags) && ok;
+        ok = wait(&sm.value_full[stage], (tile / L::kValues) & 1, &sm.weighed[slot], (n + shift) & 1, sm, a.flags) && ok;
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         fence_after();
@@ -751,7 +762,7 @@ __device__ __forceinline__ bool issue_sums(const CacheSharedArgs& a, const Share
 
 // ---- the kernel ------------------------------------------------------------------------------------------------
 
-template <int P, bool kTwo, bool kRests>
+template <int P, bool kTwo, int kRests>
 __global__ void __launch_bounds__(Layout<P, kTwo, kRests>::kThreads, 1) shared_prefix_kernel(const __grid_constant__ CacheSharedArgs a)
 {
     using L = Layout<P, kTwo, kRests>;
@@ -1050,7 +1061,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) shared_join_kernel(const __gr
     if (lane == 0 && a.lse) a.lse[row] = total != 0.0f ? (r + log2f(total)) * 0.693147180559945309f : -INFINITY;
 }
 
-template <int P, bool kTwo, bool kRests>
+template <int P, bool kTwo, int kRests>
 cudaError_t launch_prefix(const CacheSharedArgs& a, cudaStream_t s)
 {
     using L = Layout<P, kTwo, kRests>;
@@ -1072,8 +1083,9 @@ cudaError_t launch_prefix(const CacheSharedArgs& a, cudaStream_t s)
 template <int P>
 cudaError_t launch_prefix_of(const CacheSharedArgs& a, cudaStream_t s)
 {
-    if (a.queries.type == LQ_BF16) return a.rests ? launch_prefix<P, false, true>(a, s) : launch_prefix<P, false, false>(a, s);
-    return a.rests ? launch_prefix<P, true, true>(a, s) : launch_prefix<P, true, false>(a, s);
+    if (a.queries.type != LQ_BF16) return a.rests ? launch_prefix<P, true, kRestsBeside>(a, s) : launch_prefix<P, true, 0>(a, s);
+    if constexpr (P == 128) { if (a.rests == kRestsInPlace) return launch_prefix<P, false, kRestsInPlace>(a, s); }
+    return a.rests ? launch_prefix<P, false, kRestsBeside>(a, s) : launch_prefix<P, false, 0>(a, s);
 }
 
 template <int P>
