@@ -84,7 +84,7 @@ struct Layout {
 struct Small {
     uint64_t key_full[4], key_empty[4], value_full[4], value_empty[4];  // a place holds a tile's keys or values; they have been read
     uint64_t scored[2], taken[2], weighed[2], summed[2];        // of a slot: its scores are there; have been taken; its weights are there, its sums
-    uint64_t brought;                   // the queries are there
+    uint64_t brought, rested[2];        // the queries are there; what their rounding left is, of a slot.  (Once each: a wait for a first phase would miss it behind the second.)
     uint64_t drained[4];
     uint32_t tensor;                    // address of tensor memory
     uint32_t failed;
@@ -711,7 +711,7 @@ __device__ __forceinline__ bool issue_scores(const CacheSharedArgs& a, const Sha
     const uint32_t at = tensor + slot * L::kSlotColumns;
     bool ok = wait(&sm.brought, 0, sm, a.flags);
     if constexpr (kRests)               // (what the queries' rounding left is there)
-        for (int w = L::kShared ? 0 : slot; w < (L::kShared ? L::kSlots : slot + 1); ++w) ok = wait(&sm.weighed[w], 0, sm, a.flags) && ok;
+        for (int w = L::kShared ? 0 : slot; w < (L::kShared ? L::kSlots : slot + 1); ++w) ok = wait(&sm.rested[w], 0, sm, a.flags) && ok;
     const uint64_t queries = operand(L::queries(s.pair ? slot : 0, 0), 16);
     for (int tile = s.pair ? 0 : slot, n = 0; tile < s.tiles; tile += s.pair ? 1 : L::kSlots, ++n) {
         const int stage = tile % L::kKeys;
@@ -740,11 +740,10 @@ __device__ __forceinline__ bool issue_sums(const CacheSharedArgs& a, const Share
     using L = Layout<P, kTwo, kRests>;
     constexpr uint32_t how = instruction(P, true);
     const uint32_t at = tensor + slot * L::kSlotColumns;
-    constexpr int shift = kRests != 0;
-    bool ok = !shift || wait(&sm.weighed[slot], 0, sm, a.flags);       // (its first phase is that of the queries' rests)
+    bool ok = true;
     for (int tile = s.pair ? 0 : slot, n = 0; tile < s.tiles; tile += s.pair ? 1 : L::kSlots, ++n) {
         const int stage = tile % L::kValues;
-        ok = wait(&sm.value_full[stage], (tile / L::kValues) & 1, &sm.weighed[slot], (n + shift) & 1, sm, a.flags) && ok;
+        ok = wait(&sm.value_full[stage], (tile / L::kValues) & 1, &sm.weighed[slot], n & 1, sm, a.flags) && ok;
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         fence_after();
@@ -789,6 +788,7 @@ __global__ void __launch_bounds__(Layout<P, kTwo, kRests>::kThreads, 1) shared_p
             for (int i = 0; i < 2; ++i) {
                 barrier_init(&sm.scored[i], 1); barrier_init(&sm.taken[i], 32 * L::kSoftmaxWarps);
                 barrier_init(&sm.weighed[i], 32 * L::kSoftmaxWarps); barrier_init(&sm.summed[i], 1);
+                barrier_init(&sm.rested[i], 32 * L::kSoftmaxWarps);
             }
             barrier_init(&sm.brought, 1);
             for (int i = 0; i < 4; ++i) barrier_init(&sm.drained[i], 1);
@@ -836,7 +836,7 @@ __global__ void __launch_bounds__(Layout<P, kTwo, kRests>::kThreads, 1) shared_p
             }
             stored();
             fence_before();
-            arrive(&sm.weighed[slot]);                                  // (its first phase: what comes before the first scores)
+            arrive(&sm.rested[slot]);
         }
         const bool live = __any_sync(0xffffffffu, my_row < (int64_t)a.batch * a.group);
         int n = 0;
