@@ -40,7 +40,7 @@ EXPORTS = ["lq_plan_create", "lq_plan_destroy", "lq_plan_padded_elems", "lq_plan
            "lq_entropy_decode", "lq_entropy_wait", "lq_entropy_status", "lq_level_probabilities", "lq_symbol_counts", "qoda_set_alt_rates", "qoda_set_average", "qoda_get_alt_scalars", "lq_get_statistics", "lq_vector_norm_static", "lq_profile_enable",
            "lq_profile_read",
            "lq_cache_create", "lq_cache_destroy", "lq_cache_page_words", "lq_cache_info", "lq_cache_set_levels", "lq_cache_get_levels",
-           "lq_cache_status", "lq_cache_write", "lq_cache_read", "lq_cache_workspace", "lq_cache_attend",
+           "lq_cache_status", "lq_cache_wait", "lq_cache_write", "lq_cache_read", "lq_cache_workspace", "lq_cache_attend",
            "lq_cache_shared_workspace", "lq_cache_attend_shared", "lq_cache_bounds_words", "lq_cache_bounds", "lq_cache_choose_workspace",
            "lq_cache_choose", "lq_cache_attend_chosen",
            "lq_error_string", "lq_last_error"]
@@ -130,6 +130,7 @@ def load_library() -> C.CDLL:
     L.lq_cache_write.argtypes = [vp, i32, rows, rows, i64, vp, vp, i64, i64, rotary, vp]
     L.lq_cache_read.argtypes = [vp, i32, vp, i64, i64, vp, rows, rows, vp]
     L.lq_cache_attend.argtypes = [vp, i32, rows, i64, i32, vp, i64, vp, i64, vp, C.c_float, i64, rotary, rows, vp, vp, i64, vp]
+    L.lq_cache_wait.argtypes = [vp, i64]
     L.lq_cache_shared_workspace.argtypes = [vp, i64, i32, i64, i64, i32, i32]; L.lq_cache_shared_workspace.restype = i64
     L.lq_cache_attend_shared.argtypes = [vp, i32, rows, i64, i32, vp, i64, vp, i64, vp, vp, i64, vp, C.c_float, rotary, rows, vp, vp, i64, vp]
     L.lq_cache_bounds_words.argtypes = [vp]; L.lq_cache_bounds_words.restype = i64
@@ -451,6 +452,10 @@ class Cache:
         flags = C.c_uint32(0)
         _check(load_library().lq_cache_status(self._h, C.byref(flags)))
         return flags.value
+
+    def lq_cache_wait(self, cycles: int = 1 << 32) -> None:
+        """How many cycles of the GPU's clock a wait inside lq_cache_attend_shared may take until it gives up."""
+        _check(load_library().lq_cache_wait(self._h, cycles))
 
     def lq_cache_write(self, layer: int, keys, values, slots, pages, step: Optional[int] = None, rotary=None, positions=None,
                        layout: str = "half") -> None:

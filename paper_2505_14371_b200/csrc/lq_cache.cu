@@ -18,6 +18,7 @@ struct lq_cache {
     uint64_t seed = 0;
     CacheTable* tables = nullptr;          // dev [layers][2]
     uint32_t* flags = nullptr;             // dev [1]
+    int64_t wait_cycles = kCacheMostWait;
     std::vector<float> levels;             // [layers][2][kCacheLevels], as rounded
 };
 
@@ -448,6 +449,14 @@ int lq_cache_status(lq_cache* cache, uint32_t* flags)
     return LQ_OK;
 }
 
+int lq_cache_wait(lq_cache* cache, int64_t cycles)
+{
+    if (!cache) return lq_set_error(LQ_EINVAL, "cache is NULL");
+    if (cycles < 0) return lq_set_error(LQ_EINVAL, "cycles = %lld is negative", (long long)cycles);
+    cache->wait_cycles = std::min(cycles, kCacheMostWait);
+    return LQ_OK;
+}
+
 int lq_cache_write(lq_cache* cache, int32_t layer, const lq_rows* keys, const lq_rows* values, int64_t tokens, const int64_t* slots,
                    uint32_t* pages, int64_t num_pages, int64_t step, const lq_rotary* rotary, void* stream)
 {
@@ -568,7 +577,7 @@ int lq_cache_attend_shared(lq_cache* cache, int32_t layer, const lq_rows* querie
     b.prefix = prefix; b.prefix_length = prefix_length; b.lengths = lengths; b.lse = lse; b.flags = cache->flags;
     b.num_pages = num_pages; b.prefix_width = prefix_width; b.prefix_most = most_tokens(cache, prefix_width); b.own_most = most_tokens(cache, table_width);
     b.scale = a.scale; b.batch = a.batch; b.group = a.group; b.splits = space.splits;
-    b.rests = space.rests; b.slots = space.slots; b.pairs = space.pairs;
+    b.rests = space.rests; b.slots = space.slots; b.pairs = space.pairs; b.wait_cycles = cache->wait_cycles;
     b.rows = reinterpret_cast<char*>(base + space.rows); b.parts = base + space.parts; b.own = base + space.own;
     a.partial = space.partial < 0 ? nullptr : base + space.partial;
     a.sums = b.own; a.before = prefix_length; a.before_most = b.prefix_most; a.lse = nullptr;

@@ -139,6 +139,7 @@ struct CacheSharedArgs {
     float scale;
     int32_t batch, group, splits;
     int32_t rests, slots, pairs;        // queries are sums of two fp16 numbers; see cache_shared_slots, cache_shared_pairs
+    int64_t wait_cycles;                // how long a wait may take
 };
 
 // Which pages a sequence's queries look at (lq_cache_choose.cu).
@@ -182,6 +183,7 @@ cudaError_t launch_cache_choose(const CacheChooseArgs& a, cudaStream_t s);
 cudaError_t launch_cache_shared_rows(const CacheSharedArgs& a, cudaStream_t s);
 cudaError_t launch_cache_shared_prefix(const CacheSharedArgs& a, cudaStream_t s);
 cudaError_t launch_cache_shared_join(const CacheSharedArgs& a, cudaStream_t s);
+constexpr int64_t kCacheMostWait = (int64_t)1 << 32;     // clock cycles: some two seconds
 // Into how many parts the prefix's tokens are split, and how many parts a query may leave of each (scores and sums of 128 rows that
 // tensor memory holds at a time; `two`: weights are sums of two fp16 numbers, `rests`: see there).
 int cache_shared_splits(int heads, bool pairs, int64_t rows, int64_t prefix_tokens, bool exact, int sms);

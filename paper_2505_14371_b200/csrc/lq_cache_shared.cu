@@ -28,7 +28,8 @@
 // Measured and not kept (that case, all kernels, us, of 114 without rests): eight warps of softmax a slot 147; 16 scores at a time in a loop 146; fragments of four
 // rows a thread, whose norms then serve four scores 148; both slots in step 122.
 //
-// Waits are bounded: after some two seconds a waiting thread sets LQ_CACHE_GAVE_UP, and all leave.
+// Waits are bounded: after the cache's limit (some two seconds unless lq_cache_wait says less) a waiting thread sets LQ_CACHE_GAVE_UP, and all leave, once
+// the matrix unit has done what it was given.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -113,16 +114,30 @@ __device__ __forceinline__ bool passed(uint64_t* b, uint32_t parity)
                  : "=r"(ok) : "r"(address_of(b)), "r"(parity) : "memory");
     return ok;
 }
-// False after some two seconds, or once another thread has given up.
-__device__ __forceinline__ bool wait(uint64_t* b, uint32_t parity, Small& sm, uint32_t* flags)
+// Without the time that try_wait may take.
+__device__ __forceinline__ bool looked(uint64_t* b, uint32_t parity)
 {
-    if (passed(b, parity)) return true;
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(ok) : "r"(address_of(b)), "r"(parity) : "memory");
+    return ok;
+}
+
+// How long a wait may take, in clock cycles (0: only what is over already is waited for), and where it is noted that it was not enough.
+struct Limit {
+    uint32_t* flags;
+    long long cycles;
+};
+// False after that time, or once another thread has given up.
+__device__ __forceinline__ bool wait(uint64_t* b, uint32_t parity, Small& sm, const Limit& limit)
+{
+    if (limit.cycles > 0 ? passed(b, parity) : looked(b, parity)) return true;
     const long long start = clock64();
-    while (!passed(b, parity)) {
+    while (limit.cycles == 0 || !passed(b, parity)) {
         if (*reinterpret_cast<volatile uint32_t*>(&sm.failed)) return false;
-        if (clock64() - start > 1ll << 32) {
+        if (clock64() - start >= limit.cycles) {
             *reinterpret_cast<volatile uint32_t*>(&sm.failed) = 1;
-            atomicOr(flags, LQ_CACHE_GAVE_UP);
+            atomicOr(limit.flags, LQ_CACHE_GAVE_UP);
             return false;
         }
     }
@@ -130,10 +145,10 @@ __device__ __forceinline__ bool wait(uint64_t* b, uint32_t parity, Small& sm, ui
 }
 
 // Two of them, looked at together.
-__device__ __forceinline__ bool wait(uint64_t* b, uint32_t parity, uint64_t* c, uint32_t other, Small& sm, uint32_t* flags)
+__device__ __forceinline__ bool wait(uint64_t* b, uint32_t parity, uint64_t* c, uint32_t other, Small& sm, const Limit& limit)
 {
-    const bool x = passed(b, parity), y = passed(c, other);
-    return (x || wait(b, parity, sm, flags)) && (y || wait(c, other, sm, flags));
+    const bool x = limit.cycles > 0 && passed(b, parity), y = limit.cycles > 0 && passed(c, other);
+    return (x || wait(b, parity, sm, limit)) && (y || wait(c, other, sm, limit));
 }
 
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
@@ -547,7 +562,7 @@ constexpr int kFar = 100;               // a weight's factor 2^up is between 2^-
 // there are none yet) moved along.  Both numbers are whole, so that what has been summed is multiplied by powers of two.  (Not inline: it is
 // rare, and what it wants to keep in registers crowds out what the usual way needs.)
 template <int P>
-__device__ __noinline__ Row moved_row(Row row, Small& sm, const uint32_t* v, int stage, uint64_t* summed, uint32_t parity, uint32_t sums, uint32_t* flags)
+__device__ __noinline__ Row moved_row(Row row, Small& sm, const uint32_t* v, int stage, uint64_t* summed, uint32_t parity, uint32_t sums, Limit limit)
 {
     const float* const keys = sm.keys[stage];
     const uint32_t seen[2] = {sm.seen[stage][0], sm.seen[stage][1]};
@@ -580,7 +595,7 @@ __device__ __noinline__ Row moved_row(Row row, Small& sm, const uint32_t* v, int
     row.scale = scale;
     row.begun = row.begun || most > -INFINITY || none_such;
     if (summed) {
-        wait(summed, parity, sm, flags);        // (a failure is met by the next wait, too)
+        wait(summed, parity, sm, limit);        // (a failure is met by the next wait, too)
         __syncwarp();
         fence_after();
 #pragma unroll 1
@@ -633,7 +648,7 @@ struct Softmax {
     }
 
     // The n-th tile of this slot, whose norms are at `stage`.
-    __device__ __forceinline__ void tile(Small& sm, int stage, int n, uint32_t* flags)
+    __device__ __forceinline__ void tile(Small& sm, int stage, int n, const Limit& limit)
     {
         const int exponent = sm.exponent[stage];
         const uint32_t seen[2] = {sm.seen[stage][0], sm.seen[stage][1]};
@@ -686,11 +701,11 @@ struct Softmax {
             uint32_t kept[kTile];
 #pragma unroll
             for (int j = 0; j < kTile; ++j) kept[j] = v[j];
-            row = moved_row<P>(row, sm, kept, stage, n > 0 ? &sm.summed[slot] : nullptr, (n - 1) & 1, columns + L::kSums, flags);
+            row = moved_row<P>(row, sm, kept, stage, n > 0 ? &sm.summed[slot] : nullptr, (n - 1) & 1, columns + L::kSums, limit);
         }
         row.total += sum;
         if (n > 0) {                    // the weights before have been used
-            wait(&sm.summed[slot], (n - 1) & 1, sm, flags);
+            wait(&sm.summed[slot], (n - 1) & 1, sm, limit);
             __syncwarp();
             fence_after();
         }
@@ -704,18 +719,19 @@ struct Softmax {
 
 // Scores of a slot's uses, by one warp, and weighted values by another: each waits only for what its own products need.
 template <int P, bool kTwo, int kRests>
-__device__ __forceinline__ bool issue_scores(const CacheSharedArgs& a, const Share& s, Small& sm, uint32_t tensor, int slot)
+__device__ __forceinline__ void issue_scores(const CacheSharedArgs& a, const Share& s, Small& sm, uint32_t tensor, int slot)
 {
     using L = Layout<P, kTwo, kRests>;
     constexpr uint32_t how = instruction(kTile, false);
+    const Limit limit = {a.flags, a.wait_cycles};
     const uint32_t at = tensor + slot * L::kSlotColumns;
-    bool ok = wait(&sm.brought, 0, sm, a.flags);
+    bool ok = wait(&sm.brought, 0, sm, limit);
     if constexpr (kRests)               // (what the queries' rounding left is there)
-        for (int w = L::kShared ? 0 : slot; w < (L::kShared ? L::kSlots : slot + 1); ++w) ok = wait(&sm.rested[w], 0, sm, a.flags) && ok;
+        for (int w = L::kShared ? 0 : slot; w < (L::kShared ? L::kSlots : slot + 1); ++w) ok = wait(&sm.rested[w], 0, sm, limit) && ok;
     const uint64_t queries = operand(L::queries(s.pair ? slot : 0, 0), 16);
     for (int tile = s.pair ? 0 : slot, n = 0; tile < s.tiles; tile += s.pair ? 1 : L::kSlots, ++n) {
         const int stage = tile % L::kKeys;
-        ok = wait(&sm.key_full[stage], (tile / L::kKeys) & 1, L::kInPlace ? &sm.summed[slot] : &sm.taken[slot], (n - 1) & 1, sm, a.flags) && ok;         // (there is no phase before the first to wait for)
+        ok = wait(&sm.key_full[stage], (tile / L::kKeys) & 1, L::kInPlace ? &sm.summed[slot] : &sm.taken[slot], (n - 1) & 1, sm, limit) && ok;         // (there is no phase before the first to wait for)
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         fence_after();
@@ -731,19 +747,19 @@ __device__ __forceinline__ bool issue_scores(const CacheSharedArgs& a, const Sha
         commit(&sm.scored[slot]);
         commit(&sm.key_empty[stage]);
     }
-    return ok;
 }
 
 template <int P, bool kTwo, int kRests>
-__device__ __forceinline__ bool issue_sums(const CacheSharedArgs& a, const Share& s, Small& sm, uint32_t tensor, int slot)
+__device__ __forceinline__ void issue_sums(const CacheSharedArgs& a, const Share& s, Small& sm, uint32_t tensor, int slot)
 {
     using L = Layout<P, kTwo, kRests>;
     constexpr uint32_t how = instruction(P, true);
+    const Limit limit = {a.flags, a.wait_cycles};
     const uint32_t at = tensor + slot * L::kSlotColumns;
     bool ok = true;
     for (int tile = s.pair ? 0 : slot, n = 0; tile < s.tiles; tile += s.pair ? 1 : L::kSlots, ++n) {
         const int stage = tile % L::kValues;
-        ok = wait(&sm.value_full[stage], (tile / L::kValues) & 1, &sm.weighed[slot], n & 1, sm, a.flags) && ok;
+        ok = wait(&sm.value_full[stage], (tile / L::kValues) & 1, &sm.weighed[slot], n & 1, sm, limit) && ok;
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         fence_after();
@@ -756,7 +772,6 @@ __device__ __forceinline__ bool issue_sums(const CacheSharedArgs& a, const Share
         commit(&sm.summed[slot]);
         commit(&sm.value_empty[stage]);
     }
-    return ok;
 }
 
 // ---- the kernel ------------------------------------------------------------------------------------------------
@@ -770,6 +785,7 @@ __global__ void __launch_bounds__(Layout<P, kTwo, kRests>::kThreads, 1) shared_p
     Small& sm = *reinterpret_cast<Small*>(shared + L::kSmallAt);
     static_assert(L::kSmallAt + sizeof(Small) <= kTableAt, "below the table");
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const Limit limit = {a.flags, a.wait_cycles};
 
     for (int i = tid; i < 512; i += L::kThreads) {                      // the look-up table: half an entry's row each
         const uint32_t v = a.tables[i & 1].pairs[i >> 1];
@@ -843,19 +859,19 @@ __global__ void __launch_bounds__(Layout<P, kTwo, kRests>::kThreads, 1) shared_p
         bool ok = true;
         for (int use = slot; use < uses && ok; use += slots, ++n) {
             const int tile = tile_of(use), stage = tile % L::kValues;
-            ok = wait(&sm.value_full[stage], (tile / L::kValues) & 1, &sm.scored[slot], n & 1, sm, a.flags);
+            ok = wait(&sm.value_full[stage], (tile / L::kValues) & 1, &sm.scored[slot], n & 1, sm, limit);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
             fence_after();
-            if (live) softmax.tile(sm, stage, n, a.flags);
+            if (live) softmax.tile(sm, stage, n, limit);
             else {                      // (its arrivals must not run ahead of the others' by a tile)
                 arrive(&sm.taken[slot]);
-                if (n > 0) wait(&sm.summed[slot], (n - 1) & 1, sm, a.flags);
+                if (n > 0) wait(&sm.summed[slot], (n - 1) & 1, sm, limit);
             }
             fence_before();
             arrive(&sm.weighed[slot]);
         }
-        if (ok && n > 0) ok = __all_sync(0xffffffffu, wait(&sm.summed[slot], (n - 1) & 1, sm, a.flags));
+        if (ok && n > 0) ok = __all_sync(0xffffffffu, wait(&sm.summed[slot], (n - 1) & 1, sm, limit));
         fence_after();
         if (live) {
             // ---- what is left of this row; of a block that is alone, one part of even tiles and one of odd ones
@@ -909,7 +925,7 @@ __global__ void __launch_bounds__(Layout<P, kTwo, kRests>::kThreads, 1) shared_p
                 int kind, panel, token;
                 item_of<P>(t + kDecodeWarps * k, kind, panel, token);
                 const int stage = kind ? tile % L::kValues : tile % L::kKeys, round = kind ? tile / L::kValues : tile / L::kKeys;
-                ok = __all_sync(0xffffffffu, wait(kind ? &sm.value_empty[stage] : &sm.key_empty[stage], (round & 1) ^ 1, sm, a.flags));
+                ok = __all_sync(0xffffffffu, wait(kind ? &sm.value_empty[stage] : &sm.key_empty[stage], (round & 1) ^ 1, sm, limit));
                 if (!ok) break;
                 if (kind && t == Codes<P>::kNorms) place_norms<P>(now, s, sm, tile, stage, lane);
                 decode<P>(now, k, a, kind ? L::values(stage) : L::keys(stage), t, lane);
@@ -934,12 +950,14 @@ __global__ void __launch_bounds__(Layout<P, kTwo, kRests>::kThreads, 1) shared_p
         }
         if (slot_of < L::kSlots) {
             const uint32_t at = __shfl_sync(0xffffffffu, tensor, 0);
-            const bool ok = me & 1 ? issue_sums<P, kTwo, kRests>(a, s, sm, at, slot_of) : issue_scores<P, kTwo, kRests>(a, s, sm, at, slot_of);
-            if (!ok || me == 0) {       // what is under way ends before tensor memory and shared memory are given back
-                if (!ok) commit(&sm.drained[me]);
-                const long long start = clock64();
-                while (!((ok || passed(&sm.drained[me], 0)) && passed(&sm.brought, 0)) && clock64() - start < 1ll << 32) {}
-            }
+            if (me & 1) issue_sums<P, kTwo, kRests>(a, s, sm, at, slot_of);
+            else issue_scores<P, kTwo, kRests>(a, s, sm, at, slot_of);
+            // what is under way ends before tensor memory and shared memory are given back, whoever has given up
+            commit(&sm.drained[me]);
+            const long long start = clock64();
+            bool ended;
+            while (!(ended = passed(&sm.drained[me], 0) && (me > 0 || passed(&sm.brought, 0))) && clock64() - start < 1ll << 32) {}
+            if (!ended) atomicOr(a.flags, LQ_CACHE_GAVE_UP);
         }
     }
     __syncthreads();
