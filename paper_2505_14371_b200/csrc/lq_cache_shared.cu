@@ -556,7 +556,10 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
     return v;
 }
 
-constexpr int kFar = 100;               // a weight's factor 2^up is between 2^-kFar (and then 0 as fp16) and 2^kFar
+// A weight's factor 2^up is at most 2^kFar.  It is part of p's exponent, so that p below 2^(-126 - up) would be lost to the denominator: no less than 2^-kLeast,
+// where p (at most 2^16) times a norm (below 2) is 0 as fp16 already, as it is for every lesser factor.  Terms down to 2^-82 of the reference's then count.
+constexpr int kFar = 100, kLeast = 44;
+static_assert(16 + 1 - kLeast < -25, "such a weight rounds to 0");
 
 // Reference and scale of a warp's rows as a tile of scores `v` wants them, the denominators and the sums (`summed`: a barrier's phase that they wait for; NULL:
 // there are none yet) moved along.  Both numbers are whole, so that what has been summed is multiplied by powers of two.  (Not inline: it is
@@ -663,7 +666,7 @@ struct Softmax {
         float sum;
 #pragma unroll 1
         for (int tries = 0;; ++tries) {
-            const int wanted = exponent - row.scale + kLift, up = max(-kFar, min(kFar, wanted));
+            const int wanted = exponent - row.scale + kLift, up = max(-kLeast, min(kFar, wanted));
             const float offset = (float)up - row.ref;
             const uint64_t f2 = pair_of(row.f, row.f), offset2 = pair_of(offset, offset);
             uint64_t total[2] = {0, 0};
