@@ -989,6 +989,8 @@ __global__ void __launch_bounds__(32 * kJoinWarps) shared_join_kernel(const __gr
     if (blockIdx.x == 0 && threadIdx.x == 0 && (*a.prefix_length < 0 || *a.prefix_length > a.prefix_most)) atomicOr(a.flags, LQ_CACHE_BAD_LENGTH);
     const int heads = a.shape.heads * a.group, sequence = there ? (int)(row / heads) : 0, head = there ? (int)(row - (int64_t)sequence * heads) : 0;
     const int64_t in_head = (int64_t)sequence * a.group + head % a.group;
+    // (where no sequence has a page of its own, no other kernel looks at its length)
+    if (there && a.own_most == 0 && head == 0 && mine == 0 && lane == 0 && a.lengths[sequence] != 0) atomicOr(a.flags, LQ_CACHE_BAD_LENGTH);
     const int blocks = (int)(((int64_t)a.batch * a.group + kRows - 1) / kRows), block = (int)(in_head / kRows);
     const bool alone = a.slots == 2 && (!a.pairs || (blocks % 2 == 1 && block == blocks - 1));
     const int before = a.splits * (alone ? 2 : 1), parts = there ? before + (a.own_most > 0 && a.lengths[sequence] > 0) : 0;
