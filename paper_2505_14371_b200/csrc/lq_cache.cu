@@ -297,7 +297,7 @@ SharedSpace shared_space(const lq_cache* c, int64_t batch, int heads, int64_t pr
     x.rests = !(type == LQ_F32 || turned) ? 0 : s.padded == 128 && !two && batch * (heads / s.heads) > 128 ? kRestsInPlace : kRestsBeside;
     x.slots = cache_shared_slots(s.padded, two, x.rests);
     x.pairs = cache_shared_pairs(s.padded, two, x.rests);
-    x.splits = batch > 0 ? cache_shared_splits(s.heads, x.pairs, batch * (heads / s.heads), most_tokens(c, prefix_width), type == LQ_F32, c->sms) : 0;
+    x.splits = batch > 0 ? cache_shared_splits(s.heads, x.pairs, batch * (heads / s.heads), most_tokens(c, prefix_width), type, c->sms) : 0;
     x.parts = x.splits > 0 ? (batch * (heads / s.heads) + 127) / 128 * s.heads * (cache_shared_block_bytes(s.padded) / 4) : 0;
     x.own = x.parts + x.splits * (int64_t)x.slots * rows * part;
     const int64_t partial = x.own + (table_width > 0 ? rows * part : 0), bytes = workspace_of(c, table_width, 0);

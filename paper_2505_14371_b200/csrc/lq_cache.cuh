@@ -186,7 +186,7 @@ cudaError_t launch_cache_shared_join(const CacheSharedArgs& a, cudaStream_t s);
 constexpr int64_t kCacheMostWait = (int64_t)1 << 32;     // clock cycles: some two seconds
 // Into how many parts the prefix's tokens are split, and how many parts a query may leave of each (scores and sums of 128 rows that
 // tensor memory holds at a time; `two`: weights are sums of two fp16 numbers, `rests`: see there).
-int cache_shared_splits(int heads, bool pairs, int64_t rows, int64_t prefix_tokens, bool exact, int sms);
+int cache_shared_splits(int heads, bool pairs, int64_t rows, int64_t prefix_tokens, int type, int sms);
 // What queries' rounding leaves: nothing, numbers beside the scores and weights, or (rows of 128 with weights of 11 bits, where tensor memory has
 // no room for them and a second block's scores) numbers beside scores that give way to their weights.  128 sequences over 16384 tokens, two blocks of
 // rows a CTA: 150 us beside (one block a CTA then), 139 in place; 32 over 4096, one block: 46 us and (with an earlier form of the kernel) 49.

@@ -1130,15 +1130,18 @@ cudaError_t launch_join(const CacheSharedArgs& a, cudaStream_t s)
 
 }  // namespace
 
-int cache_shared_splits(int heads, bool pairs, int64_t rows, int64_t prefix_tokens, bool exact, int sms)
+int cache_shared_splits(int heads, bool pairs, int64_t rows, int64_t prefix_tokens, int type, int sms)
 {
     const int64_t blocks = (rows + kRows - 1) / kRows, items = heads * (pairs ? (blocks + 1) / 2 : blocks), tiles = (prefix_tokens + kTile - 1) / kTile;
     if (tiles == 0) return 0;
     // a tile of two blocks takes twice as long as one of a block alone; what a CTA takes besides is some 8 of those
     const int64_t each = blocks > 1 && pairs ? 2 : 1;
-    // fp32 outputs: sums of 1024 tokens at most, as the matrix unit cuts off what a sum's last bit does not hold
+    // The matrix unit cuts off what a sum's last bit does not hold, in every step of 16 tokens (of both numbers of a weight): up to 2^-23 of the sum so far, on
+    // average 2^-24 of the last, and all one way.  A sum of fp32 outputs has 1024 tokens at most (2^-17 at worst, 2^-20.7 measured), of fp16 8192 and of bf16
+    // 131072: a quarter of half a step of the output at worst.  (Without: 524288 tokens of 148 heads, fp16: a step and a half off.)
+    const int64_t most = type == LQ_F32 ? 16 : type == LQ_F16 ? 128 : 2048;
     int64_t best = 1, cost = INT64_MAX;
-    for (int64_t n = exact ? (tiles + 15) / 16 : 1; n <= tiles; ++n) {
+    for (int64_t n = (tiles + most - 1) / most; n <= tiles; ++n) {
         const int64_t c = (items * n + sms - 1) / sms * ((tiles + n - 1) / n * each + 8);
         if (c < cost) { cost = c; best = n; }
         if (n >= 64 && n * items > 2 * sms) break;

@@ -44,3 +44,26 @@ def test_small_values_count_in_the_denominator(kind, batch, small, first):
     half = torch.finfo(out.dtype).eps / 2
     assert (lse.double().cpu() - l).abs().max() <= lse_bound, (float(lse[0, 0]) - l, lse_bound)
     assert np.all(np.abs(out.double().cpu().numpy() - o) <= bound + half * (np.abs(o) + bound))
+
+
+@pytest.mark.parametrize("kind,tokens,heads", [("fp16", 524288, 148), ("bf16", 1048576, 148), ("fp32", 65536, 148), ("fp16", 100003, 150), ("fp16", 40000, 3)])
+def test_sums_of_many_tokens(kind, tokens, heads):
+    """Values of one sign, so that a sum grows all the way and what the matrix unit cuts off each of its steps adds up; so many heads that each has a CTA to
+    itself.  A split ends a sum where that would come to a quarter of half a step of the outputs at worst: 2^-14, 2^-11 and (fp32, by 1024 tokens) 2^-17 of it."""
+    c = make(heads, 64, 1024)
+    rng = np.random.default_rng(tokens)
+    k, v = rng.uniform(-1, 1, tokens).astype(np.float32), rng.uniform(0.5, 1, tokens).astype(np.float32)
+    pages = plain_rows(c, k, v)
+    i32 = dict(dtype=torch.int32, device="cuda")
+    q = torch.ones((1, heads, 64), device="cuda", dtype=TYPES[kind])
+    out, lse = torch.empty_like(q), torch.empty(q.shape[:2], device="cuda")
+    c.lq_cache_attend_shared(0, q, pages, torch.arange(pages.shape[0], **i32), torch.tensor([tokens], **i32), torch.zeros((1, 0), **i32), torch.zeros(1, **i32), out,
+                             lse=lse, scale=2.0 ** -6)
+    p = np.exp(k.astype(np.float64))
+    o, l = (p @ v) / p.sum(), np.log(p.sum())
+    # scores of up to 1 and their exponentials: 2^-20 together; weights of 11 or 22 bits; sums of parts in fp32
+    cut = {"fp16": 2.0 ** -14, "bf16": 2.0 ** -11, "fp32": 2.0 ** -17}[kind]
+    bound = o * (2.0 ** -20 + (2.0 ** -12 if kind == "bf16" else 2.0 ** -21) + cut + 2.0 ** -19)
+    step = {"fp16": 2.0 ** -11, "bf16": 2.0 ** -8, "fp32": 2.0 ** -24}[kind]        # of a number from 1/2 to 1
+    assert 0.5 < o < 1 and (out.double().cpu() - o).abs().max() <= bound + step / 2, (float(out[0, 0, 0]), o)
+    assert (lse.double().cpu() - l).abs().max() <= 2.0 ** -19 + 2.0 ** -22 * l
