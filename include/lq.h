@@ -458,8 +458,8 @@ int lq_cache_get_levels(const lq_cache* cache, int32_t layer, int32_t kind, floa
 /* LQ_CACHE_* flags of the calls since the last lq_cache_status, which clears them.  Synchronises the device. */
 int lq_cache_status(lq_cache* cache, uint32_t* flags);
 
-/* How long the waits inside the kernels of lq_cache_attend_shared calls that follow may take: `cycles` >= 0 of the GPU's clock, 0 = what is
- * not there yet is not waited for, at most and by default 2^32 (some two seconds).  For tests, and callers that would rather call again. */
+/* How long the waits inside the kernels of lq_cache_attend_shared calls that follow may take: `cycles` >= 0 of the GPU's clock, 0 = they give
+ * up before they begin, at most and by default 2^32 (some two seconds).  For tests, and callers that would rather call again. */
 int lq_cache_wait(lq_cache* cache, int64_t cycles);
 
 /* Quantises rows of keys and values [tokens][kv_heads][head_dim] into slots [tokens] (dev) of one layer's pages; a negative

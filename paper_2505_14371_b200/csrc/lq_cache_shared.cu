@@ -89,6 +89,7 @@ struct Small {
     uint64_t drained[4];
     uint32_t tensor;                    // address of tensor memory
     uint32_t failed;
+    long long wait_cycles;              // how long a wait may take
     uint32_t seen[4][2];                // of a tile, beside its values: bit per token
     int32_t exponent[4];                // what the values' norms are divided by
     alignas(16) float keys[4][kTile];   // norms
@@ -114,30 +115,17 @@ __device__ __forceinline__ bool passed(uint64_t* b, uint32_t parity)
                  : "=r"(ok) : "r"(address_of(b)), "r"(parity) : "memory");
     return ok;
 }
-// Without the time that try_wait may take.
-__device__ __forceinline__ bool looked(uint64_t* b, uint32_t parity)
+__device__ __forceinline__ bool gave_up(const Small& sm) { return *reinterpret_cast<const volatile uint32_t*>(&sm.failed); }
+// False after the cache's limit, or once another thread has given up.
+__device__ __forceinline__ bool wait(uint64_t* b, uint32_t parity, Small& sm, uint32_t* flags)
 {
-    uint32_t ok;
-    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-                 : "=r"(ok) : "r"(address_of(b)), "r"(parity) : "memory");
-    return ok;
-}
-
-// How long a wait may take, in clock cycles (0: only what is over already is waited for), and where it is noted that it was not enough.
-struct Limit {
-    uint32_t* flags;
-    long long cycles;
-};
-// False after that time, or once another thread has given up.
-__device__ __forceinline__ bool wait(uint64_t* b, uint32_t parity, Small& sm, const Limit& limit)
-{
-    if (limit.cycles > 0 ? passed(b, parity) : looked(b, parity)) return true;
+    if (passed(b, parity)) return true;
     const long long start = clock64();
-    while (limit.cycles == 0 || !passed(b, parity)) {
-        if (*reinterpret_cast<volatile uint32_t*>(&sm.failed)) return false;
-        if (clock64() - start >= limit.cycles) {
+    while (!passed(b, parity)) {
+        if (gave_up(sm)) return false;
+        if (clock64() - start > sm.wait_cycles) {
             *reinterpret_cast<volatile uint32_t*>(&sm.failed) = 1;
-            atomicOr(limit.flags, LQ_CACHE_GAVE_UP);
+            atomicOr(flags, LQ_CACHE_GAVE_UP);
             return false;
         }
     }
@@ -145,10 +133,10 @@ __device__ __forceinline__ bool wait(uint64_t* b, uint32_t parity, Small& sm, co
 }
 
 // Two of them, looked at together.
-__device__ __forceinline__ bool wait(uint64_t* b, uint32_t parity, uint64_t* c, uint32_t other, Small& sm, const Limit& limit)
+__device__ __forceinline__ bool wait(uint64_t* b, uint32_t parity, uint64_t* c, uint32_t other, Small& sm, uint32_t* flags)
 {
-    const bool x = limit.cycles > 0 && passed(b, parity), y = limit.cycles > 0 && passed(c, other);
-    return (x || wait(b, parity, sm, limit)) && (y || wait(c, other, sm, limit));
+    const bool x = passed(b, parity), y = passed(c, other);
+    return (x || wait(b, parity, sm, flags)) && (y || wait(c, other, sm, flags));
 }
 
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
@@ -565,7 +553,7 @@ static_assert(16 + 1 - kLeast < -25, "such a weight rounds to 0");
 // there are none yet) moved along.  Both numbers are whole, so that what has been summed is multiplied by powers of two.  (Not inline: it is
 // rare, and what it wants to keep in registers crowds out what the usual way needs.)
 template <int P>
-__device__ __noinline__ Row moved_row(Row row, Small& sm, const uint32_t* v, int stage, uint64_t* summed, uint32_t parity, uint32_t sums, Limit limit)
+__device__ __noinline__ Row moved_row(Row row, Small& sm, const uint32_t* v, int stage, uint64_t* summed, uint32_t parity, uint32_t sums, uint32_t* flags)
 {
     const float* const keys = sm.keys[stage];
     const uint32_t seen[2] = {sm.seen[stage][0], sm.seen[stage][1]};
@@ -598,7 +586,7 @@ __device__ __noinline__ Row moved_row(Row row, Small& sm, const uint32_t* v, int
     row.scale = scale;
     row.begun = row.begun || most > -INFINITY || none_such;
     if (summed) {
-        wait(summed, parity, sm, limit);        // (a failure is met by the next wait, too)
+        wait(summed, parity, sm, flags);        // (a failure is met by the next wait, too)
         __syncwarp();
         fence_after();
 #pragma unroll 1
@@ -651,7 +639,7 @@ struct Softmax {
     }
 
     // The n-th tile of this slot, whose norms are at `stage`.
-    __device__ __forceinline__ void tile(Small& sm, int stage, int n, const Limit& limit)
+    __device__ __forceinline__ void tile(Small& sm, int stage, int n, uint32_t* flags)
     {
         const int exponent = sm.exponent[stage];
         const uint32_t seen[2] = {sm.seen[stage][0], sm.seen[stage][1]};
@@ -704,11 +692,11 @@ struct Softmax {
             uint32_t kept[kTile];
 #pragma unroll
             for (int j = 0; j < kTile; ++j) kept[j] = v[j];
-            row = moved_row<P>(row, sm, kept, stage, n > 0 ? &sm.summed[slot] : nullptr, (n - 1) & 1, columns + L::kSums, limit);
+            row = moved_row<P>(row, sm, kept, stage, n > 0 ? &sm.summed[slot] : nullptr, (n - 1) & 1, columns + L::kSums, flags);
         }
         row.total += sum;
         if (n > 0) {                    // the weights before have been used
-            wait(&sm.summed[slot], (n - 1) & 1, sm, limit);
+            wait(&sm.summed[slot], (n - 1) & 1, sm, flags);
             __syncwarp();
             fence_after();
         }
@@ -726,15 +714,14 @@ __device__ __forceinline__ void issue_scores(const CacheSharedArgs& a, const Sha
 {
     using L = Layout<P, kTwo, kRests>;
     constexpr uint32_t how = instruction(kTile, false);
-    const Limit limit = {a.flags, a.wait_cycles};
     const uint32_t at = tensor + slot * L::kSlotColumns;
-    bool ok = wait(&sm.brought, 0, sm, limit);
+    bool ok = wait(&sm.brought, 0, sm, a.flags);
     if constexpr (kRests)               // (what the queries' rounding left is there)
-        for (int w = L::kShared ? 0 : slot; w < (L::kShared ? L::kSlots : slot + 1); ++w) ok = wait(&sm.rested[w], 0, sm, limit) && ok;
+        for (int w = L::kShared ? 0 : slot; w < (L::kShared ? L::kSlots : slot + 1); ++w) ok = wait(&sm.rested[w], 0, sm, a.flags) && ok;
     const uint64_t queries = operand(L::queries(s.pair ? slot : 0, 0), 16);
     for (int tile = s.pair ? 0 : slot, n = 0; tile < s.tiles; tile += s.pair ? 1 : L::kSlots, ++n) {
         const int stage = tile % L::kKeys;
-        ok = wait(&sm.key_full[stage], (tile / L::kKeys) & 1, L::kInPlace ? &sm.summed[slot] : &sm.taken[slot], (n - 1) & 1, sm, limit) && ok;         // (there is no phase before the first to wait for)
+        ok = wait(&sm.key_full[stage], (tile / L::kKeys) & 1, L::kInPlace ? &sm.summed[slot] : &sm.taken[slot], (n - 1) & 1, sm, a.flags) && ok;         // (there is no phase before the first to wait for)
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         fence_after();
@@ -757,12 +744,11 @@ __device__ __forceinline__ void issue_sums(const CacheSharedArgs& a, const Share
 {
     using L = Layout<P, kTwo, kRests>;
     constexpr uint32_t how = instruction(P, true);
-    const Limit limit = {a.flags, a.wait_cycles};
     const uint32_t at = tensor + slot * L::kSlotColumns;
     bool ok = true;
     for (int tile = s.pair ? 0 : slot, n = 0; tile < s.tiles; tile += s.pair ? 1 : L::kSlots, ++n) {
         const int stage = tile % L::kValues;
-        ok = wait(&sm.value_full[stage], (tile / L::kValues) & 1, &sm.weighed[slot], n & 1, sm, limit) && ok;
+        ok = wait(&sm.value_full[stage], (tile / L::kValues) & 1, &sm.weighed[slot], n & 1, sm, a.flags) && ok;
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         fence_after();
@@ -788,7 +774,6 @@ __global__ void __launch_bounds__(Layout<P, kTwo, kRests>::kThreads, 1) shared_p
     Small& sm = *reinterpret_cast<Small*>(shared + L::kSmallAt);
     static_assert(L::kSmallAt + sizeof(Small) <= kTableAt, "below the table");
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const Limit limit = {a.flags, a.wait_cycles};
 
     for (int i = tid; i < 512; i += L::kThreads) {                      // the look-up table: half an entry's row each
         const uint32_t v = a.tables[i & 1].pairs[i >> 1];
@@ -811,7 +796,8 @@ __global__ void __launch_bounds__(Layout<P, kTwo, kRests>::kThreads, 1) shared_p
             }
             barrier_init(&sm.brought, 1);
             for (int i = 0; i < 4; ++i) barrier_init(&sm.drained[i], 1);
-            sm.failed = 0;
+            sm.failed = a.wait_cycles == 0;     // (nothing is brought then)
+            sm.wait_cycles = a.wait_cycles;
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         }
         __syncwarp();
@@ -862,19 +848,19 @@ __global__ void __launch_bounds__(Layout<P, kTwo, kRests>::kThreads, 1) shared_p
         bool ok = true;
         for (int use = slot; use < uses && ok; use += slots, ++n) {
             const int tile = tile_of(use), stage = tile % L::kValues;
-            ok = wait(&sm.value_full[stage], (tile / L::kValues) & 1, &sm.scored[slot], n & 1, sm, limit);
+            ok = wait(&sm.value_full[stage], (tile / L::kValues) & 1, &sm.scored[slot], n & 1, sm, a.flags);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
             fence_after();
-            if (live) softmax.tile(sm, stage, n, limit);
+            if (live) softmax.tile(sm, stage, n, a.flags);
             else {                      // (its arrivals must not run ahead of the others' by a tile)
                 arrive(&sm.taken[slot]);
-                if (n > 0) wait(&sm.summed[slot], (n - 1) & 1, sm, limit);
+                if (n > 0) wait(&sm.summed[slot], (n - 1) & 1, sm, a.flags);
             }
             fence_before();
             arrive(&sm.weighed[slot]);
         }
-        if (ok && n > 0) ok = __all_sync(0xffffffffu, wait(&sm.summed[slot], (n - 1) & 1, sm, limit));
+        if (ok && n > 0) ok = __all_sync(0xffffffffu, wait(&sm.summed[slot], (n - 1) & 1, sm, a.flags));
         fence_after();
         if (live) {
             // ---- what is left of this row; of a block that is alone, one part of even tiles and one of odd ones
@@ -917,7 +903,7 @@ __global__ void __launch_bounds__(Layout<P, kTwo, kRests>::kThreads, 1) shared_p
         const int page = page_of(a, s, 0, s.tiles > 0, lane);
         int next = page_of(a, s, 1, s.tiles > 1, lane), after = page_of(a, s, 2, s.tiles > 2, lane);
         if (s.tiles > 0) fetch<P>(codes, a, s, 0, page, t, lane);
-        for (int tile = 0; tile < s.tiles && t < Codes<P>::kItems; ++tile) {
+        for (int tile = 0; tile < s.tiles && t < Codes<P>::kItems && !__any_sync(0xffffffffu, gave_up(sm)); ++tile) {
             const Codes<P> now = codes;
             if (tile + 1 < s.tiles) fetch<P>(codes, a, s, tile + 1, next, t, lane);
             next = after;
@@ -928,7 +914,7 @@ __global__ void __launch_bounds__(Layout<P, kTwo, kRests>::kThreads, 1) shared_p
                 int kind, panel, token;
                 item_of<P>(t + kDecodeWarps * k, kind, panel, token);
                 const int stage = kind ? tile % L::kValues : tile % L::kKeys, round = kind ? tile / L::kValues : tile / L::kKeys;
-                ok = __all_sync(0xffffffffu, wait(kind ? &sm.value_empty[stage] : &sm.key_empty[stage], (round & 1) ^ 1, sm, limit));
+                ok = __all_sync(0xffffffffu, wait(kind ? &sm.value_empty[stage] : &sm.key_empty[stage], (round & 1) ^ 1, sm, a.flags));
                 if (!ok) break;
                 if (kind && t == Codes<P>::kNorms) place_norms<P>(now, s, sm, tile, stage, lane);
                 decode<P>(now, k, a, kind ? L::values(stage) : L::keys(stage), t, lane);
@@ -955,15 +941,19 @@ __global__ void __launch_bounds__(Layout<P, kTwo, kRests>::kThreads, 1) shared_p
             const uint32_t at = __shfl_sync(0xffffffffu, tensor, 0);
             if (me & 1) issue_sums<P, kTwo, kRests>(a, s, sm, at, slot_of);
             else issue_scores<P, kTwo, kRests>(a, s, sm, at, slot_of);
-            // what is under way ends before tensor memory and shared memory are given back, whoever has given up
-            commit(&sm.drained[me]);
-            const long long start = clock64();
-            bool ended;
-            while (!(ended = passed(&sm.drained[me], 0) && (me > 0 || passed(&sm.brought, 0))) && clock64() - start < 1ll << 32) {}
-            if (!ended) atomicOr(a.flags, LQ_CACHE_GAVE_UP);
         }
     }
     __syncthreads();
+    if (gave_up(sm)) {                  // what is under way ends before tensor memory and shared memory are given back
+        const int me = warp - L::kIssuer;
+        if (me >= 0 && me < 2 * L::kSlots) {
+            commit(&sm.drained[me]);
+            const long long start = clock64();
+            while (!(passed(&sm.drained[me], 0) && passed(&sm.brought, 0)) && clock64() - start < kCacheMostWait) {}
+        }
+        if (tid == 0) atomicOr(a.flags, LQ_CACHE_GAVE_UP);
+        __syncthreads();
+    }
     if (warp == L::kIssuer) {
         fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(tensor), "n"(kColumns));
