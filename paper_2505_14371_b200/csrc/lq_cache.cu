@@ -294,7 +294,7 @@ SharedSpace shared_space(const lq_cache* c, int64_t batch, int heads, int64_t pr
     const int64_t rows = batch * heads, part = cache_part_floats(s.padded);
     SharedSpace x{};
     const bool two = type != LQ_BF16;   // weights as sums of two fp16 numbers; queries: fp32 and turned ones
-    x.rests = !(type == LQ_F32 || turned) ? 0 : s.padded == 128 && !two && batch * (heads / s.heads) > 128 ? kRestsInPlace : kRestsBeside;
+    x.rests = !(type == LQ_F32 || turned) ? 0 : cache_shared_rests(s.padded, two, batch * (heads / s.heads));
     x.slots = cache_shared_slots(s.padded, two, x.rests);
     x.pairs = cache_shared_pairs(s.padded, two, x.rests);
     x.splits = batch > 0 ? cache_shared_splits(s.heads, x.pairs, batch * (heads / s.heads), most_tokens(c, prefix_width), type, c->sms) : 0;
@@ -577,7 +577,7 @@ int lq_cache_attend_shared(lq_cache* cache, int32_t layer, const lq_rows* querie
     b.prefix = prefix; b.prefix_length = prefix_length; b.lengths = lengths; b.lse = lse; b.flags = cache->flags;
     b.num_pages = num_pages; b.prefix_width = prefix_width; b.prefix_most = most_tokens(cache, prefix_width); b.own_most = most_tokens(cache, table_width);
     b.scale = a.scale; b.batch = a.batch; b.group = a.group; b.splits = space.splits;
-    b.rests = space.rests; b.slots = space.slots; b.pairs = space.pairs; b.wait_cycles = cache->wait_cycles;
+    b.rests = space.rests; b.slots = space.slots; b.pairs = space.pairs; b.wait_cycles = cache->wait_cycles; b.sms = cache->sms;
     b.rows = reinterpret_cast<char*>(base + space.rows); b.parts = base + space.parts; b.own = base + space.own;
     a.partial = space.partial < 0 ? nullptr : base + space.partial;
     a.sums = b.own; a.before = prefix_length; a.before_most = b.prefix_most; a.lse = nullptr;

@@ -138,7 +138,7 @@ struct CacheSharedArgs {
     int64_t num_pages, prefix_width, prefix_most, own_most;     // tokens that the lengths can mean
     float scale;
     int32_t batch, group, splits;
-    int32_t rests, slots, pairs;        // queries are sums of two fp16 numbers; see cache_shared_slots, cache_shared_pairs
+    int32_t rests, slots, pairs, sms;   // what the queries' rounding leaves (cache_shared_rests), see cache_shared_slots, cache_shared_pairs
     int64_t wait_cycles;                // how long a wait may take
 };
 
@@ -188,9 +188,16 @@ constexpr int64_t kCacheMostWait = (int64_t)1 << 32;     // clock cycles: some t
 // tensor memory holds at a time; `two`: weights are sums of two fp16 numbers, `rests`: see there).
 int cache_shared_splits(int heads, bool pairs, int64_t rows, int64_t prefix_tokens, int type, int sms);
 // What queries' rounding leaves: nothing, numbers beside the scores and weights, or (rows of 128 with weights of 11 bits, where tensor memory has
-// no room for them and a second block's scores) numbers beside scores that give way to their weights.  128 sequences over 16384 tokens, two blocks of
-// rows a CTA: 150 us beside (one block a CTA then), 139 in place; 32 over 4096, one block: 46 us and (with an earlier form of the kernel) 49.
+// no room for them and a second block's scores) numbers beside scores that give way to their weights.  In place a CTA has two blocks of rows and decodes for both,
+// but a slot's next scores wait for its sums: that pays from four blocks on, if none is left alone.  8 heads, 4 queries each, sequences of 100 tokens of their
+// own, prefixes of 2048, 16384 and 32768, us beside | in place: one block (4096 instead of 2048) 42, 56, 75 | 43, 59, 79; two 41, 75, 112 | 41, 78, 114;
+// three 50, 99, 158 | 55, 119, 191; four 58, 130, 212 | 60, 123, 195; five 68, 162, 260 | 71, 165, 274; six 74, 171, 284 | 77, 172, 281; eight 95, 234, 410 | 91, 233, 375.
 constexpr int kRestsBeside = 1, kRestsInPlace = 2;
+__host__ __device__ constexpr int cache_shared_rests(int padded, bool two, int64_t rows)
+{
+    const int64_t blocks = (rows + 127) / 128;
+    return padded == 128 && !two && blocks >= 4 && blocks % 2 == 0 ? kRestsInPlace : kRestsBeside;
+}
 __host__ __device__ constexpr int cache_shared_slots(int padded, bool two, int rests) { return padded == 256 || (padded == 128 && two && rests) ? 1 : 2; }
 // Whether a CTA takes two blocks of rows where there are two.
 __host__ __device__ constexpr bool cache_shared_pairs(int padded, bool two, int rests)

@@ -1113,8 +1113,10 @@ template <int P>
 cudaError_t launch_join(const CacheSharedArgs& a, cudaStream_t s)
 {
     const int64_t rows = (int64_t)a.batch * a.shape.heads * a.group;
-    // as many warps a row as the GPU holds at once
-    const int share = rows <= 1184 ? 8 : rows <= 2368 ? 4 : 2, per = kJoinWarps / share;
+    // Warps a row: each reads all parts' references and its share of the sums.  Eight, four and two of them, us of the whole call (8 heads, 4 queries each, bf16,
+    // prefixes of 512, 8192 and 32768): 256 rows 23.2, 32.3, 55.6 | 23.3, 33.4, 56.8 | 24.1, 35.6, 59.1; 512 rows 26.0, 35.5, 59.3 | 24.4, 34.8, 58.7 | 25.0, 37.0, 61.1;
+    // 1152 rows 31.4, 45.2, 84.4 | 27.7, 41.9, 80.9 | 27.2, 41.6, 80.2; 2048 rows 43.0, 58.3, 97.8 | 36.5, 51.6, 90.5 | 35.2, 50.4, 89.6.
+    const int share = rows <= 3 * a.sms ? 8 : rows <= 7 * a.sms ? 4 : 2, per = kJoinWarps / share;
     return launch(shared_join_kernel<P>, (unsigned)((rows + per - 1) / per), 32 * kJoinWarps, 0, s, a, share);
 }
 

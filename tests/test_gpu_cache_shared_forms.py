@@ -53,9 +53,9 @@ def test_own_tokens_of_several_teams(heads, group, dim, page, bits, kind, rot, l
 # ---- blocks of 128 rows that are left over -----------------------------------------------------------------
 
 @pytest.mark.parametrize("length", [1, 64, 65, 129, 200, 1000, 3001])
-@pytest.mark.parametrize("heads,group,batch", [(1, 4, 96), (1, 5, 65), (40, 4, 72), (2, 4, 160)])
+@pytest.mark.parametrize("heads,group,batch", [(1, 4, 96), (1, 5, 65), (40, 4, 72), (2, 4, 160), (1, 4, 127), (30, 3, 130), (2, 8, 94)])
 def test_a_block_that_is_left_over(heads, group, batch, length):
-    """Rotated bf16 queries of rows of 128 in three blocks and five, whose last has no other beside it; one of few rows."""
+    """Rotated bf16 queries of rows of 128 in three blocks and five, whose last has no other beside it, and in four and six; last blocks of few rows."""
     import paper_2505_14371_b200 as lq
     gen = torch.Generator("cuda").manual_seed(length + batch)
     c = make(heads, 128, 64, (3, 7))

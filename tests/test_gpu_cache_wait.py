@@ -9,7 +9,7 @@ pytestmark = pytest.mark.gpu
 
 # heads, group, dim, batch, type, rotary: every form of the prefix's kernel, one block of rows, two and three
 FORMS = [(2, 2, 64, 3, "bf16", 0), (2, 2, 64, 3, "bf16", 64), (2, 2, 64, 3, "fp16", 0), (2, 2, 64, 70, "fp32", 0), (3, 4, 128, 5, "bf16", 0), (3, 4, 128, 5, "bf16", 128),
-         (1, 4, 128, 64, "bf16", 128), (1, 4, 128, 96, "bf16", 128), (2, 3, 128, 50, "fp16", 0), (2, 3, 128, 50, "fp32", 0), (2, 1, 256, 4, "bf16", 0),
+         (1, 4, 128, 64, "bf16", 128), (1, 4, 128, 96, "bf16", 128), (1, 4, 128, 128, "bf16", 128), (2, 3, 128, 50, "fp16", 0), (2, 3, 128, 50, "fp32", 0), (2, 1, 256, 4, "bf16", 0),
          (2, 1, 256, 4, "bf16", 256), (2, 2, 256, 70, "fp16", 0), (2, 1, 256, 4, "fp32", 0)]
 
 
