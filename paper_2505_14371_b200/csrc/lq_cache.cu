@@ -575,7 +575,7 @@ int lq_cache_attend_shared(lq_cache* cache, int32_t layer, const lq_rows* querie
     CacheSharedArgs b{};
     b.shape = s; b.tables = a.tables; b.queries = a.queries; b.out = a.out; b.rotary = a.rotary; b.pages = pages;
     b.prefix = prefix; b.prefix_length = prefix_length; b.lengths = lengths; b.lse = lse; b.flags = cache->flags;
-    b.num_pages = num_pages; b.prefix_width = prefix_width; b.prefix_most = most_tokens(cache, prefix_width); b.own_most = most_tokens(cache, table_width);
+    b.num_pages = num_pages; b.prefix_most = most_tokens(cache, prefix_width); b.own_most = most_tokens(cache, table_width);
     b.scale = a.scale; b.batch = a.batch; b.group = a.group; b.splits = space.splits;
     b.rests = space.rests; b.slots = space.slots; b.pairs = space.pairs; b.wait_cycles = cache->wait_cycles; b.sms = cache->sms;
     b.rows = reinterpret_cast<char*>(base + space.rows); b.parts = base + space.parts; b.own = base + space.own;

@@ -131,11 +131,11 @@ struct CacheSharedArgs {
     const int32_t* prefix_length;       // dev [1]
     const int32_t* lengths;             // dev [batch]: the sequences' own tokens
     float* lse;
-    char* rows;                         // the queries as the matrix unit reads them (cache_shared_rows_bytes), see lq_cache_shared.cu
-    float* parts;                       // [splits][batch][heads * group] parts of the prefix (cache_part_floats)
+    char* rows;                         // the queries as the matrix unit reads them, cache_shared_block_bytes a block of 128 rows (lq_cache_shared.cu)
+    float* parts;                       // [splits * slots][batch][heads * group] parts of the prefix (cache_part_floats)
     float* own;                         // [batch][heads * group] parts of the sequences' own tokens
     uint32_t* flags;
-    int64_t num_pages, prefix_width, prefix_most, own_most;     // tokens that the lengths can mean
+    int64_t num_pages, prefix_most, own_most;   // the latter: tokens that the lengths can mean
     float scale;
     int32_t batch, group, splits;
     int32_t rests, slots, pairs, sms;   // what the queries' rounding leaves (cache_shared_rests), see cache_shared_slots, cache_shared_pairs

@@ -460,37 +460,35 @@ __device__ __forceinline__ void decode(const Codes<P>& c, int k, const CacheShar
     int kind, panel, token;
     item_of<P>(warp + kDecodeWarps * k, kind, panel, token);
     token += lane;
-    {
-        const uint32_t row = piece + panel * kPanel + token * 128, copies = kTableAt + 4 * lane + 128 * kind;
-        const uint32_t turn = (token & 7) << 4;
-        const uint32_t (&w)[16] = c.w[k];
-        // (16 look-ups before their stores: the compiler moves no load of shared memory above a store)
-        if ((kind ? a.shape.sym_bits[1] : a.shape.sym_bits[0]) == 8) {
-            auto two = [](uint32_t x, uint32_t y) { return __byte_perm(x, y, 0x5410); };
+    const uint32_t row = piece + panel * kPanel + token * 128, copies = kTableAt + 4 * lane + 128 * kind;
+    const uint32_t turn = (token & 7) << 4;
+    const uint32_t (&w)[16] = c.w[k];
+    // (16 look-ups before their stores: the compiler moves no load of shared memory above a store)
+    if ((kind ? a.shape.sym_bits[1] : a.shape.sym_bits[0]) == 8) {
+        auto two = [](uint32_t x, uint32_t y) { return __byte_perm(x, y, 0x5410); };
 #pragma unroll
-            for (int j = 0; j < 8; j += 2) {
-                uint32_t v[8];
+        for (int j = 0; j < 8; j += 2) {
+            uint32_t v[8];
 #pragma unroll
-                for (int m = 0; m < 4; ++m) {
-                    const uint32_t x = w[2 * j + m];
-                    v[2 * m] = two(look<0>(x, copies), look<1>(x, copies));
-                    v[2 * m + 1] = two(look<2>(x, copies), look<3>(x, copies));
-                }
-                store16(row + ((16 * j) ^ turn), v[0], v[1], v[2], v[3]);
-                store16(row + ((16 * j + 16) ^ turn), v[4], v[5], v[6], v[7]);
+            for (int m = 0; m < 4; ++m) {
+                const uint32_t x = w[2 * j + m];
+                v[2 * m] = two(look<0>(x, copies), look<1>(x, copies));
+                v[2 * m + 1] = two(look<2>(x, copies), look<3>(x, copies));
             }
-        } else {
+            store16(row + ((16 * j) ^ turn), v[0], v[1], v[2], v[3]);
+            store16(row + ((16 * j + 16) ^ turn), v[4], v[5], v[6], v[7]);
+        }
+    } else {
 #pragma unroll
-            for (int j = 0; j < 8; j += 4) {
-                uint32_t v[4][4];
+        for (int j = 0; j < 8; j += 4) {
+            uint32_t v[4][4];
 #pragma unroll
-                for (int m = 0; m < 4; ++m) {
-                    v[m][0] = look<0>(w[j + m], copies); v[m][1] = look<1>(w[j + m], copies);
-                    v[m][2] = look<2>(w[j + m], copies); v[m][3] = look<3>(w[j + m], copies);
-                }
-#pragma unroll
-                for (int m = 0; m < 4; ++m) store16(row + ((16 * (j + m)) ^ turn), v[m][0], v[m][1], v[m][2], v[m][3]);
+            for (int m = 0; m < 4; ++m) {
+                v[m][0] = look<0>(w[j + m], copies); v[m][1] = look<1>(w[j + m], copies);
+                v[m][2] = look<2>(w[j + m], copies); v[m][3] = look<3>(w[j + m], copies);
             }
+#pragma unroll
+            for (int m = 0; m < 4; ++m) store16(row + ((16 * (j + m)) ^ turn), v[m][0], v[m][1], v[m][2], v[m][3]);
         }
     }
 }
@@ -499,28 +497,26 @@ __device__ __forceinline__ void decode(const Codes<P>& c, int k, const CacheShar
 template <int P>
 __device__ __forceinline__ void place_norms(const Codes<P>& c, const Share& s, Small& sm, int tile, int stage, int lane)
 {
-    {
-        const int64_t first = (int64_t)(s.tile0 + tile) * kTile;
-        uint32_t seen[2];
-        int most = -127;
+    const int64_t first = (int64_t)(s.tile0 + tile) * kTile;
+    uint32_t seen[2];
+    int most = -127;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int token = lane + 32 * i;
-            const bool there = (c.seen >> (token >> 4) & 1) && first + token < s.length;
-            seen[i] = __ballot_sync(0xffffffffu, there);
-            if (there) most = max(most, exponent_of(c.values[i]));
-        }
-        most = __reduce_max_sync(0xffffffffu, most);
-        const int half = most / 2;
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int token = lane + 32 * i;
-            const bool there = seen[i] >> lane & 1;
-            sm.keys[stage][token] = there ? c.keys[i] : 0.0f;
-            sm.values[stage][token] = there ? c.values[i] * power(-half) * power(half - most) : 0.0f;
-        }
-        if (lane == 0) { sm.seen[stage][0] = seen[0]; sm.seen[stage][1] = seen[1]; sm.exponent[stage] = most; }
+    for (int i = 0; i < 2; ++i) {
+        const int token = lane + 32 * i;
+        const bool there = (c.seen >> (token >> 4) & 1) && first + token < s.length;
+        seen[i] = __ballot_sync(0xffffffffu, there);
+        if (there) most = max(most, exponent_of(c.values[i]));
     }
+    most = __reduce_max_sync(0xffffffffu, most);
+    const int half = most / 2;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int token = lane + 32 * i;
+        const bool there = seen[i] >> lane & 1;
+        sm.keys[stage][token] = there ? c.keys[i] : 0.0f;
+        sm.values[stage][token] = there ? c.values[i] * power(-half) * power(half - most) : 0.0f;
+    }
+    if (lane == 0) { sm.seen[stage][0] = seen[0]; sm.seen[stage][1] = seen[1]; sm.exponent[stage] = most; }
 }
 
 // ---- softmax ---------------------------------------------------------------------------------------------------
