@@ -493,7 +493,9 @@ int lq_cache_attend(lq_cache* cache, int32_t layer, const lq_rows* queries, int6
  * lengths[b] of its own pages table[b].  The prefix is read once for all of them.  prefix_length: dev [1].  Without rotary->at a query stands
  * at its sequence's last position, *prefix_length + lengths[b] - 1.  Either part may be empty; no window.  batch * heads up to 2^26.
  * Roundings as above; the prefix's sums are those of the matrix unit, which cuts off, over 1024 tokens at most for fp32 outputs, 8192 for fp16
- * and 131072 for bf16.  Between calls nothing is kept: the workspace holds what a call's kernels hand on.  (`type`: that of queries and out;
+ * and 131072 for bf16.  Between calls nothing is kept: the workspace holds what a call's kernels hand on.
+ * Faster than lq_cache_attend over tables that begin with the prefix's pages from some 8 sequences on, where the prefix's rows, read once a
+ * sequence, would come to some 140 MB (a B200); below that, join the tables.  (`type`: that of queries and out;
  * `turned`: not 0 if there will be a rotary.) */
 int64_t lq_cache_shared_workspace(const lq_cache* cache, int64_t batch, int32_t heads, int64_t prefix_width, int64_t table_width, int32_t type,
                                   int32_t turned);

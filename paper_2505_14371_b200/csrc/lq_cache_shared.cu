@@ -25,7 +25,9 @@
 // What bounds it: the softmax.  Of a tile of 128 rows x 64 tokens its warps' 525 instructions each take some 2000 cycles beside decoding and waits, where the
 // special-function unit alone would need 512 and the products 640 (960 with rests): 16384 tokens for 512 rows of 8 heads of 128, 35 GFLOP, 64 us in
 // pairs of blocks without rests (550 TFLOP/s, the tensor pipe busy for 27 %), some 88 with.  Few rows or tokens: the chain of four kernels, some 24 us.
-// Measured and not kept (that case, all kernels, us, of 114 without rests): eight warps of softmax a slot 147; 16 scores at a time in a loop 146; fragments of four
+// Registers: the softmax's forms with two slots spill, those of weights as two numbers some 240 bytes a thread, the others 40 to 90; a stack frame of 256 bytes
+// holds the scores that moved_row looks at.
+// Measured and not kept (that case with queries of one number, all kernels, us, of 114 when tried): eight warps of softmax a slot 147; 16 scores at a time in a loop 146; fragments of four
 // rows a thread, whose norms then serve four scores 148; both slots in step 122.
 //
 // Waits are bounded: after the cache's limit (some two seconds unless lq_cache_wait says less) a waiting thread sets LQ_CACHE_GAVE_UP, and all leave, once
